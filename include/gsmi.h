@@ -623,6 +623,211 @@ gs_status gs_admission_gate(const uint32_t* RB, const uint32_t* D, const gs_gate
                             gs_gate_result* result, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Token operators.  A network that writes rows of the pool (one token per
+ * primitive, region or view; its gradient arrives as gs_raster_bwd's rows)
+ * runs its norms, rotations by position and attention through the calls
+ * below; its plain matrix products stay with the caller's library.
+ *
+ * Token matrices: [rows, heads, dim] views, element (r, h, c) at
+ * ptr + r * ld_row + h * ld_head + c (strides in elements; elements of a head
+ * contiguous).  Types: GS_F32 where a call says so, GS_BF16, GS_F16.  Sums,
+ * statistics and products are held in fp32 whatever the type.
+ * ------------------------------------------------------------------------ */
+
+enum { GS_F32 = 0, GS_BF16 = 1, GS_F16 = 2 };
+
+typedef struct {
+    void* ptr;
+    int64_t ld_row, ld_head;
+} gs_rows;
+
+/*
+ * Root-mean-square norm with the residual's addition, a row at a time:
+ *   s = x + residual;  y = s * w / sqrt(mean(s^2) + eps)
+ * y is formed from the fp32 sum, not from its rounding into `total`.
+ *   x, residual, total, y: [rows, cols] of `dtype` (any of the three types),
+ *     rows ld_* elements apart (>= cols); residual NULL: s = x; total NULL:
+ *     the sum is not written; y NULL: y is not written.  total may be x or
+ *     residual itself, y may be x (the same rows, not shifted ones).
+ *   weight [cols] fp32
+ *   q [rows, ld_q] uint8 or NULL: y in 8 bits (e4m3: 4 exponent bits, 3
+ *     mantissa bits, largest 448), in blocks of GS_NORM_BLOCK columns (the last
+ *     may be shorter), each with its scale: y ~ scale * q, ties to even.
+ *   q_scale [rows, ld_scale] fp32 (with q): max|y| of the block / 448, at least
+ *     2^-126; 1 for a block of zeros.  A NaN becomes a NaN of q and does not
+ *     touch the scale; an infinity makes the scale infinite and q NaN.
+ * Errors: GS_ERR_INVALID_ARG (null pointers, sizes below 0, a row stride below
+ * cols, pointers that are not a multiple of the element size, eps negative or
+ * not finite, nothing to write); GS_ERR_UNSUPPORTED for cols above
+ * GS_NORM_MAX_COLS.
+ */
+#define GS_NORM_BLOCK 128
+#define GS_NORM_MAX_COLS 16384
+
+typedef struct {
+    int32_t rows, cols, dtype;
+    float eps;
+    const void* x;
+    const void* residual;
+    const float* weight;
+    void* total;
+    void* y;
+    uint8_t* q;
+    float* q_scale;
+    int64_t ld_x, ld_residual, ld_total, ld_y, ld_q, ld_scale;
+} gs_norm_args;
+
+gs_status gs_rms_norm(const gs_norm_args* args, void* stream);
+
+/*
+ * Its gradient, with r = 1/sqrt(mean(total^2) + eps) and n = total * r:
+ *   dx = r * (dy*w - n * mean(dy*w*n)) + dtotal;  dweight = sum over rows of dy*n
+ * dx is the gradient of x and of residual alike.  dweight is summed in a fixed
+ * order: the same call gives the same bits.
+ *   dy, total (the forward's sum, or x without a residual), dtotal (NULL: 0;
+ *   the gradient that reaches the sum past the norm), dx: [rows, cols] of
+ *   `dtype`; dx may be dy, total or dtotal.  dweight [cols] fp32.
+ *   ws: gs_rms_norm_bwd_ws_bytes(rows, cols) bytes, 16-byte aligned
+ * Errors as for gs_rms_norm, and GS_ERR_WORKSPACE.
+ */
+typedef struct {
+    int32_t rows, cols, dtype;
+    float eps;
+    const void* dy;
+    const void* total;
+    const void* dtotal;
+    const float* weight;
+    void* dx;
+    float* dweight;
+    int64_t ld_dy, ld_total, ld_dtotal, ld_dx;
+} gs_norm_bwd_args;
+
+size_t gs_rms_norm_bwd_ws_bytes(int32_t rows, int32_t cols);
+gs_status gs_rms_norm_bwd(const gs_norm_bwd_args* args, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rotation by position.  Pair j of every head (j < pairs, 2 * pairs <= dim) is
+ * turned by the angle pos[token, axis(j)] * freq[j]:
+ *   (a, b) -> amplitude * (a cos - b sin, a sin + b cos)
+ * (inverse: by the negative angle, which is also the gradient's way back); the
+ * head's other dim - 2*pairs elements are copied.  The first axis_pairs[0]
+ * pairs follow axis 0, the next axis_pairs[1] axis 1, and so on, so that a
+ * primitive's place in space turns its token along three axes.
+ *   interleaved 0: pair j is elements (j, j + pairs); 1: (2j, 2j + 1)
+ *   pos [tokens, ld_pos] fp32 (n_axes of them used; the pool's mean with its
+ *     row stride is such an array); freq [pairs] fp32
+ *   n_tensors 1 or 2 (queries and keys in one call): in[i] -> out[i], [tokens,
+ *     heads[i], dim] of `dtype` (any of the three types); out[i] may be in[i]
+ *     with the same strides
+ * The angle is formed and reduced in fp64 (a product in fp32 would be off by
+ * 0.004 at position 65536), its sine and cosine in fp32.
+ * Errors: GS_ERR_INVALID_ARG (null pointers, negative sizes, pairs against dim
+ * or axis_pairs, misaligned elements, an amplitude that is not finite);
+ * GS_ERR_UNSUPPORTED for dim above GS_ROTARY_MAX_DIM or more than 2^31 - 1
+ * rows of heads.
+ */
+#define GS_ROTARY_MAX_DIM 512
+
+typedef struct {
+    int32_t dtype, tokens, dim, pairs;
+    int32_t n_axes, axis_pairs[3];
+    int32_t interleaved, inverse;
+    float amplitude;
+    const float* pos;
+    int64_t ld_pos;
+    const float* freq;
+    int32_t n_tensors, heads[2];
+    gs_rows in[2], out[2];
+} gs_rotary_args;
+
+gs_status gs_rotary(const gs_rotary_args* args, void* stream);
+
+/*
+ * Frequencies of one axis (host memory, computed in fp64): freq[j] =
+ * base^(-j/pairs), then for positions `factor` times as far as trained:
+ *   GS_ROPE_PLAIN   as they are
+ *   GS_ROPE_LINEAR  freq[j] / factor (positions drawn together)
+ *   GS_ROPE_BASE    base * factor^(pairs/(pairs-1)) for base: the fastest pair
+ *                   unchanged, the slowest drawn together by factor (pairs >= 2)
+ *   GS_ROPE_PARTS   pair j turns n_j = trained * freq[j] / (2 pi) times over the
+ *                   trained length: t = clamp((n_j - slow) / (fast - slow), 0, 1)
+ *                   of it stays, the rest is divided by factor; *amplitude
+ *                   = 1 + ln(factor) / 10
+ * *amplitude is 1 for the other kinds; NULL: not written.
+ * Errors: GS_ERR_INVALID_ARG (null freq, pairs < 1, base <= 1, factor < 1, and
+ * for GS_ROPE_PARTS trained <= 0 or fast <= slow).
+ */
+enum { GS_ROPE_PLAIN = 0, GS_ROPE_LINEAR = 1, GS_ROPE_BASE = 2, GS_ROPE_PARTS = 3 };
+gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double factor, double trained, double slow,
+                          double fast, float* freq, float* amplitude);
+
+/*
+ * Attention over ragged segments (the regions of a scene, the views of a unit).
+ * Row i of a segment with nq rows and nk keys stands at place i + nk - nq (its
+ * last row on its last key) and admits key j when
+ *   place - left <= j <= place + right (left, right < 0: no bound),
+ *   and key_on[j] != 0 (key_on NULL: all are on):
+ *   s_j = scale * q_i . k_j;  out_i = sum_j exp(s_j) v_j / sum_j exp(s_j);
+ *   lse_i = log sum_j exp(s_j)
+ * left = -1, right = 0 is the ordered (causal) form, right = left = -1 all keys.
+ * A row that admits no key, or none with a score above -infinity, has out 0,
+ * lse -infinity and passes no gradient.  Head h reads key head h / (heads /
+ * kv_heads).  The rows of k and v that key_on switches off are not read at all:
+ * NaN or infinities there reach nothing, and their dk, dv are 0.  A NaN or
+ * infinity in a key that is on may reach every row of its segment.
+ *   cu_q, cu_k [n_seg + 1] int32, ascending from 0 to n_q and n_k: the segments'
+ *     first rows (empty ones allowed); both NULL: n_seg segments of equal
+ *     length (n_seg divides n_q and n_k).  Values outside [0, n] are taken as
+ *     the nearest in it; rows outside every segment are not written.
+ *   q [n_q, heads, dim], k, v [n_k, kv_heads, dim]; GS_BF16 or GS_F16; pointers
+ *     16-byte aligned, strides and dim multiples of 8 elements, dim <= 128.
+ *     key_on [n_k] uint8.
+ *   out: as q; lse [n_q, heads] fp32, dense
+ *   ws: gs_attention_ws_bytes(a, 0) bytes (can be 0: ws may be NULL), 16-byte
+ *     aligned.  The size follows from the sizes in `a`, not from cu_*'s values.
+ * The probabilities are rounded to the tokens' type for their product with v
+ * (the matrix unit's operand); the sums stay in fp32.  Keys are taken in an
+ * order that the sizes alone fix: the same call gives the same bits.
+ * Errors: GS_ERR_INVALID_ARG (null pointers, sizes, alignment, one of cu_q and
+ * cu_k without the other, a scale that is not a positive finite number, dtype);
+ * GS_ERR_UNSUPPORTED (dim above 128, n_q * heads or n_k * kv_heads above
+ * 2^31 - 1); GS_ERR_WORKSPACE.
+ */
+#define GS_ATTN_MAX_DIM 128
+
+typedef struct {
+    int32_t dtype;
+    int32_t n_q, n_k, n_seg;
+    int32_t heads, kv_heads, dim;
+    int32_t left, right;
+    float scale;
+    const int32_t* cu_q;
+    const int32_t* cu_k;
+    const uint8_t* key_on;
+    gs_rows q, k, v;
+} gs_attn;
+
+size_t gs_attention_ws_bytes(const gs_attn* a, int32_t backward);
+gs_status gs_attention(const gs_attn* a, const gs_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its gradient.  The probabilities are recomputed from lse; with
+ * delta_i = dout_i . out_i and ds_ij = scale * p_ij (dout_i . v_j - delta_i):
+ *   dq_i = sum_j ds_ij k_j;  dk_j = sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
+ * dk and dv of a shared head are summed over the heads that read it.  Nothing is
+ * summed by atomics: the same call gives the same bits.
+ *   out, dout, dq: as q; dk, dv: as k; lse as gs_attention left it
+ *   ws: gs_attention_ws_bytes(a, 1) bytes, 16-byte aligned
+ * Errors as for gs_attention.
+ */
+typedef struct {
+    gs_rows out, dout, dq, dk, dv;
+    const float* lse;
+} gs_attn_grads;
+
+gs_status gs_attention_bwd(const gs_attn* a, const gs_attn_grads* g, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Ahead-of-time planner (host).  The three calls below run on the CPU over
  * host memory, synchronously, before training; they take no stream and
  * allocate host scratch internally.  Views are items 0..n-1.  Results are

@@ -2,7 +2,9 @@
 // No entry point allocates, frees or synchronizes.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -517,6 +519,212 @@ gs_status gs_admission_gate(const uint32_t* RB, const uint32_t* D, const gs_gate
     if (ws_bytes < gsmi::scope_ws_bytes(n)) return fail(GS_ERR_WORKSPACE, "gs_admission_gate: workspace too small");
     return hip_status(gsmi::launch_admission_gate(RB, D, *args, n, result, ws, static_cast<hipStream_t>(stream)),
                       "gs_admission_gate");
+}
+
+static size_t type_size(int32_t dtype) { return dtype == GS_F32 ? 4 : 2; }
+
+// A token matrix: whole elements, rows and heads that do not run into each other's elements by a negative stride.
+static gs_status check_matrix(const void* p, int64_t ld, int32_t rows, int32_t cols, size_t esize, const char* name,
+                              const char* what) {
+    GS_REQUIRE(p != nullptr || rows == 0 || cols == 0, "%s: null %s", what, name);
+    GS_REQUIRE(aligned(p, esize), "%s: %s is not aligned to its elements", what, name);
+    GS_REQUIRE(ld >= cols, "%s: row stride %lld of %s below %d", what, (long long)ld, name, cols);
+    return GS_OK;
+}
+
+static gs_status check_norm_sizes(int32_t rows, int32_t cols, int32_t dtype, float eps, const float* weight,
+                                  const char* what) {
+    GS_REQUIRE(dtype == GS_F32 || dtype == GS_BF16 || dtype == GS_F16, "%s: bad dtype %d", what, dtype);
+    GS_REQUIRE(rows >= 0 && cols >= 1, "%s: rows < 0 or cols < 1", what);
+    GS_REQUIRE(eps >= 0.0f && std::isfinite(eps), "%s: eps must be finite and >= 0", what);
+    GS_REQUIRE(weight != nullptr && aligned(weight, 4), "%s: null or misaligned weight", what);
+    if (cols > GS_NORM_MAX_COLS) return fail(GS_ERR_UNSUPPORTED, "%s: cols %d above %d", what, cols, GS_NORM_MAX_COLS);
+    return GS_OK;
+}
+
+gs_status gs_rms_norm(const gs_norm_args* a, void* stream) {
+    const char* what = "gs_rms_norm";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_norm_sizes(a->rows, a->cols, a->dtype, a->eps, a->weight, what)) != GS_OK) return s;
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(a->x, a->ld_x, a->rows, a->cols, es, "x", what)) != GS_OK) return s;
+    if (a->residual && (s = check_matrix(a->residual, a->ld_residual, a->rows, a->cols, es, "residual", what)) != GS_OK)
+        return s;
+    if (a->total && (s = check_matrix(a->total, a->ld_total, a->rows, a->cols, es, "total", what)) != GS_OK) return s;
+    if (a->y && (s = check_matrix(a->y, a->ld_y, a->rows, a->cols, es, "y", what)) != GS_OK) return s;
+    if (a->q) {
+        if ((s = check_matrix(a->q, a->ld_q, a->rows, a->cols, 1, "q", what)) != GS_OK) return s;
+        if ((s = check_matrix(a->q_scale, a->ld_scale, a->rows, (a->cols + GS_NORM_BLOCK - 1) / GS_NORM_BLOCK, 4,
+                              "q_scale", what)) != GS_OK)
+            return s;
+    }
+    GS_REQUIRE(a->rows == 0 || a->total || a->y || a->q, "%s: no output", what);
+    if (a->rows == 0) return ok();
+    return hip_status(gsmi::launch_rms_norm(*a, static_cast<hipStream_t>(stream)), what);
+}
+
+size_t gs_rms_norm_bwd_ws_bytes(int32_t rows, int32_t cols) {
+    if (rows < 0 || cols < 0) return 0;
+    return gsmi::rms_norm_bwd_ws_bytes(rows, cols);
+}
+
+gs_status gs_rms_norm_bwd(const gs_norm_bwd_args* a, void* ws, size_t ws_bytes, void* stream) {
+    const char* what = "gs_rms_norm_bwd";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_norm_sizes(a->rows, a->cols, a->dtype, a->eps, a->weight, what)) != GS_OK) return s;
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(a->dy, a->ld_dy, a->rows, a->cols, es, "dy", what)) != GS_OK) return s;
+    if ((s = check_matrix(a->total, a->ld_total, a->rows, a->cols, es, "total", what)) != GS_OK) return s;
+    if (a->dtotal && (s = check_matrix(a->dtotal, a->ld_dtotal, a->rows, a->cols, es, "dtotal", what)) != GS_OK)
+        return s;
+    if ((s = check_matrix(a->dx, a->ld_dx, a->rows, a->cols, es, "dx", what)) != GS_OK) return s;
+    GS_REQUIRE(a->dweight != nullptr && aligned(a->dweight, 4), "%s: null or misaligned dweight", what);
+    GS_REQUIRE(ws != nullptr && aligned(ws, 16), "%s: workspace must be 16-byte aligned device memory", what);
+    if (ws_bytes < gsmi::rms_norm_bwd_ws_bytes(a->rows, a->cols))
+        return fail(GS_ERR_WORKSPACE, "%s: workspace too small", what);
+    return hip_status(gsmi::launch_rms_norm_bwd(*a, ws, static_cast<hipStream_t>(stream)), what);
+}
+
+gs_status gs_rotary(const gs_rotary_args* a, void* stream) {
+    const char* what = "gs_rotary";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    GS_REQUIRE(a->dtype == GS_F32 || a->dtype == GS_BF16 || a->dtype == GS_F16, "%s: bad dtype %d", what, a->dtype);
+    GS_REQUIRE(a->tokens >= 0 && a->dim >= 1 && a->pairs >= 0, "%s: bad size", what);
+    GS_REQUIRE(a->pairs <= a->dim / 2, "%s: %d pairs in a head of %d elements", what, a->pairs, a->dim);
+    if (a->dim > GS_ROTARY_MAX_DIM)
+        return fail(GS_ERR_UNSUPPORTED, "%s: dim %d above %d", what, a->dim, GS_ROTARY_MAX_DIM);
+    GS_REQUIRE(a->n_axes >= 1 && a->n_axes <= 3, "%s: 1..3 axes", what);
+    int64_t pairs = 0;
+    for (int i = 0; i < a->n_axes; ++i) {
+        GS_REQUIRE(a->axis_pairs[i] >= 0, "%s: negative axis_pairs", what);
+        pairs += a->axis_pairs[i];
+    }
+    GS_REQUIRE(pairs == a->pairs, "%s: axis_pairs sum to %lld, not to %d", what, (long long)pairs, a->pairs);
+    GS_REQUIRE(std::isfinite(a->amplitude), "%s: amplitude not finite", what);
+    GS_REQUIRE(a->n_tensors == 1 || a->n_tensors == 2, "%s: 1 or 2 tensors", what);
+    GS_REQUIRE(a->pairs == 0 || (a->freq && aligned(a->freq, 4)), "%s: null or misaligned freq", what);
+    if (a->pairs > 0 && a->tokens > 0) {
+        GS_REQUIRE(a->pos && aligned(a->pos, 4), "%s: null or misaligned pos", what);
+        GS_REQUIRE(a->ld_pos >= a->n_axes, "%s: ld_pos below the axes", what);
+    }
+    const size_t es = type_size(a->dtype);
+    int64_t rows = 0;
+    for (int i = 0; i < a->n_tensors; ++i) {
+        GS_REQUIRE(a->heads[i] >= 0, "%s: negative heads", what);
+        rows += (int64_t)a->heads[i] * a->tokens;
+        if (a->heads[i] == 0 || a->tokens == 0) continue;
+        for (const gs_rows* r : {&a->in[i], &a->out[i]}) {
+            GS_REQUIRE(r->ptr != nullptr && aligned(r->ptr, es), "%s: null or misaligned tensor %d", what, i);
+            GS_REQUIRE(a->heads[i] == 1 || r->ld_head >= a->dim || r->ld_head <= -(int64_t)a->dim,
+                       "%s: head stride of tensor %d below dim", what, i);
+            GS_REQUIRE(a->tokens == 1 || r->ld_row >= a->dim || r->ld_row <= -(int64_t)a->dim,
+                       "%s: row stride of tensor %d below dim", what, i);
+        }
+        GS_REQUIRE(a->in[i].ptr != a->out[i].ptr ||
+                       (a->in[i].ld_row == a->out[i].ld_row && a->in[i].ld_head == a->out[i].ld_head),
+                   "%s: tensor %d in place with other strides", what, i);
+    }
+    if (rows > 0x7FFFFFFF) return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows of heads", what);
+    if (rows == 0) return ok();
+    return hip_status(gsmi::launch_rotary(*a, static_cast<hipStream_t>(stream)), what);
+}
+
+gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double factor, double trained, double slow,
+                          double fast, float* freq, float* amplitude) {
+    const char* what = "gs_rotary_freqs";
+    GS_REQUIRE(freq != nullptr && pairs >= 1, "%s: null freq or pairs < 1", what);
+    GS_REQUIRE(scaling >= GS_ROPE_PLAIN && scaling <= GS_ROPE_PARTS, "%s: bad scaling %d", what, scaling);
+    GS_REQUIRE(base > 1.0 && std::isfinite(base), "%s: base must be above 1", what);
+    GS_REQUIRE(scaling == GS_ROPE_PLAIN || (factor >= 1.0 && std::isfinite(factor)), "%s: factor below 1", what);
+    GS_REQUIRE(scaling != GS_ROPE_BASE || pairs >= 2, "%s: GS_ROPE_BASE needs 2 pairs", what);
+    if (scaling == GS_ROPE_PARTS)
+        GS_REQUIRE(trained > 0.0 && std::isfinite(trained) && fast > slow && std::isfinite(fast) && std::isfinite(slow),
+                   "%s: trained length or slow/fast bounds", what);
+    const double b = scaling == GS_ROPE_BASE ? base * std::pow(factor, (double)pairs / (pairs - 1)) : base;
+    for (int32_t j = 0; j < pairs; ++j) {
+        double f = std::pow(b, -(double)j / pairs);
+        if (scaling == GS_ROPE_LINEAR) f /= factor;
+        if (scaling == GS_ROPE_PARTS) {
+            const double turns = trained * f / 6.283185307179586476925;
+            const double t = std::min(1.0, std::max(0.0, (turns - slow) / (fast - slow)));
+            f = t * f + (1.0 - t) * f / factor;
+        }
+        freq[j] = (float)f;
+    }
+    if (amplitude) *amplitude = scaling == GS_ROPE_PARTS ? (float)(1.0 + 0.1 * std::log(factor)) : 1.0f;
+    return ok();
+}
+
+static gs_status check_attn_rows(const gs_rows& r, int32_t rows, const char* name, const char* what) {
+    if (rows == 0) return GS_OK;
+    GS_REQUIRE(r.ptr != nullptr, "%s: null %s", what, name);
+    GS_REQUIRE(aligned(r.ptr, 16), "%s: %s must be 16-byte aligned", what, name);
+    GS_REQUIRE(r.ld_row % 8 == 0 && r.ld_head % 8 == 0, "%s: strides of %s must be multiples of 8 elements", what, name);
+    return GS_OK;
+}
+
+static gs_status check_attn(const gs_attn* a, const char* what) {
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    GS_REQUIRE(a->dtype == GS_BF16 || a->dtype == GS_F16, "%s: dtype %d is neither GS_BF16 nor GS_F16", what, a->dtype);
+    GS_REQUIRE(a->n_q >= 0 && a->n_k >= 0 && a->n_seg >= 1, "%s: bad row or segment count", what);
+    GS_REQUIRE(a->heads >= 1 && a->kv_heads >= 1 && a->heads % a->kv_heads == 0,
+               "%s: kv_heads %d must divide heads %d", what, a->kv_heads, a->heads);
+    GS_REQUIRE(a->dim >= 8 && a->dim % 8 == 0, "%s: dim %d must be a multiple of 8", what, a->dim);
+    if (a->dim > GS_ATTN_MAX_DIM) return fail(GS_ERR_UNSUPPORTED, "%s: dim %d above %d", what, a->dim, GS_ATTN_MAX_DIM);
+    GS_REQUIRE(a->scale > 0.0f && std::isfinite(a->scale), "%s: scale must be positive and finite", what);
+    GS_REQUIRE((a->cu_q != nullptr) == (a->cu_k != nullptr), "%s: cu_q and cu_k are given together", what);
+    GS_REQUIRE(aligned(a->cu_q, 4) && aligned(a->cu_k, 4), "%s: cu_q or cu_k misaligned", what);
+    GS_REQUIRE(a->cu_q != nullptr || (a->n_q % a->n_seg == 0 && a->n_k % a->n_seg == 0),
+               "%s: %d segments of equal length do not divide %d rows and %d keys", what, a->n_seg, a->n_q, a->n_k);
+    if ((int64_t)a->n_q * a->heads > 0x7FFFFFFF || (int64_t)a->n_k * a->kv_heads > 0x7FFFFFFF ||
+        a->n_seg > (1 << 24))
+        return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows of heads or 2^24 segments", what);
+    gs_status s;
+    if ((s = check_attn_rows(a->q, a->n_q, "q", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(a->k, a->n_k, "k", what)) != GS_OK) return s;
+    return check_attn_rows(a->v, a->n_k, "v", what);
+}
+
+size_t gs_attention_ws_bytes(const gs_attn* a, int32_t backward) {
+    if (a == nullptr || a->n_q < 0 || a->n_k < 0 || a->n_seg < 1 || a->heads < 1 || a->kv_heads < 1 || a->dim < 1 ||
+        a->heads % a->kv_heads != 0 || a->dim > GS_ATTN_MAX_DIM)
+        return 0;
+    return backward ? gsmi::attention_bwd_ws_bytes(*a) : gsmi::attention_ws_bytes(*a);
+}
+
+gs_status gs_attention(const gs_attn* a, const gs_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    const char* what = "gs_attention";
+    gs_status s;
+    if ((s = check_attn(a, what)) != GS_OK) return s;
+    GS_REQUIRE(out != nullptr, "%s: null out", what);
+    if (a->n_q == 0) return ok();
+    if ((s = check_attn_rows(*out, a->n_q, "out", what)) != GS_OK) return s;
+    GS_REQUIRE(lse != nullptr && aligned(lse, 4), "%s: null or misaligned lse", what);
+    const size_t need = gsmi::attention_ws_bytes(*a);
+    GS_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), "%s: workspace must be 16-byte aligned device memory",
+               what);
+    if (ws_bytes < need) return fail(GS_ERR_WORKSPACE, "%s: workspace too small", what);
+    return hip_status(gsmi::launch_attention(*a, *out, lse, ws, static_cast<hipStream_t>(stream)), what);
+}
+
+gs_status gs_attention_bwd(const gs_attn* a, const gs_attn_grads* g, void* ws, size_t ws_bytes, void* stream) {
+    const char* what = "gs_attention_bwd";
+    gs_status s;
+    if ((s = check_attn(a, what)) != GS_OK) return s;
+    GS_REQUIRE(g != nullptr, "%s: null gradients", what);
+    if ((s = check_attn_rows(g->out, a->n_q, "out", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dout, a->n_q, "dout", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dq, a->n_q, "dq", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dk, a->n_k, "dk", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dv, a->n_k, "dv", what)) != GS_OK) return s;
+    GS_REQUIRE(a->n_q == 0 || (g->lse != nullptr && aligned(g->lse, 4)), "%s: null or misaligned lse", what);
+    const size_t need = gsmi::attention_bwd_ws_bytes(*a);
+    GS_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), "%s: workspace must be 16-byte aligned device memory",
+               what);
+    if (ws_bytes < need) return fail(GS_ERR_WORKSPACE, "%s: workspace too small", what);
+    return hip_status(gsmi::launch_attention_bwd(*a, *g, ws, static_cast<hipStream_t>(stream)), what);
 }
 
 gs_status gs_rlg_build(int32_t n_items, int32_t n_tracks, const int64_t* item_ptr, const int32_t* item_tracks,

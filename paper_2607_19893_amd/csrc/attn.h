@@ -1,0 +1,186 @@
+// Pieces that the attention kernels share (device code; gfx950).
+//
+// Matrix products run on v_mfma_f32_32x32x16 (16-bit operands, fp32 sums):
+//   A [32 x 16]: lane l holds row l & 31, elements 8 (l >> 5) .. +7 of the 16;
+//   B [16 x 32]: lane l holds column l & 31, the same 8 of the 16;
+//   C [32 x 32]: lane l holds column l & 31; its register r is row
+//     8 (r >> 2) + 4 (l >> 5) + (r & 3).
+// A sum over the 16 takes them in any order as long as A and B agree.  So
+// registers 8u .. 8u+7 of a C tile, rounded to 16 bits, are the B operand (or,
+// the tile being its own transpose's A) of a product over the tile's rows
+// 16u .. 16u+15, in the order 16u + 8 (i >> 2) + 4 (l >> 5) + (i & 3) for
+// element i: softmax probabilities go from one product into the next without
+// leaving their lane.
+#pragma once
+
+#include "common.h"
+#include "internal.h"
+#include "vec16.h"
+
+namespace gsmi {
+
+typedef float acc16 __attribute__((ext_vector_type(16)));
+
+template <typename T>
+using op8 = T __attribute__((ext_vector_type(8)));
+template <typename T>
+using op4 = T __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ acc16 mfma(op8<bf16_t> a, op8<bf16_t> b, acc16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ acc16 mfma(op8<f16_t> a, op8<f16_t> b, acc16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// A tile of token rows in LDS: rows of P elements (a power of two), each cut
+// into 16-byte pieces that are stored at piece ^ key(row).  Two readers have
+// to find their 64 lanes' pieces in different banks: one takes the same piece
+// of 32 rows (16 bytes a lane), the other 64 bytes of each of four adjacent
+// rows (transposed, 8 bytes a lane).  With 16 pieces a row, row & 3 in the upper
+// two bits of the key spreads four adjacent rows over the 256 bytes of all
+// banks, and (row >> 2) & 3 below spreads the next ones; with 8 and 4 pieces,
+// two and four rows share 256 bytes and fewer bits are left to set.
+template <int P>
+__device__ __forceinline__ int piece_key(int row) {
+    if (P == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    if (P == 64) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    return (row >> 2) & 3;
+}
+
+// Elements between the tile's start and 16-byte piece `piece` of row `row`.
+template <int P>
+__device__ __forceinline__ int piece_at(int row, int piece) {
+    return row * P + ((piece ^ piece_key<P>(row)) << 3);
+}
+
+// Transposed read of four rows by sixteen columns for every group of 16 lanes:
+// lane l of the group points at four elements of row l >> 2, column 4 (l & 3),
+// and gets the four rows' elements of column l.
+typedef short s4 __attribute__((ext_vector_type(4)));
+template <typename T>
+__device__ __forceinline__ op4<T> read_columns(const T* p) {
+    const s4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s4*)(const_cast<T*>(p)));
+    return __builtin_bit_cast(op4<T>, v);
+}
+
+// A operand from the columns of a tile: rows (of the operand) are the tile's
+// columns col0 .. col0+31, the 16 of the sum are its rows row0 .. row0+15 in
+// the order a C tile's registers have.
+template <typename T, int P>
+__device__ __forceinline__ op8<T> columns_operand(const T* tile, int row0, int col0) {
+    const int l = lane_id();
+    const int row = row0 + 4 * (l >> 5) + ((l & 15) >> 2);
+    const int col = col0 + 16 * ((l >> 4) & 1) + 4 * (l & 3);
+    const op4<T> lo = read_columns(tile + piece_at<P>(row, col >> 3) + (col & 7));
+    const op4<T> hi = read_columns(tile + piece_at<P>(row + 8, col >> 3) + (col & 7));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// A or B operand from the rows of a tile: lane l gets row row0 + (l & 31),
+// elements 16 t + 8 (l >> 5) .. +7.
+template <typename T, int P>
+__device__ __forceinline__ op8<T> rows_operand(const T* tile, int row0, int t) {
+    const int l = lane_id();
+    return *reinterpret_cast<const op8<T>*>(tile + piece_at<P>(row0 + (l & 31), 2 * t + (l >> 5)));
+}
+
+// Registers 8u .. 8u+7 of a C tile as an operand.
+template <typename T>
+__device__ __forceinline__ op8<T> tile_operand(const acc16& c, int u) {
+    op8<T> o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (T)c[8 * u + i];
+    return o;
+}
+
+struct AttnArgs {
+    const void *q, *k, *v;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+    const int32_t *cu_q, *cu_k;
+    const uint8_t* key_on;
+    int32_t n_q, n_k, n_seg, heads, kv_heads, group, dim, left, right;
+    float scale;
+    int32_t tiles;             // workgroups' tiles per key head
+};
+
+inline AttnArgs attn_args(const gs_attn& a) {
+    AttnArgs r;
+    r.q = a.q.ptr;
+    r.k = a.k.ptr;
+    r.v = a.v.ptr;
+    r.q_row = a.q.ld_row;
+    r.q_head = a.q.ld_head;
+    r.k_row = a.k.ld_row;
+    r.k_head = a.k.ld_head;
+    r.v_row = a.v.ld_row;
+    r.v_head = a.v.ld_head;
+    r.cu_q = a.cu_q;
+    r.cu_k = a.cu_k;
+    r.key_on = a.key_on;
+    r.n_q = a.n_q;
+    r.n_k = a.n_k;
+    r.n_seg = a.n_seg;
+    r.heads = a.heads;
+    r.kv_heads = a.kv_heads;
+    r.group = a.heads / a.kv_heads;
+    r.dim = a.dim;
+    r.left = a.left;
+    r.right = a.right;
+    r.scale = a.scale;
+    r.tiles = 0;
+    return r;
+}
+
+// Tiles of `size` rows over ragged segments whose lengths only the device
+// knows: segment s starts at tile start(s)/size + s, which is at least as many
+// tiles as its rows need, for rows / size + n_seg tiles in all (some empty).
+struct Segment {
+    int q0, nq, k0, nk;        // first row and rows of the queries and keys
+    int tile;                  // the tile's number within the segment
+};
+
+__device__ __forceinline__ int cu_at(const int32_t* cu, int s, int n_seg, int n) {
+    if (cu == nullptr) return (int)((int64_t)n * s / n_seg);
+    return min(max(cu[s], 0), n);
+}
+
+// `cu`, `n`, `mul`: the rows that are tiled (mul of them a token).
+__device__ __forceinline__ Segment find_segment(const AttnArgs& a, const int32_t* cu, int n, int mul, int size,
+                                                int tile) {
+    int lo = 0, hi = a.n_seg - 1;          // the last segment whose first tile is at or before `tile`
+    while (lo < hi) {
+        const int m = (lo + hi + 1) >> 1;
+        const int first = (int)((int64_t)cu_at(cu, m, a.n_seg, n) * mul / size) + m;
+        if (first <= tile) lo = m;
+        else hi = m - 1;
+    }
+    Segment s;
+    s.q0 = cu_at(a.cu_q, lo, a.n_seg, a.n_q);
+    s.nq = max(cu_at(a.cu_q, lo + 1, a.n_seg, a.n_q) - s.q0, 0);
+    s.k0 = cu_at(a.cu_k, lo, a.n_seg, a.n_k);
+    s.nk = max(cu_at(a.cu_k, lo + 1, a.n_seg, a.n_k) - s.k0, 0);
+    s.tile = tile - ((int)((int64_t)cu_at(cu, lo, a.n_seg, n) * mul / size) + lo);
+    return s;
+}
+
+// Keys [lo, hi) that any of the places first .. last can admit.
+__device__ __forceinline__ void admitted(const AttnArgs& a, int nk, int first, int last, int& lo, int& hi) {
+    lo = a.left >= 0 ? max((int64_t)0, (int64_t)first - a.left) : 0;
+    hi = a.right >= 0 ? min((int64_t)nk, (int64_t)last + a.right + 1) : nk;
+}
+
+inline int attn_tiles(int64_t rows, int size, int n_seg) { return (int)(rows / size) + n_seg; }
+
+// Order of the workgroups: consecutive ids go to the eight chiplets in turn,
+// each with its own L2.  Cutting the list of (key head, tile) into eight runs
+// keeps the tiles that read the same keys on one chiplet.
+__device__ __forceinline__ int chiplet_order(int id, int n) {
+    const int per = (n + 7) >> 3;
+    return (id & 7) * per + (id >> 3);
+}
+
+inline uint32_t chiplet_grid(int64_t n) { return (uint32_t)((n + 7) / 8 * 8); }
+
+}  // namespace gsmi

@@ -120,4 +120,16 @@ hipError_t launch_delta_apply(const void* msg, size_t msg_capacity, const gs_gro
                               int32_t n_rows, int32_t max_rows, int32_t mode, uint32_t* prim_version,
                               gs_device_status* status, hipStream_t st);
 
+// tokens.hip
+hipError_t launch_rms_norm(const gs_norm_args& a, hipStream_t st);
+size_t rms_norm_bwd_ws_bytes(int32_t rows, int32_t cols);
+hipError_t launch_rms_norm_bwd(const gs_norm_bwd_args& a, void* ws, hipStream_t st);
+hipError_t launch_rotary(const gs_rotary_args& a, hipStream_t st);
+
+// attention.hip, attention_bwd.hip
+size_t attention_ws_bytes(const gs_attn& a);
+hipError_t launch_attention(const gs_attn& a, const gs_rows& out, float* lse, void* ws, hipStream_t st);
+size_t attention_bwd_ws_bytes(const gs_attn& a);
+hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* ws, hipStream_t st);
+
 }  // namespace gsmi

@@ -1,0 +1,462 @@
+// Token operators that a row's bytes bound: the root-mean-square norm with the
+// residual's addition (into the tokens' type or 8 bits), its gradient, and the
+// rotation by position.
+#include <cmath>
+#include <algorithm>
+
+#include "common.h"
+#include "internal.h"
+#include "vec16.h"
+
+namespace gsmi {
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// Norm.  A row is read once, kept in registers as floats, reduced, and written:
+// s = x + residual, y = s w / sqrt(mean s^2 + eps).  Bound by HBM bytes.
+// WAVES waves share a row; thread t of them owns the 16-byte pieces t, t + 64
+// WAVES, ... (E elements in registers).  One wave a row needs no barrier and is
+// taken while a row fits 32 elements a lane; longer rows take four.
+// ---------------------------------------------------------------------------
+
+template <int WAVES>
+__device__ __forceinline__ float row_sum(float v, float* part) {
+    v = wave_sum(v);
+    if (WAVES == 1) return v;
+    const int w = threadIdx.x / GS_WAVE;
+    if (lane_id() == 0) part[w] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) v += part[i];
+    __syncthreads();
+    return v;
+}
+
+// Maximum over the lanes that own one block of GS_NORM_BLOCK columns: 16 lanes
+// of 16-bit pieces, 32 of fp32 pieces (adjacent lanes, a block starts at a
+// multiple of its lanes).
+template <int LANES>
+__device__ __forceinline__ float block_max(float v) {
+#pragma unroll
+    for (int d = 1; d < LANES; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, GS_WAVE));
+    return v;
+}
+
+template <typename T, bool WHOLE, int WAVES, int E>
+__global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
+    constexpr int N = Piece<T>::N, CH = E / N, TPR = WAVES * GS_WAVE, RPB = GS_BLOCK / TPR;
+    __shared__ float part[GS_BLOCK / GS_WAVE];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (RPB > 1 && row >= a.rows) return;      // whole waves; RPB 1 launches no such row
+    const T* __restrict__ x = static_cast<const T*>(a.x) + row * a.ld_x;
+    const T* __restrict__ r = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_residual : nullptr;
+    float s[CH][N];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * TPR + t) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[c][i] = 0.0f;
+        if (col < a.cols) load_piece<T, WHOLE>(x + col, a.cols - col, s[c]);
+    }
+    if (r) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * TPR + t) * N;
+            if (col >= a.cols) continue;
+            float f[N];
+            load_piece<T, WHOLE>(r + col, a.cols - col, f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[c][i] += f[i];
+        }
+    }
+    float ss = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < N; ++i) ss = fmaf(s[c][i], s[c][i], ss);
+    ss = row_sum<WAVES>(ss, part);
+    const float rho = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+    if (a.total) {
+        T* __restrict__ o = static_cast<T*>(a.total) + row * a.ld_total;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * TPR + t) * N;
+            if (col < a.cols) store_piece<T, WHOLE>(o + col, a.cols - col, s[c]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * TPR + t) * N;
+        float w[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = WHOLE ? (col < a.cols ? a.weight[col + i] : 0.0f)
+                                                 : (col + i < a.cols ? a.weight[col + i] : 0.0f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[c][i] *= rho * w[i];
+        if (a.y && col < a.cols)
+            store_piece<T, WHOLE>(static_cast<T*>(a.y) + row * a.ld_y + col, a.cols - col, s[c]);
+    }
+    if (a.q == nullptr) return;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * TPR + t) * N;
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(s[c][i]));
+        m = block_max<GS_NORM_BLOCK / N>(m);
+        if (col >= a.cols) continue;           // below: no lane exchange
+        const float scale = m > 0.0f ? fmaxf(m / 448.0f, 1.17549435e-38f) : 1.0f;
+        const float inv = 1.0f / scale;
+        if (col % GS_NORM_BLOCK == 0) a.q_scale[row * a.ld_scale + col / GS_NORM_BLOCK] = scale;
+        uint32_t b[N / 4];
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            int v = 0;
+            v = __builtin_amdgcn_cvt_pk_fp8_f32(s[c][i] * inv, s[c][i + 1] * inv, v, false);
+            v = __builtin_amdgcn_cvt_pk_fp8_f32(s[c][i + 2] * inv, s[c][i + 3] * inv, v, true);
+            b[i / 4] = (uint32_t)v;
+        }
+        uint8_t* __restrict__ q = a.q + row * a.ld_q + col;
+        if (WHOLE) {
+            if (N == 8) *reinterpret_cast<uint2*>(q) = make_uint2(b[0], b[N / 4 - 1]);
+            else *reinterpret_cast<uint32_t*>(q) = b[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (col + i < a.cols) q[i] = (uint8_t)(b[i / 4] >> (8 * (i % 4)));
+        }
+    }
+}
+
+// Gradient of the norm: dx = r (g - n mean(g n)) + dtotal with g = dy w, n =
+// total r, one read of dy, total and dtotal.  Every workgroup walks rows in
+// steps of the grid and keeps dy n of its columns in registers; it writes one
+// row of partial sums, and k_norm_dweight adds those in ascending order.
+// PARTS rows of partial sums in ws: the grid, set by kNormParts.
+constexpr int kNormParts = 512;                // two workgroups a compute unit
+
+inline int norm_parts(int32_t rows, int rpb) {
+    const int64_t b = ((int64_t)rows + rpb - 1) / rpb;
+    return (int)(b < kNormParts ? (b < 1 ? 1 : b) : kNormParts);
+}
+
+template <typename T, bool WHOLE, int WAVES, int E>
+__global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(gs_norm_bwd_args a,
+                                                                               float* __restrict__ parts) {
+    constexpr int N = Piece<T>::N, CH = E / N, TPR = WAVES * GS_WAVE, RPB = WAVES == 1 ? 4 : 1;
+    __shared__ float part[16];
+    __shared__ float comb[RPB > 1 ? RPB * GS_WAVE * N : 1];
+    const int t = threadIdx.x % TPR;
+    float dw[CH][N], w[CH][N];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * TPR + t) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            dw[c][i] = 0.0f;
+            w[c][i] = col + i < a.cols ? a.weight[col + i] : 0.0f;
+        }
+    }
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+        const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
+        const T* tot = static_cast<const T*>(a.total) + row * a.ld_total;
+        float s[CH][N], g[CH][N];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * TPR + t) * N;
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[c][i] = g[c][i] = 0.0f;
+            if (col < a.cols) {
+                load_piece<T, WHOLE>(tot + col, a.cols - col, s[c]);
+                load_piece<T, WHOLE>(dy + col, a.cols - col, g[c]);
+            }
+        }
+        float ss = 0.0f, gs = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ss = fmaf(s[c][i], s[c][i], ss);
+                gs = fmaf(g[c][i] * w[c][i], s[c][i], gs);
+            }
+        ss = row_sum<WAVES>(ss, part);
+        gs = row_sum<WAVES>(gs, part);
+        const float r = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+        const float mean = gs * r / (float)a.cols;         // mean of g n
+        T* dx = static_cast<T*>(a.dx) + row * a.ld_dx;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * TPR + t) * N;
+            if (col >= a.cols) continue;
+            float d[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) d[i] = 0.0f;
+            if (a.dtotal)
+                load_piece<T, WHOLE>(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, a.cols - col, d);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float n = s[c][i] * r;
+                dw[c][i] = fmaf(g[c][i], n, dw[c][i]);
+                d[i] += r * (g[c][i] * w[c][i] - n * mean);
+            }
+            store_piece<T, WHOLE>(dx + col, a.cols - col, d);
+        }
+    }
+    float* __restrict__ out = parts + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * TPR + t) * N;
+        if (RPB > 1) {                                     // the four waves' rows, in wave order
+            float* mine = comb + threadIdx.x * N;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) mine[i] = dw[c][i];
+            __syncthreads();
+            for (int k = threadIdx.x; k < GS_WAVE * N; k += GS_BLOCK) {
+                float v = 0.0f;
+#pragma unroll
+                for (int u = 0; u < RPB; ++u) v += comb[u * GS_WAVE * N + k];
+                if (c * TPR * N + k < a.cols) out[c * TPR * N + k] = v;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (col + i < a.cols) out[col + i] = dw[c][i];
+        }
+    }
+}
+
+// Sum of the partial rows, a column each: 64 columns by 16 slices of the rows
+// in a workgroup, then the slices in ascending order.
+__global__ void __launch_bounds__(1024) k_norm_dweight(const float* __restrict__ parts, int n, int cols,
+                                                       float* __restrict__ dweight) {
+    __shared__ float sum[16][GS_WAVE];
+    const int l = threadIdx.x % GS_WAVE, w = threadIdx.x / GS_WAVE;
+    const int col = blockIdx.x * GS_WAVE + l;
+    const int per = (n + 15) / 16;
+    float v = 0.0f;
+    if (col < cols)
+        for (int i = w * per; i < n && i < (w + 1) * per; ++i) v += parts[(int64_t)i * cols + col];
+    sum[w][l] = v;
+    __syncthreads();
+    if (w == 0 && col < cols) {
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v += sum[i][l];
+        dweight[col] = v;
+    }
+}
+
+__global__ void k_zero_f32(float* p, int n) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) p[i] = 0.0f;
+}
+
+template <typename T>
+bool whole(const void* p, int64_t ld, int bytes) {
+    return p == nullptr || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && (ld * (int64_t)sizeof(T)) % bytes == 0);
+}
+
+template <typename T, bool WHOLE>
+hipError_t norm_go(const gs_norm_args& a, hipStream_t st) {
+    const uint32_t by4 = div_up(a.rows, 4);
+    if (a.cols <= 1024) k_rms_norm<T, WHOLE, 1, 16><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 2048) k_rms_norm<T, WHOLE, 1, 32><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 8192) k_rms_norm<T, WHOLE, 4, 32><<<a.rows, GS_BLOCK, 0, st>>>(a);
+    else k_rms_norm<T, WHOLE, 4, 64><<<a.rows, GS_BLOCK, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_type(const gs_norm_args& a, hipStream_t st) {
+    const bool w = a.cols % Piece<T>::N == 0 && whole<T>(a.x, a.ld_x, 16) && whole<T>(a.residual, a.ld_residual, 16) &&
+                   whole<T>(a.total, a.ld_total, 16) && whole<T>(a.y, a.ld_y, 16) &&
+                   whole<uint8_t>(a.q, a.ld_q, Piece<T>::N);
+    return w ? norm_go<T, true>(a, st) : norm_go<T, false>(a, st);
+}
+
+template <typename T, bool WHOLE>
+hipError_t norm_bwd_go(const gs_norm_bwd_args& a, float* parts, hipStream_t st) {
+    int n = norm_parts(a.rows, 1);
+    if (a.cols <= 2048) {
+        n = norm_parts(a.rows, 4);
+        if (a.cols <= 1024) k_rms_norm_bwd<T, WHOLE, 1, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
+        else k_rms_norm_bwd<T, WHOLE, 1, 32><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    } else if (a.cols <= 4096) {
+        k_rms_norm_bwd<T, WHOLE, 4, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    } else {
+        k_rms_norm_bwd<T, WHOLE, 16, 16><<<n, 1024, 0, st>>>(a, parts);
+    }
+    k_norm_dweight<<<div_up(a.cols, GS_WAVE), 1024, 0, st>>>(parts, n, a.cols, a.dweight);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_bwd_type(const gs_norm_bwd_args& a, float* parts, hipStream_t st) {
+    const bool w = a.cols % Piece<T>::N == 0 && whole<T>(a.dy, a.ld_dy, 16) && whole<T>(a.total, a.ld_total, 16) &&
+                   whole<T>(a.dtotal, a.ld_dtotal, 16) && whole<T>(a.dx, a.ld_dx, 16);
+    return w ? norm_bwd_go<T, true>(a, parts, st) : norm_bwd_go<T, false>(a, parts, st);
+}
+
+// ---------------------------------------------------------------------------
+// Rotation by position.  Bound by HBM bytes: every element is read and written
+// once.  A workgroup takes `per` tokens: their cosines and sines (one fp64
+// product, one reduction and one sincos a pair) go to LDS once and serve every
+// head of both tensors; then each thread turns V pairs at a time, which are
+// two V-element pieces of the head in either layout, and copies what is left
+// of the heads.
+// ---------------------------------------------------------------------------
+
+constexpr int kRotTrig = 2048;                 // pairs of a workgroup's tokens in LDS (16 KB)
+
+struct RotArgs {
+    gs_rotary_args a;
+    int per;                                   // tokens of a workgroup
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load_some(const T* p, float* f) {
+    typedef T vec __attribute__((ext_vector_type(V)));
+    if (V == 1) {
+        f[0] = (float)p[0];
+    } else {
+        const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = (float)v[i];
+    }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_some(T* p, const float* f) {
+    typedef T vec __attribute__((ext_vector_type(V)));
+    if (V == 1) {
+        p[0] = (T)f[0];
+    } else {
+        vec v;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (T)f[i];
+        *reinterpret_cast<vec*>(p) = v;
+    }
+}
+
+template <typename T, int V, bool INTER>
+__global__ void __launch_bounds__(GS_BLOCK) k_rotary(RotArgs ra) {
+    const gs_rotary_args& a = ra.a;
+    __shared__ __attribute__((aligned(16))) float2 trig[kRotTrig];
+    const int t0 = blockIdx.x * ra.per;
+    const int n = min(ra.per, a.tokens - t0);
+    const int P = a.pairs;
+    for (int i = threadIdx.x; i < n * P; i += GS_BLOCK) {
+        const int t = i / P, j = i - t * P;
+        int axis = 0;
+        if (j >= a.axis_pairs[0]) axis = 1;
+        if (axis == 1 && j >= a.axis_pairs[0] + a.axis_pairs[1]) axis = 2;
+        const double turns = (double)a.pos[(int64_t)(t0 + t) * a.ld_pos + axis] * (double)a.freq[j] *
+                             0.15915494309189533577;
+        float sn, cs;
+        sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+        trig[i] = make_float2(a.amplitude * cs, a.amplitude * (a.inverse ? -sn : sn));
+    }
+    __syncthreads();
+    const int turn = P / V, rest = (a.dim - 2 * P + V - 1) / V, items = turn + rest;
+#pragma unroll 1
+    for (int k = 0; k < a.n_tensors; ++k) {
+        const bool same = a.in[k].ptr == a.out[k].ptr;     // in place: nothing to copy
+        const int used = same ? turn : items;
+        const int each = a.heads[k] * used;
+        const T* in = static_cast<const T*>(a.in[k].ptr);
+        T* out = static_cast<T*>(a.out[k].ptr);
+        for (int i = threadIdx.x; i < n * each; i += GS_BLOCK) {
+            const int t = i / each, h = (i - t * each) / used, m = i - t * each - h * used;
+            const T* p = in + (int64_t)(t0 + t) * a.in[k].ld_row + (int64_t)h * a.in[k].ld_head;
+            T* o = out + (int64_t)(t0 + t) * a.out[k].ld_row + (int64_t)h * a.out[k].ld_head;
+            if (m < turn) {
+                const int j = m * V, e0 = INTER ? 2 * j : j, e1 = INTER ? 2 * j + V : P + j;
+                float u[2 * V], y[2 * V];
+                load_some<T, V>(p + e0, u);
+                load_some<T, V>(p + e1, u + V);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float2 cs = trig[t * P + j + v];
+                    const int ia = INTER ? 2 * v : v, ib = INTER ? 2 * v + 1 : V + v;
+                    y[ia] = u[ia] * cs.x - u[ib] * cs.y;
+                    y[ib] = u[ia] * cs.y + u[ib] * cs.x;
+                }
+                store_some<T, V>(o + e0, y);
+                store_some<T, V>(o + e1, y + V);
+            } else {
+                const int e = 2 * P + (m - turn) * V;
+                float u[V];
+                load_some<T, V>(p + e, u);
+                store_some<T, V>(o + e, u);
+            }
+        }
+    }
+}
+
+template <typename T, int V>
+hipError_t rotary_go(const RotArgs& r, hipStream_t st) {
+    const uint32_t grid = div_up(r.a.tokens, r.per);
+    if (r.a.interleaved) k_rotary<T, V, true><<<grid, GS_BLOCK, 0, st>>>(r);
+    else k_rotary<T, V, false><<<grid, GS_BLOCK, 0, st>>>(r);
+    return hipGetLastError();
+}
+
+// Whether every V-element piece that the kernel touches is aligned to its size.
+template <typename T>
+bool pieces(const gs_rotary_args& a, int V) {
+    if (a.pairs % V != 0 || a.dim % V != 0) return false;
+    for (int i = 0; i < a.n_tensors; ++i)
+        for (const gs_rows* r : {&a.in[i], &a.out[i]})
+            if (!whole<T>(r->ptr, r->ld_row, V * (int)sizeof(T)) || !whole<T>(r->ptr, r->ld_head, V * (int)sizeof(T)))
+                return false;
+    return true;
+}
+
+template <typename T>
+hipError_t rotary_type(const gs_rotary_args& a, hipStream_t st) {
+    RotArgs r;
+    r.a = a;
+    // tokens of a workgroup: about eight pieces a thread, as many as the
+    // cosines' LDS holds, and enough workgroups to fill the chip
+    const int64_t row = (int64_t)(a.heads[0] + (a.n_tensors > 1 ? a.heads[1] : 0)) * a.dim / (2 * Piece<T>::N) + 1;
+    int64_t per = std::max<int64_t>(1, 2048 / row);
+    if (a.pairs > 0) per = std::min<int64_t>(per, kRotTrig / a.pairs);
+    per = std::min<int64_t>(per, std::max<int64_t>(1, a.tokens / 1024));
+    r.per = (int)std::max<int64_t>(1, per);
+    constexpr int N = Piece<T>::N;
+    if (pieces<T>(a, N)) return rotary_go<T, N>(r, st);
+    if (N > 4 && pieces<T>(a, 4)) return rotary_go<T, 4>(r, st);
+    return rotary_go<T, 1>(r, st);
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const gs_norm_args& a, hipStream_t st) {
+    if (a.dtype == GS_F32) return norm_type<float>(a, st);
+    return a.dtype == GS_BF16 ? norm_type<bf16_t>(a, st) : norm_type<f16_t>(a, st);
+}
+
+size_t rms_norm_bwd_ws_bytes(int32_t rows, int32_t cols) {
+    return align256((size_t)norm_parts(rows, cols <= 2048 ? 4 : 1) * (size_t)cols * 4);
+}
+
+hipError_t launch_rms_norm_bwd(const gs_norm_bwd_args& a, void* ws, hipStream_t st) {
+    float* parts = static_cast<float*>(ws);
+    if (a.rows == 0) {
+        k_zero_f32<<<div_up(a.cols, GS_BLOCK), GS_BLOCK, 0, st>>>(a.dweight, a.cols);
+        return hipGetLastError();
+    }
+    if (a.dtype == GS_F32) return norm_bwd_type<float>(a, parts, st);
+    return a.dtype == GS_BF16 ? norm_bwd_type<bf16_t>(a, parts, st) : norm_bwd_type<f16_t>(a, parts, st);
+}
+
+hipError_t launch_rotary(const gs_rotary_args& a, hipStream_t st) {
+    if (a.dtype == GS_F32) return rotary_type<float>(a, st);
+    return a.dtype == GS_BF16 ? rotary_type<bf16_t>(a, st) : rotary_type<f16_t>(a, st);
+}
+
+}  // namespace gsmi

@@ -30,6 +30,9 @@ GS_PRED_U32_NONZERO, GS_PRED_U8_NONZERO, GS_PRED_BITMAP, GS_PRED_U8_NONZERO_CLEA
 GS_APPLY_ADD, GS_APPLY_OVERWRITE = 0, 1
 GS_DEV_PAIR_OVERFLOW, GS_DEV_MSG_OVERFLOW, GS_DEV_MSG_MISMATCH, GS_DEV_MSG_ORDER = 1, 2, 4, 8
 GS_MSG_MAGIC = 0x47534D31
+GS_F32, GS_BF16, GS_F16 = 0, 1, 2
+GS_ROPE_PLAIN, GS_ROPE_LINEAR, GS_ROPE_BASE, GS_ROPE_PARTS = 0, 1, 2, 3
+GS_NORM_BLOCK, GS_NORM_MAX_COLS, GS_ROTARY_MAX_DIM, GS_ATTN_MAX_DIM = 128, 16384, 512, 128
 GS_MAX_GROUPS = 8
 
 
@@ -72,6 +75,38 @@ class gs_gate_result(ctypes.Structure):
     _fields_ = [("admit", u32), ("reason", u32), ("n_read", u32), ("n_delayed", u32), ("n_active", u32),
                 ("n_missing", u32), ("n_second", u32), ("reserved", u32), ("rho", ctypes.c_double),
                 ("mean_g", ctypes.c_double), ("max_g", ctypes.c_double), ("threshold", ctypes.c_double)]
+
+
+class gs_rows(ctypes.Structure):
+    _fields_ = [("ptr", P), ("ld_row", i64), ("ld_head", i64)]
+
+
+class gs_norm_args(ctypes.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("dtype", i32), ("eps", f32), ("x", P), ("residual", P), ("weight", P),
+                ("total", P), ("y", P), ("q", P), ("q_scale", P), ("ld_x", i64), ("ld_residual", i64),
+                ("ld_total", i64), ("ld_y", i64), ("ld_q", i64), ("ld_scale", i64)]
+
+
+class gs_norm_bwd_args(ctypes.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("dtype", i32), ("eps", f32), ("dy", P), ("total", P), ("dtotal", P),
+                ("weight", P), ("dx", P), ("dweight", P), ("ld_dy", i64), ("ld_total", i64), ("ld_dtotal", i64),
+                ("ld_dx", i64)]
+
+
+class gs_rotary_args(ctypes.Structure):
+    _fields_ = [("dtype", i32), ("tokens", i32), ("dim", i32), ("pairs", i32), ("n_axes", i32), ("axis_pairs", i32 * 3),
+                ("interleaved", i32), ("inverse", i32), ("amplitude", f32), ("pos", P), ("ld_pos", i64), ("freq", P),
+                ("n_tensors", i32), ("heads", i32 * 2), ("inp", gs_rows * 2), ("out", gs_rows * 2)]
+
+
+class gs_attn(ctypes.Structure):
+    _fields_ = [("dtype", i32), ("n_q", i32), ("n_k", i32), ("n_seg", i32), ("heads", i32), ("kv_heads", i32),
+                ("dim", i32), ("left", i32), ("right", i32), ("scale", f32), ("cu_q", P), ("cu_k", P), ("key_on", P),
+                ("q", gs_rows), ("k", gs_rows), ("v", gs_rows)]
+
+
+class gs_attn_grads(ctypes.Structure):
+    _fields_ = [("out", gs_rows), ("dout", gs_rows), ("dq", gs_rows), ("dk", gs_rows), ("dv", gs_rows), ("lse", P)]
 
 
 def scope_words(n) -> int:
@@ -119,6 +154,17 @@ _lib.gs_scope_from_ids.argtypes = [P, P, i32, i32, i32, P, P]
 _lib.gs_scope_from_pred.argtypes = [i32, P, i32, i32, P, P]
 _lib.gs_scope_conflicts.argtypes = [P, P, P, P, i32, P, P, P, P, P, P, P, P, sz, P]
 _lib.gs_admission_gate.argtypes = [P, P, ctypes.POINTER(gs_gate_args), i32, P, P, sz, P]
+_lib.gs_rms_norm.argtypes = [ctypes.POINTER(gs_norm_args), P]
+_lib.gs_rms_norm_bwd_ws_bytes.restype = sz
+_lib.gs_rms_norm_bwd_ws_bytes.argtypes = [i32, i32]
+_lib.gs_rms_norm_bwd.argtypes = [ctypes.POINTER(gs_norm_bwd_args), P, sz, P]
+_lib.gs_rotary.argtypes = [ctypes.POINTER(gs_rotary_args), P]
+_lib.gs_rotary_freqs.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                 ctypes.c_double, P, P]
+_lib.gs_attention_ws_bytes.restype = sz
+_lib.gs_attention_ws_bytes.argtypes = [ctypes.POINTER(gs_attn), i32]
+_lib.gs_attention.argtypes = [ctypes.POINTER(gs_attn), ctypes.POINTER(gs_rows), P, P, sz, P]
+_lib.gs_attention_bwd.argtypes = [ctypes.POINTER(gs_attn), ctypes.POINTER(gs_attn_grads), P, sz, P]
 _lib.gs_rlg_build.argtypes = [i32, i32, P, P, i32, i32, P, P, P, ctypes.c_int64, P]
 _lib.gs_lp_partition.argtypes = [i32, P, P, P, P, i32, i32, P, P, P]
 _lib.gs_sds_order.argtypes = [i32, P, i32, P, P, P, P, i32, P, P, P, P, P, P]
@@ -126,7 +172,8 @@ for _name in ("gs_project", "gs_visible_set", "gs_visible_set_noalloc", "gs_bin_
               "gs_raster_bwd_pixels", "gs_raster_bwd_project", "gs_sparse_adam", "gs_sparse_adam_publish",
               "gs_delta_pack", "gs_delta_apply", "gs_scope_from_ids", "gs_scope_from_pred", "gs_scope_conflicts",
               "gs_admission_gate", "gs_publish_commit", "gs_raster_bwd_project_accum", "gs_raster_fwd_l1",
-              "gs_rlg_build", "gs_lp_partition", "gs_sds_order"):
+              "gs_rlg_build", "gs_lp_partition", "gs_sds_order", "gs_rms_norm", "gs_rms_norm_bwd", "gs_rotary",
+              "gs_rotary_freqs", "gs_attention", "gs_attention_bwd"):
     getattr(_lib, _name).restype = i32
 
 EXPORTS = ["gs_abi_version", "gs_status_string", "gs_last_error", "gs_workspace_bytes", "gs_delta_msg_bytes",
@@ -134,7 +181,9 @@ EXPORTS = ["gs_abi_version", "gs_status_string", "gs_last_error", "gs_workspace_
            "gs_raster_bwd", "gs_raster_bwd_pixels", "gs_raster_bwd_project", "gs_sparse_adam", "gs_sparse_adam_publish",
            "gs_delta_pack", "gs_delta_apply", "gs_scope_from_ids", "gs_scope_from_pred", "gs_scope_conflicts",
            "gs_admission_gate", "gs_publish_commit", "gs_raster_bwd_project_accum", "gs_raster_fwd_l1",
-           "gs_rlg_build", "gs_lp_partition", "gs_sds_order"]
+           "gs_rlg_build", "gs_lp_partition", "gs_sds_order", "gs_rms_norm", "gs_rms_norm_bwd_ws_bytes",
+           "gs_rms_norm_bwd", "gs_rotary", "gs_rotary_freqs", "gs_attention_ws_bytes", "gs_attention",
+           "gs_attention_bwd"]
 
 
 class GsmiError(RuntimeError):
@@ -420,6 +469,128 @@ def gate_result_from(buf) -> gs_gate_result:
     if hasattr(buf, "cpu"):
         buf = buf.detach().cpu().numpy().tobytes()
     return gs_gate_result.from_buffer_copy(bytes(buf)[:ctypes.sizeof(gs_gate_result)])
+
+
+# ---- token operators ----------------------------------------------------------
+
+def _ws(ws):
+    return (ptr(ws), ws.numel() * ws.element_size()) if ws is not None else (None, 0)
+
+
+def token_dtype(t) -> int:
+    import torch
+    d = {torch.float32: GS_F32, torch.bfloat16: GS_BF16, torch.float16: GS_F16}
+    if t.dtype not in d:
+        raise ValueError("tokens are float32, bfloat16 or float16, not %s" % t.dtype)
+    return d[t.dtype]
+
+
+def make_rows(t) -> gs_rows:
+    """A [rows, heads, dim] tensor whose heads' elements are contiguous."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("a token matrix is [rows, heads, dim] with contiguous elements, not %s with strides %s"
+                         % (tuple(t.shape), t.stride()))
+    return gs_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _ld(t, rows, cols, what, like=None):
+    """Row stride of a [rows, cols] tensor with contiguous rows (0 for None)."""
+    if t is None:
+        return 0
+    if tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError("%s is [%d, %d] with contiguous rows, not %s with strides %s"
+                         % (what, rows, cols, tuple(t.shape), t.stride()))
+    if like is not None and t.dtype != like.dtype:
+        raise ValueError("%s is %s, not %s" % (what, like.dtype, t.dtype))
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def gs_rms_norm(x, weight, eps, y=None, residual=None, total=None, q=None, q_scale=None, stream=None):
+    rows, cols = x.shape
+    blocks = -(-cols // GS_NORM_BLOCK)
+    a = gs_norm_args(rows, cols, token_dtype(x), float(eps), x.data_ptr(), ptr(residual), ptr(weight), ptr(total),
+                     ptr(y), ptr(q), ptr(q_scale), _ld(x, rows, cols, "x"), _ld(residual, rows, cols, "residual", x),
+                     _ld(total, rows, cols, "total", x), _ld(y, rows, cols, "y", x), _ld(q, rows, cols, "q"),
+                     _ld(q_scale, rows, blocks, "q_scale"))
+    return _check("gs_rms_norm", _lib.gs_rms_norm(ctypes.byref(a), stream if stream is not None else current_stream()))
+
+
+def gs_rms_norm_bwd_ws_bytes(rows, cols) -> int:
+    return int(_lib.gs_rms_norm_bwd_ws_bytes(int(rows), int(cols)))
+
+
+def gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=None, stream=None):
+    rows, cols = total.shape
+    a = gs_norm_bwd_args(rows, cols, token_dtype(total), float(eps), dy.data_ptr(), total.data_ptr(), ptr(dtotal),
+                         ptr(weight), dx.data_ptr(), ptr(dweight), _ld(dy, rows, cols, "dy", total),
+                         _ld(total, rows, cols, "total"), _ld(dtotal, rows, cols, "dtotal", total),
+                         _ld(dx, rows, cols, "dx", total))
+    p, n = _ws(ws)
+    return _check("gs_rms_norm_bwd", _lib.gs_rms_norm_bwd(ctypes.byref(a), p, n,
+                                                          stream if stream is not None else current_stream()))
+
+
+def gs_rotary(inputs, outputs, pos, freq, axis_pairs, interleaved=False, inverse=False, amplitude=1.0, stream=None):
+    """inputs, outputs: one or two [tokens, heads, dim] tensors each; pos [tokens, axes] fp32."""
+    a = gs_rotary_args()
+    x = inputs[0]
+    a.dtype, a.tokens, a.dim = token_dtype(x), x.shape[0], x.shape[2]
+    a.n_axes = len(axis_pairs)
+    for i, n in enumerate(axis_pairs[:3]):
+        a.axis_pairs[i] = int(n)
+    a.pairs = sum(int(n) for n in axis_pairs)
+    a.interleaved, a.inverse, a.amplitude = int(interleaved), int(inverse), float(amplitude)
+    a.pos, a.ld_pos, a.freq = pos.data_ptr(), row_stride(pos), freq.data_ptr()
+    a.n_tensors = len(inputs)
+    if not 1 <= len(inputs) <= 2 or len(outputs) != len(inputs):
+        raise ValueError("one or two tensors, with an output each")
+    for i, (t, o) in enumerate(zip(inputs, outputs)):
+        if t.shape != o.shape or t.dtype != x.dtype or o.dtype != x.dtype or t.shape[0] != a.tokens or t.shape[2] != a.dim:
+            raise ValueError("tensors and outputs share tokens, dim and type; got %s -> %s" % (t.shape, o.shape))
+        a.heads[i], a.inp[i], a.out[i] = t.shape[1], make_rows(t), make_rows(o)
+    return _check("gs_rotary", _lib.gs_rotary(ctypes.byref(a), stream if stream is not None else current_stream()))
+
+
+def gs_rotary_freqs(pairs, base=10000.0, scaling=GS_ROPE_PLAIN, factor=1.0, trained=0.0, slow=1.0, fast=32.0):
+    """Returns (freq [pairs] numpy float32, amplitude)."""
+    import numpy as np
+    freq = np.zeros(max(int(pairs), 1), np.float32)
+    amp = ctypes.c_float(1.0)
+    _check("gs_rotary_freqs", _lib.gs_rotary_freqs(int(pairs), float(base), int(scaling), float(factor), float(trained),
+                                                   float(slow), float(fast), ctypes.c_void_p(freq.ctypes.data),
+                                                   ctypes.byref(amp)))
+    return freq[:int(pairs)], float(amp.value)
+
+
+def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-1, right=-1) -> gs_attn:
+    if k.shape != v.shape or k.shape[2] != q.shape[2] or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k, v do not fit: %s, %s, %s" % (q.shape, k.shape, v.shape))
+    if cu_q is not None:
+        n_seg = cu_q.numel() - 1
+        if cu_k is None or cu_k.numel() != cu_q.numel() or "int32" not in str(cu_q.dtype) or "int32" not in str(cu_k.dtype):
+            raise ValueError("cu_q and cu_k are int32 of the same length")
+    if key_on is not None and (key_on.numel() != k.shape[0] or key_on.element_size() != 1):
+        raise ValueError("key_on is one byte per key")
+    return gs_attn(token_dtype(q), q.shape[0], k.shape[0], int(n_seg), q.shape[1], k.shape[1], q.shape[2], int(left),
+                   int(right), float(scale), ptr(cu_q), ptr(cu_k), ptr(key_on), make_rows(q), make_rows(k),
+                   make_rows(v))
+
+
+def gs_attention_ws_bytes(attn: gs_attn, backward=False) -> int:
+    return int(_lib.gs_attention_ws_bytes(ctypes.byref(attn), int(backward)))
+
+
+def gs_attention(attn: gs_attn, out, lse, ws=None, stream=None):
+    p, n = _ws(ws)
+    return _check("gs_attention", _lib.gs_attention(ctypes.byref(attn), ctypes.byref(make_rows(out)), ptr(lse), p, n,
+                                                    stream if stream is not None else current_stream()))
+
+
+def gs_attention_bwd(attn: gs_attn, out, lse, dout, dq, dk, dv, ws, stream=None):
+    g = gs_attn_grads(make_rows(out), make_rows(dout), make_rows(dq), make_rows(dk), make_rows(dv), lse.data_ptr())
+    p, n = _ws(ws)
+    return _check("gs_attention_bwd", _lib.gs_attention_bwd(ctypes.byref(attn), ctypes.byref(g), p, n,
+                                                            stream if stream is not None else current_stream()))
 
 
 def raw():

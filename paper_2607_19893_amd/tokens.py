@@ -1,0 +1,164 @@
+"""Token operators for a network that writes rows of the pool: the norm with
+the residual's addition, the rotation by position and attention over ragged
+segments, each with its gradient.
+
+The functions allocate their outputs and workspaces with torch on the current
+stream and call the gs_* entry points there; every step runs in libgsmi's
+kernels.  `RmsNorm`, `Rotary` and `Attention` put them under torch's autograd.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import gsmi
+
+
+class Normed(NamedTuple):
+    """What rms_norm returns: y (None in 8 bits), the sum (x itself without a
+    residual), and with eight_bit the rows as float8_e4m3fn and their scales
+    [rows, ceil(cols / 128)]: y ~ q * scale."""
+    y: Optional[torch.Tensor]
+    total: torch.Tensor
+    q: Optional[torch.Tensor] = None
+    scale: Optional[torch.Tensor] = None
+
+
+def _same_device(*tensors):
+    d = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != d:
+            raise ValueError("tensors on %s and %s" % (d, t.device))
+    if d.type != "cuda":
+        raise ValueError("tokens live on the GPU, not on %s" % d)
+
+
+def _fp32(t, n, what):
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s is %d contiguous float32 values" % (what, n))
+
+
+def _workspace(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None, eight_bit=False) -> Normed:
+    """s = x + residual; y = s * weight / sqrt(mean(s^2) + eps), for x [rows, cols]."""
+    _same_device(x, weight, residual)
+    rows, cols = x.shape
+    _fp32(weight, cols, "weight")
+    total = torch.empty_like(x, memory_format=torch.contiguous_format) if residual is not None else None
+    y = q = scale = None
+    if eight_bit:
+        q = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
+        scale = torch.empty(rows, -(-cols // gsmi.GS_NORM_BLOCK), dtype=torch.float32, device=x.device)
+    else:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    gsmi.gs_rms_norm(x, weight, eps, y=y, residual=residual, total=total, q=q, q_scale=scale)
+    return Normed(y, x if total is None else total, q, scale)
+
+
+def rms_norm_backward(dy, total, weight, eps=1e-6, dtotal=None):
+    """(dx, dweight) of rms_norm; dx is the gradient of x and of residual."""
+    _same_device(dy, total, weight, dtotal)
+    rows, cols = total.shape
+    _fp32(weight, cols, "weight")
+    dx = torch.empty_like(total, memory_format=torch.contiguous_format)
+    dweight = torch.empty_like(weight)
+    ws = _workspace(gsmi.gs_rms_norm_bwd_ws_bytes(rows, cols), total.device)
+    gsmi.gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=dtotal)
+    return dx, dweight
+
+
+def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amplitude=1.0, inplace=False):
+    """Turns one or two [tokens, heads, dim] tensors by pos [tokens, axes]; returns them as a tuple."""
+    tensors = (tensors,) if isinstance(tensors, torch.Tensor) else tuple(tensors)
+    _same_device(*tensors, pos, freq)
+    if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape != (tensors[0].shape[0], len(axis_pairs)):
+        raise ValueError("pos is float32 [tokens, %d]" % len(axis_pairs))
+    _fp32(freq, sum(axis_pairs), "freq")
+    out = tensors if inplace else tuple(torch.empty_like(t, memory_format=torch.contiguous_format) for t in tensors)
+    gsmi.gs_rotary(tensors, out, pos, freq, axis_pairs, interleaved, inverse, amplitude)
+    return out
+
+
+def attention(q, k, v, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, left=-1, right=-1):
+    """(out, lse): q [n_q, heads, dim] over k, v [n_k, kv_heads, dim], segment by segment."""
+    _same_device(q, k, v, cu_q, cu_k, key_on)
+    a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+    gsmi.gs_attention(a, out, lse, _workspace(gsmi.gs_attention_ws_bytes(a), q.device))
+    return out, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, left=-1,
+                       right=-1):
+    """(dq, dk, dv) of attention, from its result and log sums."""
+    _same_device(q, k, v, dout, out, lse, cu_q, cu_k, key_on)
+    for t, what in ((dout, "dout"), (out, "out")):
+        if t.shape != q.shape or t.dtype != q.dtype:
+            raise ValueError("%s has q's shape and type" % what)
+    _fp32(lse, q.shape[0] * q.shape[1], "lse")
+    a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
+    dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
+    gsmi.gs_attention_bwd(a, out, lse, dout, dq, dk, dv, _workspace(gsmi.gs_attention_ws_bytes(a, True), q.device))
+    return dq, dk, dv
+
+
+class RmsNorm(torch.autograd.Function):
+    """RmsNorm.apply(x, residual or None, weight, eps) -> (y, total)."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        r = rms_norm(x, weight, eps, residual=residual)
+        total = r.total if residual is not None else x.view_as(x)
+        ctx.save_for_backward(total, weight)
+        ctx.eps, ctx.has_residual = eps, residual is not None
+        ctx.set_materialize_grads(False)
+        return r.y, total
+
+    @staticmethod
+    def backward(ctx, dy, dtotal):
+        total, weight = ctx.saved_tensors
+        if dy is None:
+            return dtotal, (dtotal if ctx.has_residual else None), None, None
+        dx, dw = rms_norm_backward(dy.contiguous(), total, weight, ctx.eps,
+                                   dtotal=None if dtotal is None else dtotal.contiguous())
+        return dx, (dx if ctx.has_residual else None), dw, None
+
+
+class Rotary(torch.autograd.Function):
+    """Rotary.apply(q, k, pos, freq, axis_pairs, interleaved, amplitude) -> (q, k)."""
+
+    @staticmethod
+    def forward(ctx, q, k, pos, freq, axis_pairs, interleaved, amplitude):
+        ctx.save_for_backward(pos, freq)
+        ctx.how = (axis_pairs, interleaved, amplitude)
+        return rotary((q, k), pos, freq, axis_pairs, interleaved=interleaved, amplitude=amplitude)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        pos, freq = ctx.saved_tensors
+        axis_pairs, interleaved, amplitude = ctx.how
+        dq, dk = rotary((dq.contiguous(), dk.contiguous()), pos, freq, axis_pairs, interleaved=interleaved,
+                        inverse=True, amplitude=amplitude)
+        return dq, dk, None, None, None, None, None
+
+
+class Attention(torch.autograd.Function):
+    """Attention.apply(q, k, v, how) -> (out, lse); `how` holds attention()'s keyword arguments."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, how):
+        out, lse = attention(q, k, v, **how)
+        ctx.save_for_backward(q, k, v, out, lse)
+        ctx.how = how
+        ctx.mark_non_differentiable(lse)
+        return out, lse
+
+    @staticmethod
+    def backward(ctx, dout, _):
+        q, k, v, out, lse = ctx.saved_tensors
+        return (*attention_backward(dout.contiguous(), q, k, v, out, lse, **ctx.how), None)
