@@ -35,40 +35,45 @@ struct FwdArgs {
 __device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, GS_WAVE)); }
 __device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, GS_WAVE); }
 
-// Where a row's results go: its part (splits > 1) or the output.
-template <typename T, int D>
-__device__ __forceinline__ void store_row(const FwdArgs& f, int token, int head, int split, const acc16 (&o)[D / 32],
-                                          float m, float l) {
-    const int h = lane_id() >> 5;
+__device__ __forceinline__ float row_scale(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l); }
+__device__ __forceinline__ float row_lse(float m, float l, float scale) {
+    return l == 0.0f ? -INFINITY : m * scale + kLn2 * log2f(l);
+}
+
+// Where a row's results go: its part of the keys (splits > 1) or the output.
+// The maximum is that of the raw products, the tile holds 32 elements of a row.
+__device__ __forceinline__ void store_sums(const FwdArgs& f, int token, int head, int split, float m, float l) {
     const int64_t row = (int64_t)token * f.a.heads + head;
+    if (lane_id() >= 32) return;
+    if (f.splits > 1) f.part_ml[(int64_t)split * f.a.n_q * f.a.heads + row] = make_float2(m, l);
+    else f.lse[row] = row_lse(m, l, f.a.scale);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_tile(const FwdArgs& f, int token, int head, int split, int d, const acc16& o,
+                                           float l) {
+    const int h = lane_id() >> 5;
     if (f.splits > 1) {
-        const int64_t at = (int64_t)split * f.a.n_q * f.a.heads + row;
-        if (h == 0) f.part_ml[at] = make_float2(m, l);
-        float* p = f.part_o + at * f.a.dim;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int c = 32 * d + 8 * g + 4 * h;
-                if (c < f.a.dim)
-                    *reinterpret_cast<float4*>(p + c) =
-                        make_float4(o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]);
-            }
-        return;
-    }
-    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);    // a NaN sum stays one
-    if (h == 0) f.lse[row] = l == 0.0f ? -INFINITY : m * f.a.scale + kLn2 * log2f(l);
-    T* p = static_cast<T*>(f.out) + (int64_t)token * f.o_row + (int64_t)head * f.o_head;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+        const int64_t row = (int64_t)token * f.a.heads + head;
+        float* p = f.part_o + ((int64_t)split * f.a.n_q * f.a.heads + row) * f.a.dim;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int c = 32 * d + 8 * g + 4 * h;
-            op4<T> v;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (T)(o[d][4 * g + i] * inv);
-            if (c < f.a.dim) *reinterpret_cast<op4<T>*>(p + c) = v;
+            if (c < f.a.dim)
+                *reinterpret_cast<float4*>(p + c) = make_float4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
         }
+        return;
+    }
+    const float inv = row_scale(l);                        // a NaN sum stays one
+    T* p = static_cast<T*>(f.out) + (int64_t)token * f.o_row + (int64_t)head * f.o_head;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int c = 32 * d + 8 * g + 4 * h;
+        op4<T> v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (T)(o[4 * g + i] * inv);
+        if (c < f.a.dim) *reinterpret_cast<op4<T>*>(p + c) = v;
+    }
 }
 
 // One step of the online softmax over a tile of 32 N keys: s (raw products,
@@ -83,13 +88,13 @@ __device__ __forceinline__ float softmax_step(acc16 (&s)[N], float c, float& m, 
         for (int i = 0; i < 16; ++i) t = fmaxf(t, s[k][i]);
     t = fmaxf(m, half_max(t));
     const float base = t == -INFINITY ? 0.0f : t * c;      // nothing admitted yet: exp2(-inf) = 0 below
-    const float alpha = exp2f(m * c - base);
+    const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
     float sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[k][i] = exp2f(fmaf(s[k][i], c, -base));
+            s[k][i] = __builtin_amdgcn_exp2f(fmaf(s[k][i], c, -base));
             sum += s[k][i];
         }
     l = l * alpha + sum;                                   // this half's keys; the halves meet at the end
@@ -100,18 +105,15 @@ __device__ __forceinline__ float softmax_step(acc16 (&s)[N], float c, float& m, 
 template <typename T, int D>
 __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
-    constexpr int PIECES = D / 8, LOADS = kKeys * PIECES / GS_BLOCK;       // 16-byte pieces of a tile a thread
-    __shared__ __attribute__((aligned(16))) T ks[kKeys * P];
-    __shared__ __attribute__((aligned(16))) T vs[kKeys * P];
-    __shared__ __attribute__((aligned(4))) uint8_t on[kKeys];
+    constexpr int G = 2;                           // products whose operands are read together
+    // two buffers: a step's tiles arrive while the step before computes
+    __shared__ __attribute__((aligned(16))) T ks0[kKeys * P], vs0[kKeys * P];
+    __shared__ __attribute__((aligned(16))) T ks1[kKeys * P], vs1[kKeys * P];
     const AttnArgs& a = f.a;
-    const int total = a.tiles * a.kv_heads * f.splits;
-    int id = chiplet_order(blockIdx.x, total);
-    if (id >= total) return;
-    const int split = id % f.splits;
-    id /= f.splits;
-    const int kvh = id / a.tiles;
-    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kRows, id - kvh * a.tiles);
+    const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, f.splits);
+    const int split = place.split, kvh = place.head;
+    // the last tiles first: with ordered keys they have the most to do
+    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kRows, a.tiles - 1 - place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -146,131 +148,350 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
         j1 = min(hi, j0 + per);
     }
 
+    TileLoader<T, P, kKeys> kl, vl;
+    kl.init(a.k_row, a.dim);
+    vl.init(a.v_row, a.dim);
+    const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
+    const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    auto fetch = [&](T* ks, T* vs, int j) {
+        uint32_t skip = 0;
+        if (a.key_on != nullptr) {
+            const int first = fresh(threadIdx.x) / kl.PIECES;
+#pragma unroll
+            for (int u = 0; u < kl.LOADS; ++u) {
+                const int key = j + first + u * (GS_BLOCK / kl.PIECES);
+                if (key < sg.nk && a.key_on[sg.k0 + key] == 0) skip |= 1u << u;
+            }
+        }
+        kl.load(ks, kbase + j * a.k_row, sg.nk - j, skip);
+        vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);
+    };
+
     const float c = a.scale * kLog2e;
     float m = -INFINITY, l = 0.0f;
     acc16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = acc16{};
 
-    for (int j = j0; j < j1; j += kKeys) {
-        __syncthreads();
+    Lanes at;
+    at.init<P>();
+    auto step = [&](const T* ks, const T* vs, int j) {
+        // operands are read a group of products ahead of their use; the
+        // barriers keep the compiler from reading more of them ahead, which
+        // would not fit the registers of two waves a SIMD
+        at.refresh();
+        acc16 s[2]{};
+        op8<T> x[2][G];
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int x = threadIdx.x + u * GS_BLOCK, row = x / PIECES, piece = x % PIECES;
-            const int key = j + row;
-            op8<T> kp{}, vp{};
-            if (key < sg.nk && 8 * piece < a.dim && (a.key_on == nullptr || a.key_on[sg.k0 + key])) {
-                kp = *reinterpret_cast<const op8<T>*>(static_cast<const T*>(a.k) + (int64_t)(sg.k0 + key) * a.k_row +
-                                                      (int64_t)kvh * a.k_head + 8 * piece);
-                vp = *reinterpret_cast<const op8<T>*>(static_cast<const T*>(a.v) + (int64_t)(sg.k0 + key) * a.v_row +
-                                                      (int64_t)kvh * a.v_head + 8 * piece);
+        for (int e = 0; e < G; ++e) x[0][e] = rows_operand<T, P>(ks, at, 0, e);
+#pragma unroll
+        for (int g = 0; g < 2 * KT / G; ++g) {
+            if (g + 1 < 2 * KT / G) {
+#pragma unroll
+                for (int e = 0; e < G; ++e)
+                    x[(g + 1) & 1][e] = rows_operand<T, P>(ks, at, ((g + 1) * G + e) / KT * 32, ((g + 1) * G + e) % KT);
             }
-            *reinterpret_cast<op8<T>*>(ks + piece_at<P>(row, piece)) = kp;
-            *reinterpret_cast<op8<T>*>(vs + piece_at<P>(row, piece)) = vp;
-        }
-        if (threadIdx.x < kKeys) {
-            const int key = j + threadIdx.x;
-            on[threadIdx.x] = key < sg.nk && (a.key_on == nullptr || a.key_on[sg.k0 + key]);
-        }
-        __syncthreads();
-        acc16 s[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            s[k] = acc16{};
-#pragma unroll
-            for (int t = 0; t < KT; ++t) s[k] = mfma(rows_operand<T, P>(ks, 32 * k, t), q[t], s[k]);
+            for (int e = 0; e < G; ++e) s[(g * G + e) / KT] = mfma(x[g & 1][e], q[(g * G + e) % KT], s[(g * G + e) / KT]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (a.key_on != nullptr || j < alo || j + kKeys > ahi) {
+            uint64_t seen = bits_between(klo - j, khi - j);
+            if (a.key_on != nullptr) {
+                const int key = j + fresh(lane);
+                seen &= __ballot(key < sg.nk && a.key_on[sg.k0 + min(key, sg.nk - 1)]);
+            }
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int at = 32 * k + 8 * g + 4 * h;
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>(on + at);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = j + at + e;
-                        if (key < klo || key >= khi || ((w >> (8 * e)) & 255u) == 0) s[k][4 * g + e] = -INFINITY;
-                    }
-                }
+                for (int e = 0; e < 16; ++e)
+                    if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[k][e] = -INFINITY;
+            }
         }
         const float alpha = softmax_step<2>(s, c, m, l);
+        if (__any(alpha != 1.0f)) {                // the maxima rise in the first steps, seldom later
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] *= alpha;
+            for (int d = 0; d < DT; ++d) o[d] *= alpha;
+        }
+        op8<T> y[2][DT];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int d = 0; d < DT; ++d) y[0][d] = columns_operand<T, P>(vs, at, 0, d);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const op8<T> p = tile_operand<T>(s[k], u);
+        for (int g = 0; g < 4; ++g) {
+            if (g < 3) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
-                    o[d] = mfma(columns_operand<T, P>(vs, 32 * k + 16 * u, 32 * d), p, o[d]);
+                for (int d = 0; d < DT; ++d) y[(g + 1) & 1][d] = columns_operand<T, P>(vs, at, 16 * (g + 1), d);
             }
+            const op8<T> p = tile_operand<T>(s[g / 2], g % 2);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = mfma(y[g & 1][d], p, o[d]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    if (j0 < j1) fetch(ks0, vs0, j0);
+    __syncthreads();                               // the fetched tiles are in LDS
+    for (int j = j0; j < j1; j += 2 * kKeys) {
+        if (j + kKeys < j1) fetch(ks1, vs1, j + kKeys);
+        step(ks0, vs0, j);
+        __syncthreads();
+        if (j + kKeys >= j1) break;
+        if (j + 2 * kKeys < j1) fetch(ks0, vs0, j + 2 * kKeys);
+        step(ks1, vs1, j + kKeys);
+        __syncthreads();
     }
     l = half_sum(l);
-    if (there) store_row<T, D>(f, token, head, split, o, m, l);
+    if (!there) return;
+    store_sums(f, token, head, split, m, l);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) store_tile<T>(f, token, head, split, d, o[d], l);
 }
 
-// Joins the parts of a row: 8 lanes... one wave a row, lanes over the elements.
-template <typename T>
-__global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
-    const int64_t rows = (int64_t)f.a.n_q * f.a.heads;
-    const int64_t row = (int64_t)blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE;
-    if (row >= rows) return;
-    const int lane = lane_id();
-    float m = -INFINITY;
-    for (int s = 0; s < f.splits; ++s) m = fmaxf(m, f.part_ml[s * rows + row].x);
-    const float c = f.a.scale * kLog2e, base = m == -INFINITY ? 0.0f : m * c;
-    float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int s = 0; s < f.splits; ++s) {
-        const float2 ml = f.part_ml[s * rows + row];
-        const float w = exp2f(ml.x * c - base);
-        const float* p = f.part_o + (s * rows + row) * f.a.dim;
-        l += ml.y * w;
-        if (2 * lane < f.a.dim) {
-            const float2 v = *reinterpret_cast<const float2*>(p + 2 * lane);
-            o0 += v.x * w;
-            o1 += v.y * w;
+// Few rows over many keys: a workgroup takes 32 rows and every wave of it its
+// own keys (32 a step, its waves' steps interleaved), with a running maximum and
+// sum of its own; the waves meet in LDS at the end.  The keys' bytes bound it,
+// so a step's keys go from memory straight into the operand's registers, its
+// values through a piece of LDS that only this wave touches (no barrier in the
+// loop), and both are fetched a step ahead.
+constexpr int kFewRows = 32;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_few(FwdArgs f) {
+    constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
+    constexpr int PIECES = D / 8, LOADS = 32 * PIECES / GS_WAVE, WAVES = GS_BLOCK / GS_WAVE;
+    __shared__ __attribute__((aligned(16))) T vs[WAVES][32 * P];
+    __shared__ float ml[2][WAVES][32];
+    __shared__ float half[WAVES][32 * 33];
+    const AttnArgs& a = f.a;
+    const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, f.splits);
+    const int split = place.split, kvh = place.head;
+    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kFewRows, place.tile);
+    const int rows = sg.nq * a.group, row0 = sg.tile * kFewRows;
+    if (row0 >= rows) return;
+    const int lane = lane_id(), h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
+    const int r = row0 + (lane & 31);
+    const bool there = r < rows;
+    const int i = (there ? r : rows - 1) / a.group;
+    const int token = sg.q0 + i, head = kvh * a.group + (there ? r : rows - 1) - i * a.group;
+    const int shift = sg.nk - sg.nq;
+
+    op8<T> q[KT];
+    {
+        const T* p = static_cast<const T*>(a.q) + (int64_t)token * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            const int c = 16 * t + 8 * h;
+            if (c < a.dim) q[t] = *reinterpret_cast<const op8<T>*>(p + c);
+            else q[t] = op8<T>{};
         }
     }
-    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+    int klo, khi, lo, hi, alo, ahi;
+    admitted(a, sg.nk, i + shift, i + shift, klo, khi);
+    const int last = min(row0 + kFewRows, rows) - 1;
+    admitted(a, sg.nk, row0 / a.group + shift, last / a.group + shift, lo, hi);
+    admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
+    int j0 = lo / 32 * 32, j1 = hi;
+    if (f.splits > 1) {
+        const int per = ((max(hi - j0, 0) + f.splits - 1) / f.splits + 127) / 128 * 128;
+        j0 += split * per;
+        j1 = min(hi, j0 + per);
+    }
+    const T* kbase = static_cast<const T*>(a.k) + (int64_t)kvh * a.k_head;
+    const T* vbase = static_cast<const T*>(a.v) + (int64_t)kvh * a.v_head;
+    op8<T> kp[KT], vp[LOADS];
+    auto fetch = [&](int j) {
+        const int key = j + (lane & 31);
+        const bool on = key < sg.nk && (a.key_on == nullptr || a.key_on[sg.k0 + key]);
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            const int c = 16 * t + 8 * h;
+            kp[t] = op8<T>{};
+            if (on && c < a.dim) kp[t] = *reinterpret_cast<const op8<T>*>(kbase + (int64_t)(sg.k0 + key) * a.k_row + c);
+        }
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int x = lane + u * GS_WAVE, vkey = j + x / PIECES, piece = x % PIECES;
+            vp[u] = op8<T>{};
+            if (vkey < sg.nk && 8 * piece < a.dim && (a.key_on == nullptr || a.key_on[sg.k0 + vkey]))
+                vp[u] = *reinterpret_cast<const op8<T>*>(vbase + (int64_t)(sg.k0 + vkey) * a.v_row + 8 * piece);
+        }
+    };
+
+    const float c = a.scale * kLog2e;
+    float m = -INFINITY, l = 0.0f;
+    acc16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = acc16{};
+    Lanes at;
+    at.init<P>();
+    T* const mine = vs[wave];
+    int j = j0 + 32 * wave;
+    if (j < j1) fetch(j);
+    for (; j < j1; j += 32 * WAVES) {
+        acc16 s[1];
+        s[0] = acc16{};
+#pragma unroll
+        for (int t = 0; t < KT; ++t) s[0] = mfma(kp[t], q[t], s[0]);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int x = lane + u * GS_WAVE;
+            *reinterpret_cast<op8<T>*>(mine + piece_at<P>(x / PIECES, x % PIECES)) = vp[u];
+        }
+        if (a.key_on != nullptr || j < alo || j + 32 > ahi) {
+            const int key = j + (lane & 31);
+            const uint64_t on = __ballot(key < sg.nk && (a.key_on == nullptr || a.key_on[sg.k0 + key]));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at = 8 * (e >> 2) + 4 * h + (e & 3);
+                if (j + at < klo || j + at >= khi || ((on >> at) & 1) == 0) s[0][e] = -INFINITY;
+            }
+        }
+        if (j + 32 * WAVES < j1) fetch(j + 32 * WAVES);
+        const float alpha = softmax_step<1>(s, c, m, l);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= alpha;
+        // this wave's values are in LDS before any of its lanes reads them
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const op8<T> p = tile_operand<T>(s[0], u);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = mfma(columns_operand<T, P>(mine, at, 16 * u, d), p, o[d]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    // the waves meet: the largest maximum, every sum and tile against it
+    l = half_sum(l);
+    if (h == 0) {
+        ml[0][wave][lane] = m;
+        ml[1][wave][lane] = l;
+    }
+    __syncthreads();
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[0][w][lane & 31]);
+    const float base = top == -INFINITY ? 0.0f : top * c;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+        sum = fmaf(ml[1][w][lane & 31], __builtin_amdgcn_exp2f(fmaf(ml[0][w][lane & 31], c, -base)), sum);
+    const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            half[wave][(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + (lane & 31)] = o[d][e] * alpha;
+        __syncthreads();
+        if (wave == d % WAVES) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at = (8 * (e >> 2) + 4 * h + (e & 3)) * 33 + (lane & 31);
+                float v = half[0][at];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) v += half[w][at];
+                o[d][e] = v;
+            }
+            if (there) store_tile<T>(f, token, head, split, d, o[d], sum);
+        }
+        __syncthreads();
+    }
+    if (wave == 0 && there) store_sums(f, token, head, split, top, sum);
+}
+
+// Joins the parts of a row (at most 64): lanes take the parts' maxima and sums
+// together, then two elements each and the parts in turn.  WAVES waves share a
+// row where there are many parts.
+constexpr int kMaxSplits = 64;
+
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
+    __shared__ float2 got[WAVES][GS_WAVE];
+    const int64_t rows = (int64_t)f.a.n_q * f.a.heads;
+    const int wave = WAVES == 1 ? 0 : threadIdx.x / GS_WAVE;
+    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE : blockIdx.x;
+    if (row >= rows) return;
+    const int lane = lane_id();
+    const float2 part = lane < f.splits ? f.part_ml[lane * rows + row] : make_float2(-INFINITY, 0.0f);
+    float m = part.x;
+#pragma unroll
+    for (int d = 1; d < GS_WAVE; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, GS_WAVE));
+    const float c = f.a.scale * kLog2e, base = m == -INFINITY ? 0.0f : m * c;
+    const float w = __builtin_amdgcn_exp2f(fmaf(part.x, c, -base));
+    const float l = wave_sum(part.y * w);
+    float2 o = make_float2(0.0f, 0.0f);
+    if (2 * lane < f.a.dim) {
+        const float* p = f.part_o + row * f.a.dim + 2 * lane;
+        const int64_t step = rows * f.a.dim;
+#pragma unroll 8
+        for (int s = wave; s < f.splits; s += WAVES) {
+            const float2 v = *reinterpret_cast<const float2*>(p + s * step);
+            const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
+            o.x = fmaf(v.x, ws, o.x);
+            o.y = fmaf(v.y, ws, o.y);
+        }
+    }
+    if (WAVES > 1) {
+        got[wave][lane] = o;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) {
+            o.x += got[k][lane].x;
+            o.y += got[k][lane].y;
+        }
+    }
+    const float inv = row_scale(l);
     const int64_t token = row / f.a.heads;
     const int head = (int)(row - token * f.a.heads);
-    if (lane == 0) f.lse[row] = l == 0.0f ? -INFINITY : m * f.a.scale + kLn2 * log2f(l);
+    if (lane == 0) f.lse[row] = row_lse(m, l, f.a.scale);
     if (2 * lane < f.a.dim) {
         T* p = static_cast<T*>(f.out) + token * f.o_row + (int64_t)head * f.o_head + 2 * lane;
-        p[0] = (T)(o0 * inv);
-        p[1] = (T)(o1 * inv);
+        p[0] = (T)(o.x * inv);
+        p[1] = (T)(o.y * inv);
     }
 }
 
-// How a call is cut: from its sizes alone.
+// How a call is cut, from its sizes alone: 32-row tiles where a segment's rows
+// fit one on average, and the keys into parts until the workgroups fill the
+// chip, as long as a part keeps the keys that pay for its start and its join.
 struct Plan {
+    bool few;
     int32_t tiles, splits;
 };
 
 Plan plan(const gs_attn& a) {
+    constexpr int kUnits = 256;                            // compute units
     Plan p;
     const int group = a.heads / a.kv_heads;
-    p.tiles = attn_tiles((int64_t)a.n_q * group, kRows, a.n_seg);
-    p.splits = 1;
+    const int64_t rows = (int64_t)a.n_q * group, keys = a.n_k / a.n_seg;
+    p.few = rows <= (int64_t)kFewRows * a.n_seg;
+    p.tiles = whole_shares(attn_tiles(rows, p.few ? kFewRows : kRows, a.n_seg), a.kv_heads);
+    const int64_t groups = (int64_t)p.tiles * a.kv_heads;
+    const int64_t want = ((p.few ? 4 : 2) * kUnits + groups - 1) / groups;
+    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, keys / (p.few ? 512 : 1024), kMaxSplits}));
     return p;
 }
 
 template <typename T, int D>
-hipError_t go(const FwdArgs& f, hipStream_t st) {
-    const uint32_t grid = chiplet_grid((int64_t)f.a.tiles * f.a.kv_heads * f.splits);
-    k_attention<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
-    if (f.splits > 1) k_attention_join<T><<<div_up((uint64_t)f.a.n_q * f.a.heads, 4), GS_BLOCK, 0, st>>>(f);
+hipError_t go(const FwdArgs& f, bool few, hipStream_t st) {
+    const uint32_t grid = (uint32_t)(f.a.tiles * f.a.kv_heads * f.splits);
+    if (few) k_attention_few<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
+    else k_attention<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
+    const uint64_t rows = (uint64_t)f.a.n_q * f.a.heads;
+    if (f.splits > 8) k_attention_join<T, 4><<<(uint32_t)rows, GS_BLOCK, 0, st>>>(f);
+    else if (f.splits > 1) k_attention_join<T, 1><<<div_up(rows, 4), GS_BLOCK, 0, st>>>(f);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t by_dim(const FwdArgs& f, hipStream_t st) {
-    if (f.a.dim <= 32) return go<T, 32>(f, st);
-    if (f.a.dim <= 64) return go<T, 64>(f, st);
-    if (f.a.dim <= 96) return go<T, 96>(f, st);
-    return go<T, 128>(f, st);
+hipError_t by_dim(const FwdArgs& f, bool few, hipStream_t st) {
+    if (f.a.dim <= 32) return go<T, 32>(f, few, st);
+    if (f.a.dim <= 64) return go<T, 64>(f, few, st);
+    if (f.a.dim <= 96) return go<T, 96>(f, few, st);
+    return go<T, 128>(f, few, st);
 }
 
 }  // namespace
@@ -294,7 +515,7 @@ hipError_t launch_attention(const gs_attn& a, const gs_rows& out, float* lse, vo
     f.splits = p.splits;
     f.part_ml = static_cast<float2*>(ws);
     f.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * p.splits * sizeof(float2)));
-    return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, st) : by_dim<f16_t>(f, st);
+    return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, p.few, st) : by_dim<f16_t>(f, p.few, st);
 }
 
 }  // namespace gsmi

@@ -61,11 +61,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     __shared__ __attribute__((aligned(16))) T vs[kStep * P];
     __shared__ __attribute__((aligned(4))) uint8_t on[kStep];
     const AttnArgs& a = f.a;
-    const int total = a.tiles * a.kv_heads;
-    const int id = chiplet_order(blockIdx.x, total);
-    if (id >= total) return;
-    const int kvh = id / a.tiles;
-    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kRows, id - kvh * a.tiles);
+    const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, 1);
+    const int kvh = place.head;
+    // the last tiles first: with ordered keys they have the most to do
+    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kRows, a.tiles - 1 - place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -107,6 +106,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
 
     const float c = a.scale * kLog2e;
+    Lanes at;
+    at.init<P>();
     acc16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = acc16{};
@@ -137,28 +138,28 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
             acc16 s{}, dp{};
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
-                s = mfma(rows_operand<T, P>(ks, 32 * k, t), q[t], s);
-                dp = mfma(rows_operand<T, P>(vs, 32 * k, t), dy[t], dp);
+                s = mfma(rows_operand<T, P>(ks, at, 32 * k, t), q[t], s);
+                dp = mfma(rows_operand<T, P>(vs, at, 32 * k, t), dy[t], dp);
             }
             if (test) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int at = 32 * k + 8 * g + 4 * h;
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>(on + at);
+                    const int first = 32 * k + 8 * g + 4 * h;
+                    const uint32_t w = *reinterpret_cast<const uint32_t*>(on + first);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int key = j + at + e;
+                        const int key = j + first + e;
                         if (key < klo || key >= khi || ((w >> (8 * e)) & 255u) == 0) s[4 * g + e] = -INFINITY;
                     }
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = exp2f(fmaf(s[e], c, -base)) * (dp[e] - delta);
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -base)) * (dp[e] - delta);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const op8<T> ds = tile_operand<T>(s, u);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = mfma(columns_operand<T, P>(ks, 32 * k + 16 * u, 32 * d), ds, o[d]);
+                for (int d = 0; d < DT; ++d) o[d] = mfma(columns_operand<T, P>(ks, at, 32 * k + 16 * u, d), ds, o[d]);
             }
         }
     }
@@ -176,13 +177,9 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_dkv(BwdA
     __shared__ __attribute__((aligned(16))) float bases[kStep], deltas[kStep];
     __shared__ __attribute__((aligned(16))) int klos[kStep], khis[kStep];
     const AttnArgs& a = f.a;
-    const int total = f.key_tiles * a.kv_heads * f.splits;
-    int id = chiplet_order(blockIdx.x, total);
-    if (id >= total) return;
-    const int split = id % f.splits;
-    id /= f.splits;
-    const int kvh = id / f.key_tiles;
-    const Segment sg = find_segment(a, a.cu_k, a.n_k, 1, kRows, id - kvh * f.key_tiles);
+    const Place place = chiplet_place(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
+    const int split = place.split, kvh = place.head;
+    const Segment sg = find_segment(a, a.cu_k, a.n_k, 1, kRows, place.tile);
     const int key0 = sg.tile * kRows;
     if (key0 >= sg.nk) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -220,6 +217,8 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_dkv(BwdA
         r1 = min(end, r0 + per);
     }
     const float c = a.scale * kLog2e;
+    Lanes at;
+    at.init<P>();
     acc16 dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = acc16{};
@@ -268,21 +267,21 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_dkv(BwdA
             acc16 s{}, dp{};
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
-                s = mfma(rows_operand<T, P>(qs, 32 * k, t), kf[t], s);
-                dp = mfma(rows_operand<T, P>(ds, 32 * k, t), vf[t], dp);
+                s = mfma(rows_operand<T, P>(qs, at, 32 * k, t), kf[t], s);
+                dp = mfma(rows_operand<T, P>(ds, at, 32 * k, t), vf[t], dp);
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int at = 32 * k + 8 * g + 4 * h;
-                const float4 b = *reinterpret_cast<const float4*>(bases + at);
-                const float4 dl = *reinterpret_cast<const float4*>(deltas + at);
-                s[4 * g] = exp2f(fmaf(s[4 * g], c, -b.x));
-                s[4 * g + 1] = exp2f(fmaf(s[4 * g + 1], c, -b.y));
-                s[4 * g + 2] = exp2f(fmaf(s[4 * g + 2], c, -b.z));
-                s[4 * g + 3] = exp2f(fmaf(s[4 * g + 3], c, -b.w));
+                const int first = 32 * k + 8 * g + 4 * h;
+                const float4 b = *reinterpret_cast<const float4*>(bases + first);
+                const float4 dl = *reinterpret_cast<const float4*>(deltas + first);
+                s[4 * g] = __builtin_amdgcn_exp2f(fmaf(s[4 * g], c, -b.x));
+                s[4 * g + 1] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 1], c, -b.y));
+                s[4 * g + 2] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 2], c, -b.z));
+                s[4 * g + 3] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 3], c, -b.w));
                 if (test) {
-                    const int4 lo = *reinterpret_cast<const int4*>(klos + at);
-                    const int4 hi = *reinterpret_cast<const int4*>(khis + at);
+                    const int4 lo = *reinterpret_cast<const int4*>(klos + first);
+                    const int4 hi = *reinterpret_cast<const int4*>(khis + first);
                     if (key < lo.x || key >= hi.x) s[4 * g] = 0.0f;
                     if (key < lo.y || key >= hi.y) s[4 * g + 1] = 0.0f;
                     if (key < lo.z || key >= hi.z) s[4 * g + 2] = 0.0f;
@@ -298,8 +297,8 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_dkv(BwdA
                 const op8<T> p = tile_operand<T>(s, u), z = tile_operand<T>(dp, u);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    dv[d] = mfma(columns_operand<T, P>(ds, 32 * k + 16 * u, 32 * d), p, dv[d]);
-                    dk[d] = mfma(columns_operand<T, P>(qs, 32 * k + 16 * u, 32 * d), z, dk[d]);
+                    dv[d] = mfma(columns_operand<T, P>(ds, at, 32 * k + 16 * u, d), p, dv[d]);
+                    dk[d] = mfma(columns_operand<T, P>(qs, at, 32 * k + 16 * u, d), z, dk[d]);
                 }
             }
         }
@@ -353,9 +352,9 @@ int dkv_splits(const gs_attn& a) { return 1; }
 template <typename T, int D>
 hipError_t go(const BwdArgs& f, hipStream_t st) {
     if (f.a.n_q > 0)
-        k_attention_dq<T, D><<<chiplet_grid((int64_t)f.a.tiles * f.a.kv_heads), GS_BLOCK, 0, st>>>(f);
+        k_attention_dq<T, D><<<(uint32_t)(f.a.tiles * f.a.kv_heads), GS_BLOCK, 0, st>>>(f);
     if (f.a.n_k > 0) {
-        k_attention_dkv<T, D><<<chiplet_grid((int64_t)f.key_tiles * f.a.kv_heads * f.splits), GS_BLOCK, 0, st>>>(f);
+        k_attention_dkv<T, D><<<(uint32_t)(f.key_tiles * f.a.kv_heads * f.splits), GS_BLOCK, 0, st>>>(f);
         if (f.splits > 1)
             k_attention_dkv_join<T>
                 <<<div_up((uint64_t)f.a.n_k * f.a.kv_heads * f.a.dim / 2, GS_BLOCK), GS_BLOCK, 0, st>>>(f);
@@ -382,8 +381,8 @@ size_t attention_bwd_ws_bytes(const gs_attn& a) {
 hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* ws, hipStream_t st) {
     BwdArgs f;
     f.a = attn_args(a);
-    f.a.tiles = attn_tiles((int64_t)a.n_q * f.a.group, kRows, a.n_seg);
-    f.key_tiles = attn_tiles(a.n_k, kRows, a.n_seg);
+    f.a.tiles = whole_shares(attn_tiles((int64_t)a.n_q * f.a.group, kRows, a.n_seg), a.kv_heads);
+    f.key_tiles = whole_shares(attn_tiles(a.n_k, kRows, a.n_seg), a.kv_heads);
     f.out = g.out.ptr;
     f.o_row = g.out.ld_row;
     f.o_head = g.out.ld_head;

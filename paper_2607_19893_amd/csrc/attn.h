@@ -65,25 +65,52 @@ __device__ __forceinline__ op4<T> read_columns(const T* p) {
     return __builtin_bit_cast(op4<T>, v);
 }
 
+// The same value, of which the compiler knows nothing: what follows from it is
+// computed where it is used.  Otherwise the sums of a lane's places and every
+// tile's start are kept in a register each over a whole loop, in place of the
+// instruction's offset.
+__device__ __forceinline__ int fresh(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// Where a lane's pieces of a tile are, in bytes: `rows` for operands made of the
+// tile's rows, `cols` for those made of its columns.  The key only moves 16-byte
+// pieces within a row, so the other places follow by an exclusive or: 32 t for
+// the t-th 16 elements of a row, 64 d for columns 32 d on, 32 for the rows 8
+// below.
+struct Lanes {
+    int rows, cols;
+
+    template <int P>
+    __device__ __forceinline__ void init() {
+        const int l = lane_id();
+        rows = 2 * piece_at<P>(l & 31, l >> 5);
+        cols = 2 * piece_at<P>(4 * (l >> 5) + ((l & 15) >> 2), 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) + 8 * (l & 1);
+    }
+    __device__ __forceinline__ void refresh() {
+        rows = fresh(rows);
+        cols = fresh(cols);
+    }
+};
+
 // A operand from the columns of a tile: rows (of the operand) are the tile's
-// columns col0 .. col0+31, the 16 of the sum are its rows row0 .. row0+15 in
-// the order a C tile's registers have.
+// columns 32 d .. +31, the 16 of the sum are its rows row0 .. row0+15 in the
+// order a C tile's registers have.
 template <typename T, int P>
-__device__ __forceinline__ op8<T> columns_operand(const T* tile, int row0, int col0) {
-    const int l = lane_id();
-    const int row = row0 + 4 * (l >> 5) + ((l & 15) >> 2);
-    const int col = col0 + 16 * ((l >> 4) & 1) + 4 * (l & 3);
-    const op4<T> lo = read_columns(tile + piece_at<P>(row, col >> 3) + (col & 7));
-    const op4<T> hi = read_columns(tile + piece_at<P>(row + 8, col >> 3) + (col & 7));
+__device__ __forceinline__ op8<T> columns_operand(const T* tile, const Lanes& at, int row0, int d) {
+    const char* p = reinterpret_cast<const char*>(tile) + row0 * P * 2;
+    const op4<T> lo = read_columns(reinterpret_cast<const T*>(p + (at.cols ^ (64 * d))));
+    const op4<T> hi = read_columns(reinterpret_cast<const T*>(p + 16 * P + (at.cols ^ (64 * d) ^ 32)));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // A or B operand from the rows of a tile: lane l gets row row0 + (l & 31),
 // elements 16 t + 8 (l >> 5) .. +7.
 template <typename T, int P>
-__device__ __forceinline__ op8<T> rows_operand(const T* tile, int row0, int t) {
-    const int l = lane_id();
-    return *reinterpret_cast<const op8<T>*>(tile + piece_at<P>(row0 + (l & 31), 2 * t + (l >> 5)));
+__device__ __forceinline__ op8<T> rows_operand(const T* tile, const Lanes& at, int row0, int t) {
+    const char* p = reinterpret_cast<const char*>(tile) + row0 * P * 2;
+    return *reinterpret_cast<const op8<T>*>(p + (at.rows ^ (32 * t)));
 }
 
 // Registers 8u .. 8u+7 of a C tile as an operand.
@@ -93,6 +120,52 @@ __device__ __forceinline__ op8<T> tile_operand(const acc16& c, int u) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = (T)c[8 * u + i];
     return o;
+}
+
+// Copies tiles of ROWS token rows from memory into LDS without passing through
+// registers (buffer loads that write LDS): each of the LOADS instructions of a
+// wave fills 1 KB, 16 bytes a lane in lane order, so the lane that fills a
+// piece's place reads the piece that belongs there.  Rows at or past the
+// segment's end and pieces past the head's end lie outside the buffer's range
+// and arrive as zeros.
+template <typename T, int P, int ROWS>
+struct TileLoader {
+    static constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK;
+    static constexpr int kRange = 0x7FFFFF00, kOutside = 0x7FFFFFF0;
+    int off[LOADS];                        // bytes from the tile's first row
+    int64_t ld;
+
+    __device__ __forceinline__ void init(int64_t row_stride, int dim) {
+        ld = row_stride;
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int x = threadIdx.x + u * GS_BLOCK, row = x / PIECES;
+            const int piece = (x % PIECES) ^ piece_key<P>(row);
+            off[u] = 8 * piece < dim ? (int)(row * ld * 2) + piece * 16 : kOutside;
+        }
+    }
+
+    // base: the tile's first row; rows: how many there are from it on; skip:
+    // bit u leaves load u's row out (zeros).
+    __device__ __forceinline__ void load(T* tile, const T* base, int rows, uint32_t skip) const {
+#ifdef __HIP_DEVICE_COMPILE__              // the host pass has no buffer descriptors
+        const int64_t bytes = rows * ld * 2;
+        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<T*>(base), 0, (int)(bytes < kRange ? bytes : kRange), 0x00027000);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                buf, (__attribute__((address_space(3))) void*)(tile + (u * GS_BLOCK + wave * GS_WAVE) * 8), 16,
+                (skip >> u) & 1 ? kOutside : off[u], 0, 0, 0);
+#endif
+    }
+};
+
+// Bits [lo, hi) of 64, ends clamped.
+__device__ __forceinline__ uint64_t bits_between(int lo, int hi) {
+    const uint64_t below = hi <= 0 ? 0ull : (hi >= 64 ? ~0ull : (1ull << hi) - 1);
+    return lo <= 0 ? below : (lo >= 64 ? 0ull : below & (~0ull << lo));
 }
 
 struct AttnArgs {
@@ -142,7 +215,7 @@ struct Segment {
 };
 
 __device__ __forceinline__ int cu_at(const int32_t* cu, int s, int n_seg, int n) {
-    if (cu == nullptr) return (int)((int64_t)n * s / n_seg);
+    if (cu == nullptr) return n / n_seg * s;
     return min(max(cu[s], 0), n);
 }
 
@@ -156,12 +229,13 @@ __device__ __forceinline__ Segment find_segment(const AttnArgs& a, const int32_t
         if (first <= tile) lo = m;
         else hi = m - 1;
     }
+    lo = __builtin_amdgcn_readfirstlane(lo);           // the same in every lane: held in scalar registers
     Segment s;
-    s.q0 = cu_at(a.cu_q, lo, a.n_seg, a.n_q);
-    s.nq = max(cu_at(a.cu_q, lo + 1, a.n_seg, a.n_q) - s.q0, 0);
-    s.k0 = cu_at(a.cu_k, lo, a.n_seg, a.n_k);
-    s.nk = max(cu_at(a.cu_k, lo + 1, a.n_seg, a.n_k) - s.k0, 0);
-    s.tile = tile - ((int)((int64_t)cu_at(cu, lo, a.n_seg, n) * mul / size) + lo);
+    s.q0 = __builtin_amdgcn_readfirstlane(cu_at(a.cu_q, lo, a.n_seg, a.n_q));
+    s.nq = __builtin_amdgcn_readfirstlane(max(cu_at(a.cu_q, lo + 1, a.n_seg, a.n_q) - s.q0, 0));
+    s.k0 = __builtin_amdgcn_readfirstlane(cu_at(a.cu_k, lo, a.n_seg, a.n_k));
+    s.nk = __builtin_amdgcn_readfirstlane(max(cu_at(a.cu_k, lo + 1, a.n_seg, a.n_k) - s.k0, 0));
+    s.tile = tile - __builtin_amdgcn_readfirstlane((int)((int64_t)cu_at(cu, lo, a.n_seg, n) * mul / size) + lo);
     return s;
 }
 
@@ -173,14 +247,38 @@ __device__ __forceinline__ void admitted(const AttnArgs& a, int nk, int first, i
 
 inline int attn_tiles(int64_t rows, int size, int n_seg) { return (int)(rows / size) + n_seg; }
 
-// Order of the workgroups: consecutive ids go to the eight chiplets in turn,
-// each with its own L2.  Cutting the list of (key head, tile) into eight runs
-// keeps the tiles that read the same keys on one chiplet.
-__device__ __forceinline__ int chiplet_order(int id, int n) {
-    const int per = (n + 7) >> 3;
-    return (id & 7) * per + (id >> 3);
+// Order of the workgroups.  Consecutive ids go to the eight chiplets in turn,
+// each with its own L2, so the list of (key head, tile) is cut into eight runs:
+// the tiles that read the same keys stay on one chiplet.  Where a run is less
+// than a head or not whole heads, a head's tiles are dealt into 8 / gcd(8,
+// heads) equal shares, every so many-th tile, so that no chiplet gets all the
+// long ones (ordered keys: the last rows; dealt in runs, one chiplet had three
+// times another's work).
+inline int chiplet_shares(int heads) {
+    return heads % 8 == 0 ? 1 : (heads % 4 == 0 ? 2 : (heads % 2 == 0 ? 4 : 8));
 }
 
-inline uint32_t chiplet_grid(int64_t n) { return (uint32_t)((n + 7) / 8 * 8); }
+struct Place {
+    int head, tile, split;
+};
+
+// tiles: a multiple of the shares; ids: 0 .. tiles * heads * splits - 1.
+__device__ __forceinline__ Place chiplet_place(int id, int tiles, int heads, int splits) {
+    const int shares = heads % 8 == 0 ? 1 : (heads % 4 == 0 ? 2 : (heads % 2 == 0 ? 4 : 8));
+    const int each = tiles / shares;
+    int at = (id & 7) * (each * splits * (heads * shares / 8)) + (id >> 3);
+    Place p;
+    p.split = at % splits;
+    at /= splits;
+    const int share = at / each;
+    p.head = share / shares;
+    p.tile = (at - share * each) * shares + share - p.head * shares;
+    return p;
+}
+
+inline int whole_shares(int tiles, int heads) {
+    const int s = chiplet_shares(heads);
+    return (tiles + s - 1) / s * s;
+}
 
 }  // namespace gsmi
