@@ -155,14 +155,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
     const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
     auto fetch = [&](T* ks, T* vs, int j) {
         uint32_t skip = 0;
-        if (a.key_on != nullptr) {
-            const int first = fresh(threadIdx.x) / kl.PIECES;
-#pragma unroll
-            for (int u = 0; u < kl.LOADS; ++u) {
-                const int key = j + first + u * (GS_BLOCK / kl.PIECES);
-                if (key < sg.nk && a.key_on[sg.k0 + key] == 0) skip |= 1u << u;
-            }
-        }
+        if (a.key_on != nullptr) skip = rows_off<P, kKeys>(a.key_on + sg.k0, j, sg.nk);
         kl.load(ks, kbase + j * a.k_row, sg.nk - j, skip);
         vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);
     };
@@ -236,9 +229,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
         if (j + kKeys < j1) fetch(ks1, vs1, j + kKeys);
         step(ks0, vs0, j);
         __syncthreads();
-        if (j + kKeys >= j1) break;
-        if (j + 2 * kKeys < j1) fetch(ks0, vs0, j + 2 * kKeys);
-        step(ks1, vs1, j + kKeys);
+        if (j + kKeys < j1) {
+            if (j + 2 * kKeys < j1) fetch(ks0, vs0, j + 2 * kKeys);
+            step(ks1, vs1, j + kKeys);
+        }
         __syncthreads();
     }
     l = half_sum(l);

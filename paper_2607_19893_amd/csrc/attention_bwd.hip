@@ -27,7 +27,8 @@ struct BwdArgs {
     void *dq, *dk, *dv;
     int64_t o_row, o_head, do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
     const float* lse;
-    float* delta;                          // [n_q * heads]
+    float* base;                           // [heads][n_q]: the rows' log sums in powers of two
+    float* delta;                          // [heads][n_q], behind base
     int32_t key_tiles;
     int32_t splits;                        // parts that a key tile's rows are cut into
     float* part;                           // [splits][2][n_k * kv_heads][dim]: dk, dv
@@ -56,10 +57,9 @@ __device__ __forceinline__ void store_tiles(T* p, const acc16 (&o)[DT], float sc
 template <typename T, int D>
 __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
-    constexpr int PIECES = D / 8, LOADS = kStep * PIECES / GS_BLOCK;
-    __shared__ __attribute__((aligned(16))) T ks[kStep * P];
-    __shared__ __attribute__((aligned(16))) T vs[kStep * P];
-    __shared__ __attribute__((aligned(4))) uint8_t on[kStep];
+    // two buffers: a step's tiles arrive while the step before computes
+    __shared__ __attribute__((aligned(16))) T ks0[kStep * P], vs0[kStep * P];
+    __shared__ __attribute__((aligned(16))) T ks1[kStep * P], vs1[kStep * P];
     const AttnArgs& a = f.a;
     const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, 1);
     const int kvh = place.head;
@@ -73,8 +73,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     const int i = (there ? r : rows - 1) / a.group;
     const int token = sg.q0 + i, head = kvh * a.group + (there ? r : rows - 1) - i * a.group;
     const int shift = sg.nk - sg.nq;
-    const int64_t row = (int64_t)token * a.heads + head;
-    const float lse = f.lse[row];
+    const float lse = f.lse[(int64_t)token * a.heads + head];
     const float base = row_base(lse);
 
     op8<T> q[KT], dy[KT];
@@ -97,7 +96,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
         }
     }
     delta += __shfl_xor(delta, 32, GS_WAVE);
-    if (there && h == 0) f.delta[row] = delta;
+    if (there && h == 0) {
+        f.base[(int64_t)head * a.n_q + token] = base;
+        f.delta[(int64_t)head * a.n_q + token] = delta;
+    }
 
     int klo, khi, lo, hi, alo, ahi;
     admitted(a, sg.nk, i + shift, i + shift, klo, khi);
@@ -105,77 +107,105 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     admitted(a, sg.nk, row0 / a.group + shift, last / a.group + shift, lo, hi);
     admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
 
+    TileLoader<T, P, kStep> kl, vl;
+    kl.init(a.k_row, a.dim);
+    vl.init(a.v_row, a.dim);
+    const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
+    const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    auto fetch = [&](T* ks, T* vs, int j) {
+        uint32_t skip = 0;
+        if (a.key_on != nullptr) skip = rows_off<P, kStep>(a.key_on + sg.k0, j, sg.nk);
+        kl.load(ks, kbase + j * a.k_row, sg.nk - j, skip);
+        vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);
+    };
+
     const float c = a.scale * kLog2e;
     Lanes at;
     at.init<P>();
     acc16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = acc16{};
-    for (int j = lo / kStep * kStep; j < hi; j += kStep) {
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int x = threadIdx.x + u * GS_BLOCK, kr = x / PIECES, piece = x % PIECES;
-            const int key = j + kr;
-            op8<T> kp{}, vp{};
-            if (key < sg.nk && 8 * piece < a.dim && (a.key_on == nullptr || a.key_on[sg.k0 + key])) {
-                kp = *reinterpret_cast<const op8<T>*>(static_cast<const T*>(a.k) + (int64_t)(sg.k0 + key) * a.k_row +
-                                                      (int64_t)kvh * a.k_head + 8 * piece);
-                vp = *reinterpret_cast<const op8<T>*>(static_cast<const T*>(a.v) + (int64_t)(sg.k0 + key) * a.v_row +
-                                                      (int64_t)kvh * a.v_head + 8 * piece);
-            }
-            *reinterpret_cast<op8<T>*>(ks + piece_at<P>(kr, piece)) = kp;
-            *reinterpret_cast<op8<T>*>(vs + piece_at<P>(kr, piece)) = vp;
-        }
-        if (threadIdx.x < kStep) {
-            const int key = j + threadIdx.x;
-            on[threadIdx.x] = key < sg.nk && (a.key_on == nullptr || a.key_on[sg.k0 + key]);
-        }
-        __syncthreads();
+    auto step = [&](const T* ks, const T* vs, int j) {
+        at.refresh();
         const bool test = a.key_on != nullptr || j < alo || j + kStep > ahi;
+        uint64_t seen = ~0ull;
+        if (test) {
+            seen = bits_between(klo - j, khi - j);
+            if (a.key_on != nullptr) {
+                const int key = j + fresh(lane);
+                seen &= __ballot(key < sg.nk && a.key_on[sg.k0 + min(key, sg.nk - 1)]);
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kStep / 32; ++k) {
+            // operands are read one product ahead of their use; the barriers keep
+            // the compiler from reading more of them ahead, which would not fit
+            // the registers of two waves a SIMD
             acc16 s{}, dp{};
+            op8<T> x[2], y[2];
+            x[0] = rows_operand<T, P>(ks, at, 32 * k, 0);
+            y[0] = rows_operand<T, P>(vs, at, 32 * k, 0);
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
-                s = mfma(rows_operand<T, P>(ks, at, 32 * k, t), q[t], s);
-                dp = mfma(rows_operand<T, P>(vs, at, 32 * k, t), dy[t], dp);
+                if (t + 1 < KT) {
+                    x[(t + 1) & 1] = rows_operand<T, P>(ks, at, 32 * k, t + 1);
+                    y[(t + 1) & 1] = rows_operand<T, P>(vs, at, 32 * k, t + 1);
+                }
+                s = mfma(x[t & 1], q[t], s);
+                dp = mfma(y[t & 1], dy[t], dp);
+                __builtin_amdgcn_sched_barrier(0);
             }
             if (test) {
+                const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int first = 32 * k + 8 * g + 4 * h;
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>(on + first);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = j + first + e;
-                        if (key < klo || key >= khi || ((w >> (8 * e)) & 255u) == 0) s[4 * g + e] = -INFINITY;
-                    }
-                }
+                for (int e = 0; e < 16; ++e)
+                    if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[e] = -INFINITY;
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -base)) * (dp[e] - delta);
+            op8<T> z[2], ds;
+            z[0] = columns_operand<T, P>(ks, at, 32 * k, 0);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const op8<T> ds = tile_operand<T>(s, u);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = mfma(columns_operand<T, P>(ks, at, 32 * k + 16 * u, d), ds, o[d]);
+            for (int e = 0; e < 2 * DT; ++e) {
+                if (e + 1 < 2 * DT)
+                    z[(e + 1) & 1] = columns_operand<T, P>(ks, at, 32 * k + 16 * ((e + 1) / DT), (e + 1) % DT);
+                if (e % DT == 0) ds = tile_operand<T>(s, e / DT);
+                o[e % DT] = mfma(z[e & 1], ds, o[e % DT]);
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
+    };
+    const int j0 = lo / kStep * kStep;
+    if (j0 < hi) fetch(ks0, vs0, j0);
+    __syncthreads();                               // the fetched tiles are in LDS
+    for (int j = j0; j < hi; j += 2 * kStep) {
+        if (j + kStep < hi) fetch(ks1, vs1, j + kStep);
+        step(ks0, vs0, j);
+        __syncthreads();
+        if (j + kStep < hi) {
+            if (j + 2 * kStep < hi) fetch(ks0, vs0, j + 2 * kStep);
+            step(ks1, vs1, j + kStep);
+        }
+        __syncthreads();
     }
     if (there)
         store_tiles<T, DT>(static_cast<T*>(f.dq) + (int64_t)token * f.dq_row + (int64_t)head * f.dq_head, o, a.scale,
                            a.dim);
 }
 
+// The sums of dk and dv take a lane's registers twice the head's size; keys and
+// values beside them leave no room for two waves a SIMD from 96 elements on, so
+// there the values are read from LDS (a quarter more of its traffic) and a step
+// is 32 rows.
 template <typename T, int D>
-__global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_dkv(BwdArgs f) {
+__global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
-    constexpr int PIECES = D / 8, LOADS = kStep * PIECES / GS_BLOCK;
-    __shared__ __attribute__((aligned(16))) T qs[kStep * P];
-    __shared__ __attribute__((aligned(16))) T ds[kStep * P];
-    __shared__ __attribute__((aligned(16))) float bases[kStep], deltas[kStep];
-    __shared__ __attribute__((aligned(16))) int klos[kStep], khis[kStep];
+    constexpr bool BIG = D > 64;
+    constexpr int ST = BIG ? 32 : 64, NK = ST / 32;
+    __shared__ __attribute__((aligned(16))) T qs0[ST * P], ds0[ST * P];
+    __shared__ __attribute__((aligned(16))) T qs1[ST * P], ds1[ST * P];
+    __shared__ __attribute__((aligned(16))) float st0[2 * 64], st1[2 * 64];            // bases, then deltas
+    __shared__ __attribute__((aligned(16))) T vs[BIG ? kRows * P : 8];
     const AttnArgs& a = f.a;
     const Place place = chiplet_place(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
@@ -183,128 +213,175 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_dkv(BwdA
     const int key0 = sg.tile * kRows;
     if (key0 >= sg.nk) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
-    const int mine = key0 + 32 * wave + (lane & 31);
-    const bool there = mine < sg.nk;
-    const bool on = there && (a.key_on == nullptr || a.key_on[sg.k0 + mine]);
-    const int key = on ? mine : -1;                        // below every row's first key
-    const int shift = sg.nk - sg.nq, rows = sg.nq * a.group;
+    const int key = key0 + 32 * wave + (lane & 31);
+    const bool there = key < sg.nk;
+    const bool on = there && (a.key_on == nullptr || a.key_on[sg.k0 + key]);
+    const int shift = sg.nk - sg.nq;
 
-    op8<T> kf[KT], vf[KT];
+    op8<T> kf[KT], vf[BIG ? 1 : KT];
     {
-        const int64_t at = sg.k0 + (there ? mine : key0);
-        const T* pk = static_cast<const T*>(a.k) + at * a.k_row + (int64_t)kvh * a.k_head;
-        const T* pv = static_cast<const T*>(a.v) + at * a.v_row + (int64_t)kvh * a.v_head;
+        const int64_t row = sg.k0 + (there ? key : key0);
+        const T* pk = static_cast<const T*>(a.k) + row * a.k_row + (int64_t)kvh * a.k_head;
+        const T* pv = static_cast<const T*>(a.v) + row * a.v_row + (int64_t)kvh * a.v_head;
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
             const int c = 16 * t + 8 * h;
-            kf[t] = vf[t] = op8<T>{};
-            if (c < a.dim && on) {
-                kf[t] = *reinterpret_cast<const op8<T>*>(pk + c);
-                vf[t] = *reinterpret_cast<const op8<T>*>(pv + c);
+            kf[t] = op8<T>{};
+            if (c < a.dim && on) kf[t] = *reinterpret_cast<const op8<T>*>(pk + c);
+            if (!BIG) {
+                vf[t] = op8<T>{};
+                if (c < a.dim && on) vf[t] = *reinterpret_cast<const op8<T>*>(pv + c);
             }
         }
     }
-    // rows that admit any of the workgroup's keys: place in [first key - right, last key + left]
-    const int last = min(key0 + kRows, sg.nk) - 1;
-    const int64_t i0 = a.right >= 0 ? max((int64_t)0, (int64_t)key0 - a.right - shift) : 0;
-    const int64_t i1 = a.left >= 0 ? min((int64_t)sg.nq, (int64_t)last + a.left - shift + 1) : sg.nq;
-    int r0 = (int)min((int64_t)rows, i0 * a.group) / kStep * kStep;
-    int r1 = (int)max((int64_t)0, i1 * a.group);
-    if (f.splits > 1) {
-        const int per = ((max(r1 - r0, 0) + f.splits - 1) / f.splits + kStep - 1) / kStep * kStep;
-        const int end = r1;
-        r0 += split * per;
-        r1 = min(end, r0 + per);
+    if (BIG) {
+        TileLoader<T, P, kRows> vl;
+        vl.init(a.v_row, a.dim);
+        uint32_t skip = 0;
+        if (a.key_on != nullptr) skip = rows_off<P, kRows>(a.key_on + sg.k0, key0, sg.nk);
+        vl.load(vs, static_cast<const T*>(a.v) + (sg.k0 + key0) * a.v_row + (int64_t)kvh * a.v_head, sg.nk - key0,
+                skip);
     }
+    // tokens that admit any of the workgroup's keys, and those that all do
+    const int last = min(key0 + kRows, sg.nk) - 1;
+    int lo, hi, alo, ahi, ilo, ihi;
+    admitting(a, sg.nq, shift, key0, last, lo, hi);
+    admitting(a, sg.nq, shift, last, key0, alo, ahi);
+    admitting(a, sg.nq, shift, key, key, ilo, ihi);
+    if (!on) ihi = ilo;
+    const bool whole = a.key_on == nullptr && key0 + kRows <= sg.nk;
+    // the heads' tokens are one list of steps, a head after the other
+    const int t0 = lo / ST * ST, per = max(hi - t0 + ST - 1, 0) / ST;
+    int n0 = 0, n1 = per * a.group;
+    if (f.splits > 1) {
+        const int each = (n1 + f.splits - 1) / f.splits;
+        n0 = split * each;
+        n1 = min(n1, n0 + each);
+    }
+    // a token that admits no key at all may hold anything: its row is left out
+    const bool empties = a.key_on != nullptr || (a.right >= 0 && shift + a.right < 0);
+
+    TileLoader<T, P, ST> ql, dl;
+    ql.init(a.q_row, a.dim);
+    dl.init(f.do_row, a.dim);
+    const int64_t qbase = sg.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
+    const int64_t dbase = sg.q0 * f.do_row + (int64_t)kvh * a.group * f.do_head;
+    auto fetch = [&](T* qs, T* ds, float* st, int n) {
+        const int g = n / per, t = t0 + (n - g * per) * ST;
+        const float* bases = f.base + (int64_t)(kvh * a.group + g) * a.n_q + sg.q0;
+        uint32_t skip = 0;
+        if (empties) {
+            const int first = fresh(threadIdx.x) / ql.PIECES;
+#pragma unroll
+            for (int u = 0; u < ql.LOADS; ++u) {
+                const int row = t + first + u * (GS_BLOCK / ql.PIECES);
+                if (row < sg.nq && bases[row] == INFINITY) skip |= 1u << u;
+            }
+        }
+        ql.load(qs, static_cast<const T*>(a.q) + qbase + g * a.q_head + t * a.q_row, sg.nq - t, skip);
+        dl.load(ds, static_cast<const T*>(f.dout) + dbase + g * f.do_head + t * f.do_row, sg.nq - t, skip);
+        // bases by the first wave, deltas by the second
+        if (wave < 2)
+            load_words(st + wave * 64, (wave ? bases + (f.delta - f.base) : bases) + t, sg.nq - t);
+    };
+
     const float c = a.scale * kLog2e;
     Lanes at;
     at.init<P>();
     acc16 dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = acc16{};
-    for (int r = r0; r < r1; r += kStep) {
-        __syncthreads();
+    auto step = [&](const T* qs, const T* ds, const float* st, int n) {
+        at.refresh();
+        const int t = t0 + n % per * ST;
+        const bool test = !whole || t < alo || t + ST > ahi;
+        uint64_t seen = ~0ull;
+        if (test) seen = bits_between(ilo - t, ihi - t);
+        acc16 s[NK]{}, dp[NK]{};
+        // operands are read one product ahead of their use; the barriers keep
+        // the compiler from reading more of them ahead, which would not fit the
+        // registers of two waves a SIMD
+        auto products = [&](int k) {
+            op8<T> x[2], y[2], z[2];
+            auto read = [&](int e) {
+                x[e & 1] = rows_operand<T, P>(qs, at, 32 * k, e);
+                y[e & 1] = rows_operand<T, P>(ds, at, 32 * k, e);
+                z[e & 1] = BIG ? rows_operand<T, P>(vs, at, 32 * wave, e) : vf[BIG ? 0 : e];
+            };
+            read(0);
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int x = threadIdx.x + u * GS_BLOCK, rr = x / PIECES, piece = x % PIECES;
-            op8<T> qp{}, dp{};
-            if (r + rr < rows && 8 * piece < a.dim) {
-                const int i = (r + rr) / a.group, head = kvh * a.group + (r + rr) - i * a.group;
-                const int64_t token = sg.q0 + i;
-                if (f.lse[token * a.heads + head] != -INFINITY) {
-                    qp = *reinterpret_cast<const op8<T>*>(static_cast<const T*>(a.q) + token * a.q_row +
-                                                          (int64_t)head * a.q_head + 8 * piece);
-                    dp = *reinterpret_cast<const op8<T>*>(static_cast<const T*>(f.dout) + token * f.do_row +
-                                                          (int64_t)head * f.do_head + 8 * piece);
-                }
+            for (int e = 0; e < KT; ++e) {
+                if (e + 1 < KT) read(e + 1);
+                s[k] = mfma(x[e & 1], kf[e], s[k]);
+                dp[k] = mfma(y[e & 1], z[e & 1], dp[k]);
+                if (BIG) __builtin_amdgcn_sched_barrier(0);
             }
-            *reinterpret_cast<op8<T>*>(qs + piece_at<P>(rr, piece)) = qp;
-            *reinterpret_cast<op8<T>*>(ds + piece_at<P>(rr, piece)) = dp;
-        }
-        if (threadIdx.x < kStep) {
-            const int rr = r + threadIdx.x;
-            float base = INFINITY, delta = 0.0f;
-            int lo = 0, hi = 0;
-            if (rr < rows) {
-                const int i = rr / a.group, head = kvh * a.group + rr - i * a.group;
-                const int64_t at = (int64_t)(sg.q0 + i) * a.heads + head;
-                base = row_base(f.lse[at]);
-                delta = f.delta[at];
-                admitted(a, sg.nk, i + shift, i + shift, lo, hi);
-            }
-            bases[threadIdx.x] = base;
-            deltas[threadIdx.x] = delta;
-            klos[threadIdx.x] = lo;
-            khis[threadIdx.x] = hi;
-        }
-        __syncthreads();
-        // the step's rows all admit all of the workgroup's keys: no test
-        int alo, ahi;
-        admitted(a, sg.nk, (min(r + kStep, rows) - 1) / a.group + shift, r / a.group + shift, alo, ahi);
-        const bool test = a.key_on != nullptr || key0 + kRows > sg.nk || key0 < alo || last >= ahi || r + kStep > rows;
+        };
+        auto gradients = [&](int k) {
+            if (test) {
+                const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
 #pragma unroll
-        for (int k = 0; k < kStep / 32; ++k) {
-            acc16 s{}, dp{};
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                s = mfma(rows_operand<T, P>(qs, at, 32 * k, t), kf[t], s);
-                dp = mfma(rows_operand<T, P>(ds, at, 32 * k, t), vf[t], dp);
+                for (int e = 0; e < 16; ++e)
+                    if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[k][e] = -INFINITY;
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int first = 32 * k + 8 * g + 4 * h;
-                const float4 b = *reinterpret_cast<const float4*>(bases + first);
-                const float4 dl = *reinterpret_cast<const float4*>(deltas + first);
-                s[4 * g] = __builtin_amdgcn_exp2f(fmaf(s[4 * g], c, -b.x));
-                s[4 * g + 1] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 1], c, -b.y));
-                s[4 * g + 2] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 2], c, -b.z));
-                s[4 * g + 3] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 3], c, -b.w));
-                if (test) {
-                    const int4 lo = *reinterpret_cast<const int4*>(klos + first);
-                    const int4 hi = *reinterpret_cast<const int4*>(khis + first);
-                    if (key < lo.x || key >= hi.x) s[4 * g] = 0.0f;
-                    if (key < lo.y || key >= hi.y) s[4 * g + 1] = 0.0f;
-                    if (key < lo.z || key >= hi.z) s[4 * g + 2] = 0.0f;
-                    if (key < lo.w || key >= hi.w) s[4 * g + 3] = 0.0f;
-                }
-                dp[4 * g] = s[4 * g] * (dp[4 * g] - dl.x);
-                dp[4 * g + 1] = s[4 * g + 1] * (dp[4 * g + 1] - dl.y);
-                dp[4 * g + 2] = s[4 * g + 2] * (dp[4 * g + 2] - dl.z);
-                dp[4 * g + 3] = s[4 * g + 3] * (dp[4 * g + 3] - dl.w);
-            }
+                const float4 b = *reinterpret_cast<const float4*>(st + first);
+                const float4 d = *reinterpret_cast<const float4*>(st + 64 + first);
+                const float bs[4] = {b.x, b.y, b.z, b.w}, dl[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const op8<T> p = tile_operand<T>(s, u), z = tile_operand<T>(dp, u);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    dv[d] = mfma(columns_operand<T, P>(ds, at, 32 * k + 16 * u, d), p, dv[d]);
-                    dk[d] = mfma(columns_operand<T, P>(qs, at, 32 * k + 16 * u, d), z, dk[d]);
+                for (int e = 0; e < 4; ++e) {
+                    s[k][4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[k][4 * g + e], c, -bs[e]));
+                    dp[k][4 * g + e] = s[k][4 * g + e] * (dp[k][4 * g + e] - dl[e]);
                 }
             }
+        };
+        auto sums = [&](int k) {
+            op8<T> x[2], y[2], p, z;
+            auto read = [&](int e) {               // e: u * DT + d
+                x[e & 1] = columns_operand<T, P>(ds, at, 32 * k + 16 * (e / DT), e % DT);
+                y[e & 1] = columns_operand<T, P>(qs, at, 32 * k + 16 * (e / DT), e % DT);
+            };
+            read(0);
+#pragma unroll
+            for (int e = 0; e < 2 * DT; ++e) {
+                if (e + 1 < 2 * DT) read(e + 1);
+                if (e % DT == 0) {
+                    p = tile_operand<T>(s[k], e / DT);
+                    z = tile_operand<T>(dp[k], e / DT);
+                }
+                dv[e % DT] = mfma(x[e & 1], p, dv[e % DT]);
+                dk[e % DT] = mfma(y[e & 1], z, dk[e % DT]);
+                if (BIG) __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        products(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (NK > 1) products(NK - 1);              // beside the first half's exponentials
+        gradients(0);
+        __builtin_amdgcn_sched_barrier(0);
+        sums(0);                                   // beside the second half's
+        if (NK > 1) {
+            gradients(NK - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            sums(NK - 1);
         }
+    };
+    if (n0 < n1) fetch(qs0, ds0, st0, n0);
+    __syncthreads();                               // the fetched tiles are in LDS
+    for (int n = n0; n < n1; n += 2) {
+        if (n + 1 < n1) fetch(qs1, ds1, st1, n + 1);
+        step(qs0, ds0, st0, n);
+        __syncthreads();
+        if (n + 1 < n1) {
+            if (n + 2 < n1) fetch(qs0, ds0, st0, n + 2);
+            step(qs1, ds1, st1, n + 1);
+        }
+        __syncthreads();
     }
     if (!there) return;
-    const int64_t token = sg.k0 + mine;
+    const int64_t token = sg.k0 + key;
     if (f.splits > 1) {
         const int64_t n = (int64_t)a.n_k * a.kv_heads;
         float* pk = f.part + ((int64_t)split * 2 * n + token * a.kv_heads + kvh) * a.dim;
@@ -347,7 +424,15 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_dkv_join(BwdArgs f) {
     *reinterpret_cast<op4<T>*>(p + c) = o;
 }
 
-int dkv_splits(const gs_attn& a) { return 1; }
+// Parts that a key tile's rows are cut into, from the sizes alone: enough
+// workgroups for two a compute unit, as long as a part keeps eight steps.
+int dkv_splits(const gs_attn& a) {
+    constexpr int kUnits = 256, kMost = 16;
+    const int group = a.heads / a.kv_heads;
+    const int64_t groups = (int64_t)attn_tiles(a.n_k, kRows, a.n_seg) * a.kv_heads;
+    const int64_t steps = ((int64_t)a.n_q / a.n_seg + kStep - 1) / kStep * group;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(2 * kUnits + groups - 1) / groups, steps / 8, kMost}));
+}
 
 template <typename T, int D>
 hipError_t go(const BwdArgs& f, hipStream_t st) {
@@ -375,7 +460,7 @@ hipError_t by_dim(const BwdArgs& f, hipStream_t st) {
 size_t attention_bwd_ws_bytes(const gs_attn& a) {
     const int splits = dkv_splits(a);
     const size_t parts = splits > 1 ? (size_t)splits * 2 * a.n_k * a.kv_heads * a.dim * sizeof(float) : 0;
-    return align256((size_t)a.n_q * a.heads * sizeof(float)) + align256(parts);
+    return align256((size_t)a.n_q * a.heads * 2 * sizeof(float)) + align256(parts);
 }
 
 hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* ws, hipStream_t st) {
@@ -399,9 +484,10 @@ hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* 
     f.dv_row = g.dv.ld_row;
     f.dv_head = g.dv.ld_head;
     f.lse = g.lse;
-    f.delta = static_cast<float*>(ws);
+    f.base = static_cast<float*>(ws);
+    f.delta = f.base + (size_t)a.n_q * a.heads;
     f.splits = dkv_splits(a);
-    f.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * sizeof(float)));
+    f.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * 2 * sizeof(float)));
     return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, st) : by_dim<f16_t>(f, st);
 }
 

@@ -130,37 +130,61 @@ __device__ __forceinline__ op8<T> tile_operand(const acc16& c, int u) {
 // and arrive as zeros.
 template <typename T, int P, int ROWS>
 struct TileLoader {
-    static constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK;
+    static constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK, STEP = GS_BLOCK / PIECES;
+    static_assert(STEP % 16 == 0, "the key repeats every 16 rows: a lane's loads differ by whole rows");
     static constexpr int kRange = 0x7FFFFF00, kOutside = 0x7FFFFFF0;
-    int off[LOADS];                        // bytes from the tile's first row
+    int off;                               // bytes from the tile's first row; load u is u * STEP rows on
     int64_t ld;
 
     __device__ __forceinline__ void init(int64_t row_stride, int dim) {
         ld = row_stride;
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int x = threadIdx.x + u * GS_BLOCK, row = x / PIECES;
-            const int piece = (x % PIECES) ^ piece_key<P>(row);
-            off[u] = 8 * piece < dim ? (int)(row * ld * 2) + piece * 16 : kOutside;
-        }
+        const int row = threadIdx.x / PIECES, piece = (threadIdx.x % PIECES) ^ piece_key<P>(row);
+        off = 8 * piece < dim ? (int)(row * ld * 2) + piece * 16 : kOutside;
     }
 
     // base: the tile's first row; rows: how many there are from it on; skip:
     // bit u leaves load u's row out (zeros).
     __device__ __forceinline__ void load(T* tile, const T* base, int rows, uint32_t skip) const {
 #ifdef __HIP_DEVICE_COMPILE__              // the host pass has no buffer descriptors
-        const int64_t bytes = rows * ld * 2;
-        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<T*>(base), 0, (int)(bytes < kRange ? bytes : kRange), 0x00027000);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u)
+        for (int u = 0; u < LOADS; ++u) {
+            const int64_t bytes = max((int64_t)0, min((int64_t)kRange, (rows - u * STEP) * ld * 2));
+            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<T*>(base + u * STEP * ld), 0, (int)bytes, 0x00027000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 buf, (__attribute__((address_space(3))) void*)(tile + (u * GS_BLOCK + wave * GS_WAVE) * 8), 16,
-                (skip >> u) & 1 ? kOutside : off[u], 0, 0, 0);
+                (skip >> u) & 1 ? kOutside : off, 0, 0, 0);
+        }
 #endif
     }
 };
+
+// 64 words from `base` on into LDS, a lane of the wave each; those at or past
+// `n` are zeros.
+__device__ __forceinline__ void load_words(float* to, const float* base, int n) {
+#ifdef __HIP_DEVICE_COMPILE__
+    const __amdgpu_buffer_rsrc_t buf =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, min(n, 1 << 16) * 4, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)to, 4, lane_id() * 4, 0, 0,
+                                             0);
+#endif
+}
+
+// TileLoader's skip bits for the rows j .. of a segment with n keys whose flag
+// is 0.
+template <int P, int ROWS>
+__device__ __forceinline__ uint32_t rows_off(const uint8_t* on, int j, int n) {
+    constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK;
+    const int first = j + fresh(threadIdx.x) / PIECES;
+    uint32_t skip = 0;
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+        const int row = first + u * (GS_BLOCK / PIECES);
+        if (row < n && on[row] == 0) skip |= 1u << u;
+    }
+    return skip;
+}
 
 // Bits [lo, hi) of 64, ends clamped.
 __device__ __forceinline__ uint64_t bits_between(int lo, int hi) {
@@ -243,6 +267,12 @@ __device__ __forceinline__ Segment find_segment(const AttnArgs& a, const int32_t
 __device__ __forceinline__ void admitted(const AttnArgs& a, int nk, int first, int last, int& lo, int& hi) {
     lo = a.left >= 0 ? max((int64_t)0, (int64_t)first - a.left) : 0;
     hi = a.right >= 0 ? min((int64_t)nk, (int64_t)last + a.right + 1) : nk;
+}
+
+// Tokens [lo, hi) that admit any of the keys first .. last.
+__device__ __forceinline__ void admitting(const AttnArgs& a, int nq, int shift, int first, int last, int& lo, int& hi) {
+    lo = a.right >= 0 ? (int)max((int64_t)0, min((int64_t)nq, (int64_t)first - a.right - shift)) : 0;
+    hi = a.left >= 0 ? (int)max((int64_t)0, min((int64_t)nq, (int64_t)last + a.left - shift + 1)) : nq;
 }
 
 inline int attn_tiles(int64_t rows, int size, int n_seg) { return (int)(rows / size) + n_seg; }
