@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kRows = 128;                 // rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a step
+constexpr int kPart = 1024, kPartFew = 512;    // least keys of a part
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -112,8 +113,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
     const AttnArgs& a = f.a;
     const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
-    // the last tiles first: with ordered keys they have the most to do
-    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kRows, a.tiles - 1 - place.tile);
+    const Segment sg = find_segment<false, true>(a, kRows, a.tiles, place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -143,9 +143,13 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
     admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
     int j0 = lo / kKeys * kKeys, j1 = hi;
     if (f.splits > 1) {
-        const int per = ((max(hi - j0, 0) + f.splits - 1) / f.splits + kKeys - 1) / kKeys * kKeys;
+        const int per = max(((max(hi - j0, 0) + f.splits - 1) / f.splits + kKeys - 1) / kKeys * kKeys, kPart);
         j0 += split * per;
         j1 = min(hi, j0 + per);
+        if (j0 >= j1 && split > 0) {                       // nothing left for this part
+            if (there) store_sums(f, token, head, split, -INFINITY, 0.0f);
+            return;
+        }
     }
 
     TileLoader<T, P, kKeys> kl, vl;
@@ -251,16 +255,16 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
 constexpr int kFewRows = 32;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_few(FwdArgs f) {
+__global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
-    constexpr int PIECES = D / 8, LOADS = 32 * PIECES / GS_WAVE, WAVES = GS_BLOCK / GS_WAVE;
+    constexpr int PIECES = P / 8, LOADS = 32 * PIECES / GS_WAVE, WAVES = GS_BLOCK / GS_WAVE;
     __shared__ __attribute__((aligned(16))) T vs[WAVES][32 * P];
     __shared__ float ml[2][WAVES][32];
     __shared__ float half[WAVES][32 * 33];
     const AttnArgs& a = f.a;
     const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
-    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kFewRows, place.tile);
+    const Segment sg = find_segment<false, false>(a, kFewRows, a.tiles, place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kFewRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5;
@@ -288,28 +292,38 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_few(FwdA
     admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
     int j0 = lo / 32 * 32, j1 = hi;
     if (f.splits > 1) {
-        const int per = ((max(hi - j0, 0) + f.splits - 1) / f.splits + 127) / 128 * 128;
+        const int per = max(((max(hi - j0, 0) + f.splits - 1) / f.splits + 127) / 128 * 128, kPartFew);
         j0 += split * per;
         j1 = min(hi, j0 + per);
+        if (j0 >= j1 && split > 0) {                       // nothing left for this part
+            if (wave == 0 && there) store_sums(f, token, head, split, -INFINITY, 0.0f);
+            return;
+        }
     }
-    const T* kbase = static_cast<const T*>(a.k) + (int64_t)kvh * a.k_head;
-    const T* vbase = static_cast<const T*>(a.v) + (int64_t)kvh * a.v_head;
+    const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
+    const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    // loads outside a buffer's range give zeros: keys past the segment's end,
+    // pieces past the head's end, keys that are off
+    constexpr int STEP = GS_WAVE / PIECES, kOutside = 0x7FFFFFF0;
+    const int koff = (int)((lane & 31) * a.k_row * 2) + 16 * h;
+    const int voff = 8 * (lane % PIECES) < a.dim ? (int)(lane / PIECES * a.v_row * 2) + 16 * (lane % PIECES) : kOutside;
     op8<T> kp[KT], vp[LOADS];
     auto fetch = [&](int j) {
-        const int key = j + (lane & 31);
-        const bool on = key < sg.nk && (a.key_on == nullptr || a.key_on[sg.k0 + key]);
+        const int ln = fresh(lane);
+        const bool off = a.key_on != nullptr && j + (ln & 31) < sg.nk && a.key_on[sg.k0 + j + (ln & 31)] == 0;
+        const T* kt = kbase + j * a.k_row;
+        const T* vt = vbase + j * a.v_row;
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            const int c = 16 * t + 8 * h;
-            kp[t] = op8<T>{};
-            if (on && c < a.dim) kp[t] = *reinterpret_cast<const op8<T>*>(kbase + (int64_t)(sg.k0 + key) * a.k_row + c);
-        }
+        for (int t = 0; t < KT; ++t)
+            kp[t] = buffer_piece<T>(kt, (sg.nk - j) * a.k_row * 2, off || 16 * t + 8 * h >= a.dim ? kOutside : koff, 32 * t);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int x = lane + u * GS_WAVE, vkey = j + x / PIECES, piece = x % PIECES;
-            vp[u] = op8<T>{};
-            if (vkey < sg.nk && 8 * piece < a.dim && (a.key_on == nullptr || a.key_on[sg.k0 + vkey]))
-                vp[u] = *reinterpret_cast<const op8<T>*>(vbase + (int64_t)(sg.k0 + vkey) * a.v_row + 8 * piece);
+            bool out = false;
+            if (a.key_on != nullptr) {
+                const int key = j + u * STEP + ln / PIECES;
+                out = key < sg.nk && a.key_on[sg.k0 + key] == 0;
+            }
+            vp[u] = buffer_piece<T>(vt + u * STEP * a.v_row, (sg.nk - j - u * STEP) * a.v_row * 2, out ? kOutside : voff, 0);
         }
     };
 
@@ -324,6 +338,7 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_few(FwdA
     int j = j0 + 32 * wave;
     if (j < j1) fetch(j);
     for (; j < j1; j += 32 * WAVES) {
+        at.refresh();
         acc16 s[1];
         s[0] = acc16{};
 #pragma unroll
@@ -334,13 +349,15 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_few(FwdA
             *reinterpret_cast<op8<T>*>(mine + piece_at<P>(x / PIECES, x % PIECES)) = vp[u];
         }
         if (a.key_on != nullptr || j < alo || j + 32 > ahi) {
-            const int key = j + (lane & 31);
-            const uint64_t on = __ballot(key < sg.nk && (a.key_on == nullptr || a.key_on[sg.k0 + key]));
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int at = 8 * (e >> 2) + 4 * h + (e & 3);
-                if (j + at < klo || j + at >= khi || ((on >> at) & 1) == 0) s[0][e] = -INFINITY;
+            uint32_t seen = (uint32_t)bits_between(klo - j, khi - j);
+            if (a.key_on != nullptr) {
+                const int key = j + (fresh(lane) & 31);
+                seen &= (uint32_t)__ballot(key < sg.nk && a.key_on[sg.k0 + min(key, sg.nk - 1)]);
             }
+            seen >>= 4 * h;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if ((seen & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[0][e] = -INFINITY;
         }
         if (j + 32 * WAVES < j1) fetch(j + 32 * WAVES);
         const float alpha = softmax_step<1>(s, c, m, l);
@@ -353,7 +370,10 @@ __global__ void __launch_bounds__(GS_BLOCK, D > 64 ? 1 : 2) k_attention_few(FwdA
         for (int u = 0; u < 2; ++u) {
             const op8<T> p = tile_operand<T>(s[0], u);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = mfma(columns_operand<T, P>(mine, at, 16 * u, d), p, o[d]);
+            for (int d = 0; d < DT; ++d) {
+                o[d] = mfma(columns_operand<T, P>(mine, at, 16 * u, d), p, o[d]);
+                if (d & 1) __builtin_amdgcn_sched_barrier(0);      // no operands further ahead: two waves a SIMD
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -421,6 +441,7 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
         const int64_t step = rows * f.a.dim;
 #pragma unroll 8
         for (int s = wave; s < f.splits; s += WAVES) {
+            if (__int_as_float(__builtin_amdgcn_readlane(__float_as_int(part.y), s)) == 0.0f) continue;   // holds nothing
             const float2 v = *reinterpret_cast<const float2*>(p + s * step);
             const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
             o.x = fmaf(v.x, ws, o.x);
@@ -464,8 +485,13 @@ Plan plan(const gs_attn& a) {
     p.few = rows <= (int64_t)kFewRows * a.n_seg;
     p.tiles = whole_shares(attn_tiles(rows, p.few ? kFewRows : kRows, a.n_seg), a.kv_heads);
     const int64_t groups = (int64_t)p.tiles * a.kv_heads;
-    const int64_t want = ((p.few ? 4 : 2) * kUnits + groups - 1) / groups;
-    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, keys / (p.few ? 512 : 1024), kMaxSplits}));
+    int64_t want = ((p.few ? 4 : 2) * kUnits + groups - 1) / groups;
+    // ragged: segments are longer than the average, and a part is no shorter
+    // than kPart, so more parts than the average needs even the load out
+    if (p.few && a.cu_q != nullptr && a.n_seg > 1 && want > 1) want *= 4;
+    const int64_t most = a.n_seg > 1 && a.cu_q != nullptr ? kMaxSplits : keys / (p.few ? kPartFew : kPart);
+    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, most, kMaxSplits}));
+    if (keys < 2 * (p.few ? kPartFew : kPart)) p.splits = 1;
     return p;
 }
 

@@ -63,8 +63,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     const AttnArgs& a = f.a;
     const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, 1);
     const int kvh = place.head;
-    // the last tiles first: with ordered keys they have the most to do
-    const Segment sg = find_segment(a, a.cu_q, a.n_q, a.group, kRows, a.tiles - 1 - place.tile);
+    const Segment sg = find_segment<false, true>(a, kRows, a.tiles, place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -209,7 +208,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     const AttnArgs& a = f.a;
     const Place place = chiplet_place(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
-    const Segment sg = find_segment(a, a.cu_k, a.n_k, 1, kRows, place.tile);
+    const Segment sg = find_segment<true, false>(a, kRows, f.key_tiles, place.tile);
     const int key0 = sg.tile * kRows;
     if (key0 >= sg.nk) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;

@@ -160,6 +160,21 @@ struct TileLoader {
     }
 };
 
+// 16 bytes at `off` + `more` of a buffer of `bytes` (more: a constant); zeros
+// outside of it.
+template <typename T>
+__device__ __forceinline__ op8<T> buffer_piece(const T* base, int64_t bytes, int off, int more) {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<T*>(base), 0, (int)max((int64_t)0, min((int64_t)0x7FFFFF00, bytes)), 0x00027000);
+    const u4 v = __builtin_amdgcn_raw_buffer_load_b128(buf, off + more, 0, 0);
+    return __builtin_bit_cast(op8<T>, v);
+#else
+    return op8<T>{};
+#endif
+}
+
 // 64 words from `base` on into LDS, a lane of the wave each; those at or past
 // `n` are zeros.
 __device__ __forceinline__ void load_words(float* to, const float* base, int n) {
@@ -230,9 +245,8 @@ inline AttnArgs attn_args(const gs_attn& a) {
     return r;
 }
 
-// Tiles of `size` rows over ragged segments whose lengths only the device
-// knows: segment s starts at tile start(s)/size + s, which is at least as many
-// tiles as its rows need, for rows / size + n_seg tiles in all (some empty).
+// Tiles of `size` rows (or keys) over ragged segments whose lengths only the
+// device knows, for rows / size + n_seg tiles at most.
 struct Segment {
     int q0, nq, k0, nk;        // first row and rows of the queries and keys
     int tile;                  // the tile's number within the segment
@@ -243,18 +257,55 @@ __device__ __forceinline__ int cu_at(const int32_t* cu, int s, int n_seg, int n)
     return min(max(cu[s], 0), n);
 }
 
-// `cu`, `n`, `mul`: the rows that are tiled (mul of them a token).
-__device__ __forceinline__ Segment find_segment(const AttnArgs& a, const int32_t* cu, int n, int mul, int size,
-                                                int tile) {
+__device__ __forceinline__ int of_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// KEYS: the keys are tiled, a token each; otherwise the query rows, `group` of
+// them a token.  LAST_FIRST: a segment's last tile comes first (with ordered
+// keys it has the most to do).
+//   Up to 64 segments: a lane holds each, and the tiles are numbered from the
+// segment with the longest other side on, so that the workgroups with the most
+// steps start first.  A loop over the segments gives every lane its first tile.
+//   More: segment s starts at tile start(s) / size + s, at least as many tiles as
+// its rows need (some stay empty), found by a search with 64 probes a round.
+template <bool KEYS, bool LAST_FIRST>
+__device__ __forceinline__ Segment find_segment(const AttnArgs& a, int size, int tiles, int tile) {
+    const int lane = lane_id(), mul = KEYS ? 1 : a.group;
+    Segment s;
+    if (a.n_seg <= GS_WAVE) {
+        const int at = min(lane, a.n_seg - 1);
+        const int q0 = cu_at(a.cu_q, at, a.n_seg, a.n_q), k0 = cu_at(a.cu_k, at, a.n_seg, a.n_k);
+        const int nq = max(cu_at(a.cu_q, at + 1, a.n_seg, a.n_q) - q0, 0);
+        const int nk = max(cu_at(a.cu_k, at + 1, a.n_seg, a.n_k) - k0, 0);
+        const int has = lane < a.n_seg ? (int)(((KEYS ? (int64_t)nk : (int64_t)nq * mul) + size - 1) / size) : 0;
+        const int work = KEYS ? nq : nk;
+        int first = 0;
+        for (int t = 0; t < a.n_seg; ++t) {
+            const int w = of_lane(work, t), n = of_lane(has, t);
+            first += w > work || (w == work && t < lane) ? n : 0;
+        }
+        const uint64_t hit = __ballot(tile >= first && tile - first < has);
+        if (hit == 0) return Segment{0, 0, 0, 0, 0};
+        const int l = __builtin_ctzll(hit);
+        s.q0 = of_lane(q0, l);
+        s.nq = of_lane(nq, l);
+        s.k0 = of_lane(k0, l);
+        s.nk = of_lane(nk, l);
+        s.tile = tile - of_lane(first, l);
+        if (LAST_FIRST) s.tile = of_lane(has, l) - 1 - s.tile;
+        return s;
+    }
+    if (LAST_FIRST) tile = tiles - 1 - tile;
+    const int32_t* cu = KEYS ? a.cu_k : a.cu_q;
+    const int n = KEYS ? a.n_k : a.n_q;
     int lo = 0, hi = a.n_seg - 1;          // the last segment whose first tile is at or before `tile`
     while (lo < hi) {
-        const int m = (lo + hi + 1) >> 1;
-        const int first = (int)((int64_t)cu_at(cu, m, a.n_seg, n) * mul / size) + m;
-        if (first <= tile) lo = m;
-        else hi = m - 1;
+        const int step = (hi - lo + GS_WAVE - 1) / GS_WAVE;
+        const int m = lo + (lane + 1) * step;
+        const bool before = m <= hi && (int)((int64_t)cu_at(cu, m, a.n_seg, n) * mul / size) + m <= tile;
+        lo += __popcll(__ballot(before)) * step;
+        hi = min(hi, lo + step - 1);
     }
     lo = __builtin_amdgcn_readfirstlane(lo);           // the same in every lane: held in scalar registers
-    Segment s;
     s.q0 = __builtin_amdgcn_readfirstlane(cu_at(a.cu_q, lo, a.n_seg, a.n_q));
     s.nq = __builtin_amdgcn_readfirstlane(max(cu_at(a.cu_q, lo + 1, a.n_seg, a.n_q) - s.q0, 0));
     s.k0 = __builtin_amdgcn_readfirstlane(cu_at(a.cu_k, lo, a.n_seg, a.n_k));
