@@ -44,6 +44,25 @@ __device__ __forceinline__ float block_max(float v) {
     return v;
 }
 
+// N weights from column col on (zeros past the row's end).
+template <int N, bool WHOLE>
+__device__ __forceinline__ void load_weight(const float* weight, int col, int cols, float* w) {
+    if (WHOLE) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (col < cols) v = *reinterpret_cast<const float4*>(weight + col + i);
+            w[i] = v.x;
+            w[i + 1] = v.y;
+            w[i + 2] = v.z;
+            w[i + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = col + i < cols ? weight[col + i] : 0.0f;
+    }
+}
+
 template <typename T, bool WHOLE, int WAVES, int E>
 __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
     constexpr int N = Piece<T>::N, CH = E / N, TPR = WAVES * GS_WAVE, RPB = GS_BLOCK / TPR;
@@ -53,21 +72,23 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
     if (RPB > 1 && row >= a.rows) return;      // whole waves; RPB 1 launches no such row
     const T* __restrict__ x = static_cast<const T*>(a.x) + row * a.ld_x;
     const T* __restrict__ r = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_residual : nullptr;
-    float s[CH][N];
+    // every load of the row is on its way before the first is used
+    Raw<T, WHOLE> xs[CH], rs[CH];
+    float s[CH][N], w[CH][N];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * N;
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[c][i] = 0.0f;
-        if (col < a.cols) load_piece<T, WHOLE>(x + col, a.cols - col, s[c]);
+        xs[c].load(x + col, a.cols - col);
+        if (r) rs[c].load(r + col, a.cols - col);
     }
-    if (r) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int col = (c * TPR + t) * N;
-            if (col >= a.cols) continue;
+    for (int c = 0; c < CH; ++c) load_weight<N, WHOLE>(a.weight, (c * TPR + t) * N, a.cols, w[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        xs[c].floats(s[c]);
+        if (r) {
             float f[N];
-            load_piece<T, WHOLE>(r + col, a.cols - col, f);
+            rs[c].floats(f);
 #pragma unroll
             for (int i = 0; i < N; ++i) s[c][i] += f[i];
         }
@@ -90,12 +111,8 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * N;
-        float w[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = WHOLE ? (col < a.cols ? a.weight[col + i] : 0.0f)
-                                                 : (col + i < a.cols ? a.weight[col + i] : 0.0f);
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[c][i] *= rho * w[i];
+        for (int i = 0; i < N; ++i) s[c][i] *= rho * w[c][i];
         if (a.y && col < a.cols)
             store_piece<T, WHOLE>(static_cast<T*>(a.y) + row * a.ld_y + col, a.cols - col, s[c]);
     }
@@ -153,26 +170,27 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(
     float dw[CH][N], w[CH][N];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int col = (c * TPR + t) * N;
+        load_weight<N, WHOLE>(a.weight, (c * TPR + t) * N, a.cols, w[c]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            dw[c][i] = 0.0f;
-            w[c][i] = col + i < a.cols ? a.weight[col + i] : 0.0f;
-        }
+        for (int i = 0; i < N; ++i) dw[c][i] = 0.0f;
     }
     for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * RPB) {
         const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
         const T* tot = static_cast<const T*>(a.total) + row * a.ld_total;
+        Raw<T, WHOLE> ts[CH], ys[CH], ds[CH];
         float s[CH][N], g[CH][N];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * TPR + t) * N;
+            ts[c].load(tot + col, a.cols - col);
+            ys[c].load(dy + col, a.cols - col);
+            if (WHOLE && a.dtotal)
+                ds[c].load(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, a.cols - col);
+        }
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[c][i] = g[c][i] = 0.0f;
-            if (col < a.cols) {
-                load_piece<T, WHOLE>(tot + col, a.cols - col, s[c]);
-                load_piece<T, WHOLE>(dy + col, a.cols - col, g[c]);
-            }
+        for (int c = 0; c < CH; ++c) {
+            ts[c].floats(s[c]);
+            ys[c].floats(g[c]);
         }
         float ss = 0.0f, gs = 0.0f;
 #pragma unroll
@@ -194,8 +212,10 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(
             float d[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) d[i] = 0.0f;
-            if (a.dtotal)
-                load_piece<T, WHOLE>(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, a.cols - col, d);
+            if (a.dtotal) {
+                if (!WHOLE) ds[c].load(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, a.cols - col);
+                ds[c].floats(d);
+            }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float n = s[c][i] * r;
@@ -239,7 +259,8 @@ __global__ void __launch_bounds__(1024) k_norm_dweight(const float* __restrict__
     const int per = (n + 15) / 16;
     float v = 0.0f;
     if (col < cols)
-        for (int i = w * per; i < n && i < (w + 1) * per; ++i) v += parts[(int64_t)i * cols + col];
+#pragma unroll 8
+        for (int i = w * per; i < min(n, (w + 1) * per); ++i) v += parts[(int64_t)i * cols + col];
     sum[w][l] = v;
     __syncthreads();
     if (w == 0 && col < cols) {
@@ -264,6 +285,7 @@ template <typename T, bool WHOLE>
 hipError_t norm_go(const gs_norm_args& a, hipStream_t st) {
     const uint32_t by4 = div_up(a.rows, 4);
     if (a.cols <= 1024) k_rms_norm<T, WHOLE, 1, 16><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 1536) k_rms_norm<T, WHOLE, 1, 24><<<by4, GS_BLOCK, 0, st>>>(a);
     else if (a.cols <= 2048) k_rms_norm<T, WHOLE, 1, 32><<<by4, GS_BLOCK, 0, st>>>(a);
     else if (a.cols <= 8192) k_rms_norm<T, WHOLE, 4, 32><<<a.rows, GS_BLOCK, 0, st>>>(a);
     else k_rms_norm<T, WHOLE, 4, 64><<<a.rows, GS_BLOCK, 0, st>>>(a);
@@ -274,7 +296,7 @@ template <typename T>
 hipError_t norm_type(const gs_norm_args& a, hipStream_t st) {
     const bool w = a.cols % Piece<T>::N == 0 && whole<T>(a.x, a.ld_x, 16) && whole<T>(a.residual, a.ld_residual, 16) &&
                    whole<T>(a.total, a.ld_total, 16) && whole<T>(a.y, a.ld_y, 16) &&
-                   whole<uint8_t>(a.q, a.ld_q, Piece<T>::N);
+                   whole<uint8_t>(a.q, a.ld_q, Piece<T>::N) && whole<float>(a.weight, 0, 16);
     return w ? norm_go<T, true>(a, st) : norm_go<T, false>(a, st);
 }
 
@@ -284,6 +306,7 @@ hipError_t norm_bwd_go(const gs_norm_bwd_args& a, float* parts, hipStream_t st) 
     if (a.cols <= 2048) {
         n = norm_parts(a.rows, 4);
         if (a.cols <= 1024) k_rms_norm_bwd<T, WHOLE, 1, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
+        else if (a.cols <= 1536) k_rms_norm_bwd<T, WHOLE, 1, 24><<<n, GS_BLOCK, 0, st>>>(a, parts);
         else k_rms_norm_bwd<T, WHOLE, 1, 32><<<n, GS_BLOCK, 0, st>>>(a, parts);
     } else if (a.cols <= 4096) {
         k_rms_norm_bwd<T, WHOLE, 4, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
@@ -297,7 +320,7 @@ hipError_t norm_bwd_go(const gs_norm_bwd_args& a, float* parts, hipStream_t st) 
 template <typename T>
 hipError_t norm_bwd_type(const gs_norm_bwd_args& a, float* parts, hipStream_t st) {
     const bool w = a.cols % Piece<T>::N == 0 && whole<T>(a.dy, a.ld_dy, 16) && whole<T>(a.total, a.ld_total, 16) &&
-                   whole<T>(a.dtotal, a.ld_dtotal, 16) && whole<T>(a.dx, a.ld_dx, 16);
+                   whole<T>(a.dtotal, a.ld_dtotal, 16) && whole<T>(a.dx, a.ld_dx, 16) && whole<float>(a.weight, 0, 16);
     return w ? norm_bwd_go<T, true>(a, parts, st) : norm_bwd_go<T, false>(a, parts, st);
 }
 

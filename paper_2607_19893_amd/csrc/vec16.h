@@ -15,20 +15,30 @@ struct Piece {
     typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
 };
 
-// N consecutive elements at p as floats.  WHOLE: one 16-byte load (p aligned,
-// all N there); otherwise the first `there` elements one by one, zeros behind.
+// N consecutive elements at p, first as they are in memory (so that several
+// loads can be on their way), then as floats.  WHOLE: one 16-byte load (p
+// aligned) if any is there; otherwise the first `there` elements one by one.
+// Zeros behind.
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void load_piece(const T* p, int there, float* f) {
-    constexpr int N = Piece<T>::N;
-    if (WHOLE) {
-        const typename Piece<T>::vec v = *reinterpret_cast<const typename Piece<T>::vec*>(p);
+struct Raw {
+    static constexpr int N = Piece<T>::N;
+    typename Piece<T>::vec v;
+
+    __device__ __forceinline__ void load(const T* p, int there) {
+        v = typename Piece<T>::vec{};
+        if (WHOLE) {
+            if (there > 0) v = *reinterpret_cast<const typename Piece<T>::vec*>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < there) v[i] = p[i];
+        }
+    }
+    __device__ __forceinline__ void floats(float* f) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = (float)v[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = i < there ? (float)p[i] : 0.0f;
     }
-}
+};
 
 // The way back, rounded to nearest even.
 template <typename T, bool WHOLE>
