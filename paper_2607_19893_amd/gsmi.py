@@ -206,9 +206,22 @@ def ptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+_raw_stream = None
+
+
 def current_stream():
-    import torch
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """The current HIP stream of torch's current device, as an address."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.current_stream()                # torch sets the GPU up
+        # torch's own short way to the address (an object per call costs 3 us)
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        if raw is not None and device is not None:
+            _raw_stream = lambda: raw(device())
+        else:
+            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream
+    return ctypes.c_void_p(_raw_stream())
 
 
 def make_camera(cam) -> gs_camera:
@@ -474,44 +487,54 @@ def gate_result_from(buf) -> gs_gate_result:
 # ---- token operators ----------------------------------------------------------
 
 def _ws(ws):
-    return (ptr(ws), ws.numel() * ws.element_size()) if ws is not None else (None, 0)
+    return (ws.data_ptr(), ws.numel() * ws.element_size()) if ws is not None else (None, 0)
+
+
+_TOKEN_TYPES = {}
 
 
 def token_dtype(t) -> int:
-    import torch
-    d = {torch.float32: GS_F32, torch.bfloat16: GS_BF16, torch.float16: GS_F16}
-    if t.dtype not in d:
+    if not _TOKEN_TYPES:
+        import torch
+        _TOKEN_TYPES.update({torch.float32: GS_F32, torch.bfloat16: GS_BF16, torch.float16: GS_F16})
+    d = _TOKEN_TYPES.get(t.dtype)
+    if d is None:
         raise ValueError("tokens are float32, bfloat16 or float16, not %s" % t.dtype)
-    return d[t.dtype]
+    return d
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def make_rows(t) -> gs_rows:
     """A [rows, heads, dim] tensor whose heads' elements are contiguous."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    st = t.stride()
+    if len(st) != 3 or (st[2] != 1 and t.shape[2] > 1):
         raise ValueError("a token matrix is [rows, heads, dim] with contiguous elements, not %s with strides %s"
-                         % (tuple(t.shape), t.stride()))
-    return gs_rows(t.data_ptr(), t.stride(0), t.stride(1))
+                         % (tuple(t.shape), st))
+    return gs_rows(t.data_ptr(), st[0], st[1])
 
 
-def _ld(t, rows, cols, what, like=None):
-    """Row stride of a [rows, cols] tensor with contiguous rows (0 for None)."""
+def _ld(t, shape, what, dtype=None):
+    """Row stride of a tensor of that shape with contiguous rows (0 for None)."""
     if t is None:
         return 0
-    if tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        raise ValueError("%s is [%d, %d] with contiguous rows, not %s with strides %s"
-                         % (what, rows, cols, tuple(t.shape), t.stride()))
-    if like is not None and t.dtype != like.dtype:
-        raise ValueError("%s is %s, not %s" % (what, like.dtype, t.dtype))
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    st = t.stride()
+    if t.shape != shape or (st[1] != 1 and shape[1] > 1):
+        raise ValueError("%s is %s with contiguous rows, not %s with strides %s" % (what, list(shape), list(t.shape), st))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s is %s, not %s" % (what, dtype, t.dtype))
+    return st[0] if shape[0] > 1 else max(shape[1], st[0])
 
 
 def gs_rms_norm(x, weight, eps, y=None, residual=None, total=None, q=None, q_scale=None, stream=None):
-    rows, cols = x.shape
-    blocks = -(-cols // GS_NORM_BLOCK)
-    a = gs_norm_args(rows, cols, token_dtype(x), float(eps), x.data_ptr(), ptr(residual), ptr(weight), ptr(total),
-                     ptr(y), ptr(q), ptr(q_scale), _ld(x, rows, cols, "x"), _ld(residual, rows, cols, "residual", x),
-                     _ld(total, rows, cols, "total", x), _ld(y, rows, cols, "y", x), _ld(q, rows, cols, "q"),
-                     _ld(q_scale, rows, blocks, "q_scale"))
+    shape, dt = x.shape, x.dtype
+    rows, cols = shape
+    a = gs_norm_args(rows, cols, token_dtype(x), eps, x.data_ptr(), _at(residual), _at(weight), _at(total),
+                     _at(y), _at(q), _at(q_scale), _ld(x, shape, "x"), _ld(residual, shape, "residual", dt),
+                     _ld(total, shape, "total", dt), _ld(y, shape, "y", dt), _ld(q, shape, "q"),
+                     _ld(q_scale, (rows, -(-cols // GS_NORM_BLOCK)), "q_scale"))
     return _check("gs_rms_norm", _lib.gs_rms_norm(ctypes.byref(a), stream if stream is not None else current_stream()))
 
 
@@ -520,11 +543,10 @@ def gs_rms_norm_bwd_ws_bytes(rows, cols) -> int:
 
 
 def gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=None, stream=None):
-    rows, cols = total.shape
-    a = gs_norm_bwd_args(rows, cols, token_dtype(total), float(eps), dy.data_ptr(), total.data_ptr(), ptr(dtotal),
-                         ptr(weight), dx.data_ptr(), ptr(dweight), _ld(dy, rows, cols, "dy", total),
-                         _ld(total, rows, cols, "total"), _ld(dtotal, rows, cols, "dtotal", total),
-                         _ld(dx, rows, cols, "dx", total))
+    shape, dt = total.shape, total.dtype
+    a = gs_norm_bwd_args(shape[0], shape[1], token_dtype(total), eps, dy.data_ptr(), total.data_ptr(), _at(dtotal),
+                         _at(weight), dx.data_ptr(), _at(dweight), _ld(dy, shape, "dy", dt),
+                         _ld(total, shape, "total"), _ld(dtotal, shape, "dtotal", dt), _ld(dx, shape, "dx", dt))
     p, n = _ws(ws)
     return _check("gs_rms_norm_bwd", _lib.gs_rms_norm_bwd(ctypes.byref(a), p, n,
                                                           stream if stream is not None else current_stream()))
@@ -563,17 +585,18 @@ def gs_rotary_freqs(pairs, base=10000.0, scaling=GS_ROPE_PLAIN, factor=1.0, trai
 
 
 def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-1, right=-1) -> gs_attn:
-    if k.shape != v.shape or k.shape[2] != q.shape[2] or k.dtype != q.dtype or v.dtype != q.dtype:
-        raise ValueError("q, k, v do not fit: %s, %s, %s" % (q.shape, k.shape, v.shape))
+    qs, ks = q.shape, k.shape
+    if ks != v.shape or ks[2] != qs[2] or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k, v do not fit: %s, %s, %s" % (qs, ks, v.shape))
     if cu_q is not None:
         n_seg = cu_q.numel() - 1
-        if cu_k is None or cu_k.numel() != cu_q.numel() or "int32" not in str(cu_q.dtype) or "int32" not in str(cu_k.dtype):
-            raise ValueError("cu_q and cu_k are int32 of the same length")
-    if key_on is not None and (key_on.numel() != k.shape[0] or key_on.element_size() != 1):
-        raise ValueError("key_on is one byte per key")
-    return gs_attn(token_dtype(q), q.shape[0], k.shape[0], int(n_seg), q.shape[1], k.shape[1], q.shape[2], int(left),
-                   int(right), float(scale), ptr(cu_q), ptr(cu_k), ptr(key_on), make_rows(q), make_rows(k),
-                   make_rows(v))
+        if cu_k is None or cu_k.numel() != n_seg + 1 or str(cu_q.dtype) != "torch.int32" or cu_k.dtype != cu_q.dtype \
+                or not cu_q.is_contiguous() or not cu_k.is_contiguous():
+            raise ValueError("cu_q and cu_k are contiguous int32 of the same length")
+    if key_on is not None and (key_on.numel() != ks[0] or key_on.element_size() != 1 or not key_on.is_contiguous()):
+        raise ValueError("key_on is one contiguous byte per key")
+    return gs_attn(token_dtype(q), qs[0], ks[0], n_seg, qs[1], ks[1], qs[2], left, right, scale, _at(cu_q), _at(cu_k),
+                   _at(key_on), make_rows(q), make_rows(k), make_rows(v))
 
 
 def gs_attention_ws_bytes(attn: gs_attn, backward=False) -> int:

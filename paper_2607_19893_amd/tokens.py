@@ -15,6 +15,9 @@ import torch
 from . import gsmi
 
 
+_DENSE = torch.contiguous_format
+
+
 class Normed(NamedTuple):
     """What rms_norm returns: y (None in 8 bits), the sum (x itself without a
     residual), and with eight_bit the rows as float8_e4m3fn and their scales
@@ -26,12 +29,12 @@ class Normed(NamedTuple):
 
 
 def _same_device(*tensors):
-    d = tensors[0].device
+    d = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != d:
-            raise ValueError("tensors on %s and %s" % (d, t.device))
-    if d.type != "cuda":
-        raise ValueError("tokens live on the GPU, not on %s" % d)
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors on %s and %s" % (tensors[0].device, t.device))
+    if d < 0:
+        raise ValueError("tokens live on the GPU, not on %s" % tensors[0].device)
 
 
 def _fp32(t, n, what):
@@ -48,13 +51,13 @@ def rms_norm(x, weight, eps=1e-6, residual=None, eight_bit=False) -> Normed:
     _same_device(x, weight, residual)
     rows, cols = x.shape
     _fp32(weight, cols, "weight")
-    total = torch.empty_like(x, memory_format=torch.contiguous_format) if residual is not None else None
+    total = torch.empty_like(x, memory_format=_DENSE) if residual is not None else None
     y = q = scale = None
     if eight_bit:
         q = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
         scale = torch.empty(rows, -(-cols // gsmi.GS_NORM_BLOCK), dtype=torch.float32, device=x.device)
     else:
-        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        y = torch.empty_like(x, memory_format=_DENSE)
     gsmi.gs_rms_norm(x, weight, eps, y=y, residual=residual, total=total, q=q, q_scale=scale)
     return Normed(y, x if total is None else total, q, scale)
 
@@ -64,7 +67,7 @@ def rms_norm_backward(dy, total, weight, eps=1e-6, dtotal=None):
     _same_device(dy, total, weight, dtotal)
     rows, cols = total.shape
     _fp32(weight, cols, "weight")
-    dx = torch.empty_like(total, memory_format=torch.contiguous_format)
+    dx = torch.empty_like(total, memory_format=_DENSE)
     dweight = torch.empty_like(weight)
     ws = _workspace(gsmi.gs_rms_norm_bwd_ws_bytes(rows, cols), total.device)
     gsmi.gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=dtotal)
@@ -78,7 +81,7 @@ def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amp
     if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape != (tensors[0].shape[0], len(axis_pairs)):
         raise ValueError("pos is float32 [tokens, %d]" % len(axis_pairs))
     _fp32(freq, sum(axis_pairs), "freq")
-    out = tensors if inplace else tuple(torch.empty_like(t, memory_format=torch.contiguous_format) for t in tensors)
+    out = tensors if inplace else tuple(torch.empty_like(t, memory_format=_DENSE) for t in tensors)
     gsmi.gs_rotary(tensors, out, pos, freq, axis_pairs, interleaved, inverse, amplitude)
     return out
 
@@ -87,7 +90,7 @@ def attention(q, k, v, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, l
     """(out, lse): q [n_q, heads, dim] over k, v [n_k, kv_heads, dim], segment by segment."""
     _same_device(q, k, v, cu_q, cu_k, key_on)
     a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
-    out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    out = torch.empty_like(q, memory_format=_DENSE)
     lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
     gsmi.gs_attention(a, out, lse, _workspace(gsmi.gs_attention_ws_bytes(a), q.device))
     return out, lse
@@ -102,7 +105,7 @@ def attention_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, n_seg=1, k
             raise ValueError("%s has q's shape and type" % what)
     _fp32(lse, q.shape[0] * q.shape[1], "lse")
     a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
-    dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
+    dq, dk, dv = (torch.empty_like(t, memory_format=_DENSE) for t in (q, k, v))
     gsmi.gs_attention_bwd(a, out, lse, dout, dq, dk, dv, _workspace(gsmi.gs_attention_ws_bytes(a, True), q.device))
     return dq, dk, dv
 
