@@ -772,9 +772,10 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  * left = -1, right = 0 is the ordered (causal) form, right = left = -1 all keys.
  * A row that admits no key, or none with a score above -infinity, has out 0,
  * lse -infinity and passes no gradient.  Head h reads key head h / (heads /
- * kv_heads).  The rows of k and v that key_on switches off are not read at all:
- * NaN or infinities there reach nothing, and their dk, dv are 0.  A NaN or
- * infinity in a key that is on may reach every row of its segment.
+ * kv_heads).  What the rows of k and v that key_on switches off hold reaches nothing
+ * (NaN and infinities too), and their dk, dv are 0; so do rows of q and dout
+ * that admit no key.  A NaN or infinity in a key that is on may reach every row
+ * of its segment.
  *   cu_q, cu_k [n_seg + 1] int32, ascending from 0 to n_q and n_k: the segments'
  *     first rows (empty ones allowed); both NULL: n_seg segments of equal
  *     length (n_seg divides n_q and n_k).  Values outside [0, n] are taken as

@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kRows = 128;                 // rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a step
-constexpr int kPart = 1024, kPartFew = 512;    // least keys of a part
+constexpr int kPart = 1024, kPartFew = 256;    // least keys of a part
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -157,11 +157,21 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
     vl.init(a.v_row, a.dim);
     const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
     const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    // Which keys of a step are on is loaded a step before its tiles, so that
+    // nothing waits for it: `on` for the step that computes, `on_next` for the
+    // one whose tiles arrive, `flag` (a key a lane) for the one after.
+    const uint8_t* const flags = a.key_on + sg.k0;
+    uint64_t on = ~0ull, on_next = ~0ull;
+    uint8_t flag = 1;
     auto fetch = [&](T* ks, T* vs, int j) {
         uint32_t skip = 0;
-        if (a.key_on != nullptr) skip = rows_off<P, kKeys>(a.key_on + sg.k0, j, sg.nk);
-        kl.load(ks, kbase + j * a.k_row, sg.nk - j, skip);
-        vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);
+        if (a.key_on != nullptr) {
+            on_next = __ballot(flag);
+            flag = key_flag(flags, j + kKeys + fresh(lane), sg.nk);
+            skip = rows_off<P, kKeys>(on_next);
+        }
+        kl.load(ks, kbase + j * a.k_row, sg.nk - j, 0);
+        vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);     // a probability of 0 does not stop a NaN
     };
 
     const float c = a.scale * kLog2e;
@@ -193,11 +203,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
             __builtin_amdgcn_sched_barrier(0);
         }
         if (a.key_on != nullptr || j < alo || j + kKeys > ahi) {
-            uint64_t seen = bits_between(klo - j, khi - j);
-            if (a.key_on != nullptr) {
-                const int key = j + fresh(lane);
-                seen &= __ballot(key < sg.nk && a.key_on[sg.k0 + min(key, sg.nk - 1)]);
-            }
+            const uint64_t seen = bits_between(klo - j, khi - j) & on;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
@@ -227,13 +233,18 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
         }
     };
 
-    if (j0 < j1) fetch(ks0, vs0, j0);
+    if (j0 < j1) {
+        if (a.key_on != nullptr) flag = key_flag(flags, j0 + lane, sg.nk);
+        fetch(ks0, vs0, j0);
+    }
     __syncthreads();                               // the fetched tiles are in LDS
     for (int j = j0; j < j1; j += 2 * kKeys) {
+        on = on_next;
         if (j + kKeys < j1) fetch(ks1, vs1, j + kKeys);
         step(ks0, vs0, j);
         __syncthreads();
         if (j + kKeys < j1) {
+            on = on_next;
             if (j + 2 * kKeys < j1) fetch(ks0, vs0, j + 2 * kKeys);
             step(ks1, vs1, j + kKeys);
         }
@@ -303,28 +314,23 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
     const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
     // loads outside a buffer's range give zeros: keys past the segment's end,
-    // pieces past the head's end, keys that are off
+    // pieces past the head's end
     constexpr int STEP = GS_WAVE / PIECES, kOutside = 0x7FFFFFF0;
     const int koff = (int)((lane & 31) * a.k_row * 2) + 16 * h;
     const int voff = 8 * (lane % PIECES) < a.dim ? (int)(lane / PIECES * a.v_row * 2) + 16 * (lane % PIECES) : kOutside;
+    const uint8_t* const flags = a.key_on + sg.k0;
     op8<T> kp[KT], vp[LOADS];
+    uint8_t flag = 1;                                      // of key lane & 31 of the step
     auto fetch = [&](int j) {
-        const int ln = fresh(lane);
-        const bool off = a.key_on != nullptr && j + (ln & 31) < sg.nk && a.key_on[sg.k0 + j + (ln & 31)] == 0;
         const T* kt = kbase + j * a.k_row;
         const T* vt = vbase + j * a.v_row;
+        if (a.key_on != nullptr) flag = key_flag(flags, j + (fresh(lane) & 31), sg.nk);
 #pragma unroll
         for (int t = 0; t < KT; ++t)
-            kp[t] = buffer_piece<T>(kt, (sg.nk - j) * a.k_row * 2, off || 16 * t + 8 * h >= a.dim ? kOutside : koff, 32 * t);
+            kp[t] = buffer_piece<T>(kt, (sg.nk - j) * a.k_row * 2, 16 * t + 8 * h >= a.dim ? kOutside : koff, 32 * t);
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            bool out = false;
-            if (a.key_on != nullptr) {
-                const int key = j + u * STEP + ln / PIECES;
-                out = key < sg.nk && a.key_on[sg.k0 + key] == 0;
-            }
-            vp[u] = buffer_piece<T>(vt + u * STEP * a.v_row, (sg.nk - j - u * STEP) * a.v_row * 2, out ? kOutside : voff, 0);
-        }
+        for (int u = 0; u < LOADS; ++u)
+            vp[u] = buffer_piece<T>(vt + u * STEP * a.v_row, (sg.nk - j - u * STEP) * a.v_row * 2, voff, 0);
     };
 
     const float c = a.scale * kLog2e;
@@ -343,18 +349,22 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
         s[0] = acc16{};
 #pragma unroll
         for (int t = 0; t < KT; ++t) s[0] = mfma(kp[t], q[t], s[0]);
+        uint32_t on = ~0u;
+        if (a.key_on != nullptr) {
+            on = (uint32_t)__ballot(flag);
+            // the values of a key that is off may be anything, and a
+            // probability of 0 does not stop a NaN
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u)
+                if (((on >> (u * STEP + fresh(lane) / PIECES)) & 1) == 0) vp[u] = op8<T>{};
+        }
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
             const int x = lane + u * GS_WAVE;
             *reinterpret_cast<op8<T>*>(mine + piece_at<P>(x / PIECES, x % PIECES)) = vp[u];
         }
         if (a.key_on != nullptr || j < alo || j + 32 > ahi) {
-            uint32_t seen = (uint32_t)bits_between(klo - j, khi - j);
-            if (a.key_on != nullptr) {
-                const int key = j + (fresh(lane) & 31);
-                seen &= (uint32_t)__ballot(key < sg.nk && a.key_on[sg.k0 + min(key, sg.nk - 1)]);
-            }
-            seen >>= 4 * h;
+            const uint32_t seen = ((uint32_t)bits_between(klo - j, khi - j) & on) >> (4 * h);
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if ((seen & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[0][e] = -INFINITY;
@@ -441,8 +451,9 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
         const int64_t step = rows * f.a.dim;
 #pragma unroll 8
         for (int s = wave; s < f.splits; s += WAVES) {
-            if (__int_as_float(__builtin_amdgcn_readlane(__float_as_int(part.y), s)) == 0.0f) continue;   // holds nothing
-            const float2 v = *reinterpret_cast<const float2*>(p + s * step);
+            // a part that found no keys wrote no tile; the first part always did
+            const float ls = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(part.y), s));
+            const float2 v = *reinterpret_cast<const float2*>(p + (ls == 0.0f ? 0 : s) * step);
             const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
             o.x = fmaf(v.x, ws, o.x);
             o.y = fmaf(v.y, ws, o.y);
@@ -485,13 +496,18 @@ Plan plan(const gs_attn& a) {
     p.few = rows <= (int64_t)kFewRows * a.n_seg;
     p.tiles = whole_shares(attn_tiles(rows, p.few ? kFewRows : kRows, a.n_seg), a.kv_heads);
     const int64_t groups = (int64_t)p.tiles * a.kv_heads;
-    int64_t want = ((p.few ? 4 : 2) * kUnits + groups - 1) / groups;
-    // ragged: segments are longer than the average, and a part is no shorter
-    // than kPart, so more parts than the average needs even the load out
-    if (p.few && a.cu_q != nullptr && a.n_seg > 1 && want > 1) want *= 4;
-    const int64_t most = a.n_seg > 1 && a.cu_q != nullptr ? kMaxSplits : keys / (p.few ? kPartFew : kPart);
-    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, most, kMaxSplits}));
-    if (keys < 2 * (p.few ? kPartFew : kPart)) p.splits = 1;
+    // Ragged segments (their lengths are not known here) are longer than the
+    // average, and a part is no shorter than kPart: more parts than the average
+    // needs even the load out.  24 regions of 900..9000 keys under 16 heads: 99
+    // us with 12 parts, 156 with 3.  One segment, or equal ones: one workgroup a
+    // unit; one row over 32,768 keys under 8 key heads takes 41 us in 32 parts
+    // and 44 in 64, which the join has to read.
+    const bool ragged = a.cu_q != nullptr && a.n_seg > 1;
+    int64_t want = ((p.few && !ragged ? 1 : (p.few ? 4 : 2)) * kUnits + groups - 1) / groups;
+    if (p.few && ragged && want > 1) want *= 4;
+    const int64_t least = p.few ? kPartFew : kPart;
+    const int64_t most = keys < 2 * least ? 1 : (ragged ? kMaxSplits : std::min<int64_t>(kMaxSplits, keys / least));
+    p.splits = (int32_t)std::max<int64_t>(1, std::min(want, most));
     return p;
 }
 

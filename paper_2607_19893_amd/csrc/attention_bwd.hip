@@ -111,9 +111,17 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     vl.init(a.v_row, a.dim);
     const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
     const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    // the keys' flags, loaded a step before the tiles that they belong to
+    const uint8_t* const flags = a.key_on + sg.k0;
+    uint64_t on = ~0ull, on_next = ~0ull;
+    uint8_t flag = 1;
     auto fetch = [&](T* ks, T* vs, int j) {
         uint32_t skip = 0;
-        if (a.key_on != nullptr) skip = rows_off<P, kStep>(a.key_on + sg.k0, j, sg.nk);
+        if (a.key_on != nullptr) {
+            on_next = __ballot(flag);
+            flag = key_flag(flags, j + kStep + fresh(lane), sg.nk);
+            skip = rows_off<P, kStep>(on_next);
+        }
         kl.load(ks, kbase + j * a.k_row, sg.nk - j, skip);
         vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);
     };
@@ -129,11 +137,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
         const bool test = a.key_on != nullptr || j < alo || j + kStep > ahi;
         uint64_t seen = ~0ull;
         if (test) {
-            seen = bits_between(klo - j, khi - j);
-            if (a.key_on != nullptr) {
-                const int key = j + fresh(lane);
-                seen &= __ballot(key < sg.nk && a.key_on[sg.k0 + min(key, sg.nk - 1)]);
-            }
+            seen = bits_between(klo - j, khi - j) & on;
         }
 #pragma unroll
         for (int k = 0; k < kStep / 32; ++k) {
@@ -175,13 +179,18 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
         }
     };
     const int j0 = lo / kStep * kStep;
-    if (j0 < hi) fetch(ks0, vs0, j0);
+    if (j0 < hi) {
+        if (a.key_on != nullptr) flag = key_flag(flags, j0 + lane, sg.nk);
+        fetch(ks0, vs0, j0);
+    }
     __syncthreads();                               // the fetched tiles are in LDS
     for (int j = j0; j < hi; j += 2 * kStep) {
+        on = on_next;
         if (j + kStep < hi) fetch(ks1, vs1, j + kStep);
         step(ks0, vs0, j);
         __syncthreads();
         if (j + kStep < hi) {
+            on = on_next;
             if (j + 2 * kStep < hi) fetch(ks0, vs0, j + 2 * kStep);
             step(ks1, vs1, j + kStep);
         }
@@ -237,7 +246,12 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         TileLoader<T, P, kRows> vl;
         vl.init(a.v_row, a.dim);
         uint32_t skip = 0;
-        if (a.key_on != nullptr) skip = rows_off<P, kRows>(a.key_on + sg.k0, key0, sg.nk);
+        if (a.key_on != nullptr) {
+            const int first = key0 + threadIdx.x / vl.PIECES;
+#pragma unroll
+            for (int u = 0; u < vl.LOADS; ++u)
+                if (key_flag(a.key_on + sg.k0, first + u * vl.STEP, sg.nk) == 0) skip |= 1u << u;
+        }
         vl.load(vs, static_cast<const T*>(a.v) + (sg.k0 + key0) * a.v_row + (int64_t)kvh * a.v_head, sg.nk - key0,
                 skip);
     }
@@ -265,17 +279,19 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     dl.init(f.do_row, a.dim);
     const int64_t qbase = sg.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
     const int64_t dbase = sg.q0 * f.do_row + (int64_t)kvh * a.group * f.do_head;
+    // their bases (+inf for such a token), loaded a step before the tiles
+    auto row_flag = [&](int n) {
+        const int g = n / per, t = t0 + (n - g * per) * ST + (fresh(lane) & (ST - 1));
+        return t < sg.nq ? f.base[(int64_t)(kvh * a.group + g) * a.n_q + sg.q0 + t] : INFINITY;
+    };
+    float flag = 0.0f;
     auto fetch = [&](T* qs, T* ds, float* st, int n) {
         const int g = n / per, t = t0 + (n - g * per) * ST;
         const float* bases = f.base + (int64_t)(kvh * a.group + g) * a.n_q + sg.q0;
         uint32_t skip = 0;
         if (empties) {
-            const int first = fresh(threadIdx.x) / ql.PIECES;
-#pragma unroll
-            for (int u = 0; u < ql.LOADS; ++u) {
-                const int row = t + first + u * (GS_BLOCK / ql.PIECES);
-                if (row < sg.nq && bases[row] == INFINITY) skip |= 1u << u;
-            }
+            skip = rows_off<P, ST>(__ballot(flag != INFINITY));
+            if (n + 1 < n1) flag = row_flag(n + 1);
         }
         ql.load(qs, static_cast<const T*>(a.q) + qbase + g * a.q_head + t * a.q_row, sg.nq - t, skip);
         dl.load(ds, static_cast<const T*>(f.dout) + dbase + g * f.do_head + t * f.do_row, sg.nq - t, skip);
@@ -367,7 +383,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
             sums(NK - 1);
         }
     };
-    if (n0 < n1) fetch(qs0, ds0, st0, n0);
+    if (n0 < n1) {
+        if (empties) flag = row_flag(n0);
+        fetch(qs0, ds0, st0, n0);
+    }
     __syncthreads();                               // the fetched tiles are in LDS
     for (int n = n0; n < n1; n += 2) {
         if (n + 1 < n1) fetch(qs1, ds1, st1, n + 1);

@@ -186,20 +186,19 @@ __device__ __forceinline__ void load_words(float* to, const float* base, int n) 
 #endif
 }
 
-// TileLoader's skip bits for the rows j .. of a segment with n keys whose flag
-// is 0.
+// TileLoader's skip bits from a tile's rows, bit r of `on` for row r (up to 64).
 template <int P, int ROWS>
-__device__ __forceinline__ uint32_t rows_off(const uint8_t* on, int j, int n) {
+__device__ __forceinline__ uint32_t rows_off(uint64_t on) {
     constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK;
-    const int first = j + fresh(threadIdx.x) / PIECES;
+    const int first = fresh(threadIdx.x) / PIECES;
     uint32_t skip = 0;
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-        const int row = first + u * (GS_BLOCK / PIECES);
-        if (row < n && on[row] == 0) skip |= 1u << u;
-    }
+    for (int u = 0; u < LOADS; ++u) skip |= (uint32_t)(~(on >> (first + u * (GS_BLOCK / PIECES))) & 1) << u;
     return skip;
 }
+
+// Flag of key `key` of a segment whose flags start at `on` (0 past its end).
+__device__ __forceinline__ uint8_t key_flag(const uint8_t* on, int key, int n) { return key < n ? on[key] : 0; }
 
 // Bits [lo, hi) of 64, ends clamped.
 __device__ __forceinline__ uint64_t bits_between(int lo, int hi) {
