@@ -33,8 +33,14 @@ struct FwdArgs {
     float2* part_ml;                       // [splits][n_q * heads] maximum (of the raw products) and sum
 };
 
-__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, GS_WAVE)); }
-__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, GS_WAVE); }
+__device__ __forceinline__ float half_max(float v) {
+    const float2 h = halves(v);
+    return fmaxf(h.x, h.y);
+}
+__device__ __forceinline__ float half_sum(float v) {
+    const float2 h = halves(v);
+    return h.x + h.y;
+}
 
 __device__ __forceinline__ float row_scale(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l); }
 __device__ __forceinline__ float row_lse(float m, float l, float scale) {
@@ -82,29 +88,31 @@ __device__ __forceinline__ void store_tile(const FwdArgs& f, int token, int head
 // c = scale * log2(e).  Returns the factor of what was summed before.
 template <int N>
 __device__ __forceinline__ float softmax_step(acc16 (&s)[N], float c, float& m, float& l) {
-    float t = s[0][0];
+    // four chains each for the maximum and the sum: one would wait for itself
+    float t4[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t = fmaxf(t, s[k][i]);
-    t = fmaxf(m, half_max(t));
+        for (int i = 0; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], s[k][i]);
+    const float t = fmaxf(m, half_max(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]))));
     const float base = t == -INFINITY ? 0.0f : t * c;      // nothing admitted yet: exp2(-inf) = 0 below
     const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
-    float sum = 0.0f;
+    float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             s[k][i] = __builtin_amdgcn_exp2f(fmaf(s[k][i], c, -base));
-            sum += s[k][i];
+            sum4[i & 3] += s[k][i];
         }
+    const float sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
     l = l * alpha + sum;                                   // this half's keys; the halves meet at the end
     m = t;
     return alpha;
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
+__global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 4 : 2) k_attention(FwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
     constexpr int G = 2;                           // products whose operands are read together
     // two buffers: a step's tiles arrive while the step before computes
@@ -153,10 +161,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
     }
 
     TileLoader<T, P, kKeys> kl, vl;
-    kl.init(a.k_row, a.dim);
-    vl.init(a.v_row, a.dim);
-    const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
-    const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    kl.init(static_cast<const T*>(a.k) + sg.k0 * a.k_row + kvh * a.k_head, sg.nk, a.k_row, a.dim);
+    vl.init(static_cast<const T*>(a.v) + sg.k0 * a.v_row + kvh * a.v_head, sg.nk, a.v_row, a.dim);
     // Which keys of a step are on is loaded a step before its tiles, so that
     // nothing waits for it: `on` for the step that computes, `on_next` for the
     // one whose tiles arrive, `flag` (a key a lane) for the one after.
@@ -170,8 +176,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
             flag = key_flag(flags, j + kKeys + fresh(lane), sg.nk);
             skip = rows_off<P, kKeys>(on_next);
         }
-        kl.load(ks, kbase + j * a.k_row, sg.nk - j, 0);
-        vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);     // a probability of 0 does not stop a NaN
+        kl.load(ks, j, 0);
+        vl.load(vs, j, skip);     // a probability of 0 does not stop a NaN
     };
 
     const float c = a.scale * kLog2e;
@@ -187,7 +193,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
         // barriers keep the compiler from reading more of them ahead, which
         // would not fit the registers of two waves a SIMD
         at.refresh();
-        acc16 s[2]{};
+        acc16 s[2];
         op8<T> x[2][G];
 #pragma unroll
         for (int e = 0; e < G; ++e) x[0][e] = rows_operand<T, P>(ks, at, 0, e);
@@ -199,7 +205,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention(FwdArgs f) {
                     x[(g + 1) & 1][e] = rows_operand<T, P>(ks, at, ((g + 1) * G + e) / KT * 32, ((g + 1) * G + e) % KT);
             }
 #pragma unroll
-            for (int e = 0; e < G; ++e) s[(g * G + e) / KT] = mfma(x[g & 1][e], q[(g * G + e) % KT], s[(g * G + e) / KT]);
+            for (int e = 0; e < G; ++e) {
+                const int n = g * G + e;
+                s[n / KT] = mfma(x[g & 1][e], q[n % KT], n % KT == 0 ? acc16{} : s[n / KT]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
         if (a.key_on != nullptr || j < alo || j + kKeys > ahi) {

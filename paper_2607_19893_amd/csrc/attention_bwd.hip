@@ -94,7 +94,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
             }
         }
     }
-    delta += __shfl_xor(delta, 32, GS_WAVE);
+    const float2 both = halves(delta);
+    delta = both.x + both.y;
     if (there && h == 0) {
         f.base[(int64_t)head * a.n_q + token] = base;
         f.delta[(int64_t)head * a.n_q + token] = delta;
@@ -107,10 +108,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
 
     TileLoader<T, P, kStep> kl, vl;
-    kl.init(a.k_row, a.dim);
-    vl.init(a.v_row, a.dim);
-    const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
-    const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
+    kl.init(static_cast<const T*>(a.k) + sg.k0 * a.k_row + kvh * a.k_head, sg.nk, a.k_row, a.dim);
+    vl.init(static_cast<const T*>(a.v) + sg.k0 * a.v_row + kvh * a.v_head, sg.nk, a.v_row, a.dim);
     // the keys' flags, loaded a step before the tiles that they belong to
     const uint8_t* const flags = a.key_on + sg.k0;
     uint64_t on = ~0ull, on_next = ~0ull;
@@ -122,8 +121,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
             flag = key_flag(flags, j + kStep + fresh(lane), sg.nk);
             skip = rows_off<P, kStep>(on_next);
         }
-        kl.load(ks, kbase + j * a.k_row, sg.nk - j, skip);
-        vl.load(vs, vbase + j * a.v_row, sg.nk - j, skip);
+        kl.load(ks, j, skip);
+        vl.load(vs, j, skip);
     };
 
     const float c = a.scale * kLog2e;
@@ -244,7 +243,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     }
     if (BIG) {
         TileLoader<T, P, kRows> vl;
-        vl.init(a.v_row, a.dim);
+        vl.init(static_cast<const T*>(a.v) + (sg.k0 + key0) * a.v_row + kvh * a.v_head, sg.nk - key0, a.v_row, a.dim);
         uint32_t skip = 0;
         if (a.key_on != nullptr) {
             const int first = key0 + threadIdx.x / vl.PIECES;
@@ -252,8 +251,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
             for (int u = 0; u < vl.LOADS; ++u)
                 if (key_flag(a.key_on + sg.k0, first + u * vl.STEP, sg.nk) == 0) skip |= 1u << u;
         }
-        vl.load(vs, static_cast<const T*>(a.v) + (sg.k0 + key0) * a.v_row + (int64_t)kvh * a.v_head, sg.nk - key0,
-                skip);
+        vl.load(vs, 0, skip);
     }
     // tokens that admit any of the workgroup's keys, and those that all do
     const int last = min(key0 + kRows, sg.nk) - 1;
@@ -274,30 +272,37 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     // a token that admits no key at all may hold anything: its row is left out
     const bool empties = a.key_on != nullptr || (a.right >= 0 && shift + a.right < 0);
 
-    TileLoader<T, P, ST> ql, dl;
-    ql.init(a.q_row, a.dim);
-    dl.init(f.do_row, a.dim);
-    const int64_t qbase = sg.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
-    const int64_t dbase = sg.q0 * f.do_row + (int64_t)kvh * a.group * f.do_head;
-    // their bases (+inf for such a token), loaded a step before the tiles
-    auto row_flag = [&](int n) {
-        const int g = n / per, t = t0 + (n - g * per) * ST + (fresh(lane) & (ST - 1));
-        return t < sg.nq ? f.base[(int64_t)(kvh * a.group + g) * a.n_q + sg.q0 + t] : INFINITY;
+    const int end = t0 + per * ST;
+    int fg = n0 / max(per, 1), ft = t0 + (n0 - fg * per) * ST;     // head of the group and token of the next fetch
+    int ct = ft;                                                    // and of the next step
+    auto q_rows = [&] { return static_cast<const T*>(a.q) + sg.q0 * a.q_row + (kvh * a.group + fg) * a.q_head; };
+    auto d_rows = [&] {
+        return static_cast<const T*>(f.dout) + sg.q0 * f.do_row + (kvh * a.group + fg) * f.do_head;
     };
+    TileLoader<T, P, ST> ql, dl;
+    ql.init(q_rows(), sg.nq, a.q_row, a.dim);
+    dl.init(d_rows(), sg.nq, f.do_row, a.dim);
+    // the rows' bases: +inf for a token that admits nothing, loaded a step before the tiles
+    auto bases = [&] { return f.base + (int64_t)(kvh * a.group + fg) * a.n_q + sg.q0; };
     float flag = 0.0f;
-    auto fetch = [&](T* qs, T* ds, float* st, int n) {
-        const int g = n / per, t = t0 + (n - g * per) * ST;
-        const float* bases = f.base + (int64_t)(kvh * a.group + g) * a.n_q + sg.q0;
-        uint32_t skip = 0;
-        if (empties) {
-            skip = rows_off<P, ST>(__ballot(flag != INFINITY));
-            if (n + 1 < n1) flag = row_flag(n + 1);
-        }
-        ql.load(qs, static_cast<const T*>(a.q) + qbase + g * a.q_head + t * a.q_row, sg.nq - t, skip);
-        dl.load(ds, static_cast<const T*>(f.dout) + dbase + g * f.do_head + t * f.do_row, sg.nq - t, skip);
+    auto load_flag = [&] {
+        const int t = ft + (fresh(lane) & (ST - 1));
+        flag = t < sg.nq ? bases()[t] : INFINITY;
+    };
+    auto fetch = [&](T* qs, T* ds, float* st, bool more) {
+        const uint32_t skip = empties ? rows_off<P, ST>(__ballot(flag != INFINITY)) : 0;
+        ql.load(qs, ft, skip);
+        dl.load(ds, ft, skip);
         // bases by the first wave, deltas by the second
-        if (wave < 2)
-            load_words(st + wave * 64, (wave ? bases + (f.delta - f.base) : bases) + t, sg.nq - t);
+        if (wave < 2) load_words(st + wave * 64, bases() + (wave ? f.delta - f.base : 0) + ft, sg.nq - ft);
+        ft += ST;
+        if (ft >= end) {
+            ft = t0;
+            ++fg;
+            ql.move(q_rows());
+            dl.move(d_rows());
+        }
+        if (empties && more) load_flag();
     };
 
     const float c = a.scale * kLog2e;
@@ -306,9 +311,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     acc16 dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = acc16{};
-    auto step = [&](const T* qs, const T* ds, const float* st, int n) {
+    auto step = [&](const T* qs, const T* ds, const float* st) {
         at.refresh();
-        const int t = t0 + n % per * ST;
+        const int t = ct;
+        ct = ct + ST < end ? ct + ST : t0;
         const bool test = !whole || t < alo || t + ST > ahi;
         uint64_t seen = ~0ull;
         if (test) seen = bits_between(ilo - t, ihi - t);
@@ -384,17 +390,17 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         }
     };
     if (n0 < n1) {
-        if (empties) flag = row_flag(n0);
-        fetch(qs0, ds0, st0, n0);
+        if (empties) load_flag();
+        fetch(qs0, ds0, st0, n0 + 1 < n1);
     }
     __syncthreads();                               // the fetched tiles are in LDS
     for (int n = n0; n < n1; n += 2) {
-        if (n + 1 < n1) fetch(qs1, ds1, st1, n + 1);
-        step(qs0, ds0, st0, n);
+        if (n + 1 < n1) fetch(qs1, ds1, st1, n + 2 < n1);
+        step(qs0, ds0, st0);
         __syncthreads();
         if (n + 1 < n1) {
-            if (n + 2 < n1) fetch(qs0, ds0, st0, n + 2);
-            step(qs1, ds1, st1, n + 1);
+            if (n + 2 < n1) fetch(qs0, ds0, st0, n + 3 < n1);
+            step(qs1, ds1, st1);
         }
         __syncthreads();
     }

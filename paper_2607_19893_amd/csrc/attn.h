@@ -33,6 +33,18 @@ __device__ __forceinline__ acc16 mfma(op8<f16_t> a, op8<f16_t> b, acc16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+// The values of the lanes l & 31 and (l & 31) + 32.
+__device__ __forceinline__ float2 halves(float v) {
+#ifdef __HIP_DEVICE_COMPILE__
+    // swaps the upper half of the first with the lower half of the second: of
+    // two copies, one is left with the lower half twice, one with the upper
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#else
+    return make_float2(v, v);
+#endif
+}
+
 // A tile of token rows in LDS: rows of P elements (a power of two), each cut
 // into 16-byte pieces that are stored at piece ^ key(row).  Two readers have
 // to find their 64 lanes' pieces in different banks: one takes the same piece
@@ -125,36 +137,53 @@ __device__ __forceinline__ op8<T> tile_operand(const acc16& c, int u) {
 // Copies tiles of ROWS token rows from memory into LDS without passing through
 // registers (buffer loads that write LDS): each of the LOADS instructions of a
 // wave fills 1 KB, 16 bytes a lane in lane order, so the lane that fills a
-// piece's place reads the piece that belongs there.  Rows at or past the
-// segment's end and pieces past the head's end lie outside the buffer's range
-// and arrive as zeros.
+// piece's place reads the piece that belongs there.  A segment is one buffer,  whose
+// rows' places fit 31 bits; rows at or past its end and pieces past the head's
+// end lie outside the buffer's range and arrive as zeros.
 template <typename T, int P, int ROWS>
 struct TileLoader {
     static constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK, STEP = GS_BLOCK / PIECES;
     static_assert(STEP % 16 == 0, "the key repeats every 16 rows: a lane's loads differ by whole rows");
     static constexpr int kRange = 0x7FFFFF00, kOutside = 0x7FFFFFF0;
-    int off;                               // bytes from the tile's first row; load u is u * STEP rows on
-    int64_t ld;
+    const T* base;                         // the segment's first row
+    const T* from;                         // the buffer's: row `row0`
+    int rows, row0, bytes, ld, off;        // ld: bytes of a row; off: a lane's place from a tile's first row
 
-    __device__ __forceinline__ void init(int64_t row_stride, int dim) {
-        ld = row_stride;
+    __device__ __forceinline__ void rebase(int row) {
+        row0 = row;
+        from = base + (int64_t)row * (ld / 2);
+        bytes = (int)max((int64_t)0, min((int64_t)kRange, (int64_t)(rows - row) * ld));
+    }
+    __device__ __forceinline__ void init(const T* first, int n, int64_t row_stride, int dim) {
+        base = first;
+        rows = n;
+        ld = (int)row_stride * 2;
         const int row = threadIdx.x / PIECES, piece = (threadIdx.x % PIECES) ^ piece_key<P>(row);
-        off = 8 * piece < dim ? (int)(row * ld * 2) + piece * 16 : kOutside;
+        off = 8 * piece < dim ? row * ld + piece * 16 : kOutside;
+        rebase(0);
     }
 
-    // base: the tile's first row; rows: how many there are from it on; skip:
-    // bit u leaves load u's row out (zeros).
-    __device__ __forceinline__ void load(T* tile, const T* base, int rows, uint32_t skip) const {
+    // On to another list of as many rows.
+    __device__ __forceinline__ void move(const T* first) {
+        base = first;
+        rebase(0);
+    }
+
+    // row: the tile's first; skip: bit u leaves load u's row out (zeros).
+    __device__ __forceinline__ void load(T* tile, int row, uint32_t skip) {
 #ifdef __HIP_DEVICE_COMPILE__              // the host pass has no buffer descriptors
+        // one buffer serves the rows of 2^29 bytes, then it moves on
+        if ((uint64_t)((int64_t)(row - row0) * ld) >= 1u << 29) rebase(row);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
+        const int at = (row - row0) * ld;
+        const __amdgpu_buffer_rsrc_t buf =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, bytes, 0x00027000);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int64_t bytes = max((int64_t)0, min((int64_t)kRange, (rows - u * STEP) * ld * 2));
-            const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-                const_cast<T*>(base + u * STEP * ld), 0, (int)bytes, 0x00027000);
+            const int place = off + (at + u * STEP * ld);  // past the range also where `off` is
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 buf, (__attribute__((address_space(3))) void*)(tile + (u * GS_BLOCK + wave * GS_WAVE) * 8), 16,
-                (skip >> u) & 1 ? kOutside : off, 0, 0, 0);
+                (skip >> u) & 1 ? kOutside : place, 0, 0, 0);
         }
 #endif
     }
