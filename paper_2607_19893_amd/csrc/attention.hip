@@ -112,14 +112,14 @@ __device__ __forceinline__ float softmax_step(acc16 (&s)[N], float c, float& m, 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 4 : 2) k_attention(FwdArgs f) {
+__global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
-    constexpr int G = 2;                           // products whose operands are read together
+    constexpr int G = KT < 4 ? 2 : 4;                           // products whose operands are read together
     // two buffers: a step's tiles arrive while the step before computes
     __shared__ __attribute__((aligned(16))) T ks0[kKeys * P], vs0[kKeys * P];
     __shared__ __attribute__((aligned(16))) T ks1[kKeys * P], vs1[kKeys * P];
     const AttnArgs& a = f.a;
-    const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, f.splits);
+    const Place place = chiplet_place<(D > 64)>(blockIdx.x, a.tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
     const Segment sg = find_segment<false, true>(a, kRows, a.tiles, place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
@@ -221,23 +221,25 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 4 : 2) k_attention(FwdArgs
                     if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[k][e] = -INFINITY;
             }
         }
+        op8<T> y[2][DT];                           // on their way while the exponentials run
+#pragma unroll
+        for (int d = 0; d < DT; ++d) y[0][d] = columns_operand<T, P>(vs, at, 0, d);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) y[1][d] = columns_operand<T, P>(vs, at, 16, d);
+        __builtin_amdgcn_sched_barrier(0);
         const float alpha = softmax_step<2>(s, c, m, l);
         if (__any(alpha != 1.0f)) {                // the maxima rise in the first steps, seldom later
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= alpha;
         }
-        op8<T> y[2][DT];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) y[0][d] = columns_operand<T, P>(vs, at, 0, d);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            if (g < 3) {
-#pragma unroll
-                for (int d = 0; d < DT; ++d) y[(g + 1) & 1][d] = columns_operand<T, P>(vs, at, 16 * (g + 1), d);
-            }
             const op8<T> p = tile_operand<T>(s[g / 2], g % 2);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = mfma(y[g & 1][d], p, o[d]);
+            for (int d = 0; d < DT; ++d) {
+                o[d] = mfma(y[g & 1][d], p, o[d]);
+                if (g < 2) y[g & 1][d] = columns_operand<T, P>(vs, at, 16 * (g + 2), d);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -282,7 +284,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     __shared__ float ml[2][WAVES][32];
     __shared__ float half[WAVES][32 * 33];
     const AttnArgs& a = f.a;
-    const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, f.splits);
+    const Place place = chiplet_place<false>(blockIdx.x, a.tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
     const Segment sg = find_segment<false, false>(a, kFewRows, a.tiles, place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kFewRows;

@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     __shared__ __attribute__((aligned(16))) T ks0[kStep * P], vs0[kStep * P];
     __shared__ __attribute__((aligned(16))) T ks1[kStep * P], vs1[kStep * P];
     const AttnArgs& a = f.a;
-    const Place place = chiplet_place(blockIdx.x, a.tiles, a.kv_heads, 1);
+    const Place place = chiplet_place<true>(blockIdx.x, a.tiles, a.kv_heads, 1);
     const int kvh = place.head;
     const Segment sg = find_segment<false, true>(a, kRows, a.tiles, place.tile);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     __shared__ __attribute__((aligned(16))) float st0[2 * 64], st1[2 * 64];            // bases, then deltas
     __shared__ __attribute__((aligned(16))) T vs[BIG ? kRows * P : 8];
     const AttnArgs& a = f.a;
-    const Place place = chiplet_place(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
+    const Place place = chiplet_place<true>(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
     const Segment sg = find_segment<true, false>(a, kRows, f.key_tiles, place.tile);
     const int key0 = sg.tile * kRows;
