@@ -28,7 +28,8 @@ struct FwdArgs {
     void* out;
     int64_t o_row, o_head;
     float* lse;
-    int32_t splits;                        // parts that a segment's keys are cut into
+    int32_t splits;                        // most parts that a segment's keys are cut into
+    int32_t chunk;                         // few rows: keys of a part; 0: every segment has `splits` parts
     float* part_o;                         // [splits][n_q * heads][dim], unnormalised
     float2* part_ml;                       // [splits][n_q * heads] maximum (of the raw products) and sum
 };
@@ -47,20 +48,21 @@ __device__ __forceinline__ float row_lse(float m, float l, float scale) {
     return l == 0.0f ? -INFINITY : m * scale + kLn2 * log2f(l);
 }
 
-// Where a row's results go: its part of the keys (splits > 1) or the output.
+// Where a row's results go: its part of the keys, or the output.
 // The maximum is that of the raw products, the tile holds 32 elements of a row.
-__device__ __forceinline__ void store_sums(const FwdArgs& f, int token, int head, int split, float m, float l) {
+__device__ __forceinline__ void store_sums(const FwdArgs& f, bool parts, int token, int head, int split, float m,
+                                           float l) {
     const int64_t row = (int64_t)token * f.a.heads + head;
     if (lane_id() >= 32) return;
-    if (f.splits > 1) f.part_ml[(int64_t)split * f.a.n_q * f.a.heads + row] = make_float2(m, l);
+    if (parts) f.part_ml[(int64_t)split * f.a.n_q * f.a.heads + row] = make_float2(m, l);
     else f.lse[row] = row_lse(m, l, f.a.scale);
 }
 
 template <typename T>
-__device__ __forceinline__ void store_tile(const FwdArgs& f, int token, int head, int split, int d, const acc16& o,
-                                           float l) {
-    const int h = lane_id() >> 5;
-    if (f.splits > 1) {
+__device__ __forceinline__ void store_tile(const FwdArgs& f, bool parts, int token, int head, int split, int d,
+                                           const acc16& o, float l) {
+    const int h = fresh(lane_id()) >> 5;
+    if (parts) {
         const int64_t row = (int64_t)token * f.a.heads + head;
         float* p = f.part_o + ((int64_t)split * f.a.n_q * f.a.heads + row) * f.a.dim;
 #pragma unroll
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
         j0 += split * per;
         j1 = min(hi, j0 + per);
         if (j0 >= j1 && split > 0) {                       // nothing left for this part
-            if (there) store_sums(f, token, head, split, -INFINITY, 0.0f);
+            if (there) store_sums(f, f.splits > 1, token, head, split, -INFINITY, 0.0f);
             return;
         }
     }
@@ -263,14 +265,16 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
     }
     l = half_sum(l);
     if (!there) return;
-    store_sums(f, token, head, split, m, l);
+    store_sums(f, f.splits > 1, token, head, split, m, l);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) store_tile<T>(f, token, head, split, d, o[d], l);
+    for (int d = 0; d < DT; ++d) store_tile<T>(f, f.splits > 1, token, head, split, d, o[d], l);
 }
 
-// Few rows over many keys: a workgroup takes 32 rows and every wave of it its
-// own keys (32 a step, its waves' steps interleaved), with a running maximum and
-// sum of its own; the waves meet in LDS at the end.  The keys' bytes bound it,
+// Few rows over many keys: a workgroup takes a part of a segment's keys, for all
+// of the segment's rows (32 at a time, seldom more), and every wave of it its own
+// keys (32 a step, its waves' steps interleaved), with a running maximum and sum
+// of its own; the waves meet in LDS at the end.  Segments are cut into parts of
+// about the same length, so long and short ones load the chip alike.  The keys' bytes bound it,
 // so a step's keys go from memory straight into the operand's registers, its
 // values through a piece of LDS that only this wave touches (no barrier in the
 // loop), and both are fetched a step ahead.
@@ -282,15 +286,19 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     constexpr int PIECES = P / 8, LOADS = 32 * PIECES / GS_WAVE, WAVES = GS_BLOCK / GS_WAVE;
     __shared__ __attribute__((aligned(16))) T vs[WAVES][32 * P];
     __shared__ float ml[2][WAVES][32];
-    __shared__ float half[WAVES][32 * 33];
+    __shared__ float tile[WAVES][16 * GS_WAVE];              // a C tile of each wave, register by register
     const AttnArgs& a = f.a;
-    const Place place = chiplet_place<false>(blockIdx.x, a.tiles, a.kv_heads, f.splits);
-    const int split = place.split, kvh = place.head;
-    const Segment sg = find_segment<false, false>(a, kFewRows, a.tiles, place.tile);
-    const int rows = sg.nq * a.group, row0 = sg.tile * kFewRows;
-    if (row0 >= rows) return;
-    const int lane = lane_id(), h = lane >> 5;
+    const Place place = chiplet_place<false>(blockIdx.x, a.tiles, a.kv_heads, 1);
+    const int kvh = place.head;
+    const Segment sg = find_segment<true, false, true>(a, f.chunk, a.tiles, place.tile);
+    const int parts = max((sg.nk + f.chunk - 1) / f.chunk, 1), split = sg.tile;
+    const int rows = sg.nq * a.group;
+    if (split >= parts) return;
+    const int per = ((sg.nk + parts - 1) / parts + 127) / 128 * 128;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
+#pragma unroll 1
+    for (int row0 = 0; row0 < rows; row0 += kFewRows) {
+    const int lane = fresh(lane_id()), h = lane >> 5;      // nothing of it is held over the loop
     const int r = row0 + (lane & 31);
     const bool there = r < rows;
     const int i = (there ? r : rows - 1) / a.group;
@@ -312,36 +320,27 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     const int last = min(row0 + kFewRows, rows) - 1;
     admitted(a, sg.nk, row0 / a.group + shift, last / a.group + shift, lo, hi);
     admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
-    int j0 = lo / 32 * 32, j1 = hi;
-    if (f.splits > 1) {
-        const int per = max(((max(hi - j0, 0) + f.splits - 1) / f.splits + 127) / 128 * 128, kPartFew);
-        j0 += split * per;
-        j1 = min(hi, j0 + per);
-        if (j0 >= j1 && split > 0) {                       // nothing left for this part
-            if (wave == 0 && there) store_sums(f, token, head, split, -INFINITY, 0.0f);
-            return;
-        }
+    const int j0 = max(lo / 32 * 32, split * per), j1 = min(hi, (split + 1) * per);
+    if (j0 >= j1 && split > 0) {                           // the window leaves nothing of this part
+        if (wave == 0 && there) store_sums(f, true, token, head, split, -INFINITY, 0.0f);
+        continue;
     }
-    const T* const kbase = static_cast<const T*>(a.k) + sg.k0 * a.k_row + (int64_t)kvh * a.k_head;
-    const T* const vbase = static_cast<const T*>(a.v) + sg.k0 * a.v_row + (int64_t)kvh * a.v_head;
-    // loads outside a buffer's range give zeros: keys past the segment's end,
-    // pieces past the head's end
-    constexpr int STEP = GS_WAVE / PIECES, kOutside = 0x7FFFFFF0;
-    const int koff = (int)((lane & 31) * a.k_row * 2) + 16 * h;
-    const int voff = 8 * (lane % PIECES) < a.dim ? (int)(lane / PIECES * a.v_row * 2) + 16 * (lane % PIECES) : kOutside;
+    constexpr int STEP = GS_WAVE / PIECES;
+    RowBuffer<T> kb, vb;
+    kb.init(static_cast<const T*>(a.k) + sg.k0 * a.k_row + kvh * a.k_head, sg.nk, a.k_row);
+    vb.init(static_cast<const T*>(a.v) + sg.k0 * a.v_row + kvh * a.v_head, sg.nk, a.v_row);
+    const int koff = (lane & 31) * kb.ld + 16 * h;
+    const int voff = 8 * (lane % PIECES) < a.dim ? lane / PIECES * vb.ld + 16 * (lane % PIECES) : vb.kOutside;
     const uint8_t* const flags = a.key_on + sg.k0;
     op8<T> kp[KT], vp[LOADS];
     uint8_t flag = 1;                                      // of key lane & 31 of the step
     auto fetch = [&](int j) {
-        const T* kt = kbase + j * a.k_row;
-        const T* vt = vbase + j * a.v_row;
         if (a.key_on != nullptr) flag = key_flag(flags, j + (fresh(lane) & 31), sg.nk);
+        const int ka = koff + kb.place(j), va = vb.place(j);
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
-            kp[t] = buffer_piece<T>(kt, (sg.nk - j) * a.k_row * 2, 16 * t + 8 * h >= a.dim ? kOutside : koff, 32 * t);
+        for (int t = 0; t < KT; ++t) kp[t] = kb.piece(16 * t + 8 * h < a.dim ? ka + 32 * t : kb.kOutside);
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u)
-            vp[u] = buffer_piece<T>(vt + u * STEP * a.v_row, (sg.nk - j - u * STEP) * a.v_row * 2, voff, 0);
+        for (int u = 0; u < LOADS; ++u) vp[u] = vb.piece(voff + (va + u * STEP * vb.ld));
     };
 
     const float c = a.scale * kLog2e;
@@ -353,7 +352,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     at.init<P>();
     T* const mine = vs[wave];
     int j = j0 + 32 * wave;
-    if (j < j1) fetch(j);
+    fetch(j < j1 ? j : sg.nk);
     for (; j < j1; j += 32 * WAVES) {
         at.refresh();
         acc16 s[1];
@@ -380,7 +379,9 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
             for (int e = 0; e < 16; ++e)
                 if ((seen & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[0][e] = -INFINITY;
         }
-        if (j + 32 * WAVES < j1) fetch(j + 32 * WAVES);
+        // behind the part's end: from past the segment's, which reads nothing
+        // (a condition on the loads would keep both outcomes' registers)
+        fetch(j + 32 * WAVES < j1 ? j + 32 * WAVES : sg.nk);
         const float alpha = softmax_step<1>(s, c, m, l);
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= alpha;
@@ -401,45 +402,45 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     }
     // the waves meet: the largest maximum, every sum and tile against it
     l = half_sum(l);
-    if (h == 0) {
-        ml[0][wave][lane] = m;
-        ml[1][wave][lane] = l;
+    const int me = fresh(lane_id()), column = me & 31;
+    if (me < 32) {
+        ml[0][wave][me] = m;
+        ml[1][wave][me] = l;
     }
     __syncthreads();
     float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[0][w][lane & 31]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[0][w][column]);
     const float base = top == -INFINITY ? 0.0f : top * c;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w)
-        sum = fmaf(ml[1][w][lane & 31], __builtin_amdgcn_exp2f(fmaf(ml[0][w][lane & 31], c, -base)), sum);
+        sum = fmaf(ml[1][w][column], __builtin_amdgcn_exp2f(fmaf(ml[0][w][column], c, -base)), sum);
     const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            half[wave][(8 * (e >> 2) + 4 * h + (e & 3)) * 33 + (lane & 31)] = o[d][e] * alpha;
+        for (int e = 0; e < 16; ++e) tile[wave][e * GS_WAVE + me] = o[d][e] * alpha;
         __syncthreads();
-        if (wave == d % WAVES) {
+        if (wave == d % WAVES && there) {
+            acc16 v;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int at = (8 * (e >> 2) + 4 * h + (e & 3)) * 33 + (lane & 31);
-                float v = half[0][at];
+                v[e] = tile[0][e * GS_WAVE + me];
 #pragma unroll
-                for (int w = 1; w < WAVES; ++w) v += half[w][at];
-                o[d][e] = v;
+                for (int w = 1; w < WAVES; ++w) v[e] += tile[w][e * GS_WAVE + me];
             }
-            if (there) store_tile<T>(f, token, head, split, d, o[d], sum);
+            store_tile<T>(f, parts > 1, token, head, split, d, v, sum);
         }
         __syncthreads();
     }
-    if (wave == 0 && there) store_sums(f, token, head, split, top, sum);
+    if (wave == 0 && there) store_sums(f, parts > 1, token, head, split, top, sum);
+    }
 }
 
-// Joins the parts of a row (at most 64): lanes take the parts' maxima and sums
-// together, then two elements each and the parts in turn.  WAVES waves share a
-// row where there are many parts.
-constexpr int kMaxSplits = 64;
+// Joins the parts of a row (at most kMaxSplits): lanes take the parts' maxima
+// and sums together, then two elements each and the parts in turn.  WAVES waves
+// share a row where there can be many parts.
+constexpr int kMaxSplits = 256;
 
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
@@ -449,23 +450,44 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
     const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE : blockIdx.x;
     if (row >= rows) return;
     const int lane = lane_id();
-    const float2 part = lane < f.splits ? f.part_ml[lane * rows + row] : make_float2(-INFINITY, 0.0f);
-    float m = part.x;
+    const int64_t token = row / f.a.heads;
+    int parts = f.splits;
+    if (f.chunk > 0) {
+        const int keys = __builtin_amdgcn_readfirstlane(keys_of_token(f.a, (int)token));
+        if (keys <= f.chunk) return;                       // one part: written where it belongs; or in no segment
+        parts = (keys + f.chunk - 1) / f.chunk;
+    }
+    constexpr int N = kMaxSplits / GS_WAVE;
+    float2 part[N];
+    float m = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int s = n * GS_WAVE + lane;
+        part[n] = s < parts ? f.part_ml[s * rows + row] : make_float2(-INFINITY, 0.0f);
+        m = fmaxf(m, part[n].x);
+    }
 #pragma unroll
     for (int d = 1; d < GS_WAVE; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, GS_WAVE));
     const float c = f.a.scale * kLog2e, base = m == -INFINITY ? 0.0f : m * c;
-    const float w = __builtin_amdgcn_exp2f(fmaf(part.x, c, -base));
-    const float l = wave_sum(part.y * w);
+    float w[N], l = 0.0f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        w[n] = __builtin_amdgcn_exp2f(fmaf(part[n].x, c, -base));
+        l = fmaf(part[n].y, w[n], l);
+    }
+    l = wave_sum(l);
     float2 o = make_float2(0.0f, 0.0f);
-    if (2 * lane < f.a.dim) {
-        const float* p = f.part_o + row * f.a.dim + 2 * lane;
-        const int64_t step = rows * f.a.dim;
+    const float* p = f.part_o + row * f.a.dim + 2 * lane;
+    const int64_t step = rows * f.a.dim;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (n * GS_WAVE >= parts || 2 * lane >= f.a.dim) continue;
 #pragma unroll 8
-        for (int s = wave; s < f.splits; s += WAVES) {
+        for (int s = wave; s < min(parts - n * GS_WAVE, GS_WAVE); s += WAVES) {
             // a part that found no keys wrote no tile; the first part always did
-            const float ls = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(part.y), s));
-            const float2 v = *reinterpret_cast<const float2*>(p + (ls == 0.0f ? 0 : s) * step);
-            const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), s));
+            const float ls = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(part[n].y), s));
+            const float2 v = *reinterpret_cast<const float2*>(p + (ls == 0.0f ? 0 : n * GS_WAVE + s) * step);
+            const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[n]), s));
             o.x = fmaf(v.x, ws, o.x);
             o.y = fmaf(v.y, ws, o.y);
         }
@@ -481,7 +503,6 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
         }
     }
     const float inv = row_scale(l);
-    const int64_t token = row / f.a.heads;
     const int head = (int)(row - token * f.a.heads);
     if (lane == 0) f.lse[row] = row_lse(m, l, f.a.scale);
     if (2 * lane < f.a.dim) {
@@ -491,40 +512,50 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
     }
 }
 
-// How a call is cut, from its sizes alone: 32-row tiles where a segment's rows
-// fit one on average, and the keys into parts until the workgroups fill the
-// chip, as long as a part keeps the keys that pay for its start and its join.
+// How a call is cut, from its sizes alone.
 struct Plan {
     bool few;
-    int32_t tiles, splits;
+    int32_t tiles, splits, chunk;
 };
 
+// Few rows: where a segment's rows fit one 32-row tile on average.  The keys of
+// all segments and key heads are cut into parts for one workgroup a compute unit
+// (three up to 64 elements, where three fit one), but at least 256 keys, which
+// pay for a start and a join; a longer segment has more of them.  24 regions of
+// 900..9000 keys of 64: 86 us for three a unit, 91 for two, 99 when every segment
+// had the same number of parts; one row over 32,768 keys of 128: 40 us for one a
+// unit, 44 for two.  The parts' sums may take 64 MB.
+// More rows: 128-row tiles, and the keys into parts where those tiles leave
+// compute units idle.
 Plan plan(const gs_attn& a) {
     constexpr int kUnits = 256;                            // compute units
     Plan p;
     const int group = a.heads / a.kv_heads;
     const int64_t rows = (int64_t)a.n_q * group, keys = a.n_k / a.n_seg;
     p.few = rows <= (int64_t)kFewRows * a.n_seg;
-    p.tiles = whole_shares(attn_tiles(rows, p.few ? kFewRows : kRows, a.n_seg), a.kv_heads);
+    if (p.few) {
+        const bool equal = a.cu_q == nullptr || a.n_seg == 1;
+        const int64_t longest = equal ? keys : a.n_k;      // as far as it is known here
+        const int64_t want = kUnits * (a.dim <= 64 ? 3 : 1);
+        const int64_t room = std::max<int64_t>(1, (64 << 20) / (std::max<int64_t>(1, (int64_t)a.n_q * a.heads) * a.dim * 4));
+        const int64_t most = std::min<int64_t>(kMaxSplits, room);
+        int64_t chunk = std::max<int64_t>({kPartFew, (int64_t)a.n_k * a.kv_heads / want, (longest + most - 1) / most});
+        chunk = (chunk + 127) / 128 * 128;
+        p.chunk = (int32_t)std::min<int64_t>(chunk, 0x7FFFFF00);
+        p.splits = (int32_t)std::max<int64_t>(1, (longest + p.chunk - 1) / p.chunk);
+        p.tiles = whole_shares(attn_tiles(a.n_k, p.chunk, a.n_seg), a.kv_heads);
+        return p;
+    }
+    p.chunk = 0;
+    p.tiles = whole_shares(attn_tiles(rows, kRows, a.n_seg), a.kv_heads);
     const int64_t groups = (int64_t)p.tiles * a.kv_heads;
-    // Ragged segments (their lengths are not known here) are longer than the
-    // average, and a part is no shorter than kPart: more parts than the average
-    // needs even the load out.  24 regions of 900..9000 keys under 16 heads: 99
-    // us with 12 parts, 156 with 3.  One segment, or equal ones: one workgroup a
-    // unit; one row over 32,768 keys under 8 key heads takes 41 us in 32 parts
-    // and 44 in 64, which the join has to read.
-    const bool ragged = a.cu_q != nullptr && a.n_seg > 1;
-    int64_t want = ((p.few && !ragged ? 1 : (p.few ? 4 : 2)) * kUnits + groups - 1) / groups;
-    if (p.few && ragged && want > 1) want *= 4;
-    const int64_t least = p.few ? kPartFew : kPart;
-    const int64_t most = keys < 2 * least ? 1 : (ragged ? kMaxSplits : std::min<int64_t>(kMaxSplits, keys / least));
-    p.splits = (int32_t)std::max<int64_t>(1, std::min(want, most));
+    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>((2 * kUnits + groups - 1) / groups, keys / kPart));
     return p;
 }
 
 template <typename T, int D>
 hipError_t go(const FwdArgs& f, bool few, hipStream_t st) {
-    const uint32_t grid = (uint32_t)(f.a.tiles * f.a.kv_heads * f.splits);
+    const uint32_t grid = (uint32_t)(f.a.tiles * f.a.kv_heads * (few ? 1 : f.splits));
     if (few) k_attention_few<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
     else k_attention<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
     const uint64_t rows = (uint64_t)f.a.n_q * f.a.heads;
@@ -560,6 +591,7 @@ hipError_t launch_attention(const gs_attn& a, const gs_rows& out, float* lse, vo
     f.o_head = out.ld_head;
     f.lse = lse;
     f.splits = p.splits;
+    f.chunk = p.chunk;
     f.part_ml = static_cast<float2*>(ws);
     f.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * p.splits * sizeof(float2)));
     return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, p.few, st) : by_dim<f16_t>(f, p.few, st);

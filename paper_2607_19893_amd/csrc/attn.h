@@ -134,75 +134,86 @@ __device__ __forceinline__ op8<T> tile_operand(const acc16& c, int u) {
     return o;
 }
 
-// Copies tiles of ROWS token rows from memory into LDS without passing through
-// registers (buffer loads that write LDS): each of the LOADS instructions of a
-// wave fills 1 KB, 16 bytes a lane in lane order, so the lane that fills a
-// piece's place reads the piece that belongs there.  A segment is one buffer,  whose
-// rows' places fit 31 bits; rows at or past its end and pieces past the head's
-// end lie outside the buffer's range and arrive as zeros.
-template <typename T, int P, int ROWS>
-struct TileLoader {
-    static constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK, STEP = GS_BLOCK / PIECES;
-    static_assert(STEP % 16 == 0, "the key repeats every 16 rows: a lane's loads differ by whole rows");
+// The rows of a segment as a buffer: a load outside of it (a row at or past the
+// segment's end, or kOutside for a lane that wants nothing) gives zeros.  One
+// descriptor serves the rows of 2^29 bytes, then it moves on.
+template <typename T>
+struct RowBuffer {
     static constexpr int kRange = 0x7FFFFF00, kOutside = 0x7FFFFFF0;
     const T* base;                         // the segment's first row
-    const T* from;                         // the buffer's: row `row0`
-    int rows, row0, bytes, ld, off;        // ld: bytes of a row; off: a lane's place from a tile's first row
+    const T* from;                         // the descriptor's: row `row0`
+    int rows, row0, bytes, ld;             // ld: bytes of a row
 
     __device__ __forceinline__ void rebase(int row) {
         row0 = row;
         from = base + (int64_t)row * (ld / 2);
         bytes = (int)max((int64_t)0, min((int64_t)kRange, (int64_t)(rows - row) * ld));
     }
-    __device__ __forceinline__ void init(const T* first, int n, int64_t row_stride, int dim) {
+    __device__ __forceinline__ void init(const T* first, int n, int64_t row_stride) {
         base = first;
         rows = n;
         ld = (int)row_stride * 2;
-        const int row = threadIdx.x / PIECES, piece = (threadIdx.x % PIECES) ^ piece_key<P>(row);
-        off = 8 * piece < dim ? row * ld + piece * 16 : kOutside;
         rebase(0);
     }
-
-    // On to another list of as many rows.
-    __device__ __forceinline__ void move(const T* first) {
-        base = first;
-        rebase(0);
-    }
-
-    // row: the tile's first; skip: bit u leaves load u's row out (zeros).
-    __device__ __forceinline__ void load(T* tile, int row, uint32_t skip) {
-#ifdef __HIP_DEVICE_COMPILE__              // the host pass has no buffer descriptors
-        // one buffer serves the rows of 2^29 bytes, then it moves on
+    // Bytes from the descriptor's start to row `row`.
+    __device__ __forceinline__ int place(int row) {
         if ((uint64_t)((int64_t)(row - row0) * ld) >= 1u << 29) rebase(row);
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
-        const int at = (row - row0) * ld;
-        const __amdgpu_buffer_rsrc_t buf =
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, bytes, 0x00027000);
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int place = off + (at + u * STEP * ld);  // past the range also where `off` is
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                buf, (__attribute__((address_space(3))) void*)(tile + (u * GS_BLOCK + wave * GS_WAVE) * 8), 16,
-                (skip >> u) & 1 ? kOutside : place, 0, 0, 0);
-        }
+        return (row - row0) * ld;
+    }
+    // 16 bytes at `at` into registers.
+    __device__ __forceinline__ op8<T> piece(int at) const {
+#ifdef __HIP_DEVICE_COMPILE__              // the host pass has no buffer descriptors
+        typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+        const u4 v = __builtin_amdgcn_raw_buffer_load_b128(
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, bytes, 0x00027000), at, 0, 0);
+        return __builtin_bit_cast(op8<T>, v);
+#else
+        return op8<T>{};
+#endif
+    }
+    // 16 bytes a lane into LDS, in lane order from `to` on.
+    __device__ __forceinline__ void piece_to(T* to, int at) const {
+#ifdef __HIP_DEVICE_COMPILE__
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, bytes, 0x00027000),
+            (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
 #endif
     }
 };
 
-// 16 bytes at `off` + `more` of a buffer of `bytes` (more: a constant); zeros
-// outside of it.
-template <typename T>
-__device__ __forceinline__ op8<T> buffer_piece(const T* base, int64_t bytes, int off, int more) {
-#ifdef __HIP_DEVICE_COMPILE__
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<T*>(base), 0, (int)max((int64_t)0, min((int64_t)0x7FFFFF00, bytes)), 0x00027000);
-    const u4 v = __builtin_amdgcn_raw_buffer_load_b128(buf, off + more, 0, 0);
-    return __builtin_bit_cast(op8<T>, v);
-#else
-    return op8<T>{};
-#endif
-}
+// Copies tiles of ROWS token rows from memory into LDS without passing through
+// registers: each of the LOADS instructions of a wave fills 1 KB, 16 bytes a
+// lane in lane order, so the lane that fills a piece's place reads the piece
+// that belongs there.  Rows past the segment's end and pieces past the head's
+// end arrive as zeros.
+template <typename T, int P, int ROWS>
+struct TileLoader {
+    static constexpr int PIECES = P / 8, LOADS = ROWS * PIECES / GS_BLOCK, STEP = GS_BLOCK / PIECES;
+    static_assert(STEP % 16 == 0, "the key repeats every 16 rows: a lane's loads differ by whole rows");
+    RowBuffer<T> buf;
+    int off;                               // a lane's place from a tile's first row
+
+    __device__ __forceinline__ void init(const T* first, int n, int64_t row_stride, int dim) {
+        buf.init(first, n, row_stride);
+        const int row = threadIdx.x / PIECES, piece = (threadIdx.x % PIECES) ^ piece_key<P>(row);
+        off = 8 * piece < dim ? row * buf.ld + piece * 16 : buf.kOutside;
+    }
+    // On to another list of as many rows.
+    __device__ __forceinline__ void move(const T* first) {
+        buf.base = first;
+        buf.rebase(0);
+    }
+    // row: the tile's first; skip: bit u leaves load u's row out (zeros).
+    __device__ __forceinline__ void load(T* tile, int row, uint32_t skip) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
+        const int at = buf.place(row);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int place = off + (at + u * STEP * buf.ld);      // past the range also where `off` is
+            buf.piece_to(tile + (u * GS_BLOCK + wave * GS_WAVE) * 8, (skip >> u) & 1 ? buf.kOutside : place);
+        }
+    }
+};
 
 // 64 words from `base` on into LDS, a lane of the wave each; those at or past
 // `n` are zeros.
@@ -295,7 +306,8 @@ __device__ __forceinline__ int of_lane(int v, int lane) { return __builtin_amdgc
 // steps start first.  A loop over the segments gives every lane its first tile.
 //   More: segment s starts at tile start(s) / size + s, at least as many tiles as
 // its rows need (some stay empty), found by a search with 64 probes a round.
-template <bool KEYS, bool LAST_FIRST>
+// EMPTY_TOO: a segment without any has one tile all the same.
+template <bool KEYS, bool LAST_FIRST, bool EMPTY_TOO = false>
 __device__ __forceinline__ Segment find_segment(const AttnArgs& a, int size, int tiles, int tile) {
     const int lane = lane_id(), mul = KEYS ? 1 : a.group;
     Segment s;
@@ -304,7 +316,9 @@ __device__ __forceinline__ Segment find_segment(const AttnArgs& a, int size, int
         const int q0 = cu_at(a.cu_q, at, a.n_seg, a.n_q), k0 = cu_at(a.cu_k, at, a.n_seg, a.n_k);
         const int nq = max(cu_at(a.cu_q, at + 1, a.n_seg, a.n_q) - q0, 0);
         const int nk = max(cu_at(a.cu_k, at + 1, a.n_seg, a.n_k) - k0, 0);
-        const int has = lane < a.n_seg ? (int)(((KEYS ? (int64_t)nk : (int64_t)nq * mul) + size - 1) / size) : 0;
+        int has = (int)(((KEYS ? (int64_t)nk : (int64_t)nq * mul) + size - 1) / size);
+        if (EMPTY_TOO) has = max(has, 1);
+        if (lane >= a.n_seg) has = 0;
         const int work = KEYS ? nq : nk;
         int first = 0;
         for (int t = 0; t < a.n_seg; ++t) {
@@ -340,6 +354,19 @@ __device__ __forceinline__ Segment find_segment(const AttnArgs& a, int size, int
     s.nk = __builtin_amdgcn_readfirstlane(max(cu_at(a.cu_k, lo + 1, a.n_seg, a.n_k) - s.k0, 0));
     s.tile = tile - __builtin_amdgcn_readfirstlane((int)((int64_t)cu_at(cu, lo, a.n_seg, n) * mul / size) + lo);
     return s;
+}
+
+// Keys of the segment that a token of the queries is in; -1 for none.
+__device__ __forceinline__ int keys_of_token(const AttnArgs& a, int token) {
+    int lo = 0, hi = a.n_seg - 1;          // the last segment that starts at or before the token
+    while (lo < hi) {
+        const int step = (hi - lo + GS_WAVE - 1) / GS_WAVE;
+        const int m = lo + (lane_id() + 1) * step;
+        lo += __popcll(__ballot(m <= hi && cu_at(a.cu_q, m, a.n_seg, a.n_q) <= token)) * step;
+        hi = min(hi, lo + step - 1);
+    }
+    if (token < cu_at(a.cu_q, lo, a.n_seg, a.n_q) || token >= cu_at(a.cu_q, lo + 1, a.n_seg, a.n_q)) return -1;
+    return max(cu_at(a.cu_k, lo + 1, a.n_seg, a.n_k) - cu_at(a.cu_k, lo, a.n_seg, a.n_k), 0);
 }
 
 // Keys [lo, hi) that any of the places first .. last can admit.

@@ -242,6 +242,9 @@ CASES = {
     "few, long parts": case([1, 2, 1], [3000, 1500, 10], heads=8, kv=8, dim=64, off=0.1),
     "few, ordered": case([7, 4], [2200, 30], heads=4, kv=4, dim=96, right=0),
     "few, window": case([3, 3], [4000, 70], heads=4, kv=2, dim=128, left=1000, right=20),
+    "two rows, more parts than lanes": case([2], [60000], heads=2, kv=1, dim=32, off=0.1),
+    "few, but for one segment": case([100, 1, 1, 0, 1, 1], [700, 300, 0, 50, 9, 2000], heads=1, dim=64, left=900, right=0),
+    "few, 70 segments": case([(i * 5) % 4 for i in range(70)], [(i * 37) % 900 for i in range(70)], 4, 1, dim=64, off=0.1),
     "wide rows split over the keys": case([40], [5000], heads=2, kv=1, dim=64, dtype=HF),
     "rows split for dk": case([2500], [130], heads=4, kv=1, dim=128),
     "dim 16": case([90], heads=2, dim=16, dtype=HF),
