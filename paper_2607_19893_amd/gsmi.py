@@ -552,24 +552,28 @@ def gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=None, stream
                                                           stream if stream is not None else current_stream()))
 
 
+_Axes, _Pair, _RowsPair = i32 * 3, i32 * 2, gs_rows * 2
+
+
 def gs_rotary(inputs, outputs, pos, freq, axis_pairs, interleaved=False, inverse=False, amplitude=1.0, stream=None):
     """inputs, outputs: one or two [tokens, heads, dim] tensors each; pos [tokens, axes] fp32."""
-    a = gs_rotary_args()
-    x = inputs[0]
-    a.dtype, a.tokens, a.dim = token_dtype(x), x.shape[0], x.shape[2]
-    a.n_axes = len(axis_pairs)
-    for i, n in enumerate(axis_pairs[:3]):
-        a.axis_pairs[i] = int(n)
-    a.pairs = sum(int(n) for n in axis_pairs)
-    a.interleaved, a.inverse, a.amplitude = int(interleaved), int(inverse), float(amplitude)
-    a.pos, a.ld_pos, a.freq = pos.data_ptr(), row_stride(pos), freq.data_ptr()
-    a.n_tensors = len(inputs)
-    if not 1 <= len(inputs) <= 2 or len(outputs) != len(inputs):
+    n = len(inputs)
+    if not 1 <= n <= 2 or len(outputs) != n:
         raise ValueError("one or two tensors, with an output each")
-    for i, (t, o) in enumerate(zip(inputs, outputs)):
-        if t.shape != o.shape or t.dtype != x.dtype or o.dtype != x.dtype or t.shape[0] != a.tokens or t.shape[2] != a.dim:
-            raise ValueError("tensors and outputs share tokens, dim and type; got %s -> %s" % (t.shape, o.shape))
-        a.heads[i], a.inp[i], a.out[i] = t.shape[1], make_rows(t), make_rows(o)
+    x = inputs[0]
+    shape, dt = x.shape, x.dtype
+    ps, axes = pos.stride(), len(axis_pairs)
+    if pos.dim() != 2 or (axes > 1 and ps[1] != 1):
+        raise ValueError("pos is [tokens, axes] with contiguous rows, not strides %s" % (ps,))
+    for t, o in zip(inputs, outputs):
+        ts = t.shape
+        if ts != o.shape or t.dtype != dt or o.dtype != dt or ts[0] != shape[0] or ts[2] != shape[2]:
+            raise ValueError("tensors and outputs share tokens, dim and type; got %s -> %s" % (ts, o.shape))
+    a = gs_rotary_args(token_dtype(x), shape[0], shape[2], sum(axis_pairs), axes, _Axes(*axis_pairs[:3]),
+                       interleaved, inverse, amplitude, pos.data_ptr(), ps[0] if shape[0] > 1 else max(axes, ps[0]),
+                       freq.data_ptr(), n,
+                       _Pair(*[t.shape[1] for t in inputs]), _RowsPair(*[make_rows(t) for t in inputs]),
+                       _RowsPair(*[make_rows(o) for o in outputs]))
     return _check("gs_rotary", _lib.gs_rotary(ctypes.byref(a), stream if stream is not None else current_stream()))
 
 
@@ -590,8 +594,8 @@ def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-
         raise ValueError("q, k, v do not fit: %s, %s, %s" % (qs, ks, v.shape))
     if cu_q is not None:
         n_seg = cu_q.numel() - 1
-        if cu_k is None or cu_k.numel() != n_seg + 1 or str(cu_q.dtype) != "torch.int32" or cu_k.dtype != cu_q.dtype \
-                or not cu_q.is_contiguous() or not cu_k.is_contiguous():
+        if cu_k is None or cu_k.numel() != n_seg + 1 or cu_q.element_size() != 4 or cu_q.is_floating_point() \
+                or cu_k.dtype != cu_q.dtype or not cu_q.is_contiguous() or not cu_k.is_contiguous():
             raise ValueError("cu_q and cu_k are contiguous int32 of the same length")
     if key_on is not None and (key_on.numel() != ks[0] or key_on.element_size() != 1 or not key_on.is_contiguous()):
         raise ValueError("key_on is one contiguous byte per key")
