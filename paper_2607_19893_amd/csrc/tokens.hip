@@ -15,21 +15,34 @@ namespace {
 // ---------------------------------------------------------------------------
 // Norm.  A row is read once, kept in registers as floats, reduced, and written:
 // s = x + residual, y = s w / sqrt(mean s^2 + eps).  Bound by HBM bytes.
-// WAVES waves share a row; thread t of them owns the 16-byte pieces t, t + 64
-// WAVES, ... (E elements in registers).  One wave a row needs no barrier and is
-// taken while a row fits 32 elements a lane; longer rows take four.
+// TPR threads share a row: thread t of them owns the 16-byte pieces t, t + TPR,
+// ... (E elements in registers).  A wave a row needs no barrier and is taken
+// while a row fits 32 elements a lane; longer rows take four.  Rows of up to 256
+// columns are taken by the lanes that own one block of GS_NORM_BLOCK columns (16
+// or 32), several to a wave: 74,724 fp32 rows of 80 columns into 8 bits took 47
+// us with a wave each, whose lanes were two thirds idle, and take 17 so.
 // ---------------------------------------------------------------------------
 
-template <int WAVES>
+template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* part) {
+    if (TPR < GS_WAVE) {
+        v = dpp_row_sum(v);
+#ifdef __HIP_DEVICE_COMPILE__
+        if (TPR == 32) {                       // odd and even rows of 16 swapped between two copies
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+#endif
+        return v;
+    }
     v = wave_sum(v);
-    if (WAVES == 1) return v;
+    if (TPR == GS_WAVE) return v;
     const int w = threadIdx.x / GS_WAVE;
     if (lane_id() == 0) part[w] = v;
     __syncthreads();
     v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) v += part[i];
+    for (int i = 0; i < TPR / GS_WAVE; ++i) v += part[i];
     __syncthreads();
     return v;
 }
@@ -39,9 +52,32 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 // multiple of its lanes).
 template <int LANES>
 __device__ __forceinline__ float block_max(float v) {
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, GS_WAVE));
+    // within a row of 16 lanes: pairs, quads, halves mirrored, the row mirrored
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, true)));
+#ifdef __HIP_DEVICE_COMPILE__
+    if (LANES == 32) {                         // and of two rows: odd and even ones swapped between two copies
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+#endif
     return v;
+}
+
+// x w (r + r_lo) rounded to odd in fp32: the exact product cut towards zero,
+// its last bit set if anything was cut.  Rounding that to fewer bits gives what
+// rounding the exact product would.
+__device__ __forceinline__ float odd_product(float x, float w, float r, float r_lo) {
+#pragma clang fp contract(off)                 // v is the rounded product wherever it stands
+    const float t = x * w, t_lo = fmaf(x, w, -t);
+    const float v = t * r, e = fmaf(t, r, -v) + fmaf(t, r_lo, t_lo * r);
+    const float hi = v + e, lo = (v - hi) + e;
+    int bits = __float_as_int(hi);
+    if (lo != 0.0f && (bits & 1) == 0 && hi != 0.0f && fabsf(hi) < INFINITY) bits += (lo > 0.0f) == (hi > 0.0f) ? 1 : -1;
+    // infinite or NaN: the parts cannot be told apart, the plain product is right
+    return fabsf(v) < INFINITY ? __int_as_float(bits) : v;
 }
 
 // N weights from column col on (zeros past the row's end).
@@ -63,13 +99,16 @@ __device__ __forceinline__ void load_weight(const float* weight, int col, int co
     }
 }
 
-template <typename T, bool WHOLE, int WAVES, int E>
+template <typename T, bool WHOLE, int TPR, int E>
 __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
-    constexpr int N = Piece<T>::N, CH = E / N, TPR = WAVES * GS_WAVE, RPB = GS_BLOCK / TPR;
+    constexpr int N = Piece<T>::N, CH = E / N, RPB = GS_BLOCK / TPR;
     __shared__ float part[GS_BLOCK / GS_WAVE];
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (RPB > 1 && row >= a.rows) return;      // whole waves; RPB 1 launches no such row
+    const int64_t mine = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (TPR >= GS_WAVE && mine >= a.rows) return;          // whole waves
+    // rows past the end of a shared wave: the last row's address, no columns
+    const int64_t row = mine < a.rows ? mine : a.rows - 1;
+    const int cols = mine < a.rows ? a.cols : 0;
     const T* __restrict__ x = static_cast<const T*>(a.x) + row * a.ld_x;
     const T* __restrict__ r = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_residual : nullptr;
     // every load of the row is on its way before the first is used
@@ -78,11 +117,11 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * N;
-        xs[c].load(x + col, a.cols - col);
-        if (r) rs[c].load(r + col, a.cols - col);
+        xs[c].load(x + col, cols - col);
+        if (r) rs[c].load(r + col, cols - col);
     }
 #pragma unroll
-    for (int c = 0; c < CH; ++c) load_weight<N, WHOLE>(a.weight, (c * TPR + t) * N, a.cols, w[c]);
+    for (int c = 0; c < CH; ++c) load_weight<N, WHOLE>(a.weight, (c * TPR + t) * N, cols, w[c]);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         xs[c].floats(s[c]);
@@ -98,42 +137,60 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < N; ++i) ss = fmaf(s[c][i], s[c][i], ss);
-    ss = row_sum<WAVES>(ss, part);
+    ss = row_sum<TPR>(ss, part);
     const float rho = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
     if (a.total) {
         T* __restrict__ o = static_cast<T*>(a.total) + row * a.ld_total;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * TPR + t) * N;
-            if (col < a.cols) store_piece<T, WHOLE>(o + col, a.cols - col, s[c]);
+            if (col < cols) store_piece<T, WHOLE>(o + col, cols - col, s[c]);
         }
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * N;
+        if (a.y && col < cols) {
+            float y[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[c][i] *= rho * w[c][i];
-        if (a.y && col < a.cols)
-            store_piece<T, WHOLE>(static_cast<T*>(a.y) + row * a.ld_y + col, a.cols - col, s[c]);
+            for (int i = 0; i < N; ++i) y[i] = s[c][i] * (rho * w[c][i]);
+            store_piece<T, WHOLE>(static_cast<T*>(a.y) + row * a.ld_y + col, cols - col, y);
+        }
     }
     if (a.q == nullptr) return;
+    // 8 bits: y / scale = (s w) * 448 / max|s w|, the row's rho falls out.  The
+    // product is carried in two floats and rounded to odd, so that the one
+    // rounding to e4m3 that follows is that of the exact value.
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * N;
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(s[c][i]));
+        for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(s[c][i] * w[c][i]));
         m = block_max<GS_NORM_BLOCK / N>(m);
-        if (col >= a.cols) continue;           // below: no lane exchange
-        const float scale = m > 0.0f ? fmaxf(m / 448.0f, 1.17549435e-38f) : 1.0f;
-        const float inv = 1.0f / scale;
+        float m_lo = -INFINITY;                // what the largest product lost in its rounding
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float p = s[c][i] * w[c][i], lo = fmaf(s[c][i], w[c][i], -p);
+            m_lo = fmaxf(m_lo, fabsf(p) == m ? (p < 0.0f ? -lo : lo) : -INFINITY);
+        }
+        m_lo = block_max<GS_NORM_BLOCK / N>(m_lo);
+        if (col >= cols) continue;           // below: no lane exchange
+        float scale = m * rho / 448.0f, r = 448.0f / m, r_lo = fmaf(-r, m_lo, fmaf(-r, m, 448.0f)) / m;
+        if (!(scale >= 1.17549435e-38f)) {     // a block of zeros, or one too small for the quotient
+            scale = m > 0.0f ? 1.17549435e-38f : 1.0f;
+            r = rho / scale;
+            r_lo = 0.0f;
+        }
         if (col % GS_NORM_BLOCK == 0) a.q_scale[row * a.ld_scale + col / GS_NORM_BLOCK] = scale;
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[c][i] = odd_product(s[c][i], w[c][i], r, r_lo);
         uint32_t b[N / 4];
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
             int v = 0;
-            v = __builtin_amdgcn_cvt_pk_fp8_f32(s[c][i] * inv, s[c][i + 1] * inv, v, false);
-            v = __builtin_amdgcn_cvt_pk_fp8_f32(s[c][i + 2] * inv, s[c][i + 3] * inv, v, true);
+            v = __builtin_amdgcn_cvt_pk_fp8_f32(s[c][i], s[c][i + 1], v, false);
+            v = __builtin_amdgcn_cvt_pk_fp8_f32(s[c][i + 2], s[c][i + 3], v, true);
             b[i / 4] = (uint32_t)v;
         }
         uint8_t* __restrict__ q = a.q + row * a.ld_q + col;
@@ -143,7 +200,7 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (col + i < a.cols) q[i] = (uint8_t)(b[i / 4] >> (8 * (i % 4)));
+                if (col + i < cols) q[i] = (uint8_t)(b[i / 4] >> (8 * (i % 4)));
         }
     }
 }
@@ -160,12 +217,12 @@ inline int norm_parts(int32_t rows, int rpb) {
     return (int)(b < kNormParts ? (b < 1 ? 1 : b) : kNormParts);
 }
 
-template <typename T, bool WHOLE, int WAVES, int E>
-__global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(gs_norm_bwd_args a,
+template <typename T, bool WHOLE, int TPR, int E>
+__global__ void __launch_bounds__(TPR > GS_BLOCK ? TPR : GS_BLOCK) k_rms_norm_bwd(gs_norm_bwd_args a,
                                                                                float* __restrict__ parts) {
-    constexpr int N = Piece<T>::N, CH = E / N, TPR = WAVES * GS_WAVE, RPB = WAVES == 1 ? 4 : 1;
+    constexpr int N = Piece<T>::N, CH = E / N, RPB = TPR < GS_BLOCK ? GS_BLOCK / TPR : 1;
     __shared__ float part[16];
-    __shared__ float comb[RPB > 1 ? RPB * GS_WAVE * N : 1];
+    __shared__ float comb[RPB > 1 ? GS_BLOCK * N : 1];
     const int t = threadIdx.x % TPR;
     float dw[CH][N], w[CH][N];
 #pragma unroll
@@ -174,7 +231,10 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(
 #pragma unroll
         for (int i = 0; i < N; ++i) dw[c][i] = 0.0f;
     }
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+    for (int64_t first = (int64_t)blockIdx.x * RPB; first < a.rows; first += (int64_t)gridDim.x * RPB) {
+        // rows past the end: the last row's address, no columns
+        const int64_t mine = first + threadIdx.x / TPR, row = mine < a.rows ? mine : a.rows - 1;
+        const int cols = mine < a.rows ? a.cols : 0;
         const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
         const T* tot = static_cast<const T*>(a.total) + row * a.ld_total;
         Raw<T, WHOLE> ts[CH], ys[CH], ds[CH];
@@ -182,10 +242,10 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * TPR + t) * N;
-            ts[c].load(tot + col, a.cols - col);
-            ys[c].load(dy + col, a.cols - col);
+            ts[c].load(tot + col, cols - col);
+            ys[c].load(dy + col, cols - col);
             if (WHOLE && a.dtotal)
-                ds[c].load(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, a.cols - col);
+                ds[c].load(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, cols - col);
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -200,20 +260,20 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(
                 ss = fmaf(s[c][i], s[c][i], ss);
                 gs = fmaf(g[c][i] * w[c][i], s[c][i], gs);
             }
-        ss = row_sum<WAVES>(ss, part);
-        gs = row_sum<WAVES>(gs, part);
+        ss = row_sum<TPR>(ss, part);
+        gs = row_sum<TPR>(gs, part);
         const float r = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
         const float mean = gs * r / (float)a.cols;         // mean of g n
         T* dx = static_cast<T*>(a.dx) + row * a.ld_dx;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * TPR + t) * N;
-            if (col >= a.cols) continue;
+            if (col >= cols) continue;
             float d[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) d[i] = 0.0f;
             if (a.dtotal) {
-                if (!WHOLE) ds[c].load(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, a.cols - col);
+                if (!WHOLE) ds[c].load(static_cast<const T*>(a.dtotal) + row * a.ld_dtotal + col, cols - col);
                 ds[c].floats(d);
             }
 #pragma unroll
@@ -222,23 +282,23 @@ __global__ void __launch_bounds__(WAVES == 16 ? 1024 : GS_BLOCK) k_rms_norm_bwd(
                 dw[c][i] = fmaf(g[c][i], n, dw[c][i]);
                 d[i] += r * (g[c][i] * w[c][i] - n * mean);
             }
-            store_piece<T, WHOLE>(dx + col, a.cols - col, d);
+            store_piece<T, WHOLE>(dx + col, cols - col, d);
         }
     }
     float* __restrict__ out = parts + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + t) * N;
-        if (RPB > 1) {                                     // the four waves' rows, in wave order
+        if (RPB > 1) {                                     // the rows side by side, in their order
             float* mine = comb + threadIdx.x * N;
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < N; ++i) mine[i] = dw[c][i];
             __syncthreads();
-            for (int k = threadIdx.x; k < GS_WAVE * N; k += GS_BLOCK) {
+            for (int k = threadIdx.x; k < TPR * N; k += GS_BLOCK) {
                 float v = 0.0f;
 #pragma unroll
-                for (int u = 0; u < RPB; ++u) v += comb[u * GS_WAVE * N + k];
+                for (int u = 0; u < RPB; ++u) v += comb[u * TPR * N + k];
                 if (c * TPR * N + k < a.cols) out[c * TPR * N + k] = v;
             }
         } else {
@@ -283,12 +343,15 @@ bool whole(const void* p, int64_t ld, int bytes) {
 
 template <typename T, bool WHOLE>
 hipError_t norm_go(const gs_norm_args& a, hipStream_t st) {
-    const uint32_t by4 = div_up(a.rows, 4);
-    if (a.cols <= 1024) k_rms_norm<T, WHOLE, 1, 16><<<by4, GS_BLOCK, 0, st>>>(a);
-    else if (a.cols <= 1536) k_rms_norm<T, WHOLE, 1, 24><<<by4, GS_BLOCK, 0, st>>>(a);
-    else if (a.cols <= 2048) k_rms_norm<T, WHOLE, 1, 32><<<by4, GS_BLOCK, 0, st>>>(a);
-    else if (a.cols <= 8192) k_rms_norm<T, WHOLE, 4, 32><<<a.rows, GS_BLOCK, 0, st>>>(a);
-    else k_rms_norm<T, WHOLE, 4, 64><<<a.rows, GS_BLOCK, 0, st>>>(a);
+    constexpr int N = Piece<T>::N, NARROW = GS_NORM_BLOCK / N;
+    const uint32_t by4 = div_up(a.rows, 4), narrow = div_up(a.rows, GS_BLOCK / NARROW);
+    if (a.cols <= GS_NORM_BLOCK) k_rms_norm<T, WHOLE, NARROW, N><<<narrow, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 2 * GS_NORM_BLOCK) k_rms_norm<T, WHOLE, NARROW, 2 * N><<<narrow, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 1024) k_rms_norm<T, WHOLE, 64, 16><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 1536) k_rms_norm<T, WHOLE, 64, 24><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 2048) k_rms_norm<T, WHOLE, 64, 32><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 8192) k_rms_norm<T, WHOLE, 256, 32><<<a.rows, GS_BLOCK, 0, st>>>(a);
+    else k_rms_norm<T, WHOLE, 256, 64><<<a.rows, GS_BLOCK, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -302,17 +365,15 @@ hipError_t norm_type(const gs_norm_args& a, hipStream_t st) {
 
 template <typename T, bool WHOLE>
 hipError_t norm_bwd_go(const gs_norm_bwd_args& a, float* parts, hipStream_t st) {
-    int n = norm_parts(a.rows, 1);
-    if (a.cols <= 2048) {
-        n = norm_parts(a.rows, 4);
-        if (a.cols <= 1024) k_rms_norm_bwd<T, WHOLE, 1, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
-        else if (a.cols <= 1536) k_rms_norm_bwd<T, WHOLE, 1, 24><<<n, GS_BLOCK, 0, st>>>(a, parts);
-        else k_rms_norm_bwd<T, WHOLE, 1, 32><<<n, GS_BLOCK, 0, st>>>(a, parts);
-    } else if (a.cols <= 4096) {
-        k_rms_norm_bwd<T, WHOLE, 4, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
-    } else {
-        k_rms_norm_bwd<T, WHOLE, 16, 16><<<n, 1024, 0, st>>>(a, parts);
-    }
+    constexpr int N = Piece<T>::N, NARROW = GS_NORM_BLOCK / N;
+    const int n = norm_parts(a.rows, a.cols <= 2 * GS_NORM_BLOCK ? GS_BLOCK / NARROW : (a.cols <= 2048 ? 4 : 1));
+    if (a.cols <= GS_NORM_BLOCK) k_rms_norm_bwd<T, WHOLE, NARROW, N><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 2 * GS_NORM_BLOCK) k_rms_norm_bwd<T, WHOLE, NARROW, 2 * N><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 1024) k_rms_norm_bwd<T, WHOLE, 64, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 1536) k_rms_norm_bwd<T, WHOLE, 64, 24><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 2048) k_rms_norm_bwd<T, WHOLE, 64, 32><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 4096) k_rms_norm_bwd<T, WHOLE, 256, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else k_rms_norm_bwd<T, WHOLE, 1024, 16><<<n, 1024, 0, st>>>(a, parts);
     k_norm_dweight<<<div_up(a.cols, GS_WAVE), 1024, 0, st>>>(parts, n, a.cols, a.dweight);
     return hipGetLastError();
 }
@@ -463,6 +524,7 @@ hipError_t launch_rms_norm(const gs_norm_args& a, hipStream_t st) {
     return a.dtype == GS_BF16 ? norm_type<bf16_t>(a, st) : norm_type<f16_t>(a, st);
 }
 
+// For the most partial rows that any type's kernel of this width writes.
 size_t rms_norm_bwd_ws_bytes(int32_t rows, int32_t cols) {
     return align256((size_t)norm_parts(rows, cols <= 2048 ? 4 : 1) * (size_t)cols * 4);
 }

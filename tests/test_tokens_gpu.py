@@ -46,7 +46,7 @@ def within(got, want, bound, what):
 # -- norm ------------------------------------------------------------------------
 
 NORMS = [(1, 1), (1, 8), (3, 7), (5, 128), (4, 129), (7, 1024), (9, 1025), (6, 1160), (5, 1536), (3, 2048), (2, 2056),
-         (2, 4099), (2, 5000), (3, 8200), (2, 16384), (0, 64), (515, 72)]
+         (2, 4099), (2, 5000), (3, 8200), (2, 16384), (0, 64), (515, 72), (1001, 250), (37, 16), (70, 256)]
 
 
 @pytest.mark.parametrize("rows,cols", NORMS)
