@@ -438,15 +438,18 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
 }
 
 // Joins the parts of a row (at most kMaxSplits): lanes take the parts' maxima
-// and sums together, then two elements each and the parts in turn.  WAVES waves
-// share a row where there can be many parts.
+// and sums together, then two elements each and the parts in turn.  Four waves
+// share 64 parts, so that a wave's 16 tiles are all on their way at once; rows
+// that all have more parts take 16 waves.
 constexpr int kMaxSplits = 256;
 
 template <typename T, int WAVES>
-__global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
+__global__ void __launch_bounds__(WAVES == 1 ? GS_BLOCK : WAVES * GS_WAVE) k_attention_join(FwdArgs f) {
+    constexpr int N = WAVES == 1 ? 1 : kMaxSplits / GS_WAVE, GROUPS = WAVES == 1 ? 1 : WAVES / 4;
+    constexpr int EACH = WAVES == 1 ? 8 : 16, STEP = WAVES == 1 ? 1 : 4;
     __shared__ float2 got[WAVES][GS_WAVE];
     const int64_t rows = (int64_t)f.a.n_q * f.a.heads;
-    const int wave = WAVES == 1 ? 0 : threadIdx.x / GS_WAVE;
+    const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
     const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE : blockIdx.x;
     if (row >= rows) return;
     const int lane = lane_id();
@@ -457,7 +460,6 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
         if (keys <= f.chunk) return;                       // one part: written where it belongs; or in no segment
         parts = (keys + f.chunk - 1) / f.chunk;
     }
-    constexpr int N = kMaxSplits / GS_WAVE;
     float2 part[N];
     float m = -INFINITY;
 #pragma unroll
@@ -477,19 +479,25 @@ __global__ void __launch_bounds__(GS_BLOCK) k_attention_join(FwdArgs f) {
     }
     l = wave_sum(l);
     float2 o = make_float2(0.0f, 0.0f);
-    const float* p = f.part_o + row * f.a.dim + 2 * lane;
+    const float* p = f.part_o + row * f.a.dim + (2 * lane < f.a.dim ? 2 * lane : 0);
     const int64_t step = rows * f.a.dim;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        if (n * GS_WAVE >= parts || 2 * lane >= f.a.dim) continue;
-#pragma unroll 8
-        for (int s = wave; s < min(parts - n * GS_WAVE, GS_WAVE); s += WAVES) {
-            // a part that found no keys wrote no tile; the first part always did
-            const float ls = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(part[n].y), s));
-            const float2 v = *reinterpret_cast<const float2*>(p + (ls == 0.0f ? 0 : n * GS_WAVE + s) * step);
-            const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[n]), s));
-            o.x = fmaf(v.x, ws, o.x);
-            o.y = fmaf(v.y, ws, o.y);
+        if (n * GS_WAVE >= parts || n % GROUPS != wave / 4) continue;
+        // a part that found no keys may have written no tile
+        const uint64_t wrote = __ballot(part[n].y != 0.0f);
+        float2 v[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            v[i] = make_float2(0.0f, 0.0f);
+            const int s = wave % 4 + STEP * i;
+            if ((wrote >> s) & 1) v[i] = *reinterpret_cast<const float2*>(p + (n * GS_WAVE + s) * step);
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[n]), wave % 4 + STEP * i));
+            o.x = fmaf(v[i].x, ws, o.x);
+            o.y = fmaf(v[i].y, ws, o.y);
         }
     }
     if (WAVES > 1) {
@@ -523,7 +531,7 @@ struct Plan {
 // (three up to 64 elements, where three fit one), but at least 256 keys, which
 // pay for a start and a join; a longer segment has more of them.  24 regions of
 // 900..9000 keys of 64: 86 us for three a unit, 91 for two, 99 when every segment
-// had the same number of parts; one row over 32,768 keys of 128: 40 us for one a
+// had the same number of parts; one row over 32,768 keys of 128: 38 us for one a
 // unit, 44 for two.  The parts' sums may take 64 MB.
 // More rows: 128-row tiles, and the keys into parts where those tiles leave
 // compute units idle.
@@ -559,7 +567,8 @@ hipError_t go(const FwdArgs& f, bool few, hipStream_t st) {
     if (few) k_attention_few<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
     else k_attention<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
     const uint64_t rows = (uint64_t)f.a.n_q * f.a.heads;
-    if (f.splits > 8) k_attention_join<T, 4><<<(uint32_t)rows, GS_BLOCK, 0, st>>>(f);
+    if (f.splits > 64 && (f.chunk == 0 || f.a.n_seg == 1)) k_attention_join<T, 16><<<(uint32_t)rows, 16 * GS_WAVE, 0, st>>>(f);
+    else if (f.splits > 8) k_attention_join<T, 4><<<(uint32_t)rows, GS_BLOCK, 0, st>>>(f);
     else if (f.splits > 1) k_attention_join<T, 1><<<div_up(rows, 4), GS_BLOCK, 0, st>>>(f);
     return hipGetLastError();
 }
