@@ -215,13 +215,8 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
         }
         if (a.key_on != nullptr || j < alo || j + kKeys > ahi) {
             const uint64_t seen = bits_between(klo - j, khi - j) & on;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[k][e] = -INFINITY;
-            }
+            keep_some(s[0], (uint32_t)seen);
+            keep_some(s[1], (uint32_t)(seen >> 32));
         }
         op8<T> y[2][DT];                           // on their way while the exponentials run
 #pragma unroll
@@ -373,12 +368,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
             const int x = lane + u * GS_WAVE;
             *reinterpret_cast<op8<T>*>(mine + piece_at<P>(x / PIECES, x % PIECES)) = vp[u];
         }
-        if (a.key_on != nullptr || j < alo || j + 32 > ahi) {
-            const uint32_t seen = ((uint32_t)bits_between(klo - j, khi - j) & on) >> (4 * h);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if ((seen & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[0][e] = -INFINITY;
-        }
+        if (a.key_on != nullptr || j < alo || j + 32 > ahi)
+            keep_some(s[0], (uint32_t)bits_between(klo - j, khi - j) & on);
         // behind the part's end: from past the segment's, which reads nothing
         // (a condition on the loads would keep both outcomes' registers)
         fetch(j + 32 * WAVES < j1 ? j + 32 * WAVES : sg.nk);

@@ -135,9 +135,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
         at.refresh();
         const bool test = a.key_on != nullptr || j < alo || j + kStep > ahi;
         uint64_t seen = ~0ull;
-        if (test) {
-            seen = bits_between(klo - j, khi - j) & on;
-        }
+        if (test) seen = bits_between(klo - j, khi - j) & on;
 #pragma unroll
         for (int k = 0; k < kStep / 32; ++k) {
             // operands are read one product ahead of their use; the barriers keep
@@ -157,12 +155,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
                 dp = mfma(y[t & 1], dy[t], dp);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (test) {
-                const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[e] = -INFINITY;
-            }
+            if (test) keep_some(s, (uint32_t)(seen >> (32 * k)));
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -base)) * (dp[e] - delta);
             op8<T> z[2], ds;
@@ -259,8 +252,6 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     admitting(a, sg.nq, shift, key0, last, lo, hi);
     admitting(a, sg.nq, shift, last, key0, alo, ahi);
     admitting(a, sg.nq, shift, key, key, ilo, ihi);
-    if (!on) ihi = ilo;
-    const bool whole = a.key_on == nullptr && key0 + kRows <= sg.nk;
     // the heads' tokens are one list of steps, a head after the other
     const int t0 = lo / ST * ST, per = max(hi - t0 + ST - 1, 0) / ST;
     int n0 = 0, n1 = per * a.group;
@@ -315,7 +306,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         at.refresh();
         const int t = ct;
         ct = ct + ST < end ? ct + ST : t0;
-        const bool test = !whole || t < alo || t + ST > ahi;
+        const bool test = t < alo || t + ST > ahi;
         uint64_t seen = ~0ull;
         if (test) seen = bits_between(ilo - t, ihi - t);
         acc16 s[NK]{}, dp[NK]{};
@@ -339,12 +330,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
             }
         };
         auto gradients = [&](int k) {
-            if (test) {
-                const uint32_t w = (uint32_t)(seen >> (32 * k)) >> (4 * h);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if ((w & (1u << (8 * (e >> 2) + (e & 3)))) == 0) s[k][e] = -INFINITY;
-            }
+            if (test) keep_some(s[k], (uint32_t)(seen >> (32 * k)));
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int first = 32 * k + 8 * g + 4 * h;
@@ -405,6 +391,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         __syncthreads();
     }
     if (!there) return;
+    if (!on) {                                     // what a key that is off has summed is in its column alone
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = acc16{};
+    }
     const int64_t token = sg.k0 + key;
     if (f.splits > 1) {
         const int64_t n = (int64_t)a.n_k * a.kv_heads;

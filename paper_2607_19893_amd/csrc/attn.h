@@ -246,6 +246,17 @@ __device__ __forceinline__ uint64_t bits_between(int lo, int hi) {
     return lo <= 0 ? below : (lo >= 64 ? 0ull : below & (~0ull << lo));
 }
 
+// -inf into a C tile's elements whose row (register e of half h is row 8 (e >> 2)
+// + (e & 3) + 4 h) has its bit off in the lane's `seen`: two instructions each.
+__device__ __forceinline__ void keep_some(acc16& s, uint32_t seen) {
+    const uint32_t mine = seen >> (4 * (lane_id() >> 5));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const uint32_t m = (int32_t)(mine << (31 - 8 * (e >> 2) - (e & 3))) >> 31;
+        s[e] = __uint_as_float((__float_as_uint(s[e]) & m) | (0xFF800000u & ~m));
+    }
+}
+
 struct AttnArgs {
     const void *q, *k, *v;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
