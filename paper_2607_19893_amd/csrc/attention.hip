@@ -86,19 +86,32 @@ __device__ __forceinline__ void store_tile(const FwdArgs& f, bool parts, int tok
 }
 
 // One step of the online softmax over a tile of 32 N keys: s (raw products,
-// -inf where not admitted) becomes the probabilities against the new maximum.
-// c = scale * log2(e).  Returns the factor of what was summed before.
+// -inf where not admitted) becomes the probabilities against the running
+// maximum m.  c = scale * log2(e).  The maximum is held until a score passes it
+// by more than kHeld powers of two: probabilities up to 2^kHeld lose nothing in
+// either type, and in most steps neither the sum nor the output is rescaled.
+// Returns whether the output is to be, by alpha.
+constexpr float kHeld = 8.0f;
+
+__device__ __forceinline__ float held(float c) { return fminf(kHeld / c, 3.0e38f); }
+
 template <int N>
-__device__ __forceinline__ float softmax_step(acc16 (&s)[N], float c, float& m, float& l) {
+__device__ __forceinline__ bool softmax_step(acc16 (&s)[N], float c, float slack, float& m, float& l, float& alpha) {
     // four chains each for the maximum and the sum: one would wait for itself
     float t4[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
         for (int i = 0; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], s[k][i]);
-    const float t = fmaxf(m, half_max(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]))));
-    const float base = t == -INFINITY ? 0.0f : t * c;      // nothing admitted yet: exp2(-inf) = 0 below
-    const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+    const float t = half_max(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+    const bool rise = __any(t > m + slack);
+    if (rise) {
+        const float top = fmaxf(m, t);
+        alpha = __builtin_amdgcn_exp2f(fmaf(m, c, top == -INFINITY ? 0.0f : -top * c));
+        l *= alpha;
+        m = top;
+    }
+    const float base = m == -INFINITY ? 0.0f : m * c;      // nothing admitted yet: exp2(-inf) = 0 below
     float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -107,10 +120,8 @@ __device__ __forceinline__ float softmax_step(acc16 (&s)[N], float c, float& m, 
             s[k][i] = __builtin_amdgcn_exp2f(fmaf(s[k][i], c, -base));
             sum4[i & 3] += s[k][i];
         }
-    const float sum = (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
-    l = l * alpha + sum;                                   // this half's keys; the halves meet at the end
-    m = t;
-    return alpha;
+    l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);        // this half's keys; the halves meet at the end
+    return rise;
 }
 
 template <typename T, int D>
@@ -182,7 +193,7 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
         vl.load(vs, j, skip);     // a probability of 0 does not stop a NaN
     };
 
-    const float c = a.scale * kLog2e;
+    const float c = a.scale * kLog2e, slack = held(c);
     float m = -INFINITY, l = 0.0f;
     acc16 o[DT];
 #pragma unroll
@@ -224,8 +235,8 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
 #pragma unroll
         for (int d = 0; d < DT; ++d) y[1][d] = columns_operand<T, P>(vs, at, 16, d);
         __builtin_amdgcn_sched_barrier(0);
-        const float alpha = softmax_step<2>(s, c, m, l);
-        if (__any(alpha != 1.0f)) {                // the maxima rise in the first steps, seldom later
+        float alpha;
+        if (softmax_step<2>(s, c, slack, m, l, alpha)) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= alpha;
         }
@@ -338,7 +349,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
         for (int u = 0; u < LOADS; ++u) vp[u] = vb.piece(voff + (va + u * STEP * vb.ld));
     };
 
-    const float c = a.scale * kLog2e;
+    const float c = a.scale * kLog2e, slack = held(c);
     float m = -INFINITY, l = 0.0f;
     acc16 o[DT];
 #pragma unroll
@@ -373,9 +384,11 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
         // behind the part's end: from past the segment's, which reads nothing
         // (a condition on the loads would keep both outcomes' registers)
         fetch(j + 32 * WAVES < j1 ? j + 32 * WAVES : sg.nk);
-        const float alpha = softmax_step<1>(s, c, m, l);
+        float alpha;
+        if (softmax_step<1>(s, c, slack, m, l, alpha)) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] *= alpha;
+            for (int d = 0; d < DT; ++d) o[d] *= alpha;
+        }
         // this wave's values are in LDS before any of its lanes reads them
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();

@@ -451,6 +451,20 @@ def test_large_scores(tk):
     check_forward(got, ref.attention(q, k, v, c))
 
 
+@pytest.mark.parametrize("nq", [40, 2])
+@pytest.mark.parametrize("rise", [4.0, -40.0, 40.0, 400.0])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_rising_scores(tk, nq, rise, dtype):
+    """Scores that climb (or fall) along the keys: the maximum that the sums stand against is passed by a little, again
+    and again, or by much in a few keys."""
+    c = case([nq], [900], 2, dim=64, dtype=dtype)
+    g, q, k, v, _ = inputs(c)
+    q[..., 0] = 8.0
+    k[..., 0] = (torch.arange(900, device="cuda") * (rise / 900))[:, None].to(dtype)
+    got = tk.attention(q, k, v, scale=c["scale"])
+    check_forward(got, ref.attention(q, k, v, c))
+
+
 def test_other_stream_and_graph(tk):
     c = case([100, 30], heads=4, kv=2, dim=64, right=0)
     g, q, k, v, _ = inputs(c)
