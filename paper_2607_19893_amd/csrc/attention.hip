@@ -534,9 +534,9 @@ struct Plan {
 // all segments and key heads are cut into parts for one workgroup a compute unit
 // (three up to 64 elements, where three fit one), but at least 256 keys, which
 // pay for a start and a join; a longer segment has more of them.  24 regions of
-// 900..9000 keys of 64: 86 us for three a unit, 91 for two, 99 when every segment
-// had the same number of parts; one row over 32,768 keys of 128: 38 us for one a
-// unit, 44 for two.  The parts' sums may take 64 MB.
+// 900..9000 keys of 64: 85 us for three a unit, 93 for two, 92 for four, 99 when
+// every segment had the same number of parts; one row over 32,768 keys of 128: 38
+// us for one a unit, 39 for two.  The parts' sums may take 64 MB.
 // More rows: 128-row tiles, and the keys into parts where those tiles leave
 // compute units idle.
 Plan plan(const gs_attn& a) {

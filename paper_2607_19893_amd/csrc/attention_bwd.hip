@@ -54,12 +54,15 @@ __device__ __forceinline__ void store_tiles(T* p, const acc16 (&o)[DT], float sc
         }
 }
 
-template <typename T, int D>
+// KEYS: keys may be off.  A step's keys then start their scores at 0 or -inf,
+// read from LDS into the tile that the products are added to.
+template <typename T, int D, bool KEYS>
 __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
     // two buffers: a step's tiles arrive while the step before computes
     __shared__ __attribute__((aligned(16))) T ks0[kStep * P], vs0[kStep * P];
     __shared__ __attribute__((aligned(16))) T ks1[kStep * P], vs1[kStep * P];
+    __shared__ __attribute__((aligned(16))) float on0[KEYS ? kStep : 4], on1[KEYS ? kStep : 4];
     const AttnArgs& a = f.a;
     const Place place = chiplet_place<true>(blockIdx.x, a.tiles, a.kv_heads, 1);
     const int kvh = place.head;
@@ -112,14 +115,13 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     vl.init(static_cast<const T*>(a.v) + sg.k0 * a.v_row + kvh * a.v_head, sg.nk, a.v_row, a.dim);
     // the keys' flags, loaded a step before the tiles that they belong to
     const uint8_t* const flags = a.key_on + sg.k0;
-    uint64_t on = ~0ull, on_next = ~0ull;
-    uint8_t flag = 1;
-    auto fetch = [&](T* ks, T* vs, int j) {
+    uint8_t flag = 0;
+    auto fetch = [&](T* ks, T* vs, float* on, int j) {
         uint32_t skip = 0;
-        if (a.key_on != nullptr) {
-            on_next = __ballot(flag);
+        if (KEYS) {
+            skip = rows_off<P, kStep>(__ballot(flag));
+            if (threadIdx.x < kStep) on[threadIdx.x] = flag ? 0.0f : -INFINITY;
             flag = key_flag(flags, j + kStep + fresh(lane), sg.nk);
-            skip = rows_off<P, kStep>(on_next);
         }
         kl.load(ks, j, skip);
         vl.load(vs, j, skip);
@@ -131,17 +133,28 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     acc16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = acc16{};
-    auto step = [&](const T* ks, const T* vs, int j) {
+    auto step = [&](const T* ks, const T* vs, const float* on, int j) {
         at.refresh();
-        const bool test = a.key_on != nullptr || j < alo || j + kStep > ahi;
+        // the window's edge, where rows differ; the segment's end has its flags
+        const bool test = j < alo || (KEYS ? min(j + kStep, sg.nk) : j + kStep) > ahi;
         uint64_t seen = ~0ull;
-        if (test) seen = bits_between(klo - j, khi - j) & on;
+        if (test) seen = bits_between(klo - j, khi - j);
 #pragma unroll
         for (int k = 0; k < kStep / 32; ++k) {
             // operands are read one product ahead of their use; the barriers keep
             // the compiler from reading more of them ahead, which would not fit
             // the registers of two waves a SIMD
             acc16 s{}, dp{};
+            if (KEYS) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 v = *reinterpret_cast<const float4*>(on + 32 * k + 8 * g + 4 * h);
+                    s[4 * g] = v.x;
+                    s[4 * g + 1] = v.y;
+                    s[4 * g + 2] = v.z;
+                    s[4 * g + 3] = v.w;
+                }
+            }
             op8<T> x[2], y[2];
             x[0] = rows_operand<T, P>(ks, at, 32 * k, 0);
             y[0] = rows_operand<T, P>(vs, at, 32 * k, 0);
@@ -172,19 +185,17 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     };
     const int j0 = lo / kStep * kStep;
     if (j0 < hi) {
-        if (a.key_on != nullptr) flag = key_flag(flags, j0 + lane, sg.nk);
-        fetch(ks0, vs0, j0);
+        if (KEYS) flag = key_flag(flags, j0 + lane, sg.nk);
+        fetch(ks0, vs0, on0, j0);
     }
     __syncthreads();                               // the fetched tiles are in LDS
     for (int j = j0; j < hi; j += 2 * kStep) {
-        on = on_next;
-        if (j + kStep < hi) fetch(ks1, vs1, j + kStep);
-        step(ks0, vs0, j);
+        if (j + kStep < hi) fetch(ks1, vs1, on1, j + kStep);
+        step(ks0, vs0, on0, j);
         __syncthreads();
         if (j + kStep < hi) {
-            on = on_next;
-            if (j + 2 * kStep < hi) fetch(ks0, vs0, j + 2 * kStep);
-            step(ks1, vs1, j + kStep);
+            if (j + 2 * kStep < hi) fetch(ks0, vs0, on0, j + 2 * kStep);
+            step(ks1, vs1, on1, j + kStep);
         }
         __syncthreads();
     }
@@ -451,7 +462,8 @@ int dkv_splits(const gs_attn& a) {
 template <typename T, int D>
 hipError_t go(const BwdArgs& f, hipStream_t st) {
     if (f.a.n_q > 0)
-        k_attention_dq<T, D><<<(uint32_t)(f.a.tiles * f.a.kv_heads), GS_BLOCK, 0, st>>>(f);
+        (f.a.key_on ? k_attention_dq<T, D, true> : k_attention_dq<T, D, false>)
+            <<<(uint32_t)(f.a.tiles * f.a.kv_heads), GS_BLOCK, 0, st>>>(f);
     if (f.a.n_k > 0) {
         k_attention_dkv<T, D><<<(uint32_t)(f.key_tiles * f.a.kv_heads * f.splits), GS_BLOCK, 0, st>>>(f);
         if (f.splits > 1)
