@@ -459,10 +459,13 @@ __global__ void __launch_bounds__(WAVES == 1 ? GS_BLOCK : WAVES * GS_WAVE) k_att
     const int lane = lane_id();
     const int64_t token = row / f.a.heads;
     int parts = f.splits;
-    if (f.chunk > 0) {
+    if (f.chunk > 0 || f.a.cu_q != nullptr) {
         const int keys = __builtin_amdgcn_readfirstlane(keys_of_token(f.a, (int)token));
-        if (keys <= f.chunk) return;                       // one part: written where it belongs; or in no segment
-        parts = (keys + f.chunk - 1) / f.chunk;
+        if (keys < 0) return;                              // in no segment
+        if (f.chunk > 0) {
+            if (keys <= f.chunk) return;                   // one part: written where it belongs
+            parts = (keys + f.chunk - 1) / f.chunk;
+        }
     }
     float2 part[N];
     float m = -INFINITY;

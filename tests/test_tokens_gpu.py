@@ -422,6 +422,18 @@ def test_rows_outside_every_segment_stay(tk, gs):
     assert torch.equal(out[5:20], want[0])
 
 
+@pytest.mark.parametrize("rows", [40, 2])
+def test_rows_outside_every_segment_stay_where_keys_are_cut(tk, gs, rows):
+    c = case([rows + 10], [5000], heads=2, kv=1, dim=64)
+    g, q, k, v, _ = inputs(c)
+    out, lse = torch.full_like(q, 7.0), torch.full((rows + 10, 2), 7.0, device="cuda")
+    cu_q, cu_k = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([5, 5 + rows], [3, 4990]))
+    a = gs.make_attn(q, k, v, 0.125, cu_q=cu_q, cu_k=cu_k)
+    gs.gs_attention(a, out, lse, torch.full((gs.gs_attention_ws_bytes(a),), 64, dtype=torch.uint8, device="cuda"))
+    for t in (out, lse):
+        assert bool((t[:5] == 7).all()) and bool((t[5 + rows:] == 7).all()) and bool((t[5:5 + rows] != 7).all())
+
+
 def test_offsets_past_32_bits(tk):
     """Keys and values whose rows lie 2^20 elements apart: the last is past 2^32 bytes and 2^31 elements."""
     n, ld = 2100, 1 << 20
