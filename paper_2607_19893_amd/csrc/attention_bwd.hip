@@ -30,7 +30,8 @@ struct BwdArgs {
     float* base;                           // [heads][n_q]: the rows' log sums in powers of two
     float* delta;                          // [heads][n_q], behind base
     int32_t key_tiles;
-    int32_t splits;                        // parts that a key tile's rows are cut into
+    int32_t splits;                        // most parts that a key tile's rows are cut into
+    int32_t chunk;                         // steps of a part (about)
     float* part;                           // [splits][2][n_k * kv_heads][dim]: dk, dv
 };
 
@@ -204,6 +205,26 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
                            a.dim);
 }
 
+// The steps of a key tile, ST tokens each, all heads of the group one after the
+// other: t0 and `per` steps a head, `parts` equal runs of them.
+template <int ST>
+struct TileRows {
+    int lo, hi;                            // tokens that admit any of the tile's keys
+    int t0, per, steps, parts;
+
+    __device__ __forceinline__ TileRows(const BwdArgs& f, const Segment& sg, int key0) {
+        const int last = min(key0 + kRows, sg.nk) - 1;
+        admitting(f.a, sg.nq, sg.nk - sg.nq, key0, last, lo, hi);
+        t0 = lo / ST * ST;
+        per = max(hi - t0 + ST - 1, 0) / ST;
+        steps = per * f.a.group;
+        parts = max(1, min(f.splits, (steps + f.chunk - 1) / f.chunk));
+    }
+};
+
+// Steps of dk's and dv's kernel: 64 tokens, 32 for heads of more than 64 elements.
+constexpr int dkv_step(int dim) { return dim > 64 ? 32 : 64; }
+
 // The sums of dk and dv take a lane's registers twice the head's size; keys and
 // values beside them leave no room for two waves a SIMD from 96 elements on, so
 // there the values are read from LDS (a quarter more of its traffic) and a step
@@ -212,7 +233,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
     constexpr bool BIG = D > 64;
-    constexpr int ST = BIG ? 32 : 64, NK = ST / 32;
+    constexpr int ST = dkv_step(D), NK = ST / 32;
     __shared__ __attribute__((aligned(16))) T qs0[ST * P], ds0[ST * P];
     __shared__ __attribute__((aligned(16))) T qs1[ST * P], ds1[ST * P];
     __shared__ __attribute__((aligned(16))) float st0[2 * 64], st1[2 * 64];            // bases, then deltas
@@ -223,6 +244,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     const Segment sg = find_segment<true, false>(a, kRows, f.key_tiles, place.tile);
     const int key0 = sg.tile * kRows;
     if (key0 >= sg.nk) return;
+    const TileRows<ST> tr(f, sg, key0);
+    if (split >= tr.parts) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
     const int key = key0 + 32 * wave + (lane & 31);
     const bool there = key < sg.nk;
@@ -257,20 +280,13 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         }
         vl.load(vs, 0, skip);
     }
-    // tokens that admit any of the workgroup's keys, and those that all do
+    // tokens that admit all of the workgroup's keys, and those that admit the lane's
     const int last = min(key0 + kRows, sg.nk) - 1;
-    int lo, hi, alo, ahi, ilo, ihi;
-    admitting(a, sg.nq, shift, key0, last, lo, hi);
+    int alo, ahi, ilo, ihi;
     admitting(a, sg.nq, shift, last, key0, alo, ahi);
     admitting(a, sg.nq, shift, key, key, ilo, ihi);
-    // the heads' tokens are one list of steps, a head after the other
-    const int t0 = lo / ST * ST, per = max(hi - t0 + ST - 1, 0) / ST;
-    int n0 = 0, n1 = per * a.group;
-    if (f.splits > 1) {
-        const int each = (n1 + f.splits - 1) / f.splits;
-        n0 = split * each;
-        n1 = min(n1, n0 + each);
-    }
+    const int t0 = tr.t0, per = tr.per;
+    const int each = (tr.steps + tr.parts - 1) / tr.parts, n0 = split * each, n1 = min(tr.steps, n0 + each);
     // a token that admits no key at all may hold anything: its row is left out
     const bool empties = a.key_on != nullptr || (a.right >= 0 && shift + a.right < 0);
 
@@ -407,7 +423,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         for (int d = 0; d < DT; ++d) dk[d] = dv[d] = acc16{};
     }
     const int64_t token = sg.k0 + key;
-    if (f.splits > 1) {
+    if (tr.parts > 1) {
         const int64_t n = (int64_t)a.n_k * a.kv_heads;
         float* pk = f.part + ((int64_t)split * 2 * n + token * a.kv_heads + kvh) * a.dim;
         store_tiles<float, DT>(pk, dk, a.scale, a.dim);
@@ -418,45 +434,72 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     store_tiles<T, DT>(static_cast<T*>(f.dv) + token * f.dv_row + (int64_t)kvh * f.dv_head, dv, 1.0f, a.dim);
 }
 
-// Sums the parts of dk and dv in ascending order, four elements a thread.
-template <typename T>
+// Sums the parts of a key tile's dk or dv in ascending order, four elements a
+// thread at a time.
+template <typename T, int ST>
 __global__ void __launch_bounds__(GS_BLOCK) k_attention_dkv_join(BwdArgs f) {
     const AttnArgs& a = f.a;
-    const int per = a.dim / 4;
-    const int64_t n = (int64_t)a.n_k * a.kv_heads;
-    const int64_t x = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x;
-    if (x >= 2 * n * per) return;
-    const int which = x >= n * per;
-    const int64_t row = (x - which * n * per) / per;
-    const int c = (int)(x - which * n * per - row * per) * 4;
-    const int64_t token = row / a.kv_heads;
-    const int head = (int)(row - token * a.kv_heads);
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s = 0; s < f.splits; ++s) {
-        const float4 w = *reinterpret_cast<const float4*>(f.part + ((int64_t)(2 * s + which) * n + row) * a.dim + c);
-        v.x += w.x;
-        v.y += w.y;
-        v.z += w.z;
-        v.w += w.w;
+    const int which = blockIdx.x & 1;
+    const Place place = chiplet_place<false>(blockIdx.x >> 1, f.key_tiles, a.kv_heads, 1);
+    const int kvh = place.head;
+    const Segment sg = find_segment<true, false>(a, kRows, f.key_tiles, place.tile);
+    const int key0 = sg.tile * kRows;
+    if (key0 >= sg.nk) return;
+    const TileRows<ST> tr(f, sg, key0);
+    if (tr.parts == 1) return;                             // written where it belongs
+    const int per = a.dim / 4, n = min(kRows, sg.nk - key0) * per;
+    const int64_t rows = (int64_t)a.n_k * a.kv_heads, token0 = sg.k0 + key0;
+    T* const out = static_cast<T*>(which ? f.dv : f.dk) + kvh * (which ? f.dv_head : f.dk_head);
+    const int64_t ld = which ? f.dv_row : f.dk_row;
+    for (int x = threadIdx.x; x < n; x += GS_BLOCK) {
+        const int key = x / per, c = 4 * (x - key * per);
+        const float* p = f.part + (which * rows + (token0 + key) * a.kv_heads + kvh) * a.dim + c;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int s = 0; s < tr.parts; ++s) {
+            const float4 w = *reinterpret_cast<const float4*>(p + 2 * s * rows * a.dim);
+            v.x += w.x;
+            v.y += w.y;
+            v.z += w.z;
+            v.w += w.w;
+        }
+        op4<T> o;
+        o[0] = (T)v.x;
+        o[1] = (T)v.y;
+        o[2] = (T)v.z;
+        o[3] = (T)v.w;
+        *reinterpret_cast<op4<T>*>(out + (token0 + key) * ld + c) = o;
     }
-    T* p = which ? static_cast<T*>(f.dv) + token * f.dv_row + (int64_t)head * f.dv_head
-                 : static_cast<T*>(f.dk) + token * f.dk_row + (int64_t)head * f.dk_head;
-    op4<T> o;
-    o[0] = (T)v.x;
-    o[1] = (T)v.y;
-    o[2] = (T)v.z;
-    o[3] = (T)v.w;
-    *reinterpret_cast<op4<T>*>(p + c) = o;
 }
 
-// Parts that a key tile's rows are cut into, from the sizes alone: enough
-// workgroups for two a compute unit, as long as a part keeps eight steps.
-int dkv_splits(const gs_attn& a) {
-    constexpr int kUnits = 256, kMost = 16;
-    const int group = a.heads / a.kv_heads;
+struct DkvPlan {
+    int splits, chunk;
+};
+
+// How the key tiles' rows are cut, from the sizes alone: into runs of about one
+// length, three to a compute unit (two fit it), as long as a run keeps 512
+// tokens.  A window makes some tiles' rows fewer, so their mean is taken over 32
+// tiles of a segment of mean length.  8192 ordered tokens, 16/4 heads of 128, the
+// whole gradient: 1050 us with every tile in two parts, 984 so; 1079 and 1032
+// with two and four runs to a unit.
+DkvPlan dkv_plan(const gs_attn& a) {
+    constexpr int kUnits = 256, kMost = 16, kTiles = 32;
+    const int group = a.heads / a.kv_heads, st = dkv_step(a.dim);
+    const int64_t nq = a.n_q / a.n_seg, nk = a.n_k / a.n_seg, shift = nk - nq;
+    int64_t rows = 0, most = 0;
+    for (int i = 0; i < kTiles; ++i) {
+        const int64_t key = nk * (2 * i + 1) / (2 * kTiles);
+        const int64_t lo = a.right >= 0 ? std::max<int64_t>(0, key - a.right - shift) : 0;
+        const int64_t hi = a.left >= 0 ? std::min<int64_t>(nq, key + a.left - shift + 1) : nq;
+        rows += std::max<int64_t>(0, hi - lo);
+        most = std::max(most, hi - lo);
+    }
     const int64_t groups = (int64_t)attn_tiles(a.n_k, kRows, a.n_seg) * a.kv_heads;
-    const int64_t steps = ((int64_t)a.n_q / a.n_seg + kStep - 1) / kStep * group;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(2 * kUnits + groups - 1) / groups, steps / 8, kMost}));
+    const int64_t steps = (rows / kTiles + st - 1) / st * group, longest = (most + st - 1) / st * group;
+    const int64_t chunk = std::max<int64_t>(512 / st, groups * steps / (3 * kUnits));
+    DkvPlan p;
+    p.chunk = (int)std::min<int64_t>(chunk, 1 << 30);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((longest + p.chunk - 1) / p.chunk, kMost));
+    return p;
 }
 
 template <typename T, int D>
@@ -465,10 +508,9 @@ hipError_t go(const BwdArgs& f, hipStream_t st) {
         (f.a.key_on ? k_attention_dq<T, D, true> : k_attention_dq<T, D, false>)
             <<<(uint32_t)(f.a.tiles * f.a.kv_heads), GS_BLOCK, 0, st>>>(f);
     if (f.a.n_k > 0) {
-        k_attention_dkv<T, D><<<(uint32_t)(f.key_tiles * f.a.kv_heads * f.splits), GS_BLOCK, 0, st>>>(f);
-        if (f.splits > 1)
-            k_attention_dkv_join<T>
-                <<<div_up((uint64_t)f.a.n_k * f.a.kv_heads * f.a.dim / 2, GS_BLOCK), GS_BLOCK, 0, st>>>(f);
+        const uint32_t tiles = (uint32_t)(f.key_tiles * f.a.kv_heads);
+        k_attention_dkv<T, D><<<tiles * f.splits, GS_BLOCK, 0, st>>>(f);
+        if (f.splits > 1) k_attention_dkv_join<T, dkv_step(D)><<<2 * tiles, GS_BLOCK, 0, st>>>(f);
     }
     return hipGetLastError();
 }
@@ -484,7 +526,7 @@ hipError_t by_dim(const BwdArgs& f, hipStream_t st) {
 }  // namespace
 
 size_t attention_bwd_ws_bytes(const gs_attn& a) {
-    const int splits = dkv_splits(a);
+    const int splits = dkv_plan(a).splits;
     const size_t parts = splits > 1 ? (size_t)splits * 2 * a.n_k * a.kv_heads * a.dim * sizeof(float) : 0;
     return align256((size_t)a.n_q * a.heads * 2 * sizeof(float)) + align256(parts);
 }
@@ -512,7 +554,9 @@ hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* 
     f.lse = g.lse;
     f.base = static_cast<float*>(ws);
     f.delta = f.base + (size_t)a.n_q * a.heads;
-    f.splits = dkv_splits(a);
+    const DkvPlan plan = dkv_plan(a);
+    f.splits = plan.splits;
+    f.chunk = plan.chunk;
     f.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * 2 * sizeof(float)));
     return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, st) : by_dim<f16_t>(f, st);
 }

@@ -434,6 +434,19 @@ def test_rows_outside_every_segment_stay_where_keys_are_cut(tk, gs, rows):
         assert bool((t[:5] == 7).all()) and bool((t[5 + rows:] == 7).all()) and bool((t[5:5 + rows] != 7).all())
 
 
+def test_keys_outside_every_segment_stay_where_rows_are_cut(tk, gs):
+    c = case([2500], [130], heads=2, kv=1, dim=64)
+    g, q, k, v, _ = inputs(c)
+    out, lse = tk.attention(q, k, v)
+    dq, dk, dv = (torch.full_like(t, 7.0) for t in (q, k, v))
+    cu_q, cu_k = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([5, 2400], [3, 120]))
+    a = gs.make_attn(q, k, v, 0.125, cu_q=cu_q, cu_k=cu_k)
+    n = gs.gs_attention_ws_bytes(a, True)
+    gs.gs_attention_bwd(a, out, lse, torch.ones_like(q), dq, dk, dv, torch.full((n,), 64, dtype=torch.uint8, device="cuda"))
+    for t, lo, hi in ((dq, 5, 2400), (dk, 3, 120), (dv, 3, 120)):
+        assert bool((t[:lo] == 7).all()) and bool((t[hi:] == 7).all()) and bool((t[lo:hi] != 7).any(-1).all())
+
+
 def test_offsets_past_32_bits(tk):
     """Keys and values whose rows lie 2^20 elements apart: the last is past 2^32 bytes and 2^31 elements."""
     n, ld = 2100, 1 << 20
