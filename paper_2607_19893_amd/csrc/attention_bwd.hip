@@ -434,27 +434,28 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     store_tiles<T, DT>(static_cast<T*>(f.dv) + token * f.dv_row + (int64_t)kvh * f.dv_head, dv, 1.0f, a.dim);
 }
 
-// Sums the parts of a key tile's dk or dv in ascending order, four elements a
-// thread at a time.
+// Sums the parts of dk or dv of 32 of a key tile's keys in ascending order, four
+// elements a thread at a time.
 template <typename T, int ST>
 __global__ void __launch_bounds__(GS_BLOCK) k_attention_dkv_join(BwdArgs f) {
     const AttnArgs& a = f.a;
-    const int which = blockIdx.x & 1;
-    const Place place = chiplet_place<false>(blockIdx.x >> 1, f.key_tiles, a.kv_heads, 1);
+    const int which = blockIdx.x & 1, key1 = blockIdx.x / 2 % 4 * 32;
+    const Place place = chiplet_place<false>(blockIdx.x / 8, f.key_tiles, a.kv_heads, 1);
     const int kvh = place.head;
     const Segment sg = find_segment<true, false>(a, kRows, f.key_tiles, place.tile);
     const int key0 = sg.tile * kRows;
-    if (key0 >= sg.nk) return;
+    if (key0 + key1 >= sg.nk) return;
     const TileRows<ST> tr(f, sg, key0);
     if (tr.parts == 1) return;                             // written where it belongs
-    const int per = a.dim / 4, n = min(kRows, sg.nk - key0) * per;
-    const int64_t rows = (int64_t)a.n_k * a.kv_heads, token0 = sg.k0 + key0;
+    const int per = a.dim / 4, n = min(32, sg.nk - key0 - key1) * per;
+    const int64_t rows = (int64_t)a.n_k * a.kv_heads, token0 = sg.k0 + key0 + key1;
     T* const out = static_cast<T*>(which ? f.dv : f.dk) + kvh * (which ? f.dv_head : f.dk_head);
     const int64_t ld = which ? f.dv_row : f.dk_row;
     for (int x = threadIdx.x; x < n; x += GS_BLOCK) {
         const int key = x / per, c = 4 * (x - key * per);
         const float* p = f.part + (which * rows + (token0 + key) * a.kv_heads + kvh) * a.dim + c;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
         for (int s = 0; s < tr.parts; ++s) {
             const float4 w = *reinterpret_cast<const float4*>(p + 2 * s * rows * a.dim);
             v.x += w.x;
@@ -479,7 +480,7 @@ struct DkvPlan {
 // length, three to a compute unit (two fit it), as long as a run keeps 512
 // tokens.  A window makes some tiles' rows fewer, so their mean is taken over 32
 // tiles of a segment of mean length.  8192 ordered tokens, 16/4 heads of 128, the
-// whole gradient: 1050 us with every tile in two parts, 984 so; 1079 and 1032
+// whole gradient: 1050 us with every tile in two parts, 967 so; 1079 and 1032
 // with two and four runs to a unit.
 DkvPlan dkv_plan(const gs_attn& a) {
     constexpr int kUnits = 256, kMost = 16, kTiles = 32;
@@ -510,7 +511,7 @@ hipError_t go(const BwdArgs& f, hipStream_t st) {
     if (f.a.n_k > 0) {
         const uint32_t tiles = (uint32_t)(f.key_tiles * f.a.kv_heads);
         k_attention_dkv<T, D><<<tiles * f.splits, GS_BLOCK, 0, st>>>(f);
-        if (f.splits > 1) k_attention_dkv_join<T, dkv_step(D)><<<2 * tiles, GS_BLOCK, 0, st>>>(f);
+        if (f.splits > 1) k_attention_dkv_join<T, dkv_step(D)><<<8 * tiles, GS_BLOCK, 0, st>>>(f);
     }
     return hipGetLastError();
 }
