@@ -124,6 +124,13 @@ __device__ __forceinline__ bool softmax_step(acc16 (&s)[N], float c, float slack
     return rise;
 }
 
+// 128 rows a workgroup, 64 keys a step.  Up to 64 elements a head three waves fit
+// a SIMD, from 96 on two.  8192 ordered tokens, 16/4 heads of 128: 281 us, 980
+// TFLOP/s of the products that the mask leaves; matrix units busy 53% of the
+// cycles and vector units 54%, at clocks that the power limit sets (operands of
+// zeros run 1.35 times faster).  40 regions of 40..1600 fp16 tokens, 8 heads of
+// 64: 48 us, matrix 29% and vector 68%: there a score's exponential, maximum, sum
+// and rounding cost more issue cycles than its 256 multiply-adds.
 template <typename T, int D>
 __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
@@ -280,10 +287,13 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
 // of the segment's rows (32 at a time, seldom more), and every wave of it its own
 // keys (32 a step, its waves' steps interleaved), with a running maximum and sum
 // of its own; the waves meet in LDS at the end.  Segments are cut into parts of
-// about the same length, so long and short ones load the chip alike.  The keys' bytes bound it,
-// so a step's keys go from memory straight into the operand's registers, its
-// values through a piece of LDS that only this wave touches (no barrier in the
-// loop), and both are fetched a step ahead.
+// about the same length, so long and short ones load the chip alike.  The keys'
+// bytes bound it, so a step's keys go from memory straight into the operand's
+// registers, its values through a piece of LDS that only this wave touches (no
+// barrier in the loop), and both are fetched a step ahead.  One token over 32,768
+// keys, 16/4 heads of 128: 27 us, 4.9 TB/s.  24 segments of 1..16 rows over
+// 900..9000 keys, 16 heads of 64: 75 us, 4.2 TB/s (two waves a SIMD; held to the
+// registers of three it took 3 us more).
 constexpr int kFewRows = 32;
 
 template <typename T, int D>
@@ -304,152 +314,155 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / GS_WAVE);
 #pragma unroll 1
     for (int row0 = 0; row0 < rows; row0 += kFewRows) {
-    const int lane = fresh(lane_id()), h = lane >> 5;      // nothing of it is held over the loop
-    const int r = row0 + (lane & 31);
-    const bool there = r < rows;
-    const int i = (there ? r : rows - 1) / a.group;
-    const int token = sg.q0 + i, head = kvh * a.group + (there ? r : rows - 1) - i * a.group;
-    const int shift = sg.nk - sg.nq;
+        const int lane = fresh(lane_id()), h = lane >> 5;      // nothing of it is held over the loop
+        const int r = row0 + (lane & 31);
+        const bool there = r < rows;
+        const int i = (there ? r : rows - 1) / a.group;
+        const int token = sg.q0 + i, head = kvh * a.group + (there ? r : rows - 1) - i * a.group;
+        const int shift = sg.nk - sg.nq;
 
-    op8<T> q[KT];
-    {
-        const T* p = static_cast<const T*>(a.q) + (int64_t)token * a.q_row + (int64_t)head * a.q_head;
+        op8<T> q[KT];
+        {
+            const T* p = static_cast<const T*>(a.q) + (int64_t)token * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            const int c = 16 * t + 8 * h;
-            if (c < a.dim) q[t] = *reinterpret_cast<const op8<T>*>(p + c);
-            else q[t] = op8<T>{};
-        }
-    }
-    int klo, khi, lo, hi, alo, ahi;
-    admitted(a, sg.nk, i + shift, i + shift, klo, khi);
-    const int last = min(row0 + kFewRows, rows) - 1;
-    admitted(a, sg.nk, row0 / a.group + shift, last / a.group + shift, lo, hi);
-    admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
-    const int j0 = max(lo / 32 * 32, split * per), j1 = min(hi, (split + 1) * per);
-    if (j0 >= j1 && split > 0) {                           // the window leaves nothing of this part
-        if (wave == 0 && there) store_sums(f, true, token, head, split, -INFINITY, 0.0f);
-        continue;
-    }
-    constexpr int STEP = GS_WAVE / PIECES;
-    RowBuffer<T> kb, vb;
-    kb.init(static_cast<const T*>(a.k) + sg.k0 * a.k_row + kvh * a.k_head, sg.nk, a.k_row);
-    vb.init(static_cast<const T*>(a.v) + sg.k0 * a.v_row + kvh * a.v_head, sg.nk, a.v_row);
-    const int koff = (lane & 31) * kb.ld + 16 * h;
-    const int voff = 8 * (lane % PIECES) < a.dim ? lane / PIECES * vb.ld + 16 * (lane % PIECES) : vb.kOutside;
-    const uint8_t* const flags = a.key_on + sg.k0;
-    op8<T> kp[KT], vp[LOADS];
-    uint8_t flag = 1;                                      // of key lane & 31 of the step
-    auto fetch = [&](int j) {
-        if (a.key_on != nullptr) flag = key_flag(flags, j + (fresh(lane) & 31), sg.nk);
-        const int ka = koff + kb.place(j), va = vb.place(j);
-#pragma unroll
-        for (int t = 0; t < KT; ++t) kp[t] = kb.piece(16 * t + 8 * h < a.dim ? ka + 32 * t : kb.kOutside);
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) vp[u] = vb.piece(voff + (va + u * STEP * vb.ld));
-    };
-
-    const float c = a.scale * kLog2e, slack = held(c);
-    float m = -INFINITY, l = 0.0f;
-    acc16 o[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = acc16{};
-    Lanes at;
-    at.init<P>();
-    T* const mine = vs[wave];
-    int j = j0 + 32 * wave;
-    fetch(j < j1 ? j : sg.nk);
-    for (; j < j1; j += 32 * WAVES) {
-        at.refresh();
-        acc16 s[1];
-        s[0] = acc16{};
-#pragma unroll
-        for (int t = 0; t < KT; ++t) s[0] = mfma(kp[t], q[t], s[0]);
-        uint32_t on = ~0u;
-        if (a.key_on != nullptr) {
-            on = (uint32_t)__ballot(flag);
-            // the values of a key that is off may be anything, and a
-            // probability of 0 does not stop a NaN
-#pragma unroll
-            for (int u = 0; u < LOADS; ++u)
-                if (((on >> (u * STEP + fresh(lane) / PIECES)) & 1) == 0) vp[u] = op8<T>{};
-        }
-#pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int x = lane + u * GS_WAVE;
-            *reinterpret_cast<op8<T>*>(mine + piece_at<P>(x / PIECES, x % PIECES)) = vp[u];
-        }
-        if (a.key_on != nullptr || j < alo || j + 32 > ahi)
-            keep_some(s[0], (uint32_t)bits_between(klo - j, khi - j) & on);
-        // behind the part's end: from past the segment's, which reads nothing
-        // (a condition on the loads would keep both outcomes' registers)
-        fetch(j + 32 * WAVES < j1 ? j + 32 * WAVES : sg.nk);
-        float alpha;
-        if (softmax_step<1>(s, c, slack, m, l, alpha)) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= alpha;
-        }
-        // this wave's values are in LDS before any of its lanes reads them
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const op8<T> p = tile_operand<T>(s[0], u);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                o[d] = mfma(columns_operand<T, P>(mine, at, 16 * u, d), p, o[d]);
-                if (d & 1) __builtin_amdgcn_sched_barrier(0);      // no operands further ahead: two waves a SIMD
+            for (int t = 0; t < KT; ++t) {
+                const int c = 16 * t + 8 * h;
+                if (c < a.dim) q[t] = *reinterpret_cast<const op8<T>*>(p + c);
+                else q[t] = op8<T>{};
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-    // the waves meet: the largest maximum, every sum and tile against it
-    l = half_sum(l);
-    const int me = fresh(lane_id()), column = me & 31;
-    if (me < 32) {
-        ml[0][wave][me] = m;
-        ml[1][wave][me] = l;
-    }
-    __syncthreads();
-    float top = -INFINITY, sum = 0.0f;
+        int klo, khi, lo, hi, alo, ahi;
+        admitted(a, sg.nk, i + shift, i + shift, klo, khi);
+        const int last = min(row0 + kFewRows, rows) - 1;
+        admitted(a, sg.nk, row0 / a.group + shift, last / a.group + shift, lo, hi);
+        admitted(a, sg.nk, last / a.group + shift, row0 / a.group + shift, alo, ahi);
+        const int j0 = max(lo / 32 * 32, split * per), j1 = min(hi, (split + 1) * per);
+        if (j0 >= j1 && split > 0) {                           // the window leaves nothing of this part
+            if (wave == 0 && there) store_sums(f, true, token, head, split, -INFINITY, 0.0f);
+            continue;
+        }
+        constexpr int STEP = GS_WAVE / PIECES;
+        RowBuffer<T> kb, vb;
+        kb.init(static_cast<const T*>(a.k) + sg.k0 * a.k_row + kvh * a.k_head, sg.nk, a.k_row);
+        vb.init(static_cast<const T*>(a.v) + sg.k0 * a.v_row + kvh * a.v_head, sg.nk, a.v_row);
+        const int koff = (lane & 31) * kb.ld + 16 * h;
+        const int voff = 8 * (lane % PIECES) < a.dim ? lane / PIECES * vb.ld + 16 * (lane % PIECES) : vb.kOutside;
+        const uint8_t* const flags = a.key_on + sg.k0;
+        op8<T> kp[KT], vp[LOADS];
+        uint8_t flag = 1;                                      // of key lane & 31 of the step
+        auto fetch = [&](int j) {
+            if (a.key_on != nullptr) flag = key_flag(flags, j + (fresh(lane) & 31), sg.nk);
+            const int ka = koff + kb.place(j), va = vb.place(j);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[0][w][column]);
-    const float base = top == -INFINITY ? 0.0f : top * c;
+            for (int t = 0; t < KT; ++t) kp[t] = kb.piece(16 * t + 8 * h < a.dim ? ka + 32 * t : kb.kOutside);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w)
-        sum = fmaf(ml[1][w][column], __builtin_amdgcn_exp2f(fmaf(ml[0][w][column], c, -base)), sum);
-    const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+            for (int u = 0; u < LOADS; ++u) vp[u] = vb.piece(voff + (va + u * STEP * vb.ld));
+        };
+
+        const float c = a.scale * kLog2e, slack = held(c);
+        float m = -INFINITY, l = 0.0f;
+        acc16 o[DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
+        for (int d = 0; d < DT; ++d) o[d] = acc16{};
+        Lanes at;
+        at.init<P>();
+        T* const mine = vs[wave];
+        int j = j0 + 32 * wave;
+        fetch(j < j1 ? j : sg.nk);
+        for (; j < j1; j += 32 * WAVES) {
+            at.refresh();
+            acc16 s[1];
+            s[0] = acc16{};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) tile[wave][e * GS_WAVE + me] = o[d][e] * alpha;
-        __syncthreads();
-        if (wave == d % WAVES && there) {
-            acc16 v;
+            for (int t = 0; t < KT; ++t) s[0] = mfma(kp[t], q[t], s[0]);
+            uint32_t on = ~0u;
+            if (a.key_on != nullptr) {
+                on = (uint32_t)__ballot(flag);
+                // the values of a key that is off may be anything, and a
+                // probability of 0 does not stop a NaN
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                v[e] = tile[0][e * GS_WAVE + me];
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w) v[e] += tile[w][e * GS_WAVE + me];
+                for (int u = 0; u < LOADS; ++u)
+                    if (((on >> (u * STEP + fresh(lane) / PIECES)) & 1) == 0) vp[u] = op8<T>{};
             }
-            store_tile<T>(f, parts > 1, token, head, split, d, v, sum);
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                const int x = lane + u * GS_WAVE;
+                *reinterpret_cast<op8<T>*>(mine + piece_at<P>(x / PIECES, x % PIECES)) = vp[u];
+            }
+            if (a.key_on != nullptr || j < alo || j + 32 > ahi)
+                keep_some(s[0], (uint32_t)bits_between(klo - j, khi - j) & on);
+            // behind the part's end: from past the segment's, which reads nothing
+            // (a condition on the loads would keep both outcomes' registers)
+            fetch(j + 32 * WAVES < j1 ? j + 32 * WAVES : sg.nk);
+            float alpha;
+            if (softmax_step<1>(s, c, slack, m, l, alpha)) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] *= alpha;
+            }
+            // this wave's values are in LDS before any of its lanes reads them
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const op8<T> p = tile_operand<T>(s[0], u);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    o[d] = mfma(columns_operand<T, P>(mine, at, 16 * u, d), p, o[d]);
+                    if (d & 1) __builtin_amdgcn_sched_barrier(0);      // no operands further ahead: two waves a SIMD
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        // the waves meet: the largest maximum, every sum and tile against it
+        l = half_sum(l);
+        const int me = fresh(lane_id()), column = me & 31;
+        if (me < 32) {
+            ml[0][wave][me] = m;
+            ml[1][wave][me] = l;
         }
         __syncthreads();
-    }
-    if (wave == 0 && there) store_sums(f, parts > 1, token, head, split, top, sum);
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ml[0][w][column]);
+        const float base = top == -INFINITY ? 0.0f : top * c;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+            sum = fmaf(ml[1][w][column], __builtin_amdgcn_exp2f(fmaf(ml[0][w][column], c, -base)), sum);
+        const float alpha = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) tile[wave][e * GS_WAVE + me] = o[d][e] * alpha;
+            __syncthreads();
+            if (wave == d % WAVES && there) {
+                acc16 v;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    v[e] = tile[0][e * GS_WAVE + me];
+#pragma unroll
+                    for (int w = 1; w < WAVES; ++w) v[e] += tile[w][e * GS_WAVE + me];
+                }
+                store_tile<T>(f, parts > 1, token, head, split, d, v, sum);
+            }
+            __syncthreads();
+        }
+        if (wave == 0 && there) store_sums(f, parts > 1, token, head, split, top, sum);
     }
 }
 
 // Joins the parts of a row (at most kMaxSplits): lanes take the parts' maxima
-// and sums together, then two elements each and the parts in turn.  Four waves
-// share 64 parts, so that a wave's 16 tiles are all on their way at once; rows
-// that all have more parts take 16 waves.
+// and sums together, then two elements each and the parts in turn, 8 or 16 tiles
+// of a wave on their way at once.  Bound by the latency of these two reads, one
+// behind the other.  A wave a row where there are up to 8 parts on average (24
+// segments, 16 heads of 64: the call 83.2 us, 84.9 with four waves), four up to
+// 64 (64 parts of 16 rows of 128: 4.2 us), 16 beyond (256 parts: the call 19.4 us,
+// 20.0 with four).
 constexpr int kMaxSplits = 256;
 
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(WAVES == 1 ? GS_BLOCK : WAVES * GS_WAVE) k_attention_join(FwdArgs f) {
-    constexpr int N = WAVES == 1 ? 1 : kMaxSplits / GS_WAVE, GROUPS = WAVES == 1 ? 1 : WAVES / 4;
+    constexpr int N = kMaxSplits / GS_WAVE, GROUPS = WAVES == 1 ? 1 : WAVES / 4;
     constexpr int EACH = WAVES == 1 ? 8 : 16, STEP = WAVES == 1 ? 1 : 4;
     __shared__ float2 got[WAVES][GS_WAVE];
     const int64_t rows = (int64_t)f.a.n_q * f.a.heads;
@@ -493,18 +506,22 @@ __global__ void __launch_bounds__(WAVES == 1 ? GS_BLOCK : WAVES * GS_WAVE) k_att
         if (n * GS_WAVE >= parts || n % GROUPS != wave / 4) continue;
         // a part that found no keys may have written no tile
         const uint64_t wrote = __ballot(part[n].y != 0.0f);
-        float2 v[EACH];
+#pragma unroll 1
+        for (int first = 0; first < min(parts - n * GS_WAVE, GS_WAVE); first += EACH * STEP) {
+            float2 v[EACH];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            v[i] = make_float2(0.0f, 0.0f);
-            const int s = wave % 4 + STEP * i;
-            if ((wrote >> s) & 1) v[i] = *reinterpret_cast<const float2*>(p + (n * GS_WAVE + s) * step);
-        }
+            for (int i = 0; i < EACH; ++i) {
+                v[i] = make_float2(0.0f, 0.0f);
+                const int s = first + wave % 4 + STEP * i;
+                if ((wrote >> s) & 1) v[i] = *reinterpret_cast<const float2*>(p + (n * GS_WAVE + s) * step);
+            }
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[n]), wave % 4 + STEP * i));
-            o.x = fmaf(v[i].x, ws, o.x);
-            o.y = fmaf(v[i].y, ws, o.y);
+            for (int i = 0; i < EACH; ++i) {
+                const int s = first + wave % 4 + STEP * i;
+                const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w[n]), s));
+                o.x = fmaf(v[i].x, ws, o.x);
+                o.y = fmaf(v[i].y, ws, o.y);
+            }
         }
     }
     if (WAVES > 1) {
@@ -552,7 +569,8 @@ Plan plan(const gs_attn& a) {
         const bool equal = a.cu_q == nullptr || a.n_seg == 1;
         const int64_t longest = equal ? keys : a.n_k;      // as far as it is known here
         const int64_t want = kUnits * (a.dim <= 64 ? 3 : 1);
-        const int64_t room = std::max<int64_t>(1, (64 << 20) / (std::max<int64_t>(1, (int64_t)a.n_q * a.heads) * a.dim * 4));
+        const int64_t part = std::max<int64_t>(1, (int64_t)a.n_q * a.heads) * a.dim * 4;
+        const int64_t room = std::max<int64_t>(1, (64 << 20) / part);
         const int64_t most = std::min<int64_t>(kMaxSplits, room);
         int64_t chunk = std::max<int64_t>({kPartFew, (int64_t)a.n_k * a.kv_heads / want, (longest + most - 1) / most});
         chunk = (chunk + 127) / 128 * 128;
@@ -574,9 +592,14 @@ hipError_t go(const FwdArgs& f, bool few, hipStream_t st) {
     if (few) k_attention_few<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
     else k_attention<T, D><<<grid, GS_BLOCK, 0, st>>>(f);
     const uint64_t rows = (uint64_t)f.a.n_q * f.a.heads;
-    if (f.splits > 64 && (f.chunk == 0 || f.a.n_seg == 1)) k_attention_join<T, 16><<<(uint32_t)rows, 16 * GS_WAVE, 0, st>>>(f);
-    else if (f.splits > 8) k_attention_join<T, 4><<<(uint32_t)rows, GS_BLOCK, 0, st>>>(f);
-    else if (f.splits > 1) k_attention_join<T, 1><<<div_up(rows, 4), GS_BLOCK, 0, st>>>(f);
+    if (f.splits > 1) {
+        // parts of a row: all have `splits`, or the mean of the segments
+        const bool equal = f.chunk == 0 || f.a.n_seg == 1;
+        const int parts = equal ? f.splits : (f.a.n_k / f.a.n_seg + f.chunk - 1) / f.chunk;
+        if (parts <= 8) k_attention_join<T, 1><<<div_up(rows, 4), GS_BLOCK, 0, st>>>(f);
+        else if (parts <= 64) k_attention_join<T, 4><<<(uint32_t)rows, GS_BLOCK, 0, st>>>(f);
+        else k_attention_join<T, 16><<<(uint32_t)rows, 16 * GS_WAVE, 0, st>>>(f);
+    }
     return hipGetLastError();
 }
 
@@ -609,7 +632,8 @@ hipError_t launch_attention(const gs_attn& a, const gs_rows& out, float* lse, vo
     f.splits = p.splits;
     f.chunk = p.chunk;
     f.part_ml = static_cast<float2*>(ws);
-    f.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * p.splits * sizeof(float2)));
+    const size_t sums = align256((size_t)a.n_q * a.heads * p.splits * sizeof(float2));
+    f.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + sums);
     return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, p.few, st) : by_dim<f16_t>(f, p.few, st);
 }
 

@@ -21,6 +21,8 @@ namespace {
 // columns are taken by the lanes that own one block of GS_NORM_BLOCK columns (16
 // or 32), several to a wave: 74,724 fp32 rows of 80 columns into 8 bits took 47
 // us with a wave each, whose lanes were two thirds idle, and take 17 so.
+//   50,001 bf16 rows of 1536 with a residual into 8 bits and scales: 96 us, 5.6
+// TB/s.  7 rows of 1024: 2.6 us, the start of a kernel and one read.
 // ---------------------------------------------------------------------------
 
 template <int TPR>
@@ -209,7 +211,8 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rms_norm(gs_norm_args a) {
 // total r, one read of dy, total and dtotal.  Every workgroup walks rows in
 // steps of the grid and keeps dy n of its columns in registers; it writes one
 // row of partial sums, and k_norm_dweight adds those in ascending order.
-// PARTS rows of partial sums in ws: the grid, set by kNormParts.
+// Bound by HBM bytes: 20,000 fp32 rows of 768: 51 us with the weight's sums, 4.9
+// TB/s; 60,000 bf16 rows of 1160: 106 us, 5.2 TB/s.
 constexpr int kNormParts = 512;                // two workgroups a compute unit
 
 inline int norm_parts(int32_t rows, int rpb) {
@@ -310,7 +313,8 @@ __global__ void __launch_bounds__(TPR > GS_BLOCK ? TPR : GS_BLOCK) k_rms_norm_bw
 }
 
 // Sum of the partial rows, a column each: 64 columns by 16 slices of the rows
-// in a workgroup, then the slices in ascending order.
+// in a workgroup, then the slices in ascending order.  Latency: 512 parts of 768
+// columns 4.4 us.
 __global__ void __launch_bounds__(1024) k_norm_dweight(const float* __restrict__ parts, int n, int cols,
                                                        float* __restrict__ dweight) {
     __shared__ float sum[16][GS_WAVE];
@@ -391,7 +395,9 @@ hipError_t norm_bwd_type(const gs_norm_bwd_args& a, float* parts, hipStream_t st
 // product, one reduction and one sincos a pair) go to LDS once and serve every
 // head of both tensors; then each thread turns V pairs at a time, which are
 // two V-element pieces of the head in either layout, and copies what is left
-// of the heads.
+// of the heads.  50,000 fp32 tokens, 8 + 8 heads of 64, three quarters turned by
+// three axes: 97 us, 4.2 TB/s; 32,768 bf16 tokens, 32 + 8 heads of 128: 132 us,
+// 5.1 TB/s.  Two and four pieces of a thread in flight took as long.
 // ---------------------------------------------------------------------------
 
 constexpr int kRotTrig = 2048;                 // pairs of a workgroup's tokens in LDS (16 KB)
