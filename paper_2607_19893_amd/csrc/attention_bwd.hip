@@ -28,7 +28,7 @@ struct BwdArgs {
     int64_t o_row, o_head, do_row, do_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
     const float* lse;
     float* base;                           // [heads][n_q]: the rows' log sums in powers of two
-    float* delta;                          // [heads][n_q], behind base
+    float* delta;                          // [heads][n_q], behind base: -delta, where dout . v starts from
     int32_t key_tiles;
     int32_t splits;                        // most parts that a key tile's rows are cut into
     int32_t chunk;                         // steps of a part (about)
@@ -106,8 +106,12 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     delta = both.x + both.y;
     if (there && h == 0) {
         f.base[(int64_t)head * a.n_q + token] = base;
-        f.delta[(int64_t)head * a.n_q + token] = delta;
+        f.delta[(int64_t)head * a.n_q + token] = -delta;
     }
+
+    acc16 minus_delta;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) minus_delta[e] = -delta;
 
     int klo, khi, lo, hi, alo, ahi;
     admitted(a, sg.nk, i + shift, i + shift, klo, khi);
@@ -149,7 +153,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
             // operands are read one product ahead of their use; the barriers keep
             // the compiler from reading more of them ahead, which would not fit
             // the registers of two waves a SIMD
-            acc16 s{}, dp{};
+            acc16 s{}, dp = minus_delta;
             if (KEYS) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -175,7 +179,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
             }
             if (test) keep_some(s, (uint32_t)(seen >> (32 * k)));
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -base)) * (dp[e] - delta);
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -base)) * dp[e];
             op8<T> z[2], ds;
             z[0] = columns_operand<T, P>(ks, at, 32 * k, 0);
 #pragma unroll
@@ -243,7 +247,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     constexpr int ST = dkv_step(D), NK = ST / 32;
     __shared__ __attribute__((aligned(16))) T qs0[ST * P], ds0[ST * P];
     __shared__ __attribute__((aligned(16))) T qs1[ST * P], ds1[ST * P];
-    __shared__ __attribute__((aligned(16))) float st0[2 * 64], st1[2 * 64];            // bases, then deltas
+    __shared__ __attribute__((aligned(16))) float st0[2 * 64], st1[2 * 64];            // bases, then -deltas
     __shared__ __attribute__((aligned(16))) T vs[BIG ? kRows * P : 8];
     const AttnArgs& a = f.a;
     const Place place = chiplet_place<true>(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
@@ -343,7 +347,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
         const bool test = t < alo || t + ST > ahi;
         uint64_t seen = ~0ull;
         if (test) seen = bits_between(ilo - t, ihi - t);
-        acc16 s[NK]{}, dp[NK]{};
+        acc16 s[NK]{}, dp[NK];
         // operands are read one product ahead of their use; the barriers keep
         // the compiler from reading more of them ahead, which would not fit the
         // registers of two waves a SIMD
@@ -354,6 +358,14 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
                 y[e & 1] = rows_operand<T, P>(ds, at, 32 * k, e);
                 z[e & 1] = BIG ? rows_operand<T, P>(vs, at, 32 * wave, e) : vf[BIG ? 0 : e];
             };
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {          // dout . v starts from -delta
+                const float4 d = *reinterpret_cast<const float4*>(st + 64 + 32 * k + 8 * g + 4 * h);
+                dp[k][4 * g] = d.x;
+                dp[k][4 * g + 1] = d.y;
+                dp[k][4 * g + 2] = d.z;
+                dp[k][4 * g + 3] = d.w;
+            }
             read(0);
 #pragma unroll
             for (int e = 0; e < KT; ++e) {
@@ -367,14 +379,12 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
             if (test) keep_some(s[k], (uint32_t)(seen >> (32 * k)));
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int first = 32 * k + 8 * g + 4 * h;
-                const float4 b = *reinterpret_cast<const float4*>(st + first);
-                const float4 d = *reinterpret_cast<const float4*>(st + 64 + first);
-                const float bs[4] = {b.x, b.y, b.z, b.w}, dl[4] = {d.x, d.y, d.z, d.w};
+                const float4 b = *reinterpret_cast<const float4*>(st + 32 * k + 8 * g + 4 * h);
+                const float bs[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[k][4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[k][4 * g + e], c, -bs[e]));
-                    dp[k][4 * g + e] = s[k][4 * g + e] * (dp[k][4 * g + e] - dl[e]);
+                    dp[k][4 * g + e] *= s[k][4 * g + e];
                 }
             }
         };
