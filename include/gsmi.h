@@ -782,7 +782,8 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  *     the nearest in it; rows outside every segment are not written.
  *   q [n_q, heads, dim], k, v [n_k, kv_heads, dim]; GS_BF16 or GS_F16; pointers
  *     16-byte aligned, strides and dim multiples of 8 elements, dim <= 128, row
- *     strides from dim to GS_ATTN_MAX_STRIDE elements.  key_on [n_k] uint8.
+ *     strides from dim to GS_ATTN_MAX_STRIDE elements (of a single row: any).
+ *     key_on [n_k] uint8.
  *   out: as q; lse [n_q, heads] fp32, dense
  *   ws: gs_attention_ws_bytes(a, 0) bytes (can be 0: ws may be NULL), 16-byte
  *     aligned.  The size follows from the sizes in `a`, not from cu_*'s values.

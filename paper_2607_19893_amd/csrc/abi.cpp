@@ -663,7 +663,7 @@ static gs_status check_attn_rows(const gs_rows& r, int32_t rows, int32_t dim, co
                "%s: row stride %lld of %s outside dim..%d", what, (long long)r.ld_row, name, GS_ATTN_MAX_STRIDE);
     GS_REQUIRE(r.ptr != nullptr, "%s: null %s", what, name);
     GS_REQUIRE(aligned(r.ptr, 16), "%s: %s must be 16-byte aligned", what, name);
-    GS_REQUIRE(r.ld_row % 8 == 0 && r.ld_head % 8 == 0, "%s: strides of %s must be multiples of 8 elements", what, name);
+    GS_REQUIRE((rows == 1 || r.ld_row % 8 == 0) && r.ld_head % 8 == 0, "%s: strides of %s must be multiples of 8 elements", what, name);
     return GS_OK;
 }
 

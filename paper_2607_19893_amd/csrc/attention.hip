@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
 #pragma unroll
             for (int t = 0; t < KT; ++t) kp[t] = kb.piece(16 * t + 8 * h < a.dim ? ka + 32 * t : kb.kOutside);
 #pragma unroll
-            for (int u = 0; u < LOADS; ++u) vp[u] = vb.piece(voff + (va + u * STEP * vb.ld));
+            for (int u = 0; u < LOADS; ++u) vp[u] = vb.piece((int)((uint32_t)voff + (uint32_t)(va + u * STEP * vb.ld)));
         };
 
         const float c = a.scale * kLog2e, slack = held(c);

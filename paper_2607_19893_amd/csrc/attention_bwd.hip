@@ -559,7 +559,7 @@ hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* 
     f.o_row = g.out.ld_row;
     f.o_head = g.out.ld_head;
     f.dout = g.dout.ptr;
-    f.do_row = g.dout.ld_row;
+    f.do_row = row_stride(g.dout, a.n_q, a.dim);
     f.do_head = g.dout.ld_head;
     f.dq = g.dq.ptr;
     f.dq_row = g.dq.ld_row;

@@ -209,7 +209,8 @@ struct TileLoader {
         const int at = buf.place(row);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            const int place = off + (at + u * STEP * buf.ld);      // past the range also where `off` is
+            // past the range also where `off` is; below 2^32, so the sum is one of unsigned numbers
+            const int place = (int)((uint32_t)off + (uint32_t)(at + u * STEP * buf.ld));
             buf.piece_to(tile + (u * GS_BLOCK + wave * GS_WAVE) * 8, (skip >> u) & 1 ? buf.kOutside : place);
         }
     }
@@ -267,16 +268,20 @@ struct AttnArgs {
     int32_t tiles;             // workgroups' tiles per key head
 };
 
+// Row stride of a tensor of n rows.  The only row of one has no next: any value
+// may stand there, and RowBuffer takes a row's bytes from it.
+inline int64_t row_stride(const gs_rows& r, int32_t n, int32_t dim) { return n == 1 ? dim : r.ld_row; }
+
 inline AttnArgs attn_args(const gs_attn& a) {
     AttnArgs r;
     r.q = a.q.ptr;
     r.k = a.k.ptr;
     r.v = a.v.ptr;
-    r.q_row = a.q.ld_row;
+    r.q_row = row_stride(a.q, a.n_q, a.dim);
     r.q_head = a.q.ld_head;
-    r.k_row = a.k.ld_row;
+    r.k_row = row_stride(a.k, a.n_k, a.dim);
     r.k_head = a.k.ld_head;
-    r.v_row = a.v.ld_row;
+    r.v_row = row_stride(a.v, a.n_k, a.dim);
     r.v_head = a.v.ld_head;
     r.cu_q = a.cu_q;
     r.cu_k = a.cu_k;

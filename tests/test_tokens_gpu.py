@@ -365,6 +365,26 @@ def test_attention_layouts(tk):
             within(a, b, e, what)
 
 
+@pytest.mark.parametrize("stride", [0, 8, 260, 1 << 30, 1 << 31])
+@pytest.mark.parametrize("nq,nk", [(1, 1), (1, 300), (50, 1), (300, 1)])
+def test_attention_of_a_single_row_with_any_row_stride(tk, nq, nk, stride):
+    """A tensor of one row may carry any row stride: it has no next row."""
+    c = case([nq], [nk], 4, 2, dim=64)
+    g, q, k, v, _ = inputs(c)
+    dout = randn(g, *q.shape, dtype=BF)
+
+    def odd(t):
+        return t.as_strided(t.shape, (stride, 64, 1)) if t.shape[0] == 1 else t
+
+    kw = dict(scale=c["scale"])
+    out, lse = tk.attention(odd(q), odd(k), odd(v), **kw)
+    check_forward((out, lse), ref.attention(q, k, v, c))
+    got = tk.attention_backward(odd(dout), odd(q), odd(k), odd(v), odd(out), lse, **kw)
+    want, bounds = ref.attention(q, k, v, c, None, lse, out, dout)
+    for a, b, e, what in zip(got, want, bounds, ("dq", "dk", "dv")):
+        within(a, b, e, what)
+
+
 @pytest.mark.parametrize("nq,nk", [([40, 200], [90, 70]), ([2, 1], [900, 1300])])
 def test_nan_in_places_that_nothing_admits(tk, nq, nk):
     """Keys that are off, rows that admit no key, and what lies beside the segments."""
