@@ -723,8 +723,8 @@ gs_status gs_rms_norm_bwd(const gs_norm_bwd_args* args, void* ws, size_t ws_byte
  * 0.004 at position 65536), its sine and cosine in fp32.
  * Errors: GS_ERR_INVALID_ARG (null pointers, negative sizes, pairs against dim
  * or axis_pairs, misaligned elements, an amplitude that is not finite);
- * GS_ERR_UNSUPPORTED for dim above GS_ROTARY_MAX_DIM or more than 2^31 - 1
- * rows of heads.
+ * GS_ERR_UNSUPPORTED for dim above GS_ROTARY_MAX_DIM, more than 2^31 - 1 rows
+ * of heads or 2^30 elements a token.
  */
 #define GS_ROTARY_MAX_DIM 512
 
@@ -792,8 +792,9 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  * order that the sizes alone fix: the same call gives the same bits.
  * Errors: GS_ERR_INVALID_ARG (null pointers, sizes, alignment, one of cu_q and
  * cu_k without the other, a scale that is not a positive finite number, dtype);
- * GS_ERR_UNSUPPORTED (dim above 128, n_q * heads or n_k * kv_heads above
- * 2^31 - 1); GS_ERR_WORKSPACE.
+ * GS_ERR_UNSUPPORTED (dim above 128, n_q * heads or n_k * kv_heads above 2^30,
+ * or these over 128 and n_seg * kv_heads together near 2^24 tiles);
+ * GS_ERR_WORKSPACE.
  */
 #define GS_ATTN_MAX_DIM 128
 #define GS_ATTN_MAX_STRIDE 8388608

@@ -614,6 +614,8 @@ gs_status gs_rotary(const gs_rotary_args* a, void* stream) {
     for (int i = 0; i < a->n_tensors; ++i) {
         GS_REQUIRE(a->heads[i] >= 0, "%s: negative heads", what);
         rows += (int64_t)a->heads[i] * a->tokens;
+        if ((int64_t)a->heads[i] * a->dim > 1 << 30)
+            return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^30 elements a token", what);
         if (a->heads[i] == 0 || a->tokens == 0) continue;
         for (const gs_rows* r : {&a->in[i], &a->out[i]}) {
             GS_REQUIRE(r->ptr != nullptr && aligned(r->ptr, es), "%s: null or misaligned tensor %d", what, i);
@@ -680,9 +682,14 @@ static gs_status check_attn(const gs_attn* a, const char* what) {
     GS_REQUIRE(aligned(a->cu_q, 4) && aligned(a->cu_k, 4), "%s: cu_q or cu_k misaligned", what);
     GS_REQUIRE(a->cu_q != nullptr || (a->n_q % a->n_seg == 0 && a->n_k % a->n_seg == 0),
                "%s: %d segments of equal length do not divide %d rows and %d keys", what, a->n_seg, a->n_q, a->n_k);
-    if ((int64_t)a->n_q * a->heads > 0x7FFFFFFF || (int64_t)a->n_k * a->kv_heads > 0x7FFFFFFF ||
-        a->n_seg > (1 << 24))
-        return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows of heads or 2^24 segments", what);
+    // The kernels' places of rows and keys are 32-bit numbers that run up to a
+    // tile or a part past the end, and a launch holds fewer than 2^24 workgroups.
+    const int64_t rows = std::max((int64_t)a->n_q * a->heads, (int64_t)a->n_k * a->kv_heads);
+    if (rows > 1 << 30)
+        return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^30 rows of heads (places have to stay below 2^31)", what);
+    if (rows / 128 + ((int64_t)a->n_seg + 8) * a->kv_heads >= 1 << 24)
+        return fail(GS_ERR_UNSUPPORTED, "%s: %d segments of %d key heads are more than 2^24 tiles", what, a->n_seg,
+                    a->kv_heads);
     gs_status s;
     if ((s = check_attn_rows(a->q, a->n_q, a->dim, "q", what)) != GS_OK) return s;
     if ((s = check_attn_rows(a->k, a->n_k, a->dim, "k", what)) != GS_OK) return s;

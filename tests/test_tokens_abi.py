@@ -131,6 +131,21 @@ def test_attention_arguments(gs):
     assert gs.gs_attention_ws_bytes(attn(gs, kv_heads=0)) == 0
 
 
+def test_attention_sizes_that_no_launch_holds(gs):
+    """Places near 2^31, and more tiles than a launch has workgroups (128 key heads of 2^25 segments wrap a 32-bit grid)."""
+    L = gs.raw()
+    out, g = gs.gs_rows(256, 128, 64), gs.gs_attn_grads(*[gs.gs_rows(256, 128, 64)] * 5, 256)
+    for word, kw in (("2^30", dict(n_k=(1 << 30) + 1, heads=1, kv_heads=1)), ("2^30", dict(n_k=0x7FFFFFFF, heads=1, kv_heads=1)),
+                     ("2^30", dict(n_q=(1 << 29) + 1)), ("tiles", dict(n_seg=1 << 25, cu_q=256, cu_k=256)),
+                     ("tiles", dict(n_seg=1 << 18, heads=128, kv_heads=128, cu_q=256, cu_k=256)),
+                     ("tiles", dict(n_seg=0x7FFFFFFF, heads=256, kv_heads=256, cu_q=256, cu_k=256))):
+        a = attn(gs, **kw)
+        refused(gs, L.gs_attention(ctypes.byref(a), ctypes.byref(out), 256, 256, 1 << 62, None), word, gs.GS_ERR_UNSUPPORTED)
+        refused(gs, L.gs_attention_bwd(ctypes.byref(a), ctypes.byref(g), 256, 1 << 62, None), word, gs.GS_ERR_UNSUPPORTED)
+    a = rotary_args(gs, heads=1 << 25)
+    refused(gs, L.gs_rotary(ctypes.byref(a), None), "2^30", gs.GS_ERR_UNSUPPORTED)
+
+
 def test_frequencies(gs):
     for pairs, base in ((1, 10000.0), (32, 10000.0), (64, 500000.0)):
         plain = base ** -(np.arange(pairs) / pairs)
