@@ -1,0 +1,66 @@
+"""The token operators at the ends of their numbers' ranges and of their layouts: tiny and special rows of the 8-bit
+norm, rows outside every segment, large scores, heads and rows whose strides mean nothing, very many rows."""
+import math
+
+import pytest
+import torch
+
+import token_refs as ref
+from test_tokens_gpu import BF, F32, HF, case, cu, gen, gs, inputs, randn, tk, within  # noqa: F401 (gs, tk: fixtures)
+
+pytestmark = pytest.mark.gpu
+LEAST = 2.0 ** -126                                    # least scale of a block
+
+
+def check_8bit(e, y):
+    """q and scale against y in double: the scale is max|y| / 448, at least 2^-126, 1 for zeros; q the nearest."""
+    rows, cols = y.shape
+    top = torch.stack([b.abs().amax(1) for b in y.split(128, 1)], 1)
+    want = torch.where(top > 0, (top / 448).clamp(min=LEAST), torch.ones_like(top))
+    # fp32: the squares' sum, root, reciprocal and two products
+    within(e.scale, want, (cols / 64 + 40) * 2.0 ** -24 * want, "scale")
+    v = y / e.scale.double()[:, torch.arange(cols, device="cuda") // 128]
+    step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3)
+    # half a step, and the scale's and the norm's own roundings (a few 2^-24 of v each)
+    within(e.q.float(), v, step * 0.5 * (1 + 1e-3) + 1e-4 * v.abs(), "q")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("weights", ["ones", "some", "tiny block"])
+def test_norm_8bit_of_tiny_values(tk, dtype, weights):
+    """Values whose quotient 448 / max|s w| or 1 / scale is past the largest fp32 number."""
+    g = gen(21)
+    cols = 300
+    x = randn(g, 8, cols)
+    x[0] *= 1e-37
+    x[1] *= 0.1
+    x[1, 128:256] *= 1e-39
+    x[1, 140:150] = 0.0
+    x[1, 256:] *= 1e-37
+    x[2] *= 1e-30
+    x[3] *= 1e-41
+    x[4] *= 1e-3
+    x[4, 128:256] *= 2e-35
+    x[5] *= 1e15
+    x[5, 128:256] *= 1e-53
+    x[6, 128:] = 0.0
+    x[7] *= 1e-37
+    x[7, 1:] = 0.0
+    x = x.to(dtype)
+    w = torch.ones(cols, device="cuda")
+    if weights != "ones":
+        w = 1 + 0.2 * randn(g, cols)
+    if weights == "tiny block":
+        w[128:256] *= 1e-37
+    for res in (None, x.flip(1).contiguous()):
+        y, _ = ref.norm(x, w, 1e-6, res)
+        check_8bit(tk.rms_norm(x, w, 1e-6, residual=res, eight_bit=True), y)
+
+
+def test_norm_8bit_without_eps(tk):
+    """Nothing added to the squares' mean: rows of any size give the same quotients."""
+    g = gen(22)
+    x = randn(g, 5, 200) * torch.tensor([1e-17, 1e-10, 1.0, 1e10, 1e17], device="cuda")[:, None]
+    w = 1 + 0.2 * randn(g, 200)
+    y, _ = ref.norm(x, w, 0.0)
+    check_8bit(tk.rms_norm(x, w, 0.0, eight_bit=True), y)
