@@ -654,8 +654,11 @@ typedef struct {
  *     mantissa bits, largest 448), in blocks of GS_NORM_BLOCK columns (the last
  *     may be shorter), each with its scale: y ~ scale * q, ties to even.
  *   q_scale [rows, ld_scale] fp32 (with q): max|y| of the block / 448, at least
- *     2^-126; 1 for a block of zeros.  A NaN becomes a NaN of q and does not
- *     touch the scale; an infinity makes the scale infinite and q NaN.
+ *     2^-126; 1 for a block whose y are all 0 or NaN.  A NaN of y becomes a NaN
+ *     of q and does not touch the scale; an infinite y makes the scale infinite
+ *     and the block's q NaN.  (A NaN in x or residual makes its row's y NaN; an
+ *     infinity there, whose row has an infinite mean, makes y NaN at its place
+ *     and 0 elsewhere.)
  * Errors: GS_ERR_INVALID_ARG (null pointers, sizes below 0, a row stride below
  * cols, pointers that are not a multiple of the element size, eps negative or
  * not finite, nothing to write); GS_ERR_UNSUPPORTED for cols above

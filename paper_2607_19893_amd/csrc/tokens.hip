@@ -244,10 +244,13 @@ __global__ void __launch_bounds__(GS_BLOCK, TPR == 64 && E == 32 && sizeof(T) ==
         asm volatile("" : "+v"(lift));         // its products are formed again, not held
         if (col >= cols) continue;           // below: no lane exchange
         float scale = m * f / 448.0f * (1.0f / up), r = 448.0f / m, r_lo = fmaf(-r, m_lo, fmaf(-r, m, 448.0f)) / m;
-        if (!(scale >= kLeast)) {              // a block of zeros, or one too small for the quotient
-            scale = some > 0.0f ? kLeast : 1.0f;
-            r = some > 0.0f ? f * (0x1p126f / up) : f;
+        if (!(scale >= kLeast)) {              // y of 0 or NaN alone, or a block too small for the quotient
+            const bool small = some > 0.0f && finite;
+            scale = small ? kLeast : 1.0f;
+            r = small ? f * (0x1p126f / up) : f;
             r_lo = 0.0f;
+        } else if (scale == INFINITY) {
+            r = NAN;
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) q[i] = odd_product(s[c][i] * lift, w[c][i], r, r_lo);

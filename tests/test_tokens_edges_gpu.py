@@ -64,3 +64,44 @@ def test_norm_8bit_without_eps(tk):
     w = 1 + 0.2 * randn(g, 200)
     y, _ = ref.norm(x, w, 0.0)
     check_8bit(tk.rms_norm(x, w, 0.0, eight_bit=True), y)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_norm_8bit_of_special_rows(tk, dtype):
+    """NaN, infinities and sums past the range: the scale is that of the block's numbers, 1 where none is left."""
+    g = gen(23)
+    x = randn(g, 5, 300)
+    x[1, 7] = math.nan                                 # y is NaN throughout
+    x[2, 200] = math.inf                               # y is NaN there and 0 elsewhere
+    x[3, 0] = 1e25                                     # the squares' sum is infinite: y is 0
+    x[4] = 0.0
+    x = x.to(dtype)
+    w = torch.ones(300, device="cuda")
+    e = tk.rms_norm(x, w, 1e-6, eight_bit=True)
+    q = e.q.float()
+    assert bool((e.scale[1:] == 1).all())
+    assert bool(q[1].isnan().all()) and bool((q[3:] == 0).all())
+    assert torch.equal(q[2].isnan(), torch.arange(300, device="cuda") == 200) and float(q[2].nan_to_num().abs().max()) == 0
+    clean = tk.rms_norm(x[:1], w, 1e-6, eight_bit=True)
+    assert torch.equal(clean.q[0].float(), q[0]) and torch.equal(clean.scale[0], e.scale[0])
+    # without eps a row of zeros is 0 / 0
+    z = tk.rms_norm(x[4:], w, 0.0, eight_bit=True)
+    assert bool((z.scale == 1).all()) and bool(z.q.float().isnan().all())
+    # a weight: NaN stays with its column, an infinity takes its block
+    for bad in (math.nan, math.inf):
+        w2 = w.clone()
+        w2[130] = bad
+        e = tk.rms_norm(x[:1], w2, 1e-6, eight_bit=True)
+        q = e.q.float()[0]
+        others = torch.arange(300, device="cuda") // 128 != 1
+        assert torch.equal(q[others], clean.q[0].float()[others])
+        assert torch.equal(e.scale[0, ::2], clean.scale[0, ::2])
+        if bad == math.inf:
+            assert float(e.scale[0, 1]) == math.inf and bool(q[128:256].isnan().all())
+        else:
+            assert bool(q[130].isnan()) and int(q.isnan().sum()) == 1
+            w2[130] = 0.0
+            without = tk.rms_norm(x[:1], w2, 1e-6, eight_bit=True)
+            assert torch.equal(e.scale, without.scale)
+            keep = torch.arange(300, device="cuda") != 130
+            assert torch.equal(q[keep], without.q.float()[0][keep])
