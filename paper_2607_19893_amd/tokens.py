@@ -4,13 +4,15 @@ segments, each with its gradient.
 
 The functions allocate their outputs and workspaces with torch on the current
 stream and call the gs_* entry points there; every step runs in libgsmi's
-kernels.  `RmsNorm`, `Rotary` and `Attention` put them under torch's autograd.
+kernels.  `RmsNorm`, `Rotary` and `Attention` put them under torch's autograd;
+their gradients have none of their own, a second derivative raises.
 """
 from __future__ import annotations
 
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import gsmi
 
@@ -123,6 +125,7 @@ class RmsNorm(torch.autograd.Function):
         return r.y, total
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dtotal):
         total, weight = ctx.saved_tensors
         if dy is None:
@@ -142,6 +145,7 @@ class Rotary(torch.autograd.Function):
         return rotary((q, k), pos, freq, axis_pairs, interleaved=interleaved, amplitude=amplitude)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         pos, freq = ctx.saved_tensors
         axis_pairs, interleaved, amplitude = ctx.how
@@ -162,6 +166,7 @@ class Attention(torch.autograd.Function):
         return out, lse
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, _):
         q, k, v, out, lse = ctx.saved_tensors
         return (*attention_backward(dout.contiguous(), q, k, v, out, lse, **ctx.how), None)

@@ -1,0 +1,85 @@
+"""How the token operators sit in torch: second derivatives, devices, tensors that change between the passes, streams.
+The library's calls are replaced by plain torch forms, so all of it runs without a GPU."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+
+@pytest.fixture
+def tk(monkeypatch):
+    from paper_2607_19893_amd import tokens
+
+    def rms_norm(x, weight, eps=1e-6, residual=None, eight_bit=False):
+        s = x if residual is None else x + residual
+        return tokens.Normed(s * weight / torch.sqrt(s.pow(2).mean(1, keepdim=True) + eps), s)
+
+    def rms_norm_backward(dy, total, weight, eps=1e-6, dtotal=None):
+        r = 1 / torch.sqrt(total.pow(2).mean(1, keepdim=True) + eps)
+        n, g = total * r, dy * weight
+        dx = r * (g - n * (g * n).mean(1, keepdim=True))
+        return dx if dtotal is None else dx + dtotal, (dy * n).sum(0)
+
+    def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amplitude=1.0, inplace=False):
+        t = (pos * freq * (-1 if inverse else 1))[:, None]
+        half = freq.numel()
+        return tuple(amplitude * torch.cat((x[..., :half] * t.cos() - x[..., half:] * t.sin(),
+                                            x[..., :half] * t.sin() + x[..., half:] * t.cos()), -1) for x in tensors)
+
+    def weights(q, k, scale, key_on):
+        z = torch.einsum("qhd,khd->hqk", q, k) * scale
+        if key_on is not None:
+            z = z.masked_fill(key_on == 0, float("-inf"))
+        return z
+
+    def attention(q, k, v, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=1.0, left=-1, right=-1):
+        z = weights(q, k, scale, key_on)
+        return torch.einsum("hqk,khd->qhd", torch.softmax(z, 2), v), torch.logsumexp(z, 2).T.contiguous()
+
+    def attention_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=1.0, left=-1,
+                           right=-1):
+        p = torch.exp(weights(q, k, scale, key_on) - lse.T[..., None])
+        ds = scale * p * (torch.einsum("qhd,khd->hqk", dout, v) - (dout * out).sum(2).T[..., None])
+        return (torch.einsum("hqk,khd->qhd", ds, k), torch.einsum("hqk,qhd->khd", ds, q),
+                torch.einsum("hqk,qhd->khd", p, dout))
+
+    for f in (rms_norm, rms_norm_backward, rotary, attention, attention_backward):
+        monkeypatch.setattr(tokens, f.__name__, f)
+    return tokens
+
+
+def rand(*shape, seed=0):
+    g = torch.Generator()
+    g.manual_seed(seed + sum(shape))
+    return torch.randn(*shape, generator=g, dtype=torch.float64)
+
+
+def norm_call(tk):
+    w = (1 + rand(16)).requires_grad_()
+    y, _ = tk.RmsNorm.apply(rand(5, 16).requires_grad_(), None, w, 1e-6)
+    return y, w
+
+
+def rotary_call(tk):
+    q = rand(5, 2, 8).requires_grad_()
+    y, _ = tk.Rotary.apply(q, rand(5, 1, 8), rand(5, 1), rand(4), (4,), False, 1.0)
+    return y, q
+
+
+def attention_call(tk):
+    q = rand(5, 2, 8).requires_grad_()
+    y, _ = tk.Attention.apply(q, rand(6, 2, 8), rand(6, 2, 8, seed=1), dict(scale=0.5))
+    return y, q
+
+
+@pytest.mark.parametrize("call", [norm_call, rotary_call, attention_call])
+def test_a_second_derivative_is_refused(tk, call):
+    """The gradients have no gradient of their own here; a penalty on them must not lose its terms in silence."""
+    y, x = call(tk)
+    (g,) = torch.autograd.grad(y.pow(2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (g.pow(2).sum() + x.sum()).backward()
+    y, x = call(tk)
+    y.pow(2).sum().backward()                          # the first one is as before
+    assert x.grad is not None and bool(torch.isfinite(x.grad).all())
