@@ -9,6 +9,7 @@ their gradients have none of their own, a second derivative raises.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import NamedTuple, Optional
 
 import torch
@@ -30,13 +31,18 @@ class Normed(NamedTuple):
     scale: Optional[torch.Tensor] = None
 
 
-def _same_device(*tensors):
+_HERE = contextlib.nullcontext()
+
+
+def _device_of(*tensors):
+    """Makes the tensors' device the current one, whose stream the call then takes."""
     d = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != d:
             raise ValueError("tensors on %s and %s" % (tensors[0].device, t.device))
     if d < 0:
         raise ValueError("tokens live on the GPU, not on %s" % tensors[0].device)
+    return _HERE if d == torch.cuda.current_device() else torch.cuda.device(d)
 
 
 def _fp32(t, n, what):
@@ -50,66 +56,66 @@ def _workspace(n, device):
 
 def rms_norm(x, weight, eps=1e-6, residual=None, eight_bit=False) -> Normed:
     """s = x + residual; y = s * weight / sqrt(mean(s^2) + eps), for x [rows, cols]."""
-    _same_device(x, weight, residual)
-    rows, cols = x.shape
-    _fp32(weight, cols, "weight")
-    total = torch.empty_like(x, memory_format=_DENSE) if residual is not None else None
-    y = q = scale = None
-    if eight_bit:
-        q = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
-        scale = torch.empty(rows, -(-cols // gsmi.GS_NORM_BLOCK), dtype=torch.float32, device=x.device)
-    else:
-        y = torch.empty_like(x, memory_format=_DENSE)
-    gsmi.gs_rms_norm(x, weight, eps, y=y, residual=residual, total=total, q=q, q_scale=scale)
-    return Normed(y, x if total is None else total, q, scale)
+    with _device_of(x, weight, residual):
+        rows, cols = x.shape
+        _fp32(weight, cols, "weight")
+        total = torch.empty_like(x, memory_format=_DENSE) if residual is not None else None
+        y = q = scale = None
+        if eight_bit:
+            q = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
+            scale = torch.empty(rows, -(-cols // gsmi.GS_NORM_BLOCK), dtype=torch.float32, device=x.device)
+        else:
+            y = torch.empty_like(x, memory_format=_DENSE)
+        gsmi.gs_rms_norm(x, weight, eps, y=y, residual=residual, total=total, q=q, q_scale=scale)
+        return Normed(y, x if total is None else total, q, scale)
 
 
 def rms_norm_backward(dy, total, weight, eps=1e-6, dtotal=None):
     """(dx, dweight) of rms_norm; dx is the gradient of x and of residual."""
-    _same_device(dy, total, weight, dtotal)
-    rows, cols = total.shape
-    _fp32(weight, cols, "weight")
-    dx = torch.empty_like(total, memory_format=_DENSE)
-    dweight = torch.empty_like(weight)
-    ws = _workspace(gsmi.gs_rms_norm_bwd_ws_bytes(rows, cols), total.device)
-    gsmi.gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=dtotal)
-    return dx, dweight
+    with _device_of(dy, total, weight, dtotal):
+        rows, cols = total.shape
+        _fp32(weight, cols, "weight")
+        dx = torch.empty_like(total, memory_format=_DENSE)
+        dweight = torch.empty_like(weight)
+        ws = _workspace(gsmi.gs_rms_norm_bwd_ws_bytes(rows, cols), total.device)
+        gsmi.gs_rms_norm_bwd(dy, total, weight, eps, dx, dweight, ws, dtotal=dtotal)
+        return dx, dweight
 
 
 def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amplitude=1.0, inplace=False):
     """Turns one or two [tokens, heads, dim] tensors by pos [tokens, axes]; returns them as a tuple."""
     tensors = (tensors,) if isinstance(tensors, torch.Tensor) else tuple(tensors)
-    _same_device(*tensors, pos, freq)
-    if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape != (tensors[0].shape[0], len(axis_pairs)):
-        raise ValueError("pos is float32 [tokens, %d]" % len(axis_pairs))
-    _fp32(freq, sum(axis_pairs), "freq")
-    out = tensors if inplace else tuple(torch.empty_like(t, memory_format=_DENSE) for t in tensors)
-    gsmi.gs_rotary(tensors, out, pos, freq, axis_pairs, interleaved, inverse, amplitude)
-    return out
+    with _device_of(*tensors, pos, freq):
+        if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape != (tensors[0].shape[0], len(axis_pairs)):
+            raise ValueError("pos is float32 [tokens, %d]" % len(axis_pairs))
+        _fp32(freq, sum(axis_pairs), "freq")
+        out = tensors if inplace else tuple(torch.empty_like(t, memory_format=_DENSE) for t in tensors)
+        gsmi.gs_rotary(tensors, out, pos, freq, axis_pairs, interleaved, inverse, amplitude)
+        return out
 
 
 def attention(q, k, v, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, left=-1, right=-1):
     """(out, lse): q [n_q, heads, dim] over k, v [n_k, kv_heads, dim], segment by segment."""
-    _same_device(q, k, v, cu_q, cu_k, key_on)
-    a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
-    out = torch.empty_like(q, memory_format=_DENSE)
-    lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
-    gsmi.gs_attention(a, out, lse, _workspace(gsmi.gs_attention_ws_bytes(a), q.device))
-    return out, lse
+    with _device_of(q, k, v, cu_q, cu_k, key_on):
+        a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
+        out = torch.empty_like(q, memory_format=_DENSE)
+        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+        gsmi.gs_attention(a, out, lse, _workspace(gsmi.gs_attention_ws_bytes(a), q.device))
+        return out, lse
 
 
 def attention_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, left=-1,
                        right=-1):
     """(dq, dk, dv) of attention, from its result and log sums."""
-    _same_device(q, k, v, dout, out, lse, cu_q, cu_k, key_on)
-    for t, what in ((dout, "dout"), (out, "out")):
-        if t.shape != q.shape or t.dtype != q.dtype:
-            raise ValueError("%s has q's shape and type" % what)
-    _fp32(lse, q.shape[0] * q.shape[1], "lse")
-    a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
-    dq, dk, dv = (torch.empty_like(t, memory_format=_DENSE) for t in (q, k, v))
-    gsmi.gs_attention_bwd(a, out, lse, dout, dq, dk, dv, _workspace(gsmi.gs_attention_ws_bytes(a, True), q.device))
-    return dq, dk, dv
+    with _device_of(q, k, v, dout, out, lse, cu_q, cu_k, key_on):
+        for t, what in ((dout, "dout"), (out, "out")):
+            if t.shape != q.shape or t.dtype != q.dtype:
+                raise ValueError("%s has q's shape and type" % what)
+        _fp32(lse, q.shape[0] * q.shape[1], "lse")
+        a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
+        dq, dk, dv = (torch.empty_like(t, memory_format=_DENSE) for t in (q, k, v))
+        gsmi.gs_attention_bwd(a, out, lse, dout, dq, dk, dv, _workspace(gsmi.gs_attention_ws_bytes(a, True), q.device))
+        return dq, dk, dv
 
 
 class RmsNorm(torch.autograd.Function):

@@ -83,3 +83,39 @@ def test_a_second_derivative_is_refused(tk, call):
     y, x = call(tk)
     y.pow(2).sum().backward()                          # the first one is as before
     assert x.grad is not None and bool(torch.isfinite(x.grad).all())
+
+
+class Elsewhere(torch.Tensor):
+    """A CPU tensor that says it lives on GPU 1."""
+
+    def get_device(self):
+        return 1
+
+
+def test_a_call_runs_on_its_tensors_device(monkeypatch):
+    """Tensors of GPU 1 while GPU 0 is current: the library's call is made with GPU 1 current, and GPU 0 is so again."""
+    from paper_2607_19893_amd import gsmi, tokens
+    now, seen = [0], []
+
+    @contextlib.contextmanager
+    def device(d):
+        before, now[0] = now[0], d
+        yield
+        now[0] = before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    for name in ("gs_rms_norm", "gs_rms_norm_bwd", "gs_rotary", "gs_attention", "gs_attention_bwd"):
+        monkeypatch.setattr(gsmi, name, lambda *a, name=name, **k: seen.append((name, now[0])))
+
+    def there(*shape, dtype=torch.float32):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(Elsewhere)
+
+    x, w, t = there(4, 64), there(64), there(4, 2, 64, dtype=torch.bfloat16)
+    tokens.rms_norm(x, w, residual=x)
+    tokens.rms_norm_backward(x, x, w)
+    tokens.rotary((t, t), there(4, 1), there(32), [32])
+    out, lse = tokens.attention(t, t, t)
+    tokens.attention_backward(t, t, t, t, out, lse.as_subclass(Elsewhere))
+    assert seen == [(n, 1) for n in ("gs_rms_norm", "gs_rms_norm_bwd", "gs_rotary", "gs_attention", "gs_attention_bwd")]
+    assert now == [0]
