@@ -782,7 +782,9 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  *   cu_q, cu_k [n_seg + 1] int32, ascending from 0 to n_q and n_k: the segments'
  *     first rows (empty ones allowed); both NULL: n_seg segments of equal
  *     length (n_seg divides n_q and n_k).  Values outside [0, n] are taken as
- *     the nearest in it; rows outside every segment are not written.
+ *     the nearest in it; rows outside every segment (before the first start,
+ *     from the last on) are not written.  With GS_ATTN_FILL added to dtype they
+ *     are: out 0, lse -infinity, dq, dk and dv 0.
  *   q [n_q, heads, dim], k, v [n_k, kv_heads, dim]; GS_BF16 or GS_F16; pointers
  *     16-byte aligned, strides and dim multiples of 8 elements, dim <= 128, row
  *     strides from dim to GS_ATTN_MAX_STRIDE elements (of a single row: any).
@@ -801,6 +803,7 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  */
 #define GS_ATTN_MAX_DIM 128
 #define GS_ATTN_MAX_STRIDE 8388608
+enum { GS_ATTN_FILL = 256 };
 
 typedef struct {
     int32_t dtype;

@@ -671,7 +671,8 @@ static gs_status check_attn_rows(const gs_rows& r, int32_t rows, int32_t dim, co
 
 static gs_status check_attn(const gs_attn* a, const char* what) {
     GS_REQUIRE(a != nullptr, "%s: null args", what);
-    GS_REQUIRE(a->dtype == GS_BF16 || a->dtype == GS_F16, "%s: dtype %d is neither GS_BF16 nor GS_F16", what, a->dtype);
+    const int32_t dtype = a->dtype & ~GS_ATTN_FILL;
+    GS_REQUIRE(dtype == GS_BF16 || dtype == GS_F16, "%s: dtype %d is neither GS_BF16 nor GS_F16", what, a->dtype);
     GS_REQUIRE(a->n_q >= 0 && a->n_k >= 0 && a->n_seg >= 1, "%s: bad row or segment count", what);
     GS_REQUIRE(a->heads >= 1 && a->kv_heads >= 1 && a->heads % a->kv_heads == 0,
                "%s: kv_heads %d must divide heads %d", what, a->kv_heads, a->heads);

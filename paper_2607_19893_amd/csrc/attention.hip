@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
     const Place place = chiplet_place<(D > 64)>(blockIdx.x, a.tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
     const Segment sg = find_segment<false, true>(a, kRows, a.tiles, place.tile);
+    if (a.fill) fill_rest(a, a.cu_q, a.n_q, a.heads, static_cast<T*>(f.out), f.o_row, f.o_head, f.lse);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -307,6 +308,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
     const Place place = chiplet_place<false>(blockIdx.x, a.tiles, a.kv_heads, 1);
     const int kvh = place.head;
     const Segment sg = find_segment<true, false, true>(a, f.chunk, a.tiles, place.tile);
+    if (a.fill) fill_rest(a, a.cu_q, a.n_q, a.heads, static_cast<T*>(f.out), f.o_row, f.o_head, f.lse);
     const int parts = max((sg.nk + f.chunk - 1) / f.chunk, 1), split = sg.tile;
     const int rows = sg.nq * a.group;
     if (split >= parts) return;
@@ -634,7 +636,7 @@ hipError_t launch_attention(const gs_attn& a, const gs_rows& out, float* lse, vo
     f.part_ml = static_cast<float2*>(ws);
     const size_t sums = align256((size_t)a.n_q * a.heads * p.splits * sizeof(float2));
     f.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + sums);
-    return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, p.few, st) : by_dim<f16_t>(f, p.few, st);
+    return (a.dtype & ~GS_ATTN_FILL) == GS_BF16 ? by_dim<bf16_t>(f, p.few, st) : by_dim<f16_t>(f, p.few, st);
 }
 
 }  // namespace gsmi

@@ -72,6 +72,7 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dq(BwdArgs f) {
     const Place place = chiplet_place<true>(blockIdx.x, a.tiles, a.kv_heads, 1);
     const int kvh = place.head;
     const Segment sg = find_segment<false, true>(a, kRows, a.tiles, place.tile);
+    if (a.fill) fill_rest(a, a.cu_q, a.n_q, a.heads, static_cast<T*>(f.dq), f.dq_row, f.dq_head, nullptr);
     const int rows = sg.nq * a.group, row0 = sg.tile * kRows;
     if (row0 >= rows) return;
     const int lane = lane_id(), h = lane >> 5, wave = threadIdx.x / GS_WAVE;
@@ -253,6 +254,10 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     const Place place = chiplet_place<true>(blockIdx.x, f.key_tiles, a.kv_heads, f.splits);
     const int split = place.split, kvh = place.head;
     const Segment sg = find_segment<true, false>(a, kRows, f.key_tiles, place.tile);
+    if (a.fill) {
+        fill_rest(a, a.cu_k, a.n_k, a.kv_heads, static_cast<T*>(f.dk), f.dk_row, f.dk_head, nullptr);
+        fill_rest(a, a.cu_k, a.n_k, a.kv_heads, static_cast<T*>(f.dv), f.dv_row, f.dv_head, nullptr);
+    }
     const int key0 = sg.tile * kRows;
     if (key0 >= sg.nk) return;
     const TileRows<ST> tr(f, sg, key0);
@@ -577,7 +582,7 @@ hipError_t launch_attention_bwd(const gs_attn& a, const gs_attn_grads& g, void* 
     f.splits = plan.splits;
     f.chunk = plan.chunk;
     f.part = reinterpret_cast<float*>(static_cast<char*>(ws) + align256((size_t)a.n_q * a.heads * 2 * sizeof(float)));
-    return a.dtype == GS_BF16 ? by_dim<bf16_t>(f, st) : by_dim<f16_t>(f, st);
+    return (a.dtype & ~GS_ATTN_FILL) == GS_BF16 ? by_dim<bf16_t>(f, st) : by_dim<f16_t>(f, st);
 }
 
 }  // namespace gsmi

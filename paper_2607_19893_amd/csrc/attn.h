@@ -266,6 +266,7 @@ struct AttnArgs {
     int32_t n_q, n_k, n_seg, heads, kv_heads, group, dim, left, right;
     float scale;
     int32_t tiles;             // workgroups' tiles per key head
+    int32_t fill;              // rows outside every segment are written
 };
 
 // Row stride of a tensor of n rows.  The only row of one has no next: any value
@@ -297,6 +298,7 @@ inline AttnArgs attn_args(const gs_attn& a) {
     r.right = a.right;
     r.scale = a.scale;
     r.tiles = 0;
+    r.fill = (a.dtype & GS_ATTN_FILL) != 0 && a.cu_q != nullptr;
     return r;
 }
 
@@ -383,6 +385,26 @@ __device__ __forceinline__ int keys_of_token(const AttnArgs& a, int token) {
     }
     if (token < cu_at(a.cu_q, lo, a.n_seg, a.n_q) || token >= cu_at(a.cu_q, lo + 1, a.n_seg, a.n_q)) return -1;
     return max(cu_at(a.cu_k, lo + 1, a.n_seg, a.n_k) - cu_at(a.cu_k, lo, a.n_seg, a.n_k), 0);
+}
+
+// Zeros into the rows outside every segment of a matrix of n rows (those before
+// the first start and from the last on), by all of the launch's workgroups;
+// lse, if given, takes -inf.
+template <typename T>
+__device__ __forceinline__ void fill_rest(const AttnArgs& a, const int32_t* cu, int n, int heads, T* p, int64_t ld_row,
+                                          int64_t ld_head, float* lse) {
+    const int first = cu_at(cu, 0, a.n_seg, n), held = max(cu_at(cu, a.n_seg, a.n_seg, n) - first, 0), rest = n - held;
+    if (rest == 0) return;
+    const int per = a.dim / 8;
+    const int64_t pieces = (int64_t)rest * heads * per, step = (int64_t)gridDim.x * GS_BLOCK;
+#pragma unroll 1
+    for (int64_t x = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x; x < pieces; x += step) {
+        const int64_t y = x / per;
+        const int c = (int)(x - y * per), i = (int)(y / heads), head = (int)(y - (int64_t)i * heads);
+        const int64_t row = i < first ? i : i + held;
+        *reinterpret_cast<op8<T>*>(p + row * ld_row + head * ld_head + 8 * c) = op8<T>{};
+        if (lse != nullptr && c == 0) lse[row * heads + head] = -INFINITY;
+    }
 }
 
 // Keys [lo, hi) that any of the places first .. last can admit.

@@ -32,6 +32,7 @@ GS_DEV_PAIR_OVERFLOW, GS_DEV_MSG_OVERFLOW, GS_DEV_MSG_MISMATCH, GS_DEV_MSG_ORDER
 GS_MSG_MAGIC = 0x47534D31
 GS_F32, GS_BF16, GS_F16 = 0, 1, 2
 GS_ROPE_PLAIN, GS_ROPE_LINEAR, GS_ROPE_BASE, GS_ROPE_PARTS = 0, 1, 2, 3
+GS_ATTN_FILL = 256
 GS_NORM_BLOCK, GS_NORM_MAX_COLS, GS_ROTARY_MAX_DIM, GS_ATTN_MAX_DIM = 128, 16384, 512, 128
 GS_MAX_GROUPS = 8
 
@@ -588,7 +589,9 @@ def gs_rotary_freqs(pairs, base=10000.0, scaling=GS_ROPE_PLAIN, factor=1.0, trai
     return freq[:int(pairs)], float(amp.value)
 
 
-def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-1, right=-1) -> gs_attn:
+def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-1, right=-1,
+              fill=False) -> gs_attn:
+    """fill: rows outside every segment are written (zeros, log sums of -inf)."""
     qs, ks = q.shape, k.shape
     if ks != v.shape or ks[2] != qs[2] or k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("q, k, v do not fit: %s, %s, %s" % (qs, ks, v.shape))
@@ -599,7 +602,7 @@ def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-
             raise ValueError("cu_q and cu_k are contiguous int32 of the same length")
     if key_on is not None and (key_on.numel() != ks[0] or key_on.element_size() != 1 or not key_on.is_contiguous()):
         raise ValueError("key_on is one contiguous byte per key")
-    return gs_attn(token_dtype(q), qs[0], ks[0], n_seg, qs[1], ks[1], qs[2], left, right, scale, _at(cu_q), _at(cu_k),
+    return gs_attn(token_dtype(q) | (GS_ATTN_FILL if fill else 0), qs[0], ks[0], n_seg, qs[1], ks[1], qs[2], left, right, scale, _at(cu_q), _at(cu_k),
                    _at(key_on), make_rows(q), make_rows(k), make_rows(v))
 
 

@@ -95,9 +95,12 @@ def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amp
 
 
 def attention(q, k, v, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, left=-1, right=-1):
-    """(out, lse): q [n_q, heads, dim] over k, v [n_k, kv_heads, dim], segment by segment."""
+    """(out, lse): q [n_q, heads, dim] over k, v [n_k, kv_heads, dim], segment by segment.
+
+    Rows outside every segment (behind the last start of a buffer at capacity) have out 0 and lse -inf."""
     with _device_of(q, k, v, cu_q, cu_k, key_on):
-        a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
+        a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right,
+                           fill=True)
         out = torch.empty_like(q, memory_format=_DENSE)
         lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
         gsmi.gs_attention(a, out, lse, _workspace(gsmi.gs_attention_ws_bytes(a), q.device))
@@ -106,13 +109,14 @@ def attention(q, k, v, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, l
 
 def attention_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, n_seg=1, key_on=None, scale=None, left=-1,
                        right=-1):
-    """(dq, dk, dv) of attention, from its result and log sums."""
+    """(dq, dk, dv) of attention, from its result and log sums; 0 for rows and keys outside every segment."""
     with _device_of(q, k, v, dout, out, lse, cu_q, cu_k, key_on):
         for t, what in ((dout, "dout"), (out, "out")):
             if t.shape != q.shape or t.dtype != q.dtype:
                 raise ValueError("%s has q's shape and type" % what)
         _fp32(lse, q.shape[0] * q.shape[1], "lse")
-        a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right)
+        a = gsmi.make_attn(q, k, v, q.shape[2] ** -0.5 if scale is None else scale, n_seg, cu_q, cu_k, key_on, left, right,
+                           fill=True)
         dq, dk, dv = (torch.empty_like(t, memory_format=_DENSE) for t in (q, k, v))
         gsmi.gs_attention_bwd(a, out, lse, dout, dq, dk, dv, _workspace(gsmi.gs_attention_ws_bytes(a, True), q.device))
         return dq, dk, dv

@@ -105,3 +105,31 @@ def test_norm_8bit_of_special_rows(tk, dtype):
             assert torch.equal(e.scale, without.scale)
             keep = torch.arange(300, device="cuda") != 130
             assert torch.equal(q[keep], without.q.float()[0][keep])
+
+
+@pytest.mark.parametrize("heads,nq,nk,starts_q,starts_k", [
+    (2, 50, 60, [5, 20, 44], [3, 30, 51]), (2, 50, 5000, [5, 45], [3, 4990]), (2, 12, 5000, [5, 7], [3, 4990]),
+    (4, 2500, 130, [5, 2400], [3, 120]), (1, 300, 400, [7] + list(range(7, 270, 3)), [9] + list(range(9, 360, 4))[:88]),
+    (2, 40, 40, [0, 0, 0], [0, 0, 0]), (2, 40, 40, [40, 40], [40, 40])])
+def test_rows_outside_every_segment_are_zeros(tk, heads, nq, nk, starts_q, starts_k):
+    """A buffer at capacity whose count is on the device: the rows past it are no one's, and no one's gradient."""
+    c = case([nq], [nk], heads, 1, dim=64)
+    g, q, k, v, _ = inputs(c)
+    dout = randn(g, *q.shape, dtype=BF)
+    cu_q, cu_k = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in (starts_q, starts_k))
+    assert len(starts_q) == len(starts_k)
+    on = torch.ones(nk, dtype=torch.uint8, device="cuda")
+    for flags in (None, on):
+        junk = [torch.full((1 << 20,), 7.0, device="cuda") for _ in range(8)]     # what fresh outputs may hold
+        junk += [torch.full((n,), 7.0, dtype=t, device="cuda") for n, t in
+                 [(q.numel(), BF), (k.numel(), BF), (nq * heads, F32)] for _ in range(4)]
+        del junk
+        out, lse = tk.attention(q, k, v, cu_q, cu_k, key_on=flags)
+        dq, dk, dv = tk.attention_backward(dout, q, k, v, out, lse, cu_q, cu_k, key_on=flags)
+        for t, (lo, hi) in ((out, (starts_q[0], starts_q[-1])), (dq, (starts_q[0], starts_q[-1])),
+                            (dk, (starts_k[0], starts_k[-1])), (dv, (starts_k[0], starts_k[-1]))):
+            assert bool((t[:lo] == 0).all()) and bool((t[hi:] == 0).all())
+            assert bool((t[lo:hi] != 0).any(-1).all())
+        lo, hi = starts_q[0], starts_q[-1]
+        assert bool((lse[:lo] == -math.inf).all()) and bool((lse[hi:] == -math.inf).all())
+        assert bool(torch.isfinite(lse[lo:hi]).all())
