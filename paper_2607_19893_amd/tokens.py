@@ -83,7 +83,10 @@ def rms_norm_backward(dy, total, weight, eps=1e-6, dtotal=None):
 
 
 def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amplitude=1.0, inplace=False):
-    """Turns one or two [tokens, heads, dim] tensors by pos [tokens, axes]; returns them as a tuple."""
+    """Turns one or two [tokens, heads, dim] tensors by pos [tokens, axes]; returns them as a tuple.
+
+    inplace: the tensors themselves are turned; autograd sees that they changed (as for the other functions here, not
+    how: `Rotary` is the form with a gradient)."""
     tensors = (tensors,) if isinstance(tensors, torch.Tensor) else tuple(tensors)
     with _device_of(*tensors, pos, freq):
         if pos.dtype != torch.float32 or pos.dim() != 2 or pos.shape != (tensors[0].shape[0], len(axis_pairs)):
@@ -91,6 +94,8 @@ def rotary(tensors, pos, freq, axis_pairs, interleaved=False, inverse=False, amp
         _fp32(freq, sum(axis_pairs), "freq")
         out = tensors if inplace else tuple(torch.empty_like(t, memory_format=_DENSE) for t in tensors)
         gsmi.gs_rotary(tensors, out, pos, freq, axis_pairs, interleaved, inverse, amplitude)
+        if inplace:
+            torch.autograd.graph.increment_version(tensors)    # what autograd has saved of them is no longer there
         return out
 
 

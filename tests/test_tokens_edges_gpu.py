@@ -133,3 +133,15 @@ def test_rows_outside_every_segment_are_zeros(tk, heads, nq, nk, starts_q, start
         lo, hi = starts_q[0], starts_q[-1]
         assert bool((lse[:lo] == -math.inf).all()) and bool((lse[hi:] == -math.inf).all())
         assert bool(torch.isfinite(lse[lo:hi]).all())
+
+
+def test_rotary_in_place_is_seen_by_autograd(tk):
+    g = gen(31)
+    x, w = randn(g, 20, 2, 64), randn(g, 20, 2, 64).requires_grad_()
+    pos, freq = randn(g, 20, 1), torch.rand(32, generator=g, device="cuda")
+    before = x._version
+    y = (x * w).sum()                                  # saves x
+    (z,) = tk.rotary(x, pos, freq, [32], inplace=True)
+    assert z is x and x._version > before
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
