@@ -577,9 +577,29 @@ hipError_t rotary_type(const gs_rotary_args& a, hipStream_t st) {
 
 }  // namespace
 
+// A launch holds fewer than 2^32 threads, a row takes up to 256: more rows than
+// 2^23 go in several.
 hipError_t launch_rms_norm(const gs_norm_args& a, hipStream_t st) {
-    if (a.dtype == GS_F32) return norm_type<float>(a, st);
-    return a.dtype == GS_BF16 ? norm_type<bf16_t>(a, st) : norm_type<f16_t>(a, st);
+    constexpr int32_t kMost = 1 << 23;
+    const int64_t size = a.dtype == GS_F32 ? 4 : 2;
+    auto at = [](const void* p, int64_t bytes) {
+        return p ? const_cast<char*>(static_cast<const char*>(p)) + bytes : nullptr;
+    };
+    for (int64_t first = 0; first < a.rows; first += kMost) {
+        gs_norm_args b = a;
+        b.rows = (int32_t)std::min<int64_t>(kMost, a.rows - first);
+        b.x = at(a.x, first * a.ld_x * size);
+        b.residual = at(a.residual, first * a.ld_residual * size);
+        b.total = at(a.total, first * a.ld_total * size);
+        b.y = at(a.y, first * a.ld_y * size);
+        b.q = reinterpret_cast<uint8_t*>(at(a.q, first * a.ld_q));
+        b.q_scale = reinterpret_cast<float*>(at(a.q_scale, first * a.ld_scale * 4));
+        const hipError_t e = b.dtype == GS_F32    ? norm_type<float>(b, st)
+                             : b.dtype == GS_BF16 ? norm_type<bf16_t>(b, st)
+                                                  : norm_type<f16_t>(b, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // For the most partial rows that any type's kernel of this width writes.

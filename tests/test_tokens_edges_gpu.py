@@ -145,3 +145,20 @@ def test_rotary_in_place_is_seen_by_autograd(tk):
     assert z is x and x._version > before
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [((1 << 23) + 5, 8, BF), ((1 << 27) + 3, 4, F32)])
+def test_norm_of_very_many_rows(tk, rows, cols, dtype):
+    """More rows than a launch of one thread group a row holds."""
+    g = gen(41)
+    x = torch.empty(rows, cols, dtype=dtype, device="cuda").normal_(generator=g)
+    w = 1 + randn(g, cols)
+    y = tk.rms_norm(x, w, 1e-6).y
+    e = tk.rms_norm(x, w, 1e-6, eight_bit=True)
+    edge = [0, 1, (1 << 22) - 1, 1 << 22, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, rows // 2, rows - 2, rows - 1]
+    at = torch.cat((torch.tensor(edge, device="cuda"),
+                    torch.randint(0, rows, (4000,), generator=g, device="cuda")))
+    want, _ = ref.norm(x[at], w, 1e-6)
+    within(y[at], want, (ref.UNIT[dtype] + 41 * 2.0 ** -24) * want.abs() + 4 * ref.TINY[dtype], "y")
+    few = tk.rms_norm(x[at], w, 1e-6, eight_bit=True)
+    assert torch.equal(e.q[at].float(), few.q.float()) and torch.equal(e.scale[at], few.scale)
