@@ -541,10 +541,22 @@ __global__ void __launch_bounds__(GS_BLOCK) k_rotary(RotArgs ra) {
 
 template <typename T, int V>
 hipError_t rotary_go(const RotArgs& r, hipStream_t st) {
-    const uint32_t grid = div_up(r.a.tokens, r.per);
-    if (r.a.interleaved) k_rotary<T, V, true><<<grid, GS_BLOCK, 0, st>>>(r);
-    else k_rotary<T, V, false><<<grid, GS_BLOCK, 0, st>>>(r);
-    return hipGetLastError();
+    // a launch holds fewer than 2^32 threads: tokens of more than 2^23 workgroups go in several
+    const int64_t most = (int64_t)r.per << 23;
+    for (int64_t first = 0; first < r.a.tokens; first += most) {
+        RotArgs s = r;
+        s.a.tokens = (int32_t)std::min<int64_t>(most, r.a.tokens - first);
+        s.a.pos = r.a.pos ? r.a.pos + first * r.a.ld_pos : nullptr;
+        for (int i = 0; i < r.a.n_tensors; ++i)
+            for (gs_rows* t : {&s.a.in[i], &s.a.out[i]})
+                if (t->ptr) t->ptr = static_cast<T*>(t->ptr) + first * t->ld_row;
+        const uint32_t grid = div_up(s.a.tokens, r.per);
+        if (r.a.interleaved) k_rotary<T, V, true><<<grid, GS_BLOCK, 0, st>>>(s);
+        else k_rotary<T, V, false><<<grid, GS_BLOCK, 0, st>>>(s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // Whether every V-element piece that the kernel touches is aligned to its size.

@@ -162,3 +162,27 @@ def test_norm_of_very_many_rows(tk, rows, cols, dtype):
     within(y[at], want, (ref.UNIT[dtype] + 41 * 2.0 ** -24) * want.abs() + 4 * ref.TINY[dtype], "y")
     few = tk.rms_norm(x[at], w, 1e-6, eight_bit=True)
     assert torch.equal(e.q[at].float(), few.q.float()) and torch.equal(e.scale[at], few.scale)
+
+
+def test_rotary_of_very_many_tokens(tk):
+    """More workgroups than a launch holds: 2^27 tokens of one head of 512, 137 GB turned in place."""
+    n, dim, slab = (1 << 27) + 9, 512, 1 << 20
+    if torch.cuda.mem_get_info()[0] < (n * dim * 2) * 5 // 4:
+        torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < (n * dim * 2) * 5 // 4:
+        pytest.skip("needs 172 GB of free memory")
+    g = gen(43)
+    x = torch.empty(n, 1, dim, dtype=BF, device="cuda")
+    some = randn(g, slab, 1, dim, dtype=BF)
+    for first in range(0, n, slab):
+        x[first:first + slab].copy_(some[:min(slab, n - first)])
+    pos = torch.rand(n, 1, generator=g, device="cuda") * 100
+    freq = torch.rand(dim // 2, generator=g, device="cuda")
+    edge = [e + d for e in (0, 1 << 25, 1 << 26, 3 << 25, 1 << 27) for d in (-1, 0, 1) if 0 <= e + d < n] + [n - 1]
+    at = torch.cat((torch.tensor(edge, device="cuda"), torch.randint(0, n, (2000,), generator=g, device="cuda")))
+    before = x[at]
+    tk.rotary(x, pos, freq, [dim // 2], inplace=True)
+    want = tk.rotary(before, pos[at], freq, [dim // 2])[0]
+    assert torch.equal(x[at], want)
+    del x, pos
+    torch.cuda.empty_cache()
