@@ -175,13 +175,15 @@ class Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, how):
         out, lse = attention(q, k, v, **how)
-        ctx.save_for_backward(q, k, v, out, lse)
-        ctx.how = how
+        tensors = {n: t for n, t in how.items() if isinstance(t, torch.Tensor)}
+        ctx.save_for_backward(q, k, v, out, lse, *tensors.values())
+        ctx.names, ctx.how = tuple(tensors), {n: t for n, t in how.items() if n not in tensors}
         ctx.mark_non_differentiable(lse)
         return out, lse
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout, _):
-        q, k, v, out, lse = ctx.saved_tensors
-        return (*attention_backward(dout.contiguous(), q, k, v, out, lse, **ctx.how), None)
+        q, k, v, out, lse, *tensors = ctx.saved_tensors
+        how = dict(ctx.how, **dict(zip(ctx.names, tensors)))
+        return (*attention_backward(dout.contiguous(), q, k, v, out, lse, **how), None)

@@ -119,3 +119,27 @@ def test_a_call_runs_on_its_tensors_device(monkeypatch):
     tokens.attention_backward(t, t, t, t, out, lse.as_subclass(Elsewhere))
     assert seen == [(n, 1) for n in ("gs_rms_norm", "gs_rms_norm_bwd", "gs_rotary", "gs_attention", "gs_attention_bwd")]
     assert now == [0]
+
+
+@pytest.mark.parametrize("name", ["cu_q", "cu_k", "key_on"])
+def test_starts_and_flags_that_change_before_the_backward_are_noticed(tk, name):
+    """A buffer that the next step fills again must not reach this step's gradient."""
+    q, k = rand(5, 2, 8).requires_grad_(), rand(6, 2, 8)
+    how = dict(scale=0.5, cu_q=torch.tensor([0, 5], dtype=torch.int32), cu_k=torch.tensor([0, 6], dtype=torch.int32),
+               key_on=torch.tensor([1, 1, 0, 1, 1, 1], dtype=torch.uint8))
+    y, _ = tk.Attention.apply(q, k, k, how)
+    how[name].zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+def test_the_arguments_are_those_of_the_forward(tk):
+    q, k, v = rand(5, 2, 8).requires_grad_(), rand(6, 2, 8), rand(6, 2, 8, seed=1)
+    grads = []
+    for change in (False, True):
+        how = dict(scale=0.5, key_on=torch.tensor([1, 1, 0, 1, 1, 1], dtype=torch.uint8))
+        y, _ = tk.Attention.apply(q, k, v, how)
+        if change:
+            how.update(scale=2.0, key_on=None)
+        grads.append(torch.autograd.grad(y.pow(2).sum(), q)[0])
+    assert torch.equal(*grads)
