@@ -787,7 +787,8 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  *     are: out 0, lse -infinity, dq, dk and dv 0.
  *   q [n_q, heads, dim], k, v [n_k, kv_heads, dim]; GS_BF16 or GS_F16; pointers
  *     16-byte aligned, strides and dim multiples of 8 elements, dim <= 128, row
- *     strides from dim to GS_ATTN_MAX_STRIDE elements (of a single row: any).
+ *     strides from dim to GS_ATTN_MAX_STRIDE elements (of a single row, and the
+ *     head stride of a single head: any).
  *     key_on [n_k] uint8.
  *   out: as q; lse [n_q, heads] fp32, dense
  *   ws: gs_attention_ws_bytes(a, 0) bytes (can be 0: ws may be NULL), 16-byte

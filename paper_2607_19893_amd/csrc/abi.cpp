@@ -659,13 +659,16 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
     return ok();
 }
 
-static gs_status check_attn_rows(const gs_rows& r, int32_t rows, int32_t dim, const char* name, const char* what) {
+static gs_status check_attn_rows(const gs_rows& r, int32_t rows, int32_t heads, int32_t dim, const char* name,
+                                 const char* what) {
     if (rows == 0) return GS_OK;
     GS_REQUIRE(rows == 1 || (r.ld_row >= dim && r.ld_row <= GS_ATTN_MAX_STRIDE),
                "%s: row stride %lld of %s outside dim..%d", what, (long long)r.ld_row, name, GS_ATTN_MAX_STRIDE);
     GS_REQUIRE(r.ptr != nullptr, "%s: null %s", what, name);
     GS_REQUIRE(aligned(r.ptr, 16), "%s: %s must be 16-byte aligned", what, name);
-    GS_REQUIRE((rows == 1 || r.ld_row % 8 == 0) && r.ld_head % 8 == 0, "%s: strides of %s must be multiples of 8 elements", what, name);
+    // the only row has no next one, nor has the only head
+    GS_REQUIRE((rows == 1 || r.ld_row % 8 == 0) && (heads == 1 || r.ld_head % 8 == 0),
+               "%s: strides of %s must be multiples of 8 elements", what, name);
     return GS_OK;
 }
 
@@ -692,9 +695,9 @@ static gs_status check_attn(const gs_attn* a, const char* what) {
         return fail(GS_ERR_UNSUPPORTED, "%s: %d segments of %d key heads are more than 2^24 tiles", what, a->n_seg,
                     a->kv_heads);
     gs_status s;
-    if ((s = check_attn_rows(a->q, a->n_q, a->dim, "q", what)) != GS_OK) return s;
-    if ((s = check_attn_rows(a->k, a->n_k, a->dim, "k", what)) != GS_OK) return s;
-    return check_attn_rows(a->v, a->n_k, a->dim, "v", what);
+    if ((s = check_attn_rows(a->q, a->n_q, a->heads, a->dim, "q", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(a->k, a->n_k, a->kv_heads, a->dim, "k", what)) != GS_OK) return s;
+    return check_attn_rows(a->v, a->n_k, a->kv_heads, a->dim, "v", what);
 }
 
 size_t gs_attention_ws_bytes(const gs_attn* a, int32_t backward) {
@@ -710,7 +713,7 @@ gs_status gs_attention(const gs_attn* a, const gs_rows* out, float* lse, void* w
     if ((s = check_attn(a, what)) != GS_OK) return s;
     GS_REQUIRE(out != nullptr, "%s: null out", what);
     if (a->n_q == 0) return ok();
-    if ((s = check_attn_rows(*out, a->n_q, a->dim, "out", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(*out, a->n_q, a->heads, a->dim, "out", what)) != GS_OK) return s;
     GS_REQUIRE(lse != nullptr && aligned(lse, 4), "%s: null or misaligned lse", what);
     const size_t need = gsmi::attention_ws_bytes(*a);
     GS_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), "%s: workspace must be 16-byte aligned device memory",
@@ -724,11 +727,11 @@ gs_status gs_attention_bwd(const gs_attn* a, const gs_attn_grads* g, void* ws, s
     gs_status s;
     if ((s = check_attn(a, what)) != GS_OK) return s;
     GS_REQUIRE(g != nullptr, "%s: null gradients", what);
-    if ((s = check_attn_rows(g->out, a->n_q, a->dim, "out", what)) != GS_OK) return s;
-    if ((s = check_attn_rows(g->dout, a->n_q, a->dim, "dout", what)) != GS_OK) return s;
-    if ((s = check_attn_rows(g->dq, a->n_q, a->dim, "dq", what)) != GS_OK) return s;
-    if ((s = check_attn_rows(g->dk, a->n_k, a->dim, "dk", what)) != GS_OK) return s;
-    if ((s = check_attn_rows(g->dv, a->n_k, a->dim, "dv", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->out, a->n_q, a->heads, a->dim, "out", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dout, a->n_q, a->heads, a->dim, "dout", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dq, a->n_q, a->heads, a->dim, "dq", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dk, a->n_k, a->kv_heads, a->dim, "dk", what)) != GS_OK) return s;
+    if ((s = check_attn_rows(g->dv, a->n_k, a->kv_heads, a->dim, "dv", what)) != GS_OK) return s;
     GS_REQUIRE(a->n_q == 0 || (g->lse != nullptr && aligned(g->lse, 4)), "%s: null or misaligned lse", what);
     const size_t need = gsmi::attention_bwd_ws_bytes(*a);
     GS_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), "%s: workspace must be 16-byte aligned device memory",

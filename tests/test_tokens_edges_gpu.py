@@ -147,6 +147,21 @@ def test_rotary_in_place_is_seen_by_autograd(tk):
         y.backward()
 
 
+@pytest.mark.parametrize("stride", [0, 3, 1 << 40])
+@pytest.mark.parametrize("nq,nk", [(150, 150), (3, 900)])
+def test_attention_of_a_single_head_with_any_head_stride(tk, nq, nk, stride):
+    """A tensor of one head may carry any head stride: it has no next head."""
+    c = case([nq], [nk], 1, dim=64)
+    g, q, k, v, _ = inputs(c)
+    dout = randn(g, *q.shape, dtype=BF)
+    want = tk.attention(q, k, v)
+    grads = tk.attention_backward(dout, q, k, v, *want)
+    q, k, v, dout, out = (t.as_strided(t.shape, (64, stride, 1)) for t in (q, k, v, dout, want[0]))
+    got = tk.attention(q, k, v)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert all(torch.equal(a, b) for a, b in zip(tk.attention_backward(dout, q, k, v, out, want[1]), grads))
+
+
 @pytest.mark.parametrize("rows,cols,dtype", [((1 << 23) + 5, 8, BF), ((1 << 27) + 3, 4, F32)])
 def test_norm_of_very_many_rows(tk, rows, cols, dtype):
     """More rows than a launch of one thread group a row holds."""
