@@ -34,16 +34,16 @@ class RegionRefiner:
         self.gain, self.eps = gain, 1e-6
         dev = trainer.dev
         n = trainer.n
-        self.base = torch.cat([p.reshape(n, -1) for p in trainer.params], 1)
-        self.shift = self.base.mean(0)
-        self.spread = self.base.std(0).clamp_min(1e-3)
+        base = self.base
+        self.shift = base.mean(0)
+        self.spread = base.std(0).clamp_min(1e-3)
         self.starts = torch.arange(0, n + self.region, self.region, device=dev).clamp_max(n)
         # a third of the pairs per axis, over distances from the pool's extent down to a thousandth of it
         per = self.dim // 2 // AXES
         freq, _ = gsmi.gs_rotary_freqs(per, base=1000.0)
         self.freq = torch.from_numpy(freq).to(dev).repeat(AXES)
         self.axis_pairs = (per,) * AXES
-        extent = float((self.base[:, :3].amax(0) - self.base[:, :3].amin(0)).amax())
+        extent = float((base[:, :3].amax(0) - base[:, :3].amin(0)).amax())
         self.place = 100.0 / max(extent, 1e-6)
         g = torch.Generator(device=dev)
         g.manual_seed(seed)
@@ -60,6 +60,15 @@ class RegionRefiner:
         self.opt = torch.optim.Adam(list(self.w.values()), lr=lr)
         self.last = None                      # (ids, h, total) of the last forward, for publish()
 
+    def rows(self, ids):
+        """[len(ids), row_len] rows of the pool, as they are now."""
+        return torch.cat([p[ids].reshape(-1, c) for p, c in zip(self.tr.params, self.tr.cols)], 1)
+
+    @property
+    def base(self):
+        """All rows of the pool."""
+        return self.rows(slice(None))
+
     def visible_ids(self, cam):
         """Ids the camera sees, ascending (synchronizes for their number)."""
         self.tr.project(cam)
@@ -67,11 +76,11 @@ class RegionRefiner:
         count = int(to_u32(self.tr.counts[0:1])[0])
         return self.tr.vis_idx[:count].long()
 
-    def corrections(self, ids):
-        """[V, row_len] corrections of the rows `ids` (ascending), under autograd."""
+    def corrections(self, ids, rows=None):
+        """[V, row_len] corrections of the rows `ids` (ascending), under autograd.  rows: those rows, if at hand."""
         bf = torch.bfloat16
         w = {k: v.to(bf) if v.dim() == 2 else v for k, v in self.w.items()}
-        rows = self.base[ids]
+        rows = self.rows(ids) if rows is None else rows
         cu = torch.searchsorted(ids, self.starts).int()
         pos = (rows[:, :AXES] * self.place).contiguous()
         x = ((rows - self.shift) / self.spread).to(bf) @ w["inp"]
@@ -96,14 +105,15 @@ class RegionRefiner:
         tensor).  target: 3*H*W floats on the device, or None for the trainer's target buffer."""
         tr = self.tr
         ids = self.visible_ids(cam)
-        delta = self.corrections(ids)
-        self.write_rows(ids, self.base[ids] + delta.detach())
+        rows = self.rows(ids)
+        delta = self.corrections(ids, rows)
+        self.write_rows(ids, rows + delta.detach())
         seen = self.visible_ids(cam)                       # of the corrected rows: some of `ids`
         tr.bin_sort()
         tr.raster_fwd_l1(target)
         tr.raster_bwd_pixels()
         tr.raster_bwd_project()
-        self.write_rows(ids, self.base[ids])
+        self.write_rows(ids, rows)
         grad = torch.zeros_like(delta)
         grad[torch.searchsorted(ids, seen)] = tr.grad_rows[:seen.numel(), :tr.row_len]
         self.opt.zero_grad(set_to_none=True)

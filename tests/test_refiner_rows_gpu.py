@@ -1,0 +1,48 @@
+"""The region refiner and a pool that others write: rows as they are now, rows put back, tokens of one state."""
+import pytest
+import torch
+
+import token_refs as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def made():
+    from paper_2607_19893_amd import scenes
+    from paper_2607_19893_amd.pipeline import ViewTrainer
+    from paper_2607_19893_amd.refiner import RegionRefiner
+    w = scenes.spatially_ordered(scenes.tiny(n=3000))
+    cam = w.cameras[0]
+    tr = ViewTrainer(w.scene, capacity=1 << 17, max_width=cam.width, max_height=cam.height)
+    tr.ensure_capacity([cam], margin=4.0)
+    tr.set_target(w.target(0))
+    return tr, cam, RegionRefiner(tr, region=257, seed=3, lr=0.05)
+
+
+def pool(tr):
+    return [p.clone() for p in tr.params]
+
+
+def test_a_step_keeps_what_others_wrote(made):
+    tr, cam, net = made
+    net.step(cam)
+    for p in tr.params:
+        p.mul_(1.001)
+    now = pool(tr)
+    net.step(cam)
+    assert all(torch.equal(a, b) for a, b in zip(now, tr.params))
+
+
+def test_corrections_follow_the_pool(made):
+    tr, cam, net = made
+    ids = net.visible_ids(cam)
+    with torch.no_grad():
+        first = net.corrections(ids)
+        saved = pool(tr)
+        for p in tr.params:
+            p.mul_(1.1)
+        assert not torch.equal(net.corrections(ids), first)
+        for p, q in zip(tr.params, saved):
+            p.copy_(q)
+        assert torch.equal(net.corrections(ids), first)
