@@ -107,13 +107,15 @@ class RegionRefiner:
         ids = self.visible_ids(cam)
         rows = self.rows(ids)
         delta = self.corrections(ids, rows)
-        self.write_rows(ids, rows + delta.detach())
-        seen = self.visible_ids(cam)                       # of the corrected rows: some of `ids`
-        tr.bin_sort()
-        tr.raster_fwd_l1(target)
-        tr.raster_bwd_pixels()
-        tr.raster_bwd_project()
-        self.write_rows(ids, rows)
+        try:
+            self.write_rows(ids, rows + delta.detach())
+            seen = self.visible_ids(cam)                   # of the corrected rows: some of `ids`
+            tr.bin_sort()
+            tr.raster_fwd_l1(target)
+            tr.raster_bwd_pixels()
+            tr.raster_bwd_project()
+        finally:
+            self.write_rows(ids, rows)
         grad = torch.zeros_like(delta)
         grad[torch.searchsorted(ids, seen)] = tr.grad_rows[:seen.numel(), :tr.row_len]
         self.opt.zero_grad(set_to_none=True)

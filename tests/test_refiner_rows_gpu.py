@@ -46,3 +46,17 @@ def test_corrections_follow_the_pool(made):
         for p, q in zip(tr.params, saved):
             p.copy_(q)
         assert torch.equal(net.corrections(ids), first)
+
+
+@pytest.mark.parametrize("phase", ["bin_sort", "raster_bwd_pixels"])
+def test_rows_are_put_back_when_a_phase_fails(made, phase, monkeypatch):
+    tr, cam, net = made
+    before = pool(tr)
+
+    def fail(*a, **k):
+        raise RuntimeError("no " + phase)
+
+    monkeypatch.setattr(tr, phase, fail)
+    with pytest.raises(RuntimeError, match="no " + phase):
+        net.step(cam)
+    assert all(torch.equal(a, b) for a, b in zip(before, tr.params))
