@@ -58,7 +58,7 @@ class RegionRefiner:
         for k in ("norm1", "norm2", "norm3"):
             self.w[k] = torch.ones(width, device=dev, requires_grad=True)
         self.opt = torch.optim.Adam(list(self.w.values()), lr=lr)
-        self.last = None                      # (ids, h, total) of the last forward, for publish()
+        self.last = self.last_norm = None     # (ids, total) of the last forward and its last norm's weight, for publish()
 
     def rows(self, ids):
         """[len(ids), row_len] rows of the pool, as they are now."""
@@ -92,7 +92,7 @@ class RegionRefiner:
         y, total = tokens.RmsNorm.apply(o.reshape(-1, self.width) @ w["out"], total, w["norm2"], self.eps)
         h = torch.nn.functional.silu(y @ w["up"]) @ w["down"]
         y, last = tokens.RmsNorm.apply(h, total, w["norm3"], self.eps)
-        self.last = (ids, last.detach())
+        self.last, self.last_norm = (ids, last.detach()), w["norm3"].detach().clone()
         return (y @ w["head"]).float() * (self.gain * self.spread)
 
     def write_rows(self, ids, rows):
@@ -137,10 +137,10 @@ class RegionRefiner:
         return gsmi.make_groups([table[:, :a], table[:, a:a + b]])
 
     def publish(self, version, table, msg, status):
-        """Stages the last step's tokens (their last norm, 8 bits) as a message: `table` [n, words] takes the rows
-        by id, the message those of the ids."""
+        """Stages the last step's tokens (their last norm with the weight of that forward, 8 bits) as a message:
+        `table` [n, words] takes the rows by id, the message those of the ids."""
         ids, total = self.last
-        r = tokens.rms_norm(total, self.w["norm3"].detach(), self.eps, eight_bit=True)
+        r = tokens.rms_norm(total, self.last_norm, self.eps, eight_bit=True)
         table[ids] = torch.cat((r.q.view(torch.float32), r.scale), 1)
         count = torch.tensor([ids.numel()], dtype=torch.int32, device=table.device)
         gsmi.gs_delta_pack(ids.int(), count, self.tr.n, self._groups(table), 2, version, msg, status)

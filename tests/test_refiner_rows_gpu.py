@@ -60,3 +60,19 @@ def test_rows_are_put_back_when_a_phase_fails(made, phase, monkeypatch):
     with pytest.raises(RuntimeError, match="no " + phase):
         net.step(cam)
     assert all(torch.equal(a, b) for a, b in zip(before, tr.params))
+
+
+def test_published_tokens_are_of_the_forward(made):
+    tr, cam, net = made
+    for _ in range(4):
+        weight = net.w["norm3"].detach().clone()
+        net.step(cam)
+    assert float((net.w["norm3"].detach() - weight).abs().max()) > 0.01     # the step moved it
+    status = torch.zeros(4, dtype=torch.int32, device=tr.dev)
+    r = net.publish(1, net.replica_table(), net.message(), status)
+    torch.cuda.synchronize()
+    ids, total = net.last
+    y, _ = ref.norm(total, weight, net.eps)
+    got = r.q.double() * r.scale.double().repeat_interleave(128, 1)[:, :net.width]
+    # e4m3: half a step of 2^-3 of an element, and half of 2^-9 of the scale near zero
+    assert bool(((got - y).abs() <= y.abs() * (2.0 ** -4 + 1e-3) + r.scale.double() * 2.0 ** -10).all())
