@@ -162,6 +162,28 @@ def test_attention_of_a_single_head_with_any_head_stride(tk, nq, nk, stride):
     assert all(torch.equal(a, b) for a, b in zip(tk.attention_backward(dout, q, k, v, out, want[1]), grads))
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_large_equal_scores_beside_rising_ones(tk, dtype):
+    """Rows whose scores are all the same large number, in a wave with one whose maximum rises at every step: what they
+    have summed keeps its weight.  Values are +1 in the first half and -1 in the second, so the mean is 0."""
+    n, heads = 8192, 8
+    q = torch.zeros(n, heads, 64, dtype=dtype, device="cuda")
+    k, v = (torch.zeros(n, heads, 64, dtype=dtype, device="cuda") for _ in range(2))
+    q[..., 0] = 64.0
+    q[::32, :, 0] = 0.0
+    q[::32, :, 1] = 64.0
+    k[..., 0] = 508.0                                  # 32512 scale log2(e) lies between two fp32 numbers
+    k[..., 1] = (torch.arange(n, device="cuda") // 64).to(dtype)[:, None]       # 8 a step: 11.5 powers of two
+    v[:n // 2], v[n // 2:] = 1.0, -1.0
+    out, lse = tk.attention(q, k, v, scale=0.125)
+    flat = torch.arange(n, device="cuda") % 32 != 0
+    # one rounding of each probability and of the result, fp32 sums (as in token_refs.attention)
+    room = ref.UNIT[dtype] + 2e-5
+    assert float(out[flat].float().abs().max()) <= room, float(out[flat].float().abs().max())
+    s = 8.0 * float(k[0, 0, 0])
+    assert float((lse[flat].double() - (s + math.log(n))).abs().max()) <= 2e-5 * (1 + s)
+
+
 @pytest.mark.parametrize("rows,cols,dtype", [((1 << 23) + 5, 8, BF), ((1 << 27) + 3, 4, F32)])
 def test_norm_of_very_many_rows(tk, rows, cols, dtype):
     """More rows than a launch of one thread group a row holds."""
