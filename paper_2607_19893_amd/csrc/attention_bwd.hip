@@ -518,7 +518,8 @@ DkvPlan dkv_plan(const gs_attn& a) {
         most = std::max(most, hi - lo);
     }
     const int64_t groups = (int64_t)attn_tiles(a.n_k, kRows, a.n_seg) * a.kv_heads;
-    const int64_t steps = (rows / kTiles + st - 1) / st * group, longest = (most + st - 1) / st * group;
+    const int64_t mean = (rows + kTiles - 1) / kTiles;     // rounded up: below one, a part would be as short as can be
+    const int64_t steps = (mean + st - 1) / st * group, longest = (most + st - 1) / st * group;
     const int64_t chunk = std::max<int64_t>(512 / st, groups * steps / (3 * kUnits));
     DkvPlan p;
     p.chunk = (int)std::min<int64_t>(chunk, 1 << 30);
