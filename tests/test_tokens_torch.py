@@ -143,3 +143,21 @@ def test_the_arguments_are_those_of_the_forward(tk):
             how.update(scale=2.0, key_on=None)
         grads.append(torch.autograd.grad(y.pow(2).sum(), q)[0])
     assert torch.equal(*grads)
+
+
+@pytest.mark.parametrize("short", [True, False])
+def test_current_stream_with_and_without_the_short_way(monkeypatch, short):
+    """torch's private calls for the stream's address are used where they exist; without them its public stream is."""
+    from paper_2607_19893_amd import gsmi
+    now = dict(device=1, streams={0: 0x1000, 1: 0x2000})
+    monkeypatch.setattr(gsmi, "_raw_stream", None)
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda: types.SimpleNamespace(cuda_stream=now["streams"][now["device"]]))
+    if short:
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: now["streams"][d], raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now["device"], raising=False)
+    else:
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    assert gsmi.current_stream().value == 0x2000
+    now["device"], now["streams"][0] = 0, 0x3000       # another device, another stream: nothing is kept
+    assert gsmi.current_stream().value == 0x3000
