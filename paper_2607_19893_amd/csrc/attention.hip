@@ -564,12 +564,15 @@ struct Plan {
 };
 
 // Few rows: where a segment's rows fit one 32-row tile on average.  The keys of
-// all segments and key heads are cut into parts for one workgroup a compute unit
-// (three up to 64 elements, where three fit one), but at least 256 keys, which
-// pay for a start and a join; a longer segment has more of them.  24 regions of
-// 900..9000 keys of 64: 85 us for three a unit, 93 for two, 92 for four, 99 when
-// every segment had the same number of parts; one row over 32,768 keys of 128: 38
-// us for one a unit, 39 for two.  The parts' sums may take 64 MB.
+// all segments and key heads are cut into parts for one workgroup a compute unit,
+// or for three where the segments' lengths may differ (two are there at a time,
+// the third evens out the ends), but at least 256 keys, which pay for a start and
+// a join; a longer segment has more of them.  Heads of 32, 64, 96 and 128, one a
+// unit against three: 24 regions of 900..9000 keys, 16 heads, 62 100 157 169
+// against 66 87 143 151 us; one row over 32,768 keys, 32/8 heads, 21 24 32 38
+// against 21 29 36 42.  Equal segments of 64, 16/8 heads: 8 of 16,384 65 against
+// 77, 64 of 1500 56 against 67, 24 of 4000 63 against 59.  The parts' sums may
+// take 64 MB.
 // More rows: 128-row tiles, and the keys into parts where those tiles leave
 // compute units idle.
 Plan plan(const gs_attn& a) {
@@ -581,7 +584,7 @@ Plan plan(const gs_attn& a) {
     if (p.few) {
         const bool equal = a.cu_q == nullptr || a.n_seg == 1;
         const int64_t longest = equal ? keys : a.n_k;      // as far as it is known here
-        const int64_t want = kUnits * (a.dim <= 64 ? 3 : 1);
+        const int64_t want = kUnits * (equal ? 1 : 3);
         const int64_t part = std::max<int64_t>(1, (int64_t)a.n_q * a.heads) * a.dim * 4;
         const int64_t room = std::max<int64_t>(1, (64 << 20) / part);
         const int64_t most = std::min<int64_t>(kMaxSplits, room);
