@@ -773,12 +773,14 @@ gs_status gs_rotary_freqs(int32_t pairs, double base, int32_t scaling, double fa
  *   s_j = scale * q_i . k_j;  out_i = sum_j exp(s_j) v_j / sum_j exp(s_j);
  *   lse_i = log sum_j exp(s_j)
  * left = -1, right = 0 is the ordered (causal) form, right = left = -1 all keys.
- * A row that admits no key, or none with a score above -infinity, has out 0,
- * lse -infinity and passes no gradient.  Head h reads key head h / (heads /
- * kv_heads).  What the rows of k and v that key_on switches off hold reaches nothing
- * (NaN and infinities too), and their dk, dv are 0; so do rows of q and dout
+ * A row that admits no key has out 0, lse -infinity and passes no gradient; so
+ * does one whose scores are all -infinity, as long as its q and dout are finite.
+ * Head h reads key head h / (heads / kv_heads).
+ * What the rows of k and v that key_on switches off hold reaches nothing (NaN and
+ * infinities too), and their dk, dv are 0; nor does what rows of q and dout hold
  * that admit no key.  A NaN or infinity in a key that is on may reach every row
- * of its segment.
+ * of its segment, and one in a row of q or dout that admits a key the dk and dv
+ * of every key there, also past the window.
  *   cu_q, cu_k [n_seg + 1] int32, ascending from 0 to n_q and n_k: the segments'
  *     first rows (empty ones allowed); both NULL: n_seg segments of equal
  *     length (n_seg divides n_q and n_k).  Values outside [0, n] are taken as
@@ -827,6 +829,10 @@ gs_status gs_attention(const gs_attn* a, const gs_rows* out, float* lse, void* w
  *   dq_i = sum_j ds_ij k_j;  dk_j = sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
  * dk and dv of a shared head are summed over the heads that read it.  Nothing is
  * summed by atomics: the same call gives the same bits.
+ * p and ds / scale are rounded to the tokens' type for their products (the matrix
+ * unit's operands); the sums stay in fp32.  GS_F16 holds 2^-24 .. 65504: ds far
+ * below 2^-14 lose bits and those past 65504 are infinite, so gradients want the
+ * scale that the type wants anyway.
  *   out, dout, dq: as q; dk, dv: as k; lse as gs_attention left it
  *   ws: gs_attention_ws_bytes(a, 1) bytes, 16-byte aligned
  * Errors as for gs_attention.

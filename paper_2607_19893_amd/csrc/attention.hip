@@ -140,8 +140,9 @@ __device__ __forceinline__ bool softmax_step(acc16 (&s)[N], float c, float slack
 // TFLOP/s of the products that the mask leaves; matrix units busy 53% of the
 // cycles and vector units 54%, at clocks that the power limit sets (operands of
 // zeros run 1.35 times faster).  40 regions of 40..1600 fp16 tokens, 8 heads of
-// 64: 48 us, matrix 29% and vector 68%: there a score's exponential, maximum, sum
-// and rounding cost more issue cycles than its 256 multiply-adds.
+// 64: 48 us, vector units busy 66% and matrix units 28%, waves waiting for data 30%
+// of their time: a score's exponential, maximum, sum and rounding cost more issue
+// cycles there than its 256 multiply-adds.
 template <typename T, int D>
 __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(GS_BLOCK, D <= 64 ? 3 : 2) k_attention(FwdArgs
 // bytes bound it, so a step's keys go from memory straight into the operand's
 // registers, its values through a piece of LDS that only this wave touches (no
 // barrier in the loop), and both are fetched a step ahead.  One token over 32,768
-// keys, 16/4 heads of 128: 27 us, 4.9 TB/s.  24 segments of 1..16 rows over
+// keys, 32/8 heads of 128: 29 us, 4.6 TB/s.  24 segments of 1..16 rows over
 // 900..9000 keys, 16 heads of 64: 75 us, 4.2 TB/s (two waves a SIMD; held to the
 // registers of three it took 3 us more).
 constexpr int kFewRows = 32;

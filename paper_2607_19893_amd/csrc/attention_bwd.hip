@@ -57,8 +57,9 @@ __device__ __forceinline__ void store_tiles(T* p, const acc16 (&o)[DT], float sc
 
 // 64 keys a step.  8192 ordered tokens, 16/4 heads of 128: 413 us, 1.0 PFLOP/s of
 // its products under the power limit.  24 regions of 3..1500 tokens, 8 heads of
-// 64, a tenth of the keys off: 52 us, vector units busy 51% of the cycles and
-// matrix units 33%.
+// 64, a tenth of the keys off: 49 us in a kernel trace, whose two kernels together
+// take 112 where the untraced call takes 101; vector units busy 47% of the cycles,
+// matrix units 34%, waves waiting for data 42% of their time.
 // KEYS: keys may be off.  A step's keys then start their scores at 0 or -inf,
 // read from LDS into the tile that the products are added to.
 template <typename T, int D, bool KEYS>
@@ -240,7 +241,7 @@ constexpr int dkv_step(int dim) { return dim > 64 ? 32 : 64; }
 // is 32 rows; at 64 elements that form took 3 us more of 107.  8192 ordered
 // tokens, 16/4 heads of 128: 0.85 PFLOP/s of its products (644 us), matrix units
 // busy 56% of the cycles: two reads of LDS a matrix instruction where dq has
-// 1.3.  24 regions of 3..1500 tokens, 8 heads of 64: 63 us.
+// 1.3.  24 regions of 3..1500 tokens, 8 heads of 64: 63 us of the same trace.
 template <typename T, int D>
 __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_dkv(BwdArgs f) {
     constexpr int P = D <= 32 ? 32 : (D <= 64 ? 64 : 128), KT = D / 16, DT = D / 32;

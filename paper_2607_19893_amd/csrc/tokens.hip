@@ -20,9 +20,10 @@ namespace {
 // while a row fits 32 elements a lane; longer rows take four.  Rows of up to 256
 // columns are taken by the lanes that own one block of GS_NORM_BLOCK columns (16
 // or 32), several to a wave: 74,724 fp32 rows of 80 columns into 8 bits took 47
-// us with a wave each, whose lanes were two thirds idle, and take 17 so.
-//   50,001 bf16 rows of 1536 with a residual into 8 bits and scales: 96 us, 5.6
-// TB/s.  7 rows of 1024: 2.6 us, the start of a kernel and one read.
+// us with a wave each, whose lanes were two thirds idle, and take 18 so.
+//   50,001 bf16 rows of 1536 with a residual into 8 bits and scales: 99 us, 5.5
+// TB/s.  Rows that are not whole aligned pieces are loaded an element at a time:
+// bf16 rows of 1001 reach 1.2 TB/s where those of 1000 reach 5.7.  7 rows of 1024: 2.6 us, the start of a kernel and one read.
 // ---------------------------------------------------------------------------
 
 template <int TPR>
@@ -449,7 +450,9 @@ hipError_t norm_bwd_type(const gs_norm_bwd_args& a, float* parts, hipStream_t st
 // two V-element pieces of the head in either layout, and copies what is left
 // of the heads.  50,000 fp32 tokens, 8 + 8 heads of 64, three quarters turned by
 // three axes: 97 us, 4.2 TB/s; 32,768 bf16 tokens, 32 + 8 heads of 128: 132 us,
-// 5.1 TB/s.  Two and four pieces of a thread in flight took as long.
+// 5.1 TB/s.  Two and four pieces of a thread in flight took as long.  Where the
+// pairs are not whole pieces a thread turns four or one at a time: heads of 128 with
+// 64, 60 and 63 pairs reach 5.1, 3.9 and 2.2 TB/s.
 // ---------------------------------------------------------------------------
 
 constexpr int kRotTrig = 2048;                 // pairs of a workgroup's tokens in LDS (16 KB)

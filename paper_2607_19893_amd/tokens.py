@@ -128,7 +128,9 @@ def attention_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, n_seg=1, k
 
 
 class RmsNorm(torch.autograd.Function):
-    """RmsNorm.apply(x, residual or None, weight, eps) -> (y, total)."""
+    """RmsNorm.apply(x, residual or None, weight, eps) -> (y, total).
+
+    The gradient reads `total` as it was rounded to the tokens' type."""
 
     @staticmethod
     def forward(ctx, x, residual, weight, eps):
@@ -151,7 +153,9 @@ class RmsNorm(torch.autograd.Function):
 
 
 class Rotary(torch.autograd.Function):
-    """Rotary.apply(q, k, pos, freq, axis_pairs, interleaved, amplitude) -> (q, k)."""
+    """Rotary.apply(q, k, pos, freq, axis_pairs, interleaved, amplitude) -> (q, k).
+
+    q and k have gradients; pos, freq and amplitude have none (a position that is trained gets nothing from here)."""
 
     @staticmethod
     def forward(ctx, q, k, pos, freq, axis_pairs, interleaved, amplitude):
@@ -170,7 +174,9 @@ class Rotary(torch.autograd.Function):
 
 
 class Attention(torch.autograd.Function):
-    """Attention.apply(q, k, v, how) -> (out, lse); `how` holds attention()'s keyword arguments."""
+    """Attention.apply(q, k, v, how) -> (out, lse); `how` holds attention()'s keyword arguments.
+
+    q, k and v have gradients through out; lse is marked as not differentiable."""
 
     @staticmethod
     def forward(ctx, q, k, v, how):
