@@ -223,3 +223,25 @@ def test_rotary_of_very_many_tokens(tk):
     assert torch.equal(x[at], want)
     del x, pos
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("cols", [1, 40, 128, 200, 256, 1000, 1536, 2048, 2500, 8200, 16384])
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+def test_norm_8bit_of_tiny_blocks_at_every_width(tk, cols, dtype):
+    """Rows that share a wave, a row a wave and a row a workgroup: tiny and zero blocks get their numbers and leave the
+    bits of the rows beside them as they are."""
+    g = gen(24 + cols)
+    x = randn(g, 37, cols)
+    w = 1 + 0.2 * randn(g, cols)
+    tiny = torch.arange(37, device="cuda") % 3 == 1
+    block = torch.arange(cols, device="cuda") // 128 % 2 == (1 if cols > 128 else 0)
+    alone = tk.rms_norm(x[~tiny].to(dtype), w, 1e-6, eight_bit=True)
+    small = 6e-8 if dtype == HF else 1e-38
+    x[tiny] = torch.where(block, x[tiny] * small, x[tiny])
+    x[1] = 0.0
+    x[4] = 0.0
+    x[4, cols // 2] = small
+    x = x.to(dtype)
+    e = tk.rms_norm(x, w, 1e-6, eight_bit=True)
+    check_8bit(e, ref.norm(x, w, 1e-6)[0])
+    assert torch.equal(e.q[~tiny].float(), alone.q.float()) and torch.equal(e.scale[~tiny], alone.scale)
