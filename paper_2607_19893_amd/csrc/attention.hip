@@ -470,8 +470,8 @@ __global__ void __launch_bounds__(GS_BLOCK, 2) k_attention_few(FwdArgs f) {
 // of a wave on their way at once.  Bound by the latency of these two reads, one
 // behind the other.  A wave a row where there are up to 8 parts on average (24
 // segments, 16 heads of 64: the call 83.2 us, 84.9 with four waves), four up to
-// 64 (64 parts of 16 rows of 128: 4.2 us), 16 beyond (256 parts: the call 19.4 us,
-// 20.0 with four).
+// 64 (32 parts of 32 rows of 128: 4.2 us), 16 beyond (one row of 128 in 256 parts:
+// the call 18.4 us, 19.9 with four).
 constexpr int kMaxSplits = 256;
 
 template <typename T, int WAVES>

@@ -3,8 +3,8 @@ the residual's addition, the rotation by position and attention over ragged
 segments, each with its gradient.
 
 The functions allocate their outputs and workspaces with torch on the current
-stream and call the gs_* entry points there; every step runs in libgsmi's
-kernels.  `RmsNorm`, `Rotary` and `Attention` put them under torch's autograd;
+stream of their tensors' GPU and call the gs_* entry points there; every step
+runs in libgsmi's kernels.  `RmsNorm`, `Rotary` and `Attention` put them under torch's autograd;
 their gradients have none of their own, a second derivative raises.
 """
 from __future__ import annotations
