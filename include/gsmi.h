@@ -625,8 +625,10 @@ gs_status gs_admission_gate(const uint32_t* RB, const uint32_t* D, const gs_gate
 /* ------------------------------------------------------------------------
  * Token operators.  A network that writes rows of the pool (one token per
  * primitive, region or view; its gradient arrives as gs_raster_bwd's rows)
- * runs its norms, rotations by position and attention through the calls
- * below; its plain matrix products stay with the caller's library.
+ * runs its lookups, norms, rotations by position, mixing of tokens (attention,
+ * or a recurrence where the cost has to be linear) and gated activations
+ * through the calls below; its plain matrix products stay with the caller's
+ * library.
  *
  * Token matrices: [rows, heads, dim] views, element (r, h, c) at
  * ptr + r * ld_row + h * ld_head + c (strides in elements; elements of a head
@@ -843,6 +845,253 @@ typedef struct {
 } gs_attn_grads;
 
 gs_status gs_attention_bwd(const gs_attn* a, const gs_attn_grads* g, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Layer norm with the residual's addition, a row at a time:
+ *   s = x + residual;  m = mean(s);  y = (s - m) * w / sqrt(mean((s - m)^2) + eps) + b
+ * y is formed from the fp32 sum, not from its rounding into `total`; the variance
+ * is summed from the differences, so a large mean costs it nothing but the
+ * mean's own rounding.
+ *   x, residual, total, y: [rows, cols] of `dtype` (any of the three types), at
+ *     any alignment of an element, rows ld_* elements apart (>= cols); residual
+ *     NULL: s = x; total or y NULL: not written.  total may be x or residual
+ *     itself, y may be x (the same rows, not shifted ones).
+ *   weight [cols] fp32; bias [cols] fp32 or NULL (0)
+ * A NaN or infinity in x or residual makes its row's y NaN.
+ * Errors: GS_ERR_INVALID_ARG (null pointers, sizes below 0, a row stride below
+ * cols, pointers that are not a multiple of the element size, eps negative or
+ * not finite, nothing to write); GS_ERR_UNSUPPORTED for cols above
+ * GS_NORM_MAX_COLS.
+ */
+typedef struct {
+    int32_t rows, cols, dtype;
+    float eps;
+    const void* x;
+    const void* residual;
+    const float* weight;
+    const float* bias;
+    void* total;
+    void* y;
+    int64_t ld_x, ld_residual, ld_total, ld_y;
+} gs_layer_args;
+
+gs_status gs_layer_norm(const gs_layer_args* args, void* stream);
+
+/*
+ * Its gradient, with r = 1/sqrt(mean((total - m)^2) + eps), n = (total - m) * r
+ * and g = dy * w:
+ *   dx = r * (g - mean(g) - n * mean(g * n)) + dtotal
+ *   dweight = sum over rows of dy * n;  dbias = sum over rows of dy
+ * dx is the gradient of x and of residual alike.  The sums are taken in a fixed
+ * order: the same call gives the same bits.
+ *   dy, total (the forward's sum, or x without a residual), dtotal (NULL: 0; the
+ *   gradient that reaches the sum past the norm), dx: [rows, cols] of `dtype`;
+ *   dx may be dy, total or dtotal.  dweight [cols] fp32; dbias [cols] fp32 or
+ *   NULL (not written).
+ *   ws: gs_layer_norm_bwd_ws_bytes(rows, cols) bytes, 16-byte aligned
+ * Errors as for gs_layer_norm, and GS_ERR_WORKSPACE.
+ */
+typedef struct {
+    int32_t rows, cols, dtype;
+    float eps;
+    const void* dy;
+    const void* total;
+    const void* dtotal;
+    const float* weight;
+    void* dx;
+    float* dweight;
+    float* dbias;
+    int64_t ld_dy, ld_total, ld_dtotal, ld_dx;
+} gs_layer_bwd_args;
+
+size_t gs_layer_norm_bwd_ws_bytes(int32_t rows, int32_t cols);
+gs_status gs_layer_norm_bwd(const gs_layer_bwd_args* args, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rows of a table by the tokens' ids (of a primitive's cell, region or kind):
+ *   out[t] = scale * table[ids[t]]
+ * and 0 for an id outside [0, rows).  The product is formed in fp32 and rounded
+ * once to the tokens' type.
+ *   ids [tokens] int32
+ *   table [rows, dim] of table_dtype: GS_F32 or the tokens' type, rows ld_table
+ *     elements apart; out [tokens, dim] of `dtype` (any of the three types), rows
+ *     ld_out apart; both at any alignment of an element, strides >= dim
+ * Errors: GS_ERR_INVALID_ARG (null pointers, negative sizes, strides, alignment,
+ * types, a scale that is not finite); GS_ERR_UNSUPPORTED for dim above
+ * GS_EMBED_MAX_DIM.
+ */
+#define GS_EMBED_MAX_DIM 16384
+
+typedef struct {
+    int32_t dtype, table_dtype, tokens, rows, dim;
+    float scale;
+    const int32_t* ids;
+    const void* table;
+    void* out;
+    int64_t ld_table, ld_out;
+} gs_embed_args;
+
+gs_status gs_embedding(const gs_embed_args* args, void* stream);
+
+/*
+ * Its gradient: row j is scale * the sum of dout[t] over the tokens with
+ * ids[t] = j, in fp32 and in an order that ids alone fix: the same call gives the
+ * same bits.  Ids outside [0, rows) add to nothing.
+ *   dout [tokens, dim] of `dtype`, rows ld_dout elements apart
+ *   unique NULL: grad [rows, ld_grad] fp32 is the table's whole gradient (rows
+ *     without a token are 0); count is not used.
+ *   unique [min(tokens, rows)] int32: the ids that have a token, ascending;
+ *     count [1] how many; grad [min(tokens, rows), ld_grad] fp32 their rows, in
+ *     that order.  What gs_sparse_adam takes as its idx, count and grad_rows.
+ *     Behind the first *count, unique and grad are left as they were.
+ *   ws: gs_embedding_bwd_ws_bytes(tokens, rows, dim, unique != NULL) bytes,
+ *     16-byte aligned
+ * Errors as for gs_embedding; GS_ERR_UNSUPPORTED for tokens above
+ * GS_EMBED_MAX_TOKENS; GS_ERR_WORKSPACE.
+ */
+#define GS_EMBED_MAX_TOKENS 268435456
+
+typedef struct {
+    int32_t dtype, tokens, rows, dim;
+    float scale;
+    const int32_t* ids;
+    const void* dout;
+    float* grad;
+    int32_t* unique;
+    int32_t* count;
+    int64_t ld_dout, ld_grad;
+} gs_embed_bwd_args;
+
+size_t gs_embedding_bwd_ws_bytes(int32_t tokens, int32_t rows, int32_t dim, int32_t touched);
+gs_status gs_embedding_bwd(const gs_embed_bwd_args* args, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated linear recurrence over ragged segments: a mixer of tokens whose cost is
+ * linear in them (the primitives of a region in their spatial order, a stream of
+ * views).  Channel by channel, along each segment from its first token to its
+ * last (reverse != 0: from the last to the first):
+ *   a_t = 1 / (1 + exp(-gate_t));  h_t = a_t * h_{t-1} + (1 - a_t) * x_t;  y_t = h_t
+ * from initial's row of the segment (NULL: 0); the last state goes to `final`.
+ * The state is held in fp32; y is it, rounded to the tokens' type.
+ *   x, gate, y: [n, cols] of `dtype` (any of the three types), at any alignment
+ *     of an element, rows ld_* elements apart (>= cols)
+ *   cu [n_seg + 1] int32, ascending: the segments' first tokens (empty ones
+ *     allowed; NULL: n_seg segments of equal length, n_seg divides n).  Values
+ *     outside [0, n] are taken as the nearest in it.  Tokens outside every
+ *     segment reach nothing, and their y is left as it was (fill != 0: 0).
+ *   initial, final [n_seg, cols] fp32, dense, or NULL (final: not written).  An
+ *     empty segment's final is its initial.
+ *   kept NULL, or [ceil(n / GS_RECUR_KEEP), cols] fp32, dense: for the gradient,
+ *     row j is the state in front of place j * GS_RECUR_KEEP (places are counted
+ *     in the direction of the recurrence), 0 where that is a segment's first or
+ *     no segment's.
+ *   ws: gs_recurrence_ws_bytes(a) bytes (can be 0: ws may be NULL), 16-byte
+ *     aligned, for gs_recurrence and its gradient alike.  The size follows from
+ *     the sizes in `a`, not from cu's values.
+ * A segment of one token is a step of a served sequence.  The tokens are taken in
+ * an order that the sizes alone fix: the same call gives the same bits.  A NaN
+ * or infinity stays in its channel and segment, from its token on.
+ * Errors: GS_ERR_INVALID_ARG (null pointers, sizes, strides, alignment, dtype,
+ * n_seg that does not divide n without cu); GS_ERR_UNSUPPORTED (n above 2^30,
+ * n_seg above 2^28, or n / 128 * cols / 128 near 2^22 and above);
+ * GS_ERR_WORKSPACE.
+ */
+#define GS_RECUR_KEEP 64
+
+typedef struct {
+    int32_t dtype, n, cols, n_seg;
+    int32_t reverse, fill;
+    const int32_t* cu;
+    const void* x;
+    const void* gate;
+    const float* initial;
+    int64_t ld_x, ld_gate;
+} gs_recur;
+
+size_t gs_recurrence_ws_bytes(const gs_recur* a);
+gs_status gs_recurrence(const gs_recur* a, void* y, int64_t ld_y, float* final, float* kept, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/*
+ * Its gradient.  With D_t = dy_t + a_{t+1} * D_{t+1} (the last token: + dfinal):
+ *   dx_t = (1 - a_t) * D_t
+ *   dgate_t = a_t * (1 - a_t) * (h_{t-1} - x_t) * D_t
+ *   dinitial = a * D of the segment's first token (an empty segment's: dfinal)
+ * The states are formed again from `kept` in fp32.
+ *   dy, dx, dgate: [n, cols] of `dtype`; tokens outside every segment have their
+ *     dx and dgate left as they were (fill != 0: 0)
+ *   dfinal [n_seg, cols] fp32 or NULL (0); dinitial [n_seg, cols] fp32 or NULL
+ *     (not written); kept as gs_recurrence left it
+ * Errors as for gs_recurrence.
+ */
+typedef struct {
+    const void* dy;
+    const float* dfinal;
+    const float* kept;
+    void* dx;
+    void* dgate;
+    float* dinitial;
+    int64_t ld_dy, ld_dx, ld_dgate;
+} gs_recur_grads;
+
+gs_status gs_recurrence_bwd(const gs_recur* a, const gs_recur_grads* g, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated SiLU whose inputs can be kept in 8 bits for the gradient:
+ *   h = u / (1 + exp(-u)) * v          (v NULL: without the factor)
+ *   u, v, h: [rows, cols] of `dtype` (any of the three types), at any alignment
+ *     of an element, rows ld_* elements apart (>= cols); h NULL: not written
+ *   u8, v8 [rows, ld_*] uint8 (NULL: not kept; both or neither where v is given):
+ *     u and v in e4m3 (4 exponent bits, 3 mantissa bits, largest 448), in blocks
+ *     of GS_KEEP_BLOCK columns of a row (the last may be shorter), with a scale
+ *     byte a block: u ~ 2^(u_scale - 127) * u8, ties to even.  The power is the
+ *     least with max|u| <= 448 * it (and 2^-127 at least).  A NaN or infinity
+ *     becomes a NaN of u8 and does not touch the scale.
+ *   u_scale, v_scale [rows, ld_*_scale] uint8 (with u8, v8)
+ * Errors: GS_ERR_INVALID_ARG (null pointers, sizes, strides, alignment, dtype,
+ * nothing to write, u8 and v8 not together); GS_ERR_UNSUPPORTED for cols above
+ * GS_SILU_MAX_COLS.
+ */
+#define GS_KEEP_BLOCK 32
+#define GS_SILU_MAX_COLS 4194304
+
+typedef struct {
+    int32_t rows, cols, dtype;
+    const void* u;
+    const void* v;
+    void* h;
+    uint8_t* u8;
+    uint8_t* u_scale;
+    uint8_t* v8;
+    uint8_t* v_scale;
+    int64_t ld_u, ld_v, ld_h, ld_u8, ld_u_scale, ld_v8, ld_v_scale;
+} gs_silu_args;
+
+gs_status gs_gated_silu(const gs_silu_args* args, void* stream);
+
+/*
+ * Its gradient at the inputs that were kept (u, v are the values that u8, v8
+ * stand for), with s = 1 / (1 + exp(-u)):
+ *   du = dh * v * s * (1 + u * (1 - s));  dv = dh * u * s;  h = u * s * v
+ *   dh, du, dv, h: [rows, cols] of `dtype`; h NULL: not formed again (it is the
+ *     operand of a weight's gradient, which then need not be held either);
+ *     v8 and dv are NULL together; du, dv or h may be dh
+ * Errors as for gs_gated_silu.
+ */
+typedef struct {
+    int32_t rows, cols, dtype;
+    const void* dh;
+    const uint8_t* u8;
+    const uint8_t* u_scale;
+    const uint8_t* v8;
+    const uint8_t* v_scale;
+    void* du;
+    void* dv;
+    void* h;
+    int64_t ld_dh, ld_u8, ld_u_scale, ld_v8, ld_v_scale, ld_du, ld_dv, ld_h;
+} gs_silu_bwd_args;
+
+gs_status gs_gated_silu_bwd(const gs_silu_bwd_args* args, void* stream);
 
 /* ------------------------------------------------------------------------
  * Ahead-of-time planner (host).  The three calls below run on the CPU over

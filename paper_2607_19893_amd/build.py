@@ -23,7 +23,8 @@ BUILD_DIR = os.path.join(os.path.dirname(HERE), "_build", "gsmi")
 ARCH = os.environ.get("GSMI_ARCH", "gfx950")
 
 SOURCES = ["project.hip", "compact.hip", "binsort.hip", "raster.hip", "adam.hip", "delta.hip", "scope.hip",
-           "tokens.hip", "attention.hip", "attention_bwd.hip", "planner.cpp", "abi.cpp"]
+           "tokens.hip", "layernorm.hip", "embedding.hip", "recurrence.hip", "silu.hip", "attention.hip",
+           "attention_bwd.hip", "planner.cpp", "abi.cpp"]
 STRICT_FP = {"project.hip", "adam.hip", "planner.cpp"}
 
 

@@ -740,6 +740,208 @@ gs_status gs_attention_bwd(const gs_attn* a, const gs_attn_grads* g, void* ws, s
     return hip_status(gsmi::launch_attention_bwd(*a, *g, ws, static_cast<hipStream_t>(stream)), what);
 }
 
+gs_status gs_layer_norm(const gs_layer_args* a, void* stream) {
+    const char* what = "gs_layer_norm";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_norm_sizes(a->rows, a->cols, a->dtype, a->eps, a->weight, what)) != GS_OK) return s;
+    GS_REQUIRE(aligned(a->bias, 4), "%s: misaligned bias", what);
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(a->x, a->ld_x, a->rows, a->cols, es, "x", what)) != GS_OK) return s;
+    if (a->residual && (s = check_matrix(a->residual, a->ld_residual, a->rows, a->cols, es, "residual", what)) != GS_OK)
+        return s;
+    if (a->total && (s = check_matrix(a->total, a->ld_total, a->rows, a->cols, es, "total", what)) != GS_OK) return s;
+    if (a->y && (s = check_matrix(a->y, a->ld_y, a->rows, a->cols, es, "y", what)) != GS_OK) return s;
+    GS_REQUIRE(a->rows == 0 || a->total || a->y, "%s: no output", what);
+    if (a->rows == 0) return ok();
+    return hip_status(gsmi::launch_layer_norm(*a, static_cast<hipStream_t>(stream)), what);
+}
+
+size_t gs_layer_norm_bwd_ws_bytes(int32_t rows, int32_t cols) {
+    if (rows < 0 || cols < 0) return 0;
+    return gsmi::layer_norm_bwd_ws_bytes(rows, cols);
+}
+
+gs_status gs_layer_norm_bwd(const gs_layer_bwd_args* a, void* ws, size_t ws_bytes, void* stream) {
+    const char* what = "gs_layer_norm_bwd";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_norm_sizes(a->rows, a->cols, a->dtype, a->eps, a->weight, what)) != GS_OK) return s;
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(a->dy, a->ld_dy, a->rows, a->cols, es, "dy", what)) != GS_OK) return s;
+    if ((s = check_matrix(a->total, a->ld_total, a->rows, a->cols, es, "total", what)) != GS_OK) return s;
+    if (a->dtotal && (s = check_matrix(a->dtotal, a->ld_dtotal, a->rows, a->cols, es, "dtotal", what)) != GS_OK)
+        return s;
+    if ((s = check_matrix(a->dx, a->ld_dx, a->rows, a->cols, es, "dx", what)) != GS_OK) return s;
+    GS_REQUIRE(a->dweight != nullptr && aligned(a->dweight, 4), "%s: null or misaligned dweight", what);
+    GS_REQUIRE(aligned(a->dbias, 4), "%s: misaligned dbias", what);
+    GS_REQUIRE(ws != nullptr && aligned(ws, 16), "%s: workspace must be 16-byte aligned device memory", what);
+    if (ws_bytes < gsmi::layer_norm_bwd_ws_bytes(a->rows, a->cols))
+        return fail(GS_ERR_WORKSPACE, "%s: workspace too small", what);
+    return hip_status(gsmi::launch_layer_norm_bwd(*a, ws, static_cast<hipStream_t>(stream)), what);
+}
+
+static gs_status check_embed(int32_t dtype, int32_t tokens, int32_t rows, int32_t dim, float scale, const int32_t* ids,
+                             const char* what) {
+    GS_REQUIRE(dtype == GS_F32 || dtype == GS_BF16 || dtype == GS_F16, "%s: bad dtype %d", what, dtype);
+    GS_REQUIRE(tokens >= 0 && rows >= 0 && dim >= 1, "%s: tokens < 0, rows < 0 or dim < 1", what);
+    GS_REQUIRE(std::isfinite(scale), "%s: scale not finite", what);
+    GS_REQUIRE(tokens == 0 || (ids != nullptr && aligned(ids, 4)), "%s: null or misaligned ids", what);
+    if (dim > GS_EMBED_MAX_DIM) return fail(GS_ERR_UNSUPPORTED, "%s: dim %d above %d", what, dim, GS_EMBED_MAX_DIM);
+    return GS_OK;
+}
+
+gs_status gs_embedding(const gs_embed_args* a, void* stream) {
+    const char* what = "gs_embedding";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_embed(a->dtype, a->tokens, a->rows, a->dim, a->scale, a->ids, what)) != GS_OK) return s;
+    GS_REQUIRE(a->table_dtype == GS_F32 || a->table_dtype == a->dtype,
+               "%s: table_dtype %d is neither GS_F32 nor the tokens' type", what, a->table_dtype);
+    if ((s = check_matrix(a->table, a->ld_table, a->rows, a->dim, type_size(a->table_dtype), "table", what)) != GS_OK)
+        return s;
+    if ((s = check_matrix(a->out, a->ld_out, a->tokens, a->dim, type_size(a->dtype), "out", what)) != GS_OK) return s;
+    if (a->tokens == 0) return ok();
+    return hip_status(gsmi::launch_embedding(*a, static_cast<hipStream_t>(stream)), what);
+}
+
+size_t gs_embedding_bwd_ws_bytes(int32_t tokens, int32_t rows, int32_t dim, int32_t touched) {
+    if (tokens < 0 || rows < 0 || dim < 1 || dim > GS_EMBED_MAX_DIM || tokens > GS_EMBED_MAX_TOKENS) return 0;
+    return gsmi::embedding_bwd_ws_bytes(tokens, rows, dim, touched != 0);
+}
+
+gs_status gs_embedding_bwd(const gs_embed_bwd_args* a, void* ws, size_t ws_bytes, void* stream) {
+    const char* what = "gs_embedding_bwd";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_embed(a->dtype, a->tokens, a->rows, a->dim, a->scale, a->ids, what)) != GS_OK) return s;
+    if (a->tokens > GS_EMBED_MAX_TOKENS)
+        return fail(GS_ERR_UNSUPPORTED, "%s: %d tokens, above %d", what, a->tokens, GS_EMBED_MAX_TOKENS);
+    if ((s = check_matrix(a->dout, a->ld_dout, a->tokens, a->dim, type_size(a->dtype), "dout", what)) != GS_OK) return s;
+    GS_REQUIRE((a->unique != nullptr) == (a->count != nullptr), "%s: unique and count are given together", what);
+    GS_REQUIRE(aligned(a->unique, 4) && aligned(a->count, 4), "%s: misaligned unique or count", what);
+    const int32_t rows = a->unique ? std::min(a->tokens, a->rows) : a->rows;
+    if ((s = check_matrix(a->grad, a->ld_grad, rows, a->dim, 4, "grad", what)) != GS_OK) return s;
+    const size_t need = gsmi::embedding_bwd_ws_bytes(a->tokens, a->rows, a->dim, a->unique != nullptr);
+    GS_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), "%s: workspace must be 16-byte aligned device memory",
+               what);
+    if (ws_bytes < need) return fail(GS_ERR_WORKSPACE, "%s: workspace too small", what);
+    if (a->rows == 0 && a->unique == nullptr) return ok();
+    return hip_status(gsmi::launch_embedding_bwd(*a, ws, static_cast<hipStream_t>(stream)), what);
+}
+
+static gs_status check_recur(const gs_recur* a, const char* what) {
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    GS_REQUIRE(a->dtype == GS_F32 || a->dtype == GS_BF16 || a->dtype == GS_F16, "%s: bad dtype %d", what, a->dtype);
+    GS_REQUIRE(a->n >= 0 && a->cols >= 1 && a->n_seg >= 1, "%s: n < 0, cols < 1 or n_seg < 1", what);
+    GS_REQUIRE(aligned(a->cu, 4) && aligned(a->initial, 4), "%s: misaligned cu or initial", what);
+    GS_REQUIRE(a->cu != nullptr || a->n % a->n_seg == 0, "%s: %d segments of equal length do not divide %d tokens", what,
+               a->n_seg, a->n);
+    // places run up to a chunk past the end, and a launch holds fewer than 2^32 threads
+    if (a->n > 1 << 30) return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^30 tokens", what);
+    if (a->n_seg > 1 << 28) return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^28 segments", what);
+    if (((int64_t)a->n / 128 + 1) * ((int64_t)a->cols / 128 + 1) >= 1 << 22)
+        return fail(GS_ERR_UNSUPPORTED, "%s: %d tokens of %d channels are more than 2^22 workgroups", what, a->n, a->cols);
+    const size_t es = type_size(a->dtype);
+    gs_status s;
+    if ((s = check_matrix(a->x, a->ld_x, a->n, a->cols, es, "x", what)) != GS_OK) return s;
+    return check_matrix(a->gate, a->ld_gate, a->n, a->cols, es, "gate", what);
+}
+
+size_t gs_recurrence_ws_bytes(const gs_recur* a) {
+    if (a == nullptr || a->n < 0 || a->cols < 1) return 0;
+    return gsmi::recurrence_ws_bytes(*a);
+}
+
+static gs_status check_recur_ws(const gs_recur* a, const void* ws, size_t ws_bytes, const char* what) {
+    const size_t need = gsmi::recurrence_ws_bytes(*a);
+    GS_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16)), "%s: workspace must be 16-byte aligned device memory",
+               what);
+    if (ws_bytes < need) return fail(GS_ERR_WORKSPACE, "%s: workspace too small", what);
+    return GS_OK;
+}
+
+gs_status gs_recurrence(const gs_recur* a, void* y, int64_t ld_y, float* final, float* kept, void* ws, size_t ws_bytes,
+                        void* stream) {
+    const char* what = "gs_recurrence";
+    gs_status s;
+    if ((s = check_recur(a, what)) != GS_OK) return s;
+    if ((s = check_matrix(y, ld_y, a->n, a->cols, type_size(a->dtype), "y", what)) != GS_OK) return s;
+    GS_REQUIRE(aligned(final, 4) && aligned(kept, 4), "%s: misaligned final or kept", what);
+    if ((s = check_recur_ws(a, ws, ws_bytes, what)) != GS_OK) return s;
+    return hip_status(gsmi::launch_recurrence(*a, y, ld_y, final, kept, ws, static_cast<hipStream_t>(stream)), what);
+}
+
+gs_status gs_recurrence_bwd(const gs_recur* a, const gs_recur_grads* g, void* ws, size_t ws_bytes, void* stream) {
+    const char* what = "gs_recurrence_bwd";
+    gs_status s;
+    if ((s = check_recur(a, what)) != GS_OK) return s;
+    GS_REQUIRE(g != nullptr, "%s: null gradients", what);
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(g->dy, g->ld_dy, a->n, a->cols, es, "dy", what)) != GS_OK) return s;
+    if ((s = check_matrix(g->dx, g->ld_dx, a->n, a->cols, es, "dx", what)) != GS_OK) return s;
+    if ((s = check_matrix(g->dgate, g->ld_dgate, a->n, a->cols, es, "dgate", what)) != GS_OK) return s;
+    GS_REQUIRE(a->n == 0 || (g->kept != nullptr && aligned(g->kept, 4)), "%s: null or misaligned kept", what);
+    GS_REQUIRE(aligned(g->dfinal, 4) && aligned(g->dinitial, 4), "%s: misaligned dfinal or dinitial", what);
+    if ((s = check_recur_ws(a, ws, ws_bytes, what)) != GS_OK) return s;
+    return hip_status(gsmi::launch_recurrence_bwd(*a, *g, ws, static_cast<hipStream_t>(stream)), what);
+}
+
+static gs_status check_silu(int32_t rows, int32_t cols, int32_t dtype, const char* what) {
+    GS_REQUIRE(dtype == GS_F32 || dtype == GS_BF16 || dtype == GS_F16, "%s: bad dtype %d", what, dtype);
+    GS_REQUIRE(rows >= 0 && cols >= 1, "%s: rows < 0 or cols < 1", what);
+    if (cols > GS_SILU_MAX_COLS) return fail(GS_ERR_UNSUPPORTED, "%s: cols %d above %d", what, cols, GS_SILU_MAX_COLS);
+    return GS_OK;
+}
+
+static gs_status check_kept(const uint8_t* q, int64_t ld_q, const uint8_t* scale, int64_t ld_scale, int32_t rows,
+                            int32_t cols, const char* q_name, const char* scale_name, const char* what) {
+    gs_status s;
+    if ((s = check_matrix(q, ld_q, rows, cols, 1, q_name, what)) != GS_OK) return s;
+    return check_matrix(scale, ld_scale, rows, (cols + GS_KEEP_BLOCK - 1) / GS_KEEP_BLOCK, 1, scale_name, what);
+}
+
+gs_status gs_gated_silu(const gs_silu_args* a, void* stream) {
+    const char* what = "gs_gated_silu";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_silu(a->rows, a->cols, a->dtype, what)) != GS_OK) return s;
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(a->u, a->ld_u, a->rows, a->cols, es, "u", what)) != GS_OK) return s;
+    if (a->v && (s = check_matrix(a->v, a->ld_v, a->rows, a->cols, es, "v", what)) != GS_OK) return s;
+    if (a->h && (s = check_matrix(a->h, a->ld_h, a->rows, a->cols, es, "h", what)) != GS_OK) return s;
+    GS_REQUIRE((a->v8 != nullptr) == (a->u8 != nullptr && a->v != nullptr), "%s: u8 and v8 are kept together, v8 with v",
+               what);
+    if (a->u8 && (s = check_kept(a->u8, a->ld_u8, a->u_scale, a->ld_u_scale, a->rows, a->cols, "u8", "u_scale", what)) != GS_OK)
+        return s;
+    if (a->v8 && (s = check_kept(a->v8, a->ld_v8, a->v_scale, a->ld_v_scale, a->rows, a->cols, "v8", "v_scale", what)) != GS_OK)
+        return s;
+    GS_REQUIRE(a->rows == 0 || a->h || a->u8, "%s: no output", what);
+    if (a->rows == 0) return ok();
+    return hip_status(gsmi::launch_gated_silu(*a, static_cast<hipStream_t>(stream)), what);
+}
+
+gs_status gs_gated_silu_bwd(const gs_silu_bwd_args* a, void* stream) {
+    const char* what = "gs_gated_silu_bwd";
+    GS_REQUIRE(a != nullptr, "%s: null args", what);
+    gs_status s;
+    if ((s = check_silu(a->rows, a->cols, a->dtype, what)) != GS_OK) return s;
+    const size_t es = type_size(a->dtype);
+    if ((s = check_matrix(a->dh, a->ld_dh, a->rows, a->cols, es, "dh", what)) != GS_OK) return s;
+    if ((s = check_kept(a->u8, a->ld_u8, a->u_scale, a->ld_u_scale, a->rows, a->cols, "u8", "u_scale", what)) != GS_OK)
+        return s;
+    if ((s = check_matrix(a->du, a->ld_du, a->rows, a->cols, es, "du", what)) != GS_OK) return s;
+    GS_REQUIRE(a->rows == 0 || (a->v8 != nullptr) == (a->dv != nullptr), "%s: v8 and dv are given together", what);
+    if (a->v8) {
+        if ((s = check_kept(a->v8, a->ld_v8, a->v_scale, a->ld_v_scale, a->rows, a->cols, "v8", "v_scale", what)) != GS_OK)
+            return s;
+        if ((s = check_matrix(a->dv, a->ld_dv, a->rows, a->cols, es, "dv", what)) != GS_OK) return s;
+    }
+    if (a->h && (s = check_matrix(a->h, a->ld_h, a->rows, a->cols, es, "h", what)) != GS_OK) return s;
+    if (a->rows == 0) return ok();
+    return hip_status(gsmi::launch_gated_silu_bwd(*a, static_cast<hipStream_t>(stream)), what);
+}
+
 gs_status gs_rlg_build(int32_t n_items, int32_t n_tracks, const int64_t* item_ptr, const int32_t* item_tracks,
                        int32_t track_cap, int32_t top_k, int64_t* edge_ptr, int32_t* edge_dst, double* edge_w,
                        int64_t edge_capacity, int64_t* n_edges) {

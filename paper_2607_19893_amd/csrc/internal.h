@@ -126,6 +126,26 @@ size_t rms_norm_bwd_ws_bytes(int32_t rows, int32_t cols);
 hipError_t launch_rms_norm_bwd(const gs_norm_bwd_args& a, void* ws, hipStream_t st);
 hipError_t launch_rotary(const gs_rotary_args& a, hipStream_t st);
 
+// layernorm.hip
+hipError_t launch_layer_norm(const gs_layer_args& a, hipStream_t st);
+size_t layer_norm_bwd_ws_bytes(int32_t rows, int32_t cols);
+hipError_t launch_layer_norm_bwd(const gs_layer_bwd_args& a, void* ws, hipStream_t st);
+
+// embedding.hip
+hipError_t launch_embedding(const gs_embed_args& a, hipStream_t st);
+size_t embedding_bwd_ws_bytes(int32_t tokens, int32_t rows, int32_t dim, bool touched);
+hipError_t launch_embedding_bwd(const gs_embed_bwd_args& a, void* ws, hipStream_t st);
+
+// recurrence.hip
+size_t recurrence_ws_bytes(const gs_recur& a);
+hipError_t launch_recurrence(const gs_recur& a, void* y, int64_t ld_y, float* final, float* kept, void* ws,
+                             hipStream_t st);
+hipError_t launch_recurrence_bwd(const gs_recur& a, const gs_recur_grads& g, void* ws, hipStream_t st);
+
+// silu.hip
+hipError_t launch_gated_silu(const gs_silu_args& a, hipStream_t st);
+hipError_t launch_gated_silu_bwd(const gs_silu_bwd_args& a, hipStream_t st);
+
 // attention.hip, attention_bwd.hip
 size_t attention_ws_bytes(const gs_attn& a);
 hipError_t launch_attention(const gs_attn& a, const gs_rows& out, float* lse, void* ws, hipStream_t st);

@@ -6,7 +6,7 @@
 
 #include "common.h"
 #include "internal.h"
-#include "vec16.h"
+#include "rows.h"
 
 namespace gsmi {
 
@@ -25,30 +25,6 @@ namespace {
 // TB/s.  Rows that are not whole aligned pieces are loaded an element at a time:
 // bf16 rows of 1001 reach 1.2 TB/s where those of 1000 reach 5.7.  7 rows of 1024: 2.6 us, the start of a kernel and one read.
 // ---------------------------------------------------------------------------
-
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* part) {
-    if (TPR < GS_WAVE) {
-        v = dpp_row_sum(v);
-#ifdef __HIP_DEVICE_COMPILE__
-        if (TPR == 32) {                       // odd and even rows of 16 swapped between two copies
-            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-            v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-        }
-#endif
-        return v;
-    }
-    v = wave_sum(v);
-    if (TPR == GS_WAVE) return v;
-    const int w = threadIdx.x / GS_WAVE;
-    if (lane_id() == 0) part[w] = v;
-    __syncthreads();
-    v = 0.0f;
-#pragma unroll
-    for (int i = 0; i < TPR / GS_WAVE; ++i) v += part[i];
-    __syncthreads();
-    return v;
-}
 
 // Maximum over the lanes that own one block of GS_NORM_BLOCK columns: 16 lanes
 // of 16-bit pieces, 32 of fp32 pieces (adjacent lanes, a block starts at a
@@ -120,25 +96,6 @@ __device__ __forceinline__ void store_eight(uint8_t* __restrict__ q, int there, 
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < there) q[i] = (uint8_t)(b[i / 4] >> (8 * (i % 4)));
-    }
-}
-
-// N weights from column col on (zeros past the row's end).
-template <int N, bool WHOLE>
-__device__ __forceinline__ void load_weight(const float* weight, int col, int cols, float* w) {
-    if (WHOLE) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (col < cols) v = *reinterpret_cast<const float4*>(weight + col + i);
-            w[i] = v.x;
-            w[i + 1] = v.y;
-            w[i + 2] = v.z;
-            w[i + 3] = v.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = col + i < cols ? weight[col + i] : 0.0f;
     }
 }
 

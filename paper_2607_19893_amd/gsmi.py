@@ -34,6 +34,8 @@ GS_F32, GS_BF16, GS_F16 = 0, 1, 2
 GS_ROPE_PLAIN, GS_ROPE_LINEAR, GS_ROPE_BASE, GS_ROPE_PARTS = 0, 1, 2, 3
 GS_ATTN_FILL = 256
 GS_NORM_BLOCK, GS_NORM_MAX_COLS, GS_ROTARY_MAX_DIM, GS_ATTN_MAX_DIM = 128, 16384, 512, 128
+GS_EMBED_MAX_DIM, GS_EMBED_MAX_TOKENS, GS_RECUR_KEEP = 16384, 1 << 28, 64
+GS_KEEP_BLOCK, GS_SILU_MAX_COLS = 32, 1 << 22
 GS_MAX_GROUPS = 8
 
 
@@ -110,6 +112,50 @@ class gs_attn_grads(ctypes.Structure):
     _fields_ = [("out", gs_rows), ("dout", gs_rows), ("dq", gs_rows), ("dk", gs_rows), ("dv", gs_rows), ("lse", P)]
 
 
+class gs_layer_args(ctypes.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("dtype", i32), ("eps", f32), ("x", P), ("residual", P), ("weight", P),
+                ("bias", P), ("total", P), ("y", P), ("ld_x", i64), ("ld_residual", i64), ("ld_total", i64),
+                ("ld_y", i64)]
+
+
+class gs_layer_bwd_args(ctypes.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("dtype", i32), ("eps", f32), ("dy", P), ("total", P), ("dtotal", P),
+                ("weight", P), ("dx", P), ("dweight", P), ("dbias", P), ("ld_dy", i64), ("ld_total", i64),
+                ("ld_dtotal", i64), ("ld_dx", i64)]
+
+
+class gs_embed_args(ctypes.Structure):
+    _fields_ = [("dtype", i32), ("table_dtype", i32), ("tokens", i32), ("rows", i32), ("dim", i32), ("scale", f32),
+                ("ids", P), ("table", P), ("out", P), ("ld_table", i64), ("ld_out", i64)]
+
+
+class gs_embed_bwd_args(ctypes.Structure):
+    _fields_ = [("dtype", i32), ("tokens", i32), ("rows", i32), ("dim", i32), ("scale", f32), ("ids", P), ("dout", P),
+                ("grad", P), ("unique", P), ("count", P), ("ld_dout", i64), ("ld_grad", i64)]
+
+
+class gs_recur(ctypes.Structure):
+    _fields_ = [("dtype", i32), ("n", i32), ("cols", i32), ("n_seg", i32), ("reverse", i32), ("fill", i32), ("cu", P),
+                ("x", P), ("gate", P), ("initial", P), ("ld_x", i64), ("ld_gate", i64)]
+
+
+class gs_recur_grads(ctypes.Structure):
+    _fields_ = [("dy", P), ("dfinal", P), ("kept", P), ("dx", P), ("dgate", P), ("dinitial", P), ("ld_dy", i64),
+                ("ld_dx", i64), ("ld_dgate", i64)]
+
+
+class gs_silu_args(ctypes.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("dtype", i32), ("u", P), ("v", P), ("h", P), ("u8", P), ("u_scale", P),
+                ("v8", P), ("v_scale", P), ("ld_u", i64), ("ld_v", i64), ("ld_h", i64), ("ld_u8", i64),
+                ("ld_u_scale", i64), ("ld_v8", i64), ("ld_v_scale", i64)]
+
+
+class gs_silu_bwd_args(ctypes.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("dtype", i32), ("dh", P), ("u8", P), ("u_scale", P), ("v8", P),
+                ("v_scale", P), ("du", P), ("dv", P), ("h", P), ("ld_dh", i64), ("ld_u8", i64), ("ld_u_scale", i64),
+                ("ld_v8", i64), ("ld_v_scale", i64), ("ld_du", i64), ("ld_dv", i64), ("ld_h", i64)]
+
+
 def scope_words(n) -> int:
     return (int(n) + 31) // 32
 
@@ -166,6 +212,20 @@ _lib.gs_attention_ws_bytes.restype = sz
 _lib.gs_attention_ws_bytes.argtypes = [ctypes.POINTER(gs_attn), i32]
 _lib.gs_attention.argtypes = [ctypes.POINTER(gs_attn), ctypes.POINTER(gs_rows), P, P, sz, P]
 _lib.gs_attention_bwd.argtypes = [ctypes.POINTER(gs_attn), ctypes.POINTER(gs_attn_grads), P, sz, P]
+_lib.gs_layer_norm.argtypes = [ctypes.POINTER(gs_layer_args), P]
+_lib.gs_layer_norm_bwd_ws_bytes.restype = sz
+_lib.gs_layer_norm_bwd_ws_bytes.argtypes = [i32, i32]
+_lib.gs_layer_norm_bwd.argtypes = [ctypes.POINTER(gs_layer_bwd_args), P, sz, P]
+_lib.gs_embedding.argtypes = [ctypes.POINTER(gs_embed_args), P]
+_lib.gs_embedding_bwd_ws_bytes.restype = sz
+_lib.gs_embedding_bwd_ws_bytes.argtypes = [i32, i32, i32, i32]
+_lib.gs_embedding_bwd.argtypes = [ctypes.POINTER(gs_embed_bwd_args), P, sz, P]
+_lib.gs_recurrence_ws_bytes.restype = sz
+_lib.gs_recurrence_ws_bytes.argtypes = [ctypes.POINTER(gs_recur)]
+_lib.gs_recurrence.argtypes = [ctypes.POINTER(gs_recur), P, i64, P, P, P, sz, P]
+_lib.gs_recurrence_bwd.argtypes = [ctypes.POINTER(gs_recur), ctypes.POINTER(gs_recur_grads), P, sz, P]
+_lib.gs_gated_silu.argtypes = [ctypes.POINTER(gs_silu_args), P]
+_lib.gs_gated_silu_bwd.argtypes = [ctypes.POINTER(gs_silu_bwd_args), P]
 _lib.gs_rlg_build.argtypes = [i32, i32, P, P, i32, i32, P, P, P, ctypes.c_int64, P]
 _lib.gs_lp_partition.argtypes = [i32, P, P, P, P, i32, i32, P, P, P]
 _lib.gs_sds_order.argtypes = [i32, P, i32, P, P, P, P, i32, P, P, P, P, P, P]
@@ -174,7 +234,9 @@ for _name in ("gs_project", "gs_visible_set", "gs_visible_set_noalloc", "gs_bin_
               "gs_delta_pack", "gs_delta_apply", "gs_scope_from_ids", "gs_scope_from_pred", "gs_scope_conflicts",
               "gs_admission_gate", "gs_publish_commit", "gs_raster_bwd_project_accum", "gs_raster_fwd_l1",
               "gs_rlg_build", "gs_lp_partition", "gs_sds_order", "gs_rms_norm", "gs_rms_norm_bwd", "gs_rotary",
-              "gs_rotary_freqs", "gs_attention", "gs_attention_bwd"):
+              "gs_rotary_freqs", "gs_attention", "gs_attention_bwd", "gs_layer_norm", "gs_layer_norm_bwd",
+              "gs_embedding", "gs_embedding_bwd", "gs_recurrence", "gs_recurrence_bwd", "gs_gated_silu",
+              "gs_gated_silu_bwd"):
     getattr(_lib, _name).restype = i32
 
 EXPORTS = ["gs_abi_version", "gs_status_string", "gs_last_error", "gs_workspace_bytes", "gs_delta_msg_bytes",
@@ -184,7 +246,9 @@ EXPORTS = ["gs_abi_version", "gs_status_string", "gs_last_error", "gs_workspace_
            "gs_admission_gate", "gs_publish_commit", "gs_raster_bwd_project_accum", "gs_raster_fwd_l1",
            "gs_rlg_build", "gs_lp_partition", "gs_sds_order", "gs_rms_norm", "gs_rms_norm_bwd_ws_bytes",
            "gs_rms_norm_bwd", "gs_rotary", "gs_rotary_freqs", "gs_attention_ws_bytes", "gs_attention",
-           "gs_attention_bwd"]
+           "gs_attention_bwd", "gs_layer_norm", "gs_layer_norm_bwd_ws_bytes", "gs_layer_norm_bwd", "gs_embedding",
+           "gs_embedding_bwd_ws_bytes", "gs_embedding_bwd", "gs_recurrence_ws_bytes", "gs_recurrence",
+           "gs_recurrence_bwd", "gs_gated_silu", "gs_gated_silu_bwd"]
 
 
 class GsmiError(RuntimeError):
@@ -621,6 +685,144 @@ def gs_attention_bwd(attn: gs_attn, out, lse, dout, dq, dk, dv, ws, stream=None)
     p, n = _ws(ws)
     return _check("gs_attention_bwd", _lib.gs_attention_bwd(ctypes.byref(attn), ctypes.byref(g), p, n,
                                                             stream if stream is not None else current_stream()))
+
+
+def gs_layer_norm(x, weight, bias, eps, y=None, residual=None, total=None, stream=None):
+    shape, dt = x.shape, x.dtype
+    a = gs_layer_args(shape[0], shape[1], token_dtype(x), eps, x.data_ptr(), _at(residual), _at(weight), _at(bias),
+                      _at(total), _at(y), _ld(x, shape, "x"), _ld(residual, shape, "residual", dt),
+                      _ld(total, shape, "total", dt), _ld(y, shape, "y", dt))
+    return _check("gs_layer_norm", _lib.gs_layer_norm(ctypes.byref(a), stream if stream is not None else current_stream()))
+
+
+def gs_layer_norm_bwd_ws_bytes(rows, cols) -> int:
+    return int(_lib.gs_layer_norm_bwd_ws_bytes(int(rows), int(cols)))
+
+
+def gs_layer_norm_bwd(dy, total, weight, eps, dx, dweight, dbias, ws, dtotal=None, stream=None):
+    shape, dt = total.shape, total.dtype
+    a = gs_layer_bwd_args(shape[0], shape[1], token_dtype(total), eps, dy.data_ptr(), total.data_ptr(), _at(dtotal),
+                          _at(weight), dx.data_ptr(), _at(dweight), _at(dbias), _ld(dy, shape, "dy", dt),
+                          _ld(total, shape, "total"), _ld(dtotal, shape, "dtotal", dt), _ld(dx, shape, "dx", dt))
+    p, n = _ws(ws)
+    return _check("gs_layer_norm_bwd", _lib.gs_layer_norm_bwd(ctypes.byref(a), p, n,
+                                                              stream if stream is not None else current_stream()))
+
+
+def _int32(t, n, what):
+    if t.numel() != n or t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous():
+        raise ValueError("%s is %d contiguous int32 values" % (what, n))
+
+
+def gs_embedding(table, ids, scale, out, stream=None):
+    """table [rows, dim], ids [tokens] int32, out [tokens, dim]."""
+    _int32(ids, out.shape[0], "ids")
+    a = gs_embed_args(token_dtype(out), token_dtype(table), out.shape[0], table.shape[0], out.shape[1], scale, _at(ids),
+                      table.data_ptr(), out.data_ptr(), _ld(table, (table.shape[0], out.shape[1]), "table"),
+                      _ld(out, out.shape, "out"))
+    return _check("gs_embedding", _lib.gs_embedding(ctypes.byref(a), stream if stream is not None else current_stream()))
+
+
+def gs_embedding_bwd_ws_bytes(tokens, rows, dim, touched=False) -> int:
+    return int(_lib.gs_embedding_bwd_ws_bytes(int(tokens), int(rows), int(dim), int(touched)))
+
+
+def gs_embedding_bwd(dout, ids, rows, scale, grad, ws, unique=None, count=None, stream=None):
+    """grad [rows, dim] fp32, or with unique and count the touched rows [min(tokens, rows), dim]."""
+    import torch
+    tokens, dim = dout.shape
+    _int32(ids, tokens, "ids")
+    most = rows
+    if unique is not None:
+        most = min(tokens, rows)
+        _int32(unique, most, "unique")
+        _int32(count, 1, "count")
+    a = gs_embed_bwd_args(token_dtype(dout), tokens, rows, dim, scale, _at(ids), dout.data_ptr(), grad.data_ptr(),
+                          _at(unique), _at(count), _ld(dout, dout.shape, "dout"),
+                          _ld(grad, (most, dim), "grad", torch.float32))
+    p, n = _ws(ws)
+    if unique is not None and most == 0:          # tensors without elements have no address
+        a.unique = a.count
+    return _check("gs_embedding_bwd", _lib.gs_embedding_bwd(ctypes.byref(a), p, n,
+                                                            stream if stream is not None else current_stream()))
+
+
+def _states(t, shape, what):
+    import torch
+    if t is not None and (t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous()):
+        raise ValueError("%s is contiguous float32 %s" % (what, list(shape)))
+
+
+def make_recur(x, gate, cu=None, n_seg=1, initial=None, reverse=False, fill=False) -> gs_recur:
+    """x, gate [n, cols]; cu [n_seg + 1] int32; initial [n_seg, cols] fp32.  fill: tokens outside every segment are
+    written (zeros)."""
+    shape = x.shape
+    if cu is not None:
+        n_seg = cu.numel() - 1
+        _int32(cu, n_seg + 1, "cu")
+    _states(initial, (n_seg, shape[1]), "initial")
+    return gs_recur(token_dtype(x), shape[0], shape[1], n_seg, reverse, fill, _at(cu), x.data_ptr(), gate.data_ptr(),
+                    _at(initial), _ld(x, shape, "x"), _ld(gate, shape, "gate", x.dtype))
+
+
+def gs_recurrence_ws_bytes(recur: gs_recur) -> int:
+    return int(_lib.gs_recurrence_ws_bytes(ctypes.byref(recur)))
+
+
+def gs_recurrence(recur: gs_recur, y, final=None, kept=None, ws=None, stream=None):
+    n, cols = y.shape
+    _states(final, (recur.n_seg, cols), "final")
+    _states(kept, (-(-n // GS_RECUR_KEEP), cols), "kept")
+    p, nb = _ws(ws)
+    return _check("gs_recurrence", _lib.gs_recurrence(ctypes.byref(recur), y.data_ptr(), _ld(y, (recur.n, recur.cols), "y"),
+                                                      _at(final), _at(kept), p, nb,
+                                                      stream if stream is not None else current_stream()))
+
+
+def gs_recurrence_bwd(recur: gs_recur, dy, kept, dx, dgate, dfinal=None, dinitial=None, ws=None, stream=None):
+    shape = (recur.n, recur.cols)
+    states = (recur.n_seg, recur.cols)
+    _states(kept, (-(-recur.n // GS_RECUR_KEEP), recur.cols), "kept")
+    _states(dfinal, states, "dfinal")
+    _states(dinitial, states, "dinitial")
+    dt = dy.dtype
+    if token_dtype(dy) != recur.dtype:
+        raise ValueError("dy has x's type")
+    g = gs_recur_grads(dy.data_ptr(), _at(dfinal), _at(kept), dx.data_ptr(), dgate.data_ptr(), _at(dinitial),
+                       _ld(dy, shape, "dy"), _ld(dx, shape, "dx", dt), _ld(dgate, shape, "dgate", dt))
+    p, n = _ws(ws)
+    return _check("gs_recurrence_bwd", _lib.gs_recurrence_bwd(ctypes.byref(recur), ctypes.byref(g), p, n,
+                                                              stream if stream is not None else current_stream()))
+
+
+def _kept8(q, scale, shape, name):
+    """(addresses and strides) of rows in 8 bits and their scale bytes."""
+    if q is None:
+        return None, None, 0, 0
+    blocks = (shape[0], -(-shape[1] // GS_KEEP_BLOCK))
+    if q.element_size() != 1 or scale is None or scale.element_size() != 1:
+        raise ValueError("%s and its scales are bytes" % name)
+    return q.data_ptr(), scale.data_ptr(), _ld(q, shape, name), _ld(scale, blocks, name + "'s scale")
+
+
+def gs_gated_silu(u, v=None, h=None, u8=None, u_scale=None, v8=None, v_scale=None, stream=None):
+    shape, dt = u.shape, u.dtype
+    up, us, ldu, ldus = _kept8(u8, u_scale, shape, "u8")
+    vp, vs, ldv, ldvs = _kept8(v8, v_scale, shape, "v8")
+    a = gs_silu_args(shape[0], shape[1], token_dtype(u), u.data_ptr(), _at(v), _at(h), up, us, vp, vs, _ld(u, shape, "u"),
+                     _ld(v, shape, "v", dt), _ld(h, shape, "h", dt), ldu, ldus, ldv, ldvs)
+    return _check("gs_gated_silu", _lib.gs_gated_silu(ctypes.byref(a), stream if stream is not None else current_stream()))
+
+
+def gs_gated_silu_bwd(dh, u8, u_scale, du, v8=None, v_scale=None, dv=None, h=None, stream=None):
+    shape, dt = dh.shape, dh.dtype
+    up, us, ldu, ldus = _kept8(u8, u_scale, shape, "u8")
+    vp, vs, ldv, ldvs = _kept8(v8, v_scale, shape, "v8")
+    a = gs_silu_bwd_args(shape[0], shape[1], token_dtype(dh), dh.data_ptr(), up, us, vp, vs, du.data_ptr(), _at(dv),
+                         _at(h), _ld(dh, shape, "dh"), ldu, ldus, ldv, ldvs, _ld(du, shape, "du", dt),
+                         _ld(dv, shape, "dv", dt), _ld(h, shape, "h", dt))
+    return _check("gs_gated_silu_bwd", _lib.gs_gated_silu_bwd(ctypes.byref(a),
+                                                              stream if stream is not None else current_stream()))
 
 
 def raw():
