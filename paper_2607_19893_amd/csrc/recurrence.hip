@@ -17,8 +17,9 @@ namespace {
 // of 128 channels, two a lane, and finds its own map with every gate and token
 // in registers; the maps of a chunk's waves meet in LDS, those of the chunks in
 // global memory.  `reverse` turns the list around (place p is token n - 1 - p).
-// Three launches for long lists: the chunks' maps, the states in front of them,
-// the tokens once more with those.
+// One pass: a chunk publishes its map, looks back over the chunks in front of it
+// to the nearest whose last state is known, publishes its own last state, and
+// goes through its tokens.  Bound by HBM bytes.
 // ---------------------------------------------------------------------------
 
 constexpr int kSteps = 16;                     // tokens of a wave
@@ -33,9 +34,9 @@ constexpr uint32_t kStart = 1, kEnd = 2, kOutside = 0xFFFFFFFFu;
 struct Recur {
     gs_recur a;
     const uint32_t* map;                       // of place p: segment << 2 | kEnd | kStart, or kOutside
-    float2* maps;                              // [chunks][blocks * kCols]: (A, B)
-    float* states;                             // [chunks][blocks * kCols]: in front of (behind, on the way back)
-    uint32_t* anew;                            // [chunks]: a segment starts (ends) in it
+    uint64_t* maps;                            // [blocks][chunks][2 * 64]: (A, B) of a lane's two channels
+    uint64_t* states;                          // [blocks][chunks][64]: a lane's two states behind the chunk
+    uint32_t* flags;                           // [blocks][chunks]: kMap, then kState; behind them the ticket
     int32_t chunks, blocks;
 };
 
@@ -71,9 +72,12 @@ __device__ __forceinline__ uint32_t place_word(const gs_recur& a, int32_t p) {
     return (uint32_t)lo << 2 | ((a.reverse ? at_first : at_last) ? kEnd : 0u) | ((a.reverse ? at_last : at_first) ? kStart : 0u);
 }
 
-__global__ void __launch_bounds__(GS_BLOCK) k_recur_map(gs_recur a, uint32_t* __restrict__ map) {
+// The places' words, and the flags and the ticket cleared.
+__global__ void __launch_bounds__(GS_BLOCK) k_recur_map(gs_recur a, uint32_t* __restrict__ map, uint32_t* __restrict__ flags,
+                                                        int32_t n_flags) {
     const int64_t p = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x;
     if (p < a.n) map[p] = place_word(a, (int32_t)p);
+    if (p < n_flags) flags[p] = 0;
 }
 
 // A wave's tokens: bit i of the masks is place p0 + i (scalars).
@@ -163,21 +167,151 @@ __global__ void __launch_bounds__(GS_BLOCK) k_recur_empty(gs_recur a, const floa
     }
 }
 
-enum { kMapsOnly = 0, kWithStates = 1, kAlone = 2 };
+// ---------------------------------------------------------------------------
+// Looking back.  The workgroups take chunks by a ticket, chunk after chunk, so
+// every chunk that one waits for belongs to a workgroup that is already running
+// and publishes its map before it waits itself: every wait ends.  (Calls that
+// run at the same time on one workspace would clear each other's flags; a wait
+// gives up after kPolls then, with NaN.)  What is published moves past the
+// caches of the units (agent scope); a flag follows the values it announces.
+// ---------------------------------------------------------------------------
 
-// Forward.  PHASE kMapsOnly: writes the chunk's map; kWithStates: the outputs,
-// from the state in front of the chunk; kAlone: the only chunk, without a map.
-template <typename T, bool TAIL, int PHASE>
-__global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur(Recur r, RecurOut o) {
+constexpr uint32_t kMap = 1, kState = 2;
+constexpr int kPolls = 1 << 22;
+constexpr int kAhead = 4;                      // maps on their way at once
+
+__device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+__device__ __forceinline__ void put(uint64_t* p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint64_t get(const uint64_t* p) {
+    return __hip_atomic_load(const_cast<uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// by the wave that wrote what the flag announces
+__device__ __forceinline__ void announce(uint32_t* flag, uint32_t what) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (lane_id() == 0) __hip_atomic_store(flag, what, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// A wave's part: publishes the chunk's map m[0] h + b[0], m[1] h + b[1] (anew:
+// its last state b), waits for the state in front of the chunk, publishes the one
+// behind it, and leaves in h the one in front.  `needed`: someone here reads it.
+__device__ __forceinline__ void look_back(const Recur& r, int chunk, int block, const float* m, const float* b, bool anew,
+                                          bool needed, float* h) {
+    const int l = lane_id();
+    const int64_t at = (int64_t)block * r.chunks;
+    uint64_t* maps = r.maps + at * (2 * GS_WAVE);
+    uint64_t* states = r.states + at * GS_WAVE;
+    uint32_t* flags = r.flags + at;
+    h[0] = h[1] = 0.0f;
+    if (anew) {
+        put(states + (int64_t)chunk * GS_WAVE + l, pair(b[0], b[1]));
+        announce(flags + chunk, kState);
+        if (!needed) return;
+    } else {
+        put(maps + (int64_t)chunk * (2 * GS_WAVE) + l, pair(m[0], b[0]));
+        put(maps + (int64_t)chunk * (2 * GS_WAVE) + GS_WAVE + l, pair(m[1], b[1]));
+        announce(flags + chunk, kMap);
+    }
+    // from the nearest chunk on: the map through those that were passed
+    float pm[2] = {1.0f, 1.0f}, pb[2] = {0.0f, 0.0f};
+    int j = chunk - 1, polls = 0;
+    for (;;) {
+        const uint32_t f = j - l >= 0 ? __hip_atomic_load(flags + j - l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+        const uint64_t known = __ballot(f == kState), there = __ballot(f != 0u);
+        const int d = known ? __ffsll((unsigned long long)known) - 1 : GS_WAVE;      // maps to pass first
+        const uint64_t need = d == GS_WAVE ? ~0ull : (1ull << d) - 1;
+        if ((there & need) != need) {
+            if (++polls > kPolls) {
+                h[0] = h[1] = NAN;
+                break;
+            }
+            __builtin_amdgcn_s_sleep(1);
+            continue;
+        }
+        asm volatile("" ::: "memory");         // the values are read behind the flags
+        uint64_t s = 0;
+        if (known) s = get(states + (int64_t)(j - d) * GS_WAVE + l);
+        for (int k = 0; k < d; k += kAhead) {
+            uint64_t v[kAhead][2];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t c = (int64_t)(j - min(k + i, d - 1)) * (2 * GS_WAVE) + l;
+                v[i][0] = get(maps + c);
+                v[i][1] = get(maps + c + GS_WAVE);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (k + i >= d) break;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float2 ab = unpair(v[i][c]);
+                    pb[c] = fmaf(pm[c], ab.y, pb[c]);
+                    pm[c] *= ab.x;
+                }
+            }
+        }
+        if (known) {
+            const float2 v = unpair(s);
+            h[0] = fmaf(pm[0], v.x, pb[0]);
+            h[1] = fmaf(pm[1], v.y, pb[1]);
+            break;
+        }
+        j -= GS_WAVE;
+    }
+    if (anew) return;
+    put(states + (int64_t)chunk * GS_WAVE + l, pair(fmaf(m[0], h[0], b[0]), fmaf(m[1], h[1], b[1])));
+    announce(flags + chunk, kState);
+}
+
+// The next chunk (in the order of the recurrence) and its block of channels; false: none is left.
+__device__ __forceinline__ bool take_chunk(const Recur& r, uint32_t* shared, int& chunk, int& block) {
+    const int32_t all = r.chunks * r.blocks;
+    if (threadIdx.x == 0) *shared = atomicAdd(r.flags + all, 1u);
+    __syncthreads();
+    const uint32_t t = __builtin_amdgcn_readfirstlane(*shared);
+    chunk = (int)(t / (uint32_t)r.blocks);
+    block = (int)(t % (uint32_t)r.blocks);
+    return t < (uint32_t)all;
+}
+
+// The chunk's own map, from those of its waves; true: a segment starts (ends) in it.
+__device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* anew, int lane, float* m, float* b) {
+    m[0] = m[1] = 1.0f;
+    b[0] = b[1] = 0.0f;
+    bool any = false;
+    for (int u = 0; u < kWaves; ++u) {
+        const float4 v = maps[u * GS_WAVE + lane];
+        if (anew[u]) {
+            any = true;
+            b[0] = v.z;
+            b[1] = v.w;
+        } else {
+            b[0] = fmaf(v.x, b[0], v.z);
+            b[1] = fmaf(v.y, b[1], v.w);
+        }
+        m[0] *= v.x;
+        m[1] *= v.y;
+    }
+    return any;
+}
+
+// ALONE: the list is one chunk, which looks nowhere and has no map of places.
+// Two workgroups a compute unit (4 waves a SIMD) where the registers allow it.
+template <typename T, bool TAIL, bool ALONE>
+__global__ void __launch_bounds__(kWaves * GS_WAVE, TAIL ? 2 : 4) k_recur(Recur r, RecurOut o) {
     __shared__ float4 maps[kWaves * GS_WAVE];
-    __shared__ uint32_t anew[kWaves];
+    __shared__ float2 front[GS_WAVE];
+    __shared__ uint32_t anew[kWaves], ticket;
     const gs_recur& a = r.a;
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
-    const int chunk = blockIdx.x / r.blocks, block = blockIdx.x % r.blocks;
+    int chunk = 0, block = blockIdx.x;
+    if (!ALONE && !take_chunk(r, &ticket, chunk, block)) return;
     const uint32_t col = block * kCols + 2 * l;
     const int there = a.cols - (int)col;
     Tokens tk;
-    tk.find<PHASE != kAlone>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
+    tk.find<!ALONE>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
     Two<T, TAIL> gs[kSteps], xs[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
@@ -213,27 +347,17 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur(Recur r, RecurOut o)
     maps[w * GS_WAVE + l] = make_float4(m[0], m[1], h[0], h[1]);
     if (l == 0) anew[w] = tk.starts != 0;
     __syncthreads();
-    const int64_t wide = (int64_t)r.blocks * kCols;
-    if (PHASE == kMapsOnly) {
-        if (w != 0) return;
-        float all[2] = {0.0f, 0.0f}, mm[2] = {1.0f, 1.0f};
-        bool any = false;
-        through(maps, anew, 0, kWaves, l, all);
-        for (int u = 0; u < kWaves; ++u) {
-            const float4 v = maps[u * GS_WAVE + l];
-            mm[0] *= v.x;
-            mm[1] *= v.y;
-            any |= anew[u] != 0;
-        }
-        reinterpret_cast<float4*>(r.maps)[(chunk * wide + block * kCols) / 2 + l] = make_float4(mm[0], all[0], mm[1], all[1]);
-        if (block == 0 && l == 0) r.anew[chunk] = any;
-        return;
-    }
     h[0] = h[1] = 0.0f;
-    if (PHASE == kWithStates) {
-        const float2 v = reinterpret_cast<const float2*>(r.states)[(chunk * wide + block * kCols) / 2 + l];
-        h[0] = v.x;
-        h[1] = v.y;
+    if (!ALONE) {
+        if (w == 0) {
+            float am[2], ab[2], f[2];
+            const bool any = whole_map(maps, anew, l, am, ab);
+            look_back(r, chunk, block, am, ab, any, !bit(tk.starts, 0), f);
+            front[l] = make_float2(f[0], f[1]);
+        }
+        __syncthreads();
+        h[0] = front[l].x;
+        h[1] = front[l].y;
     }
     through(maps, anew, 0, w, l, h);
     if (o.kept && tk.p0 % GS_RECUR_KEEP == 0 && tk.p0 < a.n)
@@ -252,42 +376,32 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur(Recur r, RecurOut o)
     }
 }
 
-// The states in front of the chunks (behind them, from the last one on, on the way back).
-__global__ void __launch_bounds__(GS_WAVE) k_recur_states(Recur r, int back) {
-    const int64_t wide = (int64_t)r.blocks * kCols, c = (int64_t)blockIdx.x * GS_WAVE + threadIdx.x;
-    float h = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < r.chunks; ++i) {
-        const int k = back ? r.chunks - 1 - i : i;
-        const float2 v = r.maps[k * wide + c];
-        r.states[k * wide + c] = h;
-        h = r.anew[k] ? v.y : fmaf(v.x, h, v.y);
-    }
-}
-
 // Gradient: D_t = dy_t + a_{t+1} D_{t+1} from the last token to the first (dfinal
 // comes in at a segment's last one), c_t = a_t D_t passes on;
 //   dx_t = (1 - a_t) D_t;  dgate_t = a_t (1 - a_t) (h_{t-1} - x_t) D_t;  dinitial = c of the first token.
 // h is formed again from the states that the forward kept every GS_RECUR_KEEP
 // tokens, in fp32, not read in the tokens' type.
-template <typename T, bool TAIL, int PHASE>
+template <typename T, bool TAIL, bool ALONE>
 __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recur_grads o) {
     __shared__ float4 maps[kWaves * GS_WAVE], back[kWaves * GS_WAVE];
-    __shared__ uint32_t anew[kWaves], ended[kWaves];
+    __shared__ float2 front[GS_WAVE];
+    __shared__ uint32_t anew[kWaves], ended[kWaves], ticket;
     const gs_recur& a = r.a;
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
-    const int chunk = blockIdx.x / r.blocks, block = blockIdx.x % r.blocks;
+    int turn = 0, block = blockIdx.x;          // chunks are taken from the last one on
+    if (!ALONE && !take_chunk(r, &ticket, turn, block)) return;
+    const int chunk = r.chunks - 1 - turn;
     const uint32_t col = block * kCols + 2 * l;
     const int there = a.cols - (int)col;
     Tokens tk;
-    tk.find<PHASE != kAlone>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
+    tk.find<!ALONE>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
     Two<T, TAIL> gs[kSteps], xs[kSteps], ds[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int64_t t = tk.token(a, i);
         gs[i].load(static_cast<const T*>(a.gate) + t * a.ld_gate, col, there);
         ds[i].load(static_cast<const T*>(o.dy) + t * o.ld_dy, col, there);
-        if (PHASE != kMapsOnly) xs[i].load(static_cast<const T*>(a.x) + t * a.ld_x, col, there);
+        xs[i].load(static_cast<const T*>(a.x) + t * a.ld_x, col, there);
     }
     // the way back through the wave's tokens: c -> m c + b
     float D[kSteps][2], S[kSteps][2], m[2] = {1.0f, 1.0f}, b[2] = {0.0f, 0.0f};
@@ -314,23 +428,6 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
     }
     back[(kWaves - 1 - w) * GS_WAVE + l] = make_float4(m[0], m[1], b[0], b[1]);
     if (l == 0) ended[kWaves - 1 - w] = tk.ends != 0;
-    const int64_t wide = (int64_t)r.blocks * kCols;
-    if (PHASE == kMapsOnly) {
-        __syncthreads();
-        if (w != 0) return;
-        float all[2] = {0.0f, 0.0f}, mm[2] = {1.0f, 1.0f};
-        bool any = false;
-        through(back, ended, 0, kWaves, l, all);
-        for (int u = 0; u < kWaves; ++u) {
-            const float4 v = back[u * GS_WAVE + l];
-            mm[0] *= v.x;
-            mm[1] *= v.y;
-            any |= ended[u] != 0;
-        }
-        reinterpret_cast<float4*>(r.maps)[(chunk * wide + block * kCols) / 2 + l] = make_float4(mm[0], all[0], mm[1], all[1]);
-        if (block == 0 && l == 0) r.anew[chunk] = any;
-        return;
-    }
     // the states again: the wave's own map, then those of the waves behind the kept state
     float h[2] = {0.0f, 0.0f}, fm[2] = {1.0f, 1.0f};
 #pragma unroll
@@ -356,6 +453,12 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
     maps[w * GS_WAVE + l] = make_float4(fm[0], fm[1], h[0], h[1]);
     if (l == 0) anew[w] = tk.starts != 0;
     __syncthreads();
+    if (!ALONE && w == kWaves - 1) {
+        float am[2], ab[2], f[2];
+        const bool any = whole_map(back, ended, l, am, ab);
+        look_back(r, turn, block, am, ab, any, !bit(tk.ends, kSteps - 1), f);
+        front[l] = make_float2(f[0], f[1]);
+    }
     h[0] = h[1] = 0.0f;
     if (tk.p0 < a.n) {
         Two<float, TAIL> v;
@@ -387,10 +490,10 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
         }
     }
     float g[2] = {0.0f, 0.0f};
-    if (PHASE == kWithStates) {
-        const float2 v = reinterpret_cast<const float2*>(r.states)[(chunk * wide + block * kCols) / 2 + l];
-        g[0] = v.x;
-        g[1] = v.y;
+    if (!ALONE) {
+        __syncthreads();
+        g[0] = front[l].x;
+        g[1] = front[l].y;
     }
     through(back, ended, 0, kWaves - 1 - w, l, g);
 #pragma unroll
@@ -419,7 +522,7 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
 
 struct RecurPlan {
     int32_t chunks, blocks;
-    size_t map, maps, states, anew, bytes;
+    size_t map, maps, states, flags, bytes;
 };
 
 RecurPlan recur_plan(int32_t n, int32_t cols) {
@@ -432,12 +535,11 @@ RecurPlan recur_plan(int32_t n, int32_t cols) {
         at += align256(bytes);
         return here;
     };
-    const size_t wide = (size_t)p.chunks * p.blocks * kCols;
-    const bool alone = p.chunks <= 1;
-    p.map = take(alone ? 0 : (size_t)n * 4);
-    p.maps = take(alone ? 0 : wide * 8);
-    p.states = take(alone ? 0 : wide * 4);
-    p.anew = take(alone ? 0 : (size_t)p.chunks * 4);
+    const size_t all = p.chunks <= 1 ? 0 : (size_t)p.chunks * p.blocks;
+    p.map = take(all ? (size_t)n * 4 : 0);
+    p.maps = take(all * GS_WAVE * 16);
+    p.states = take(all * GS_WAVE * 8);
+    p.flags = take(all ? (all + 1) * 4 : 0);
     p.bytes = at;
     return p;
 }
@@ -450,10 +552,16 @@ Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
     r.blocks = p.blocks;
     const bool alone = p.chunks <= 1;
     r.map = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.map);
-    r.maps = alone ? nullptr : reinterpret_cast<float2*>(base + p.maps);
-    r.states = alone ? nullptr : reinterpret_cast<float*>(base + p.states);
-    r.anew = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.anew);
+    r.maps = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.maps);
+    r.states = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.states);
+    r.flags = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.flags);
     return r;
+}
+
+// The map of the places and cleared flags.
+void recur_map(const Recur& r, hipStream_t st) {
+    const int32_t flags = r.chunks * r.blocks + 1;
+    k_recur_map<<<div_up(std::max(r.a.n, flags), GS_BLOCK), GS_BLOCK, 0, st>>>(r.a, const_cast<uint32_t*>(r.map), r.flags, flags);
 }
 
 void empty_segments(const gs_recur& a, const float* from, float* to, hipStream_t st) {
@@ -465,12 +573,10 @@ template <typename T, bool TAIL>
 hipError_t recur_go(const Recur& r, const RecurOut& o, hipStream_t st) {
     const uint32_t grid = (uint32_t)r.chunks * r.blocks;
     if (r.chunks == 1) {
-        k_recur<T, TAIL, kAlone><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        k_recur<T, TAIL, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
     } else {
-        k_recur_map<<<div_up(r.a.n, GS_BLOCK), GS_BLOCK, 0, st>>>(r.a, const_cast<uint32_t*>(r.map));
-        k_recur<T, TAIL, kMapsOnly><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
-        k_recur_states<<<r.blocks * (kCols / GS_WAVE), GS_WAVE, 0, st>>>(r, 0);
-        k_recur<T, TAIL, kWithStates><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        recur_map(r, st);
+        k_recur<T, TAIL, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
     }
     return hipGetLastError();
 }
@@ -479,12 +585,10 @@ template <typename T, bool TAIL>
 hipError_t recur_bwd_go(const Recur& r, const gs_recur_grads& g, hipStream_t st) {
     const uint32_t grid = (uint32_t)r.chunks * r.blocks;
     if (r.chunks == 1) {
-        k_recur_bwd<T, TAIL, kAlone><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
+        k_recur_bwd<T, TAIL, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
     } else {
-        k_recur_map<<<div_up(r.a.n, GS_BLOCK), GS_BLOCK, 0, st>>>(r.a, const_cast<uint32_t*>(r.map));
-        k_recur_bwd<T, TAIL, kMapsOnly><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
-        k_recur_states<<<r.blocks * (kCols / GS_WAVE), GS_WAVE, 0, st>>>(r, 1);
-        k_recur_bwd<T, TAIL, kWithStates><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
+        recur_map(r, st);
+        k_recur_bwd<T, TAIL, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
     }
     return hipGetLastError();
 }
