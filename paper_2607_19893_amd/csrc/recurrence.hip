@@ -14,7 +14,7 @@ namespace {
 // h -> A h + B, and two runs in a row by (A2 A1, A2 B1 + B2); a segment's first
 // token starts anew (B alone, whatever the state was).  So all segments are one
 // list of tokens, cut into chunks of kWaves * kSteps: a wave takes kSteps tokens
-// of 128 channels, two a lane, and finds its own map with every gate and token
+// of up to 128 channels, two a lane, and finds its own map with every gate and token
 // in registers; the maps of a chunk's waves meet in LDS, those of the chunks in
 // global memory.  `reverse` turns the list around (place p is token n - 1 - p).
 // One pass: a chunk publishes its map, looks back over the chunks in front of it
@@ -25,10 +25,11 @@ namespace {
 constexpr int kSteps = 16;                     // tokens of a wave
 constexpr int kWaves = 8;                      // of a workgroup
 constexpr int kChunk = kSteps * kWaves;
-constexpr int kCols = 2 * GS_WAVE;             // channels of a workgroup
+constexpr int kCols = 2 * GS_WAVE;             // channels of a workgroup at most
 constexpr int kKeptWaves = GS_RECUR_KEEP / kSteps;
 static_assert(GS_RECUR_KEEP % kSteps == 0 && kChunk % GS_RECUR_KEEP == 0, "a kept state is in front of a wave");
 
+constexpr uint32_t kAllSteps = (1u << kSteps) - 1;
 constexpr uint32_t kStart = 1, kEnd = 2, kOutside = 0xFFFFFFFFu;
 
 struct Recur {
@@ -37,7 +38,7 @@ struct Recur {
     uint64_t* maps;                            // [blocks][chunks][2 * 64]: (A, B) of a lane's two channels
     uint64_t* states;                          // [blocks][chunks][64]: a lane's two states behind the chunk
     uint32_t* flags;                           // [blocks][chunks]: kMap, then kState; behind them the ticket
-    int32_t chunks, blocks;
+    int32_t chunks, blocks, width;             // width: channels of a block
 };
 
 struct RecurOut {
@@ -94,39 +95,97 @@ struct Tokens {
         if (l < kSteps && (int64_t)first + l < r.a.n) word = MAPPED ? r.map[first + l] : place_word(r.a, first + l);
         const bool in = word != kOutside;
         inside = (uint32_t)__ballot(in);
-        starts = (uint32_t)__ballot(in && (word & kStart)) | (~inside & ((1u << kSteps) - 1));
-        ends = (uint32_t)__ballot(in && (word & kEnd)) | (~inside & ((1u << kSteps) - 1));
+        starts = (uint32_t)__ballot(in && (word & kStart)) | (~inside & kAllSteps);
+        ends = (uint32_t)__ballot(in && (word & kEnd)) | (~inside & kAllSteps);
     }
-    __device__ __forceinline__ int32_t segment(int i) const { return (int32_t)(__builtin_amdgcn_readlane((int)word, i) >> 2 & 0x3FFFFFFF); }
-    // the token of place p0 + i; behind the last place the last one, whose values are not used
-    __device__ __forceinline__ int64_t token(const gs_recur& a, int i) const {
-        const int64_t p = min((int64_t)p0 + i, (int64_t)a.n - 1);
-        return a.reverse ? a.n - 1 - p : p;
+    __device__ __forceinline__ int32_t segment(int i) const {
+        int32_t s = (int32_t)(__builtin_amdgcn_readlane((int)word, i) >> 2 & 0x3FFFFFFF);
+        asm volatile("" : "+s"(s));            // nothing of it is worked out where no segment's end is
+        return s;
     }
+    // places that are some token's
+    __device__ __forceinline__ uint32_t there(const gs_recur& a) const {
+        const int32_t left = max(0, min(kSteps, a.n - p0));
+        return (1u << left) - 1;
+    }
+    // the token of a place
+    __device__ __forceinline__ int32_t token(const gs_recur& a, int32_t p) const { return a.reverse ? a.n - 1 - p : p; }
 };
 
-// Two elements of a lane's channels at any alignment of an element, as floats;
-// `there` of them.
-template <typename T, bool TAIL>
+// Keeps a branch that is the same for the wave a branch: most waves have no
+// segment's end among their tokens, and selects would cost each of them.
+__device__ __forceinline__ void rare() { asm volatile(""); }
+
+template <typename P>
+using global = __attribute__((address_space(1))) P;
+
+// A lane's two channels of a row, at any alignment of an element, as floats.
+// The row is the same for the wave: an address is a scalar and the lane's
+// column.  ONE: there is one channel in all.
+template <typename T, bool ONE>
 struct Two {
     typedef T vec __attribute__((ext_vector_type(2)));
     typedef vec __attribute__((aligned(sizeof(T)))) loose;
     vec v;
-    // row: the same for the wave, so that an address is a scalar and the lane's column
-    __device__ __forceinline__ void load(const T* row, uint32_t col, int there) {
-        v = vec{};
-        if (there >= 2) v = *reinterpret_cast<const loose*>(row + col);
-        else if (TAIL && there == 1) v[0] = row[col];
+    // The row's address stays a scalar, the lane's part is a 32-bit offset: an
+    // address of each lane's own would take two registers a row.
+    template <typename P>
+    static __device__ __forceinline__ global<P>* at(global<char>* row, uint32_t col) {
+        return (global<P>*)(row + col * (uint32_t)sizeof(T));
     }
+    static __device__ __forceinline__ global<char>* row_of(const void* base, int64_t row, int64_t ld) {
+        return (global<char>*)const_cast<char*>(static_cast<const char*>(base)) + row * ld * (int64_t)sizeof(T);
+    }
+    __device__ __forceinline__ void load(global<char>* row, uint32_t col) {
+        if (ONE) v = vec{*at<T>(row, col), (T)0.0f};
+        else v = *at<loose>(row, col);
+    }
+    __device__ __forceinline__ void load(const void* base, int64_t row, int64_t ld, uint32_t col) { load(row_of(base, row, ld), col); }
+    // as loaded: its floats are formed again behind this, not held in registers
+    __device__ __forceinline__ void again() {
+        if (sizeof(T) == 2) {
+            uint32_t u;
+            __builtin_memcpy(&u, &v, 4);
+            loaded(u);
+            __builtin_memcpy(&v, &u, 4);
+        }
+    }
+    __device__ __forceinline__ void fill(float f) { v = vec{(T)f, (T)f}; }
     __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
-    static __device__ __forceinline__ void store(T* row, uint32_t col, int there, float a, float b) {
-        vec v;
-        v[0] = (T)a;
-        v[1] = (T)b;
-        if (there >= 2) *reinterpret_cast<loose*>(row + col) = v;
-        else if (TAIL && there == 1) row[col] = v[0];
+    static __device__ __forceinline__ void store(global<char>* row, uint32_t col, float a, float b) {
+        if (ONE) *at<T>(row, col) = (T)a;
+        else *at<loose>(row, col) = vec{(T)a, (T)b};
+    }
+    static __device__ __forceinline__ void store(void* base, int64_t row, int64_t ld, uint32_t col, float a, float b) {
+        store(row_of(base, row, ld), col, a, b);
     }
 };
+
+// The rows of a matrix along the places, from place `first` on (back: the other
+// way): one row after the other, so that no more than one address is held.
+struct Rows {
+    global<char>* p;
+    int64_t step;
+    template <typename T>
+    static __device__ __forceinline__ Rows of(const gs_recur& a, const Tokens& tk, const void* base, int64_t ld, int32_t first,
+                                              bool back) {
+        const int64_t bytes = ld * (int64_t)sizeof(T);
+        Rows r;
+        r.p = (global<char>*)const_cast<char*>(static_cast<const char*>(base)) + (int64_t)tk.token(a, first) * bytes;
+        r.step = (a.reverse != 0) != back ? -bytes : bytes;
+        return r;
+    }
+    __device__ __forceinline__ void next(bool there = true) {
+        p += there ? step : 0;
+        asm volatile("" : "+s"(p));
+    }
+};
+
+// A lane's first channel.  Lanes past the block's or the row's end take its last
+// two once more, and write the same values there: no lane is ever left out.
+__device__ __forceinline__ uint32_t column(const gs_recur& a, int block, int width) {
+    return (uint32_t)max(0, min(block * width + min(2 * lane_id(), width - 2), a.cols - 2));
+}
 
 // A gate in one register: the smaller of a and 1 - a, t / (1 + t) with t =
 // exp(-|g|), with g's sign.  The other is 1 less it, so both keep their own last
@@ -178,7 +237,6 @@ __global__ void __launch_bounds__(GS_BLOCK) k_recur_empty(gs_recur a, const floa
 
 constexpr uint32_t kMap = 1, kState = 2;
 constexpr int kPolls = 1 << 22;
-constexpr int kAhead = 4;                      // maps on their way at once
 
 __device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
 __device__ __forceinline__ float2 unpair(uint64_t v) {
@@ -194,18 +252,44 @@ __device__ __forceinline__ void announce(uint32_t* flag, uint32_t what) {
     if (lane_id() == 0) __hip_atomic_store(flag, what, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// A wave's part: publishes the chunk's map m[0] h + b[0], m[1] h + b[1] (anew:
-// its last state b), waits for the state in front of the chunk, publishes the one
+// The chunk's own map, from those of its waves; true: a segment starts (ends) in it.
+__device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* anew, int lane, float* m, float* b) {
+    m[0] = m[1] = 1.0f;
+    b[0] = b[1] = 0.0f;
+    bool any = false;
+    for (int u = 0; u < kWaves; ++u) {
+        const float4 v = maps[u * GS_WAVE + lane];
+        if (anew[u]) {
+            any = true;
+            b[0] = v.z;
+            b[1] = v.w;
+        } else {
+            b[0] = fmaf(v.x, b[0], v.z);
+            b[1] = fmaf(v.y, b[1], v.w);
+        }
+        m[0] *= v.x;
+        m[1] *= v.y;
+    }
+    return any;
+}
+
+// A wave's part: publishes the chunk's map (a chunk in which a segment starts:
+// its last state), waits for the state in front of the chunk, publishes the one
 // behind it, and leaves in h the one in front.  `needed`: someone here reads it.
-__device__ __forceinline__ void look_back(const Recur& r, int chunk, int block, const float* m, const float* b, bool anew,
+// own, anew: the waves' maps in LDS, read a second time for the state, since
+// registers are short.
+template <int kAhead>                          // maps on their way at once
+__device__ __forceinline__ void look_back(const Recur& r, int chunk, int block, const float4* own, const uint32_t* anew,
                                           bool needed, float* h) {
     const int l = lane_id();
     const int64_t at = (int64_t)block * r.chunks;
     uint64_t* maps = r.maps + at * (2 * GS_WAVE);
     uint64_t* states = r.states + at * GS_WAVE;
     uint32_t* flags = r.flags + at;
+    float m[2], b[2];
     h[0] = h[1] = 0.0f;
-    if (anew) {
+    const bool any = whole_map(own, anew, l, m, b);
+    if (any) {
         put(states + (int64_t)chunk * GS_WAVE + l, pair(b[0], b[1]));
         announce(flags + chunk, kState);
         if (!needed) return;
@@ -260,7 +344,8 @@ __device__ __forceinline__ void look_back(const Recur& r, int chunk, int block, 
         }
         j -= GS_WAVE;
     }
-    if (anew) return;
+    if (any) return;
+    whole_map(own, anew, l, m, b);
     put(states + (int64_t)chunk * GS_WAVE + l, pair(fmaf(m[0], h[0], b[0]), fmaf(m[1], h[1], b[1])));
     announce(flags + chunk, kState);
 }
@@ -276,31 +361,10 @@ __device__ __forceinline__ bool take_chunk(const Recur& r, uint32_t* shared, int
     return t < (uint32_t)all;
 }
 
-// The chunk's own map, from those of its waves; true: a segment starts (ends) in it.
-__device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* anew, int lane, float* m, float* b) {
-    m[0] = m[1] = 1.0f;
-    b[0] = b[1] = 0.0f;
-    bool any = false;
-    for (int u = 0; u < kWaves; ++u) {
-        const float4 v = maps[u * GS_WAVE + lane];
-        if (anew[u]) {
-            any = true;
-            b[0] = v.z;
-            b[1] = v.w;
-        } else {
-            b[0] = fmaf(v.x, b[0], v.z);
-            b[1] = fmaf(v.y, b[1], v.w);
-        }
-        m[0] *= v.x;
-        m[1] *= v.y;
-    }
-    return any;
-}
-
 // ALONE: the list is one chunk, which looks nowhere and has no map of places.
 // Two workgroups a compute unit (4 waves a SIMD) where the registers allow it.
-template <typename T, bool TAIL, bool ALONE>
-__global__ void __launch_bounds__(kWaves * GS_WAVE, TAIL ? 2 : 4) k_recur(Recur r, RecurOut o) {
+template <typename T, bool ONE, bool ALONE>
+__global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur(Recur r, RecurOut o) {
     __shared__ float4 maps[kWaves * GS_WAVE];
     __shared__ float2 front[GS_WAVE];
     __shared__ uint32_t anew[kWaves], ticket;
@@ -308,40 +372,52 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, TAIL ? 2 : 4) k_recur(Recur 
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
     int chunk = 0, block = blockIdx.x;
     if (!ALONE && !take_chunk(r, &ticket, chunk, block)) return;
-    const uint32_t col = block * kCols + 2 * l;
-    const int there = a.cols - (int)col;
+    const uint32_t col = column(a, block, r.width);
     Tokens tk;
     tk.find<!ALONE>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
-    Two<T, TAIL> gs[kSteps], xs[kSteps];
+    Two<T, ONE> gs[kSteps], xs[kSteps];
+    // behind the last place the last one's row, whose values are not used
+    const int32_t first = min(tk.p0, a.n - 1);
+    Rows gate = Rows::of<T>(a, tk, a.gate, a.ld_gate, first, false), x = Rows::of<T>(a, tk, a.x, a.ld_x, first, false);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const int64_t t = tk.token(a, i);
-        gs[i].load(static_cast<const T*>(a.gate) + t * a.ld_gate, col, there);
-        xs[i].load(static_cast<const T*>(a.x) + t * a.ld_x, col, there);
-    }
-    float h0[kSteps][2];
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        h0[i][0] = h0[i][1] = 0.0f;
-        if (a.initial && bit(tk.starts & tk.inside, i)) {
-            Two<float, TAIL> v;
-            v.load(a.initial + (int64_t)tk.segment(i) * a.cols, col, there);
-            h0[i][0] = v[0];
-            h0[i][1] = v[1];
-        }
+        gs[i].load(gate.p, col);
+        xs[i].load(x.p, col);
+        gate.next(tk.p0 + i + 1 < a.n);
+        x.next(tk.p0 + i + 1 < a.n);
     }
     float A[kSteps][2], B[kSteps][2], m[2] = {1.0f, 1.0f}, h[2] = {0.0f, 0.0f};
+    const uint32_t firsts = a.initial ? tk.starts & tk.inside : 0u;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {         // the initial states, all on their way at once
+        B[i][0] = B[i][1] = 0.0f;
+        if (bit(firsts, i)) {
+            Two<float, ONE> v;
+            v.load(a.initial, tk.segment(i), a.cols, col);
+            B[i][0] = v[0];
+            B[i][1] = v[1];
+        }
+    }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const bool starts = bit(tk.starts, i), in = bit(tk.inside, i);
+        if (bit(tk.starts, i)) {
+            rare();
+            m[0] = m[1] = h[0] = h[1] = 0.0f;
+        }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float z;
             open(gate_of(gs[i][c]), A[i][c], z);
-            const float zx = z * xs[i][c];
-            B[i][c] = !in ? 0.0f : starts ? (a.initial ? fmaf(A[i][c], h0[i][c], zx) : zx) : zx;
-            m[c] = starts ? 0.0f : m[c] * A[i][c];
-            h[c] = starts ? B[i][c] : fmaf(A[i][c], h[c], B[i][c]);
+            B[i][c] = fmaf(A[i][c], B[i][c], z * xs[i][c]);
+        }
+        if (!bit(tk.inside, i)) {
+            rare();
+            B[i][0] = B[i][1] = A[i][0] = A[i][1] = 0.0f;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            m[c] *= A[i][c];
+            h[c] = fmaf(A[i][c], h[c], B[i][c]);
         }
     }
     maps[w * GS_WAVE + l] = make_float4(m[0], m[1], h[0], h[1]);
@@ -350,9 +426,8 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, TAIL ? 2 : 4) k_recur(Recur 
     h[0] = h[1] = 0.0f;
     if (!ALONE) {
         if (w == 0) {
-            float am[2], ab[2], f[2];
-            const bool any = whole_map(maps, anew, l, am, ab);
-            look_back(r, chunk, block, am, ab, any, !bit(tk.starts, 0), f);
+            float f[2];
+            look_back<4>(r, chunk, block, maps, anew, !bit(tk.starts, 0), f);
             front[l] = make_float2(f[0], f[1]);
         }
         __syncthreads();
@@ -361,18 +436,21 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, TAIL ? 2 : 4) k_recur(Recur 
     }
     through(maps, anew, 0, w, l, h);
     if (o.kept && tk.p0 % GS_RECUR_KEEP == 0 && tk.p0 < a.n)
-        Two<float, TAIL>::store(o.kept + (int64_t)(tk.p0 / GS_RECUR_KEEP) * a.cols, col, there,
-                                bit(tk.starts, 0) ? 0.0f : h[0], bit(tk.starts, 0) ? 0.0f : h[1]);
+        Two<float, ONE>::store(o.kept, tk.p0 / GS_RECUR_KEEP, a.cols, col, bit(tk.starts, 0) ? 0.0f : h[0],
+                               bit(tk.starts, 0) ? 0.0f : h[1]);
+    const uint32_t written = a.fill ? tk.there(a) : tk.inside, lasts = o.final ? tk.ends & tk.inside : 0u;
+    Rows y = Rows::of<T>(a, tk, o.y, o.ld_y, first, false);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const bool starts = bit(tk.starts, i);
+        if (bit(tk.starts, i)) {
+            rare();
+            h[0] = h[1] = 0.0f;
+        }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) h[c] = starts ? B[i][c] : fmaf(A[i][c], h[c], B[i][c]);
-        const bool in = bit(tk.inside, i);
-        if (in || (a.fill && (int64_t)tk.p0 + i < a.n))
-            Two<T, TAIL>::store(static_cast<T*>(o.y) + tk.token(a, i) * o.ld_y, col, there, h[0], h[1]);
-        if (in && o.final && bit(tk.ends, i))
-            Two<float, TAIL>::store(o.final + (int64_t)tk.segment(i) * a.cols, col, there, h[0], h[1]);
+        for (int c = 0; c < 2; ++c) h[c] = fmaf(A[i][c], h[c], B[i][c]);
+        if (bit(written, i)) Two<T, ONE>::store(y.p, col, h[0], h[1]);
+        y.next();
+        if (bit(lasts, i)) Two<float, ONE>::store(o.final, tk.segment(i), a.cols, col, h[0], h[1]);
     }
 }
 
@@ -381,8 +459,8 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, TAIL ? 2 : 4) k_recur(Recur 
 //   dx_t = (1 - a_t) D_t;  dgate_t = a_t (1 - a_t) (h_{t-1} - x_t) D_t;  dinitial = c of the first token.
 // h is formed again from the states that the forward kept every GS_RECUR_KEEP
 // tokens, in fp32, not read in the tokens' type.
-template <typename T, bool TAIL, bool ALONE>
-__global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recur_grads o) {
+template <typename T, bool ONE, bool ALONE>
+__global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur_bwd(Recur r, gs_recur_grads o) {
     __shared__ float4 maps[kWaves * GS_WAVE], back[kWaves * GS_WAVE];
     __shared__ float2 front[GS_WAVE];
     __shared__ uint32_t anew[kWaves], ended[kWaves], ticket;
@@ -391,78 +469,106 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
     int turn = 0, block = blockIdx.x;          // chunks are taken from the last one on
     if (!ALONE && !take_chunk(r, &ticket, turn, block)) return;
     const int chunk = r.chunks - 1 - turn;
-    const uint32_t col = block * kCols + 2 * l;
-    const int there = a.cols - (int)col;
+    const uint32_t col = column(a, block, r.width);
     Tokens tk;
     tk.find<!ALONE>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
-    Two<T, TAIL> gs[kSteps], xs[kSteps], ds[kSteps];
+    Two<T, ONE> gs[kSteps], xs[kSteps], ds[kSteps];
+    // behind the last place the last one's row, whose values are not used
+    const int32_t first = min(tk.p0, a.n - 1), end = min(tk.p0 + kSteps, a.n) - 1;
+    Rows gate = Rows::of<T>(a, tk, a.gate, a.ld_gate, first, false), x = Rows::of<T>(a, tk, a.x, a.ld_x, first, false);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const int64_t t = tk.token(a, i);
-        gs[i].load(static_cast<const T*>(a.gate) + t * a.ld_gate, col, there);
-        ds[i].load(static_cast<const T*>(o.dy) + t * o.ld_dy, col, there);
-        xs[i].load(static_cast<const T*>(a.x) + t * a.ld_x, col, there);
+        gs[i].load(gate.p, col);
+        xs[i].load(x.p, col);
+        gate.next(tk.p0 + i + 1 < a.n);
+        x.next(tk.p0 + i + 1 < a.n);
     }
-    // the way back through the wave's tokens: c -> m c + b
-    float D[kSteps][2], S[kSteps][2], m[2] = {1.0f, 1.0f}, b[2] = {0.0f, 0.0f};
+    auto load_dy = [&]() {
+        Rows dy = Rows::of<T>(a, tk, o.dy, o.ld_dy, first, false);
 #pragma unroll
-    for (int i = kSteps - 1; i >= 0; --i) {
-        const bool in = bit(tk.inside, i), ends = bit(tk.ends, i);
-        D[i][0] = in ? ds[i][0] : 0.0f;
-        D[i][1] = in ? ds[i][1] : 0.0f;
-        if (in && ends && o.dfinal) {
-            Two<float, TAIL> v;
-            v.load(o.dfinal + (int64_t)tk.segment(i) * a.cols, col, there);
-            D[i][0] += v[0];
-            D[i][1] += v[1];
+        for (int i = 0; i < kSteps; ++i) {
+            ds[i].load(dy.p, col);
+            dy.next(tk.p0 + i + 1 < a.n);
+            if (!bit(tk.inside, i)) {
+                rare();
+                ds[i].fill(0.0f);
+            }
         }
+    };
+    load_dy();
+    // tokens outside every segment: a gate that holds, and zeros
+    if (tk.inside != kAllSteps) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+            if (!bit(tk.inside, i)) {
+                rare();
+                gs[i].fill(INFINITY);
+                xs[i].fill(0.0f);
+            }
+    }
+    const uint32_t firsts = a.initial ? tk.starts & tk.inside : 0u, lasts = o.dfinal ? tk.ends & tk.inside : 0u;
+    // states of the row's segment
+    auto state_of = [&](const float* from, int i, float* h) {
+        Two<float, ONE> v;
+        v.load(from, tk.segment(i), a.cols, col);
+        h[0] = v[0];
+        h[1] = v[1];
+    };
+    // The wave's two maps: h -> m h + h, and on the way back, whose terms are
+    // summed from the same end, c -> bm c + b up to the first token that ends a
+    // segment.  A gate is kept in one register, dy and x stay as they were
+    // loaded: floats of all would leave room for one workgroup a compute unit.
+    float S[kSteps][2], m[2] = {1.0f, 1.0f}, h[2] = {0.0f, 0.0f}, bm[2] = {1.0f, 1.0f}, b[2] = {0.0f, 0.0f};
+    const int first_end = tk.ends ? __ffs(tk.ends) - 1 : kSteps;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        if (bit(tk.starts, i)) {
+            rare();
+            m[0] = m[1] = h[0] = h[1] = 0.0f;
+            if (bit(firsts, i)) state_of(a.initial, i, h);
+        }
+        float A[2], z;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            float A, z;
             S[i][c] = gate_of(gs[i][c]);
-            open(S[i][c], A, z);
-            if (!in) A = 0.0f;
-            m[c] = ends ? 0.0f : m[c] * A;
-            b[c] = A * (ends ? D[i][c] : D[i][c] + b[c]);
+            open(S[i][c], A[c], z);
+            m[c] *= A[c];
+            h[c] = fmaf(A[c], h[c], z * xs[i][c]);
+        }
+        if (i <= first_end) {
+            rare();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                bm[c] *= A[c];
+                b[c] = fmaf(bm[c], ds[i][c], b[c]);
+            }
+            if (bit(lasts, i)) {
+                float d[2];
+                state_of(o.dfinal, i, d);
+                b[0] = fmaf(bm[0], d[0], b[0]);
+                b[1] = fmaf(bm[1], d[1], b[1]);
+            }
         }
     }
-    back[(kWaves - 1 - w) * GS_WAVE + l] = make_float4(m[0], m[1], b[0], b[1]);
-    if (l == 0) ended[kWaves - 1 - w] = tk.ends != 0;
-    // the states again: the wave's own map, then those of the waves behind the kept state
-    float h[2] = {0.0f, 0.0f}, fm[2] = {1.0f, 1.0f};
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        const bool starts = bit(tk.starts, i), in = bit(tk.inside, i);
-        float h0[2] = {0.0f, 0.0f};
-        if (in && starts && a.initial) {
-            Two<float, TAIL> v;
-            v.load(a.initial + (int64_t)tk.segment(i) * a.cols, col, there);
-            h0[0] = v[0];
-            h0[1] = v[1];
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float A, z;
-            loaded(S[i][c]);                   // opened again in each walk: held open, gates take twice the registers
-            open(S[i][c], A, z);
-            const float zx = in ? z * xs[i][c] : 0.0f;
-            fm[c] = starts ? 0.0f : fm[c] * A;
-            h[c] = !starts ? fmaf(A, h[c], zx) : in && a.initial ? fmaf(A, h0[c], zx) : zx;
-        }
+    if (tk.ends) bm[0] = bm[1] = 0.0f;
+    back[(kWaves - 1 - w) * GS_WAVE + l] = make_float4(bm[0], bm[1], b[0], b[1]);
+    maps[w * GS_WAVE + l] = make_float4(m[0], m[1], h[0], h[1]);
+    if (l == 0) {
+        ended[kWaves - 1 - w] = tk.ends != 0;
+        anew[w] = tk.starts != 0;
     }
-    maps[w * GS_WAVE + l] = make_float4(fm[0], fm[1], h[0], h[1]);
-    if (l == 0) anew[w] = tk.starts != 0;
     __syncthreads();
     if (!ALONE && w == kWaves - 1) {
-        float am[2], ab[2], f[2];
-        const bool any = whole_map(back, ended, l, am, ab);
-        look_back(r, turn, block, am, ab, any, !bit(tk.ends, kSteps - 1), f);
+        float f[2];
+        look_back<sizeof(T) == 4 ? 1 : 4>(r, turn, block, back, ended, !bit(tk.ends, kSteps - 1), f);
         front[l] = make_float2(f[0], f[1]);
+        if (sizeof(T) == 4) load_dy();         // there are no registers to hold it meanwhile
     }
+    // the states again, from the kept one in front
     h[0] = h[1] = 0.0f;
     if (tk.p0 < a.n) {
-        Two<float, TAIL> v;
-        v.load(o.kept + (int64_t)(tk.p0 / GS_RECUR_KEEP) * a.cols, col, there);
+        Two<float, ONE> v;
+        v.load(o.kept, tk.p0 / GS_RECUR_KEEP, a.cols, col);
         h[0] = v[0];
         h[1] = v[1];
     }
@@ -470,23 +576,21 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
     float K[kSteps][2];                        // a (1 - a) (h_{t-1} - x_t)
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const bool starts = bit(tk.starts, i), in = bit(tk.inside, i);
-        if (starts) {
+        if (bit(tk.starts, i)) {
+            rare();
             h[0] = h[1] = 0.0f;
-            if (in && a.initial) {
-                Two<float, TAIL> v;
-                v.load(a.initial + (int64_t)tk.segment(i) * a.cols, col, there);
-                h[0] = v[0];
-                h[1] = v[1];
-            }
+            if (bit(firsts, i)) state_of(a.initial, i, h);
         }
+        xs[i].again();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float A, z;
-            loaded(S[i][c]);
+            loaded(S[i][c]);                   // opened again in each walk: held open, gates take twice the registers
             open(S[i][c], A, z);
-            K[i][c] = A * z * (h[c] - xs[i][c]);
-            h[c] = fmaf(A, h[c], z * xs[i][c]);
+            const float x = xs[i][c];
+            K[i][c] = A * z * (h[c] - x);
+            loaded(K[i][c]);                   // here, not where it is used: its factors would be held until then
+            h[c] = fmaf(A, h[c], z * x);
         }
     }
     float g[2] = {0.0f, 0.0f};
@@ -496,39 +600,48 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE) k_recur_bwd(Recur r, gs_recu
         g[1] = front[l].y;
     }
     through(back, ended, 0, kWaves - 1 - w, l, g);
+    const uint32_t written = a.fill ? tk.there(a) : tk.inside, starts = o.dinitial ? tk.starts & tk.inside : 0u;
+    Rows dxs = Rows::of<T>(a, tk, o.dx, o.ld_dx, end, true), dgs = Rows::of<T>(a, tk, o.dgate, o.ld_dgate, end, true);
 #pragma unroll
     for (int i = kSteps - 1; i >= 0; --i) {
-        const bool in = bit(tk.inside, i), ends = bit(tk.ends, i);
+        if (bit(tk.ends, i)) {
+            rare();
+            g[0] = g[1] = 0.0f;
+            if (bit(lasts, i)) state_of(o.dfinal, i, g);
+        }
         float dx[2], dg[2];
+        ds[i].again();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float A, z;
             loaded(S[i][c]);
             open(S[i][c], A, z);
-            const float d = ends ? D[i][c] : D[i][c] + g[c];
-            dx[c] = in ? z * d : 0.0f;
-            dg[c] = in ? K[i][c] * d : 0.0f;
-            g[c] = in ? A * d : 0.0f;
+            const float d = ds[i][c] + g[c];
+            dx[c] = z * d;
+            dg[c] = K[i][c] * d;
+            g[c] = A * d;
         }
-        if (in || (a.fill && (int64_t)tk.p0 + i < a.n)) {
-            const int64_t t = tk.token(a, i);
-            Two<T, TAIL>::store(static_cast<T*>(o.dx) + t * o.ld_dx, col, there, dx[0], dx[1]);
-            Two<T, TAIL>::store(static_cast<T*>(o.dgate) + t * o.ld_dgate, col, there, dg[0], dg[1]);
+        if (bit(written, i)) {
+            Two<T, ONE>::store(dxs.p, col, dx[0], dx[1]);
+            Two<T, ONE>::store(dgs.p, col, dg[0], dg[1]);
         }
-        if (in && o.dinitial && bit(tk.starts, i))
-            Two<float, TAIL>::store(o.dinitial + (int64_t)tk.segment(i) * a.cols, col, there, g[0], g[1]);
+        dxs.next(tk.p0 + i < a.n);
+        dgs.next(tk.p0 + i < a.n);
+        if (bit(starts, i)) Two<float, ONE>::store(o.dinitial, tk.segment(i), a.cols, col, g[0], g[1]);
     }
 }
 
 struct RecurPlan {
-    int32_t chunks, blocks;
+    int32_t chunks, blocks, width;
     size_t map, maps, states, flags, bytes;
 };
 
 RecurPlan recur_plan(int32_t n, int32_t cols) {
     RecurPlan p;
     p.chunks = (int32_t)div_up(n, kChunk);
-    p.blocks = (int32_t)div_up(cols, kCols);
+    p.width = kCols;                           // so that no block has a single channel
+    while (cols > 1 && cols % p.width == 1) p.width -= 2;
+    p.blocks = (int32_t)div_up(cols, p.width);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -550,6 +663,7 @@ Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
     r.a = a;
     r.chunks = p.chunks;
     r.blocks = p.blocks;
+    r.width = p.width;
     const bool alone = p.chunks <= 1;
     r.map = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.map);
     r.maps = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.maps);
@@ -569,38 +683,38 @@ void empty_segments(const gs_recur& a, const float* from, float* to, hipStream_t
         k_recur_empty<<<std::min(a.n_seg, 4096), GS_BLOCK, 0, st>>>(a, from, to);
 }
 
-template <typename T, bool TAIL>
+template <typename T, bool ONE>
 hipError_t recur_go(const Recur& r, const RecurOut& o, hipStream_t st) {
     const uint32_t grid = (uint32_t)r.chunks * r.blocks;
     if (r.chunks == 1) {
-        k_recur<T, TAIL, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        k_recur<T, ONE, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
     } else {
         recur_map(r, st);
-        k_recur<T, TAIL, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        k_recur<T, ONE, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
     }
     return hipGetLastError();
 }
 
-template <typename T, bool TAIL>
+template <typename T, bool ONE>
 hipError_t recur_bwd_go(const Recur& r, const gs_recur_grads& g, hipStream_t st) {
     const uint32_t grid = (uint32_t)r.chunks * r.blocks;
     if (r.chunks == 1) {
-        k_recur_bwd<T, TAIL, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
+        k_recur_bwd<T, ONE, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
     } else {
         recur_map(r, st);
-        k_recur_bwd<T, TAIL, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
+        k_recur_bwd<T, ONE, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
     }
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t recur_type(const Recur& r, const RecurOut& o, hipStream_t st) {
-    return r.a.cols % 2 ? recur_go<T, true>(r, o, st) : recur_go<T, false>(r, o, st);
+    return r.a.cols == 1 ? recur_go<T, true>(r, o, st) : recur_go<T, false>(r, o, st);
 }
 
 template <typename T>
 hipError_t recur_bwd_type(const Recur& r, const gs_recur_grads& g, hipStream_t st) {
-    return r.a.cols % 2 ? recur_bwd_go<T, true>(r, g, st) : recur_bwd_go<T, false>(r, g, st);
+    return r.a.cols == 1 ? recur_bwd_go<T, true>(r, g, st) : recur_bwd_go<T, false>(r, g, st);
 }
 
 }  // namespace
