@@ -25,6 +25,8 @@ namespace {
 constexpr int kSteps = 16;                     // tokens of a wave
 constexpr int kWaves = 8;                      // of a workgroup
 constexpr int kChunk = kSteps * kWaves;
+constexpr int kAloneWaves = 16;                // of the only workgroup along the tokens
+constexpr int kAloneChunk = kSteps * kAloneWaves;
 constexpr int kCols = 2 * GS_WAVE;             // channels of a workgroup at most
 constexpr int kKeptWaves = GS_RECUR_KEEP / kSteps;
 static_assert(GS_RECUR_KEEP % kSteps == 0 && kChunk % GS_RECUR_KEEP == 0, "a kept state is in front of a wave");
@@ -34,7 +36,6 @@ constexpr uint32_t kStart = 1, kEnd = 2, kOutside = 0xFFFFFFFFu;
 
 struct Recur {
     gs_recur a;
-    const uint32_t* map;                       // of place p: segment << 2 | kEnd | kStart, or kOutside
     uint64_t* maps;                            // [blocks][chunks][2 * 64]: (A, B) of a lane's two channels
     uint64_t* states;                          // [blocks][chunks][64]: a lane's two states behind the chunk
     uint32_t* flags;                           // [blocks][chunks]: kMap, then kState; behind them the ticket
@@ -53,46 +54,89 @@ __device__ __forceinline__ int32_t start_of(const gs_recur& a, int32_t s) {
     return min(max(a.cu[s], 0), a.n);
 }
 
-// What the map holds for place p.
-__device__ __forceinline__ uint32_t place_word(const gs_recur& a, int32_t p) {
-    const int32_t t = a.reverse ? a.n - 1 - p : p;
-    int32_t lo = 0, hi = a.n_seg;              // the last s with start_of(s) <= t
-    if (a.cu == nullptr) {
-        lo = t / (a.n / a.n_seg);
-    } else {
-        while (lo < hi) {
-            const int32_t mid = (int32_t)(((int64_t)lo + hi + 1) / 2);
-            if (start_of(a, mid) <= t) lo = mid;
-            else hi = mid - 1;
-        }
-    }
-    if (lo >= a.n_seg) return kOutside;
-    const int32_t first = start_of(a, lo), end = start_of(a, lo + 1);
-    if (t < first || t >= end) return kOutside;
+// A place: segment << 2 | kEnd | kStart, or kOutside.
+__device__ __forceinline__ uint32_t word_of(const gs_recur& a, int32_t t, int32_t s, int32_t first, int32_t end) {
+    if (s < 0 || s >= a.n_seg || t < first || t >= end) return kOutside;
     const bool at_first = t == first, at_last = t == end - 1;
-    return (uint32_t)lo << 2 | ((a.reverse ? at_first : at_last) ? kEnd : 0u) | ((a.reverse ? at_last : at_first) ? kStart : 0u);
+    return (uint32_t)s << 2 | ((a.reverse ? at_first : at_last) ? kEnd : 0u) | ((a.reverse ? at_last : at_first) ? kStart : 0u);
 }
 
-// The places' words, and the flags and the ticket cleared.
-__global__ void __launch_bounds__(GS_BLOCK) k_recur_map(gs_recur a, uint32_t* __restrict__ map, uint32_t* __restrict__ flags,
-                                                        int32_t n_flags) {
-    const int64_t p = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x;
-    if (p < a.n) map[p] = place_word(a, (int32_t)p);
-    if (p < n_flags) flags[p] = 0;
+// Segments without a token pass their states on (from NULL: 0): a wave's part of
+// them, 64 segments at a time.
+__device__ __forceinline__ void pass_empty(const gs_recur& a, const float* from, float* to, int wave, int waves) {
+    if (to == nullptr || (a.cu == nullptr && a.n > 0)) return;
+    for (int32_t s0 = wave * GS_WAVE; s0 < a.n_seg; s0 += waves * GS_WAVE) {
+        const int32_t s = s0 + lane_id();
+        uint64_t empty = __ballot(s < a.n_seg && (a.cu == nullptr || start_of(a, s) >= start_of(a, s + 1)));
+        for (; empty; empty &= empty - 1) {
+            const int64_t row = (int64_t)(s0 + __ffsll((unsigned long long)empty) - 1) * a.cols;
+            for (int32_t c = lane_id(); c < a.cols; c += GS_WAVE) to[row + c] = from ? from[row + c] : 0.0f;
+        }
+    }
+}
+
+// The flags and the ticket cleared, the empty segments' states.
+__global__ void __launch_bounds__(GS_BLOCK) k_recur_clear(gs_recur a, const float* from, float* to, uint32_t* flags,
+                                                          int32_t n_flags) {
+    for (int64_t i = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x; i < n_flags; i += (int64_t)gridDim.x * GS_BLOCK) flags[i] = 0;
+    pass_empty(a, from, to, blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE, gridDim.x * (GS_BLOCK / GS_WAVE));
 }
 
 // A wave's tokens: bit i of the masks is place p0 + i (scalars).
 struct Tokens {
-    uint32_t word;                             // lane i: of place p0 + i
+    uint32_t word;                             // lane i: place p0 + i
     uint32_t starts, ends, inside;
     int32_t p0;
 
-    template <bool MAPPED>
-    __device__ __forceinline__ void find(const Recur& r, int32_t first) {
-        p0 = first;
+    // The wave looks its places up together: 64 starts at a time narrow the
+    // segments down to the first place's, then 64 starts from there on serve all
+    // places (one reading up to 63 segments, three up to 4095).
+    __device__ __forceinline__ void find(const gs_recur& a, int32_t place0) {
+        p0 = place0;
         const int l = lane_id();
+        const int32_t p = p0 + l, t = a.reverse ? a.n - 1 - p : p;
         word = kOutside;
-        if (l < kSteps && (int64_t)first + l < r.a.n) word = MAPPED ? r.map[first + l] : place_word(r.a, first + l);
+        if (p0 >= a.n) {
+            // nothing of it is a token
+        } else if (a.cu == nullptr) {
+            const int32_t len = a.n / a.n_seg, s = t / len;
+            if (l < kSteps && p < a.n) word = word_of(a, t, s, s * len, s * len + len);
+        } else {
+            const int32_t p1 = min(p0 + kSteps, a.n) - 1;
+            const int32_t low = a.reverse ? a.n - 1 - p1 : p0, high = a.reverse ? a.n - 1 - p0 : p1;
+            int32_t base = 0;
+            if (a.n_seg >= GS_WAVE) {
+                int32_t len = a.n_seg + 1;     // starts from `base` on, one of which is the last that is <= low
+                for (;;) {
+                    const int32_t step = (len + GS_WAVE - 1) / GS_WAVE, at = base + l * step;
+                    const int c = popc64(__ballot(l * step < len && start_of(a, min(at, a.n_seg)) <= low));
+                    const int32_t passed = max(c - 1, 0) * step;
+                    base += passed;
+                    if (step == 1) break;
+                    len = min(step, len - passed);
+                }
+            }
+            const int32_t mine = base + l <= a.n_seg ? start_of(a, base + l) : 0x7FFFFFFF;
+            if (__builtin_amdgcn_readlane(mine, GS_WAVE - 1) > high) {
+                int k = 0;                     // starts up to the lane's place
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const int32_t ti = a.reverse ? a.n - 1 - (p0 + i) : p0 + i;
+                    const int c = popc64(__ballot(mine <= ti));
+                    if (l == i) k = c;
+                }
+                const int32_t first = __shfl(mine, max(k - 1, 0), GS_WAVE), end = __shfl(mine, k, GS_WAVE);
+                if (l < kSteps && p < a.n) word = word_of(a, t, base + k - 1, first, end);
+            } else if (l < kSteps && p < a.n) {            // very many segments end here
+                int32_t lo = 0, hi = a.n_seg;  // the last s with start_of(s) <= t
+                while (lo < hi) {
+                    const int32_t mid = (int32_t)(((int64_t)lo + hi + 1) / 2);
+                    if (start_of(a, mid) <= t) lo = mid;
+                    else hi = mid - 1;
+                }
+                word = word_of(a, t, lo, start_of(a, lo), start_of(a, min(lo + 1, a.n_seg)));
+            }
+        }
         const bool in = word != kOutside;
         inside = (uint32_t)__ballot(in);
         starts = (uint32_t)__ballot(in && (word & kStart)) | (~inside & kAllSteps);
@@ -217,15 +261,6 @@ __device__ __forceinline__ void through(const float4* maps, const uint32_t* anew
     }
 }
 
-// Segments without a token pass their states on.
-__global__ void __launch_bounds__(GS_BLOCK) k_recur_empty(gs_recur a, const float* from, float* to) {
-    for (int32_t s = blockIdx.x; s < a.n_seg; s += gridDim.x) {
-        if (a.n > 0 && (a.cu == nullptr || start_of(a, s) < start_of(a, s + 1))) continue;
-        for (int32_t c = threadIdx.x; c < a.cols; c += GS_BLOCK)
-            to[(int64_t)s * a.cols + c] = from ? from[(int64_t)s * a.cols + c] : 0.0f;
-    }
-}
-
 // ---------------------------------------------------------------------------
 // Looking back.  The workgroups take chunks by a ticket, chunk after chunk, so
 // every chunk that one waits for belongs to a workgroup that is already running
@@ -273,81 +308,96 @@ __device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* an
     return any;
 }
 
-// A wave's part: publishes the chunk's map (a chunk in which a segment starts:
-// its last state), waits for the state in front of the chunk, publishes the one
-// behind it, and leaves in h the one in front.  `needed`: someone here reads it.
-// own, anew: the waves' maps in LDS, read a second time for the state, since
-// registers are short.
-template <int kAhead>                          // maps on their way at once
-__device__ __forceinline__ void look_back(const Recur& r, int chunk, int block, const float4* own, const uint32_t* anew,
-                                          bool needed, float* h) {
+struct Lookers {                               // in LDS
+    float4 passed[kWaves * GS_WAVE];           // a wave's maps of the chunks in front, as one
+    float2 state[GS_WAVE];                     // behind the chunk that the nearest known state is of
+    int32_t distance;                          // chunks from the nearest to that one
+};
+constexpr int kNotNeeded = -1, kGaveUp = -2;
+
+// One wave's part: publishes the chunk's map, or where a segment starts in the
+// chunk its last state; true then.
+__device__ __forceinline__ bool publish(const Recur& r, int chunk, int block, const float4* own, const uint32_t* anew) {
     const int l = lane_id();
-    const int64_t at = (int64_t)block * r.chunks;
-    uint64_t* maps = r.maps + at * (2 * GS_WAVE);
-    uint64_t* states = r.states + at * GS_WAVE;
-    uint32_t* flags = r.flags + at;
+    const int64_t at = (int64_t)block * r.chunks + chunk;
     float m[2], b[2];
-    h[0] = h[1] = 0.0f;
     const bool any = whole_map(own, anew, l, m, b);
     if (any) {
-        put(states + (int64_t)chunk * GS_WAVE + l, pair(b[0], b[1]));
-        announce(flags + chunk, kState);
-        if (!needed) return;
+        put(r.states + at * GS_WAVE + l, pair(b[0], b[1]));
+        announce(r.flags + at, kState);
     } else {
-        put(maps + (int64_t)chunk * (2 * GS_WAVE) + l, pair(m[0], b[0]));
-        put(maps + (int64_t)chunk * (2 * GS_WAVE) + GS_WAVE + l, pair(m[1], b[1]));
-        announce(flags + chunk, kMap);
+        put(r.maps + at * (2 * GS_WAVE) + l, pair(m[0], b[0]));
+        put(r.maps + at * (2 * GS_WAVE) + GS_WAVE + l, pair(m[1], b[1]));
+        announce(r.flags + at, kMap);
     }
-    // from the nearest chunk on: the map through those that were passed
-    float pm[2] = {1.0f, 1.0f}, pb[2] = {0.0f, 0.0f};
-    int j = chunk - 1, polls = 0;
-    for (;;) {
-        const uint32_t f = j - l >= 0 ? __hip_atomic_load(flags + j - l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+    return any;
+}
+
+// One wave's part: waits until a state is known within the 64 chunks in front and
+// the maps of those between are there; its distance.
+__device__ __forceinline__ int wait_for_state(const Recur& r, int chunk, int block) {
+    const int c = chunk - 1 - lane_id();
+    const uint32_t* flag = r.flags + (int64_t)block * r.chunks + c;
+    for (int polls = 0; polls < kPolls; ++polls) {
+        const uint32_t f = c >= 0 ? __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
         const uint64_t known = __ballot(f == kState), there = __ballot(f != 0u);
-        const int d = known ? __ffsll((unsigned long long)known) - 1 : GS_WAVE;      // maps to pass first
-        const uint64_t need = d == GS_WAVE ? ~0ull : (1ull << d) - 1;
-        if ((there & need) != need) {
-            if (++polls > kPolls) {
-                h[0] = h[1] = NAN;
-                break;
-            }
-            __builtin_amdgcn_s_sleep(1);
-            continue;
-        }
-        asm volatile("" ::: "memory");         // the values are read behind the flags
-        uint64_t s = 0;
-        if (known) s = get(states + (int64_t)(j - d) * GS_WAVE + l);
-        for (int k = 0; k < d; k += kAhead) {
-            uint64_t v[kAhead][2];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int64_t c = (int64_t)(j - min(k + i, d - 1)) * (2 * GS_WAVE) + l;
-                v[i][0] = get(maps + c);
-                v[i][1] = get(maps + c + GS_WAVE);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (k + i >= d) break;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const float2 ab = unpair(v[i][c]);
-                    pb[c] = fmaf(pm[c], ab.y, pb[c]);
-                    pm[c] *= ab.x;
-                }
-            }
-        }
-        if (known) {
-            const float2 v = unpair(s);
-            h[0] = fmaf(pm[0], v.x, pb[0]);
-            h[1] = fmaf(pm[1], v.y, pb[1]);
-            break;
-        }
-        j -= GS_WAVE;
+        if (known && (~there & ((known & -known) - 1)) == 0) return __ffsll((unsigned long long)known) - 1;
+        __builtin_amdgcn_s_sleep(1);
     }
-    if (any) return;
+    return kGaveUp;
+}
+
+// Every wave's part, `distance` the same for all: the maps between are cut into
+// slices, one a wave, all on their way at once; h: the state in front of the chunk.
+template <int kAhead>                          // maps on their way at once
+__device__ __forceinline__ void front_state(const Recur& r, int chunk, int block, Lookers& s, float* h) {
+    const int l = lane_id(), w = threadIdx.x / GS_WAVE, d = s.distance;
+    h[0] = h[1] = d == kGaveUp ? NAN : 0.0f;
+    if (d < 0) return;
+    const int64_t nearest = (int64_t)block * r.chunks + chunk - 1;
+    asm volatile("" ::: "memory");             // read behind the flags
+    if (w == kWaves - 1) s.state[l] = unpair(get(r.states + (nearest - d) * GS_WAVE + l));
+    const int per = (d + kWaves - 1) / kWaves, end = min((w + 1) * per, d);
+    float pm[2] = {1.0f, 1.0f}, pb[2] = {0.0f, 0.0f};
+    for (int k = w * per; k < end; k += kAhead) {
+        uint64_t v[kAhead][2];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const uint64_t* p = r.maps + (nearest - min(k + i, end - 1)) * (2 * GS_WAVE) + l;
+            v[i][0] = get(p);
+            v[i][1] = get(p + GS_WAVE);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (k + i >= end) break;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float2 ab = unpair(v[i][c]);
+                pb[c] = fmaf(pm[c], ab.y, pb[c]);
+                pm[c] *= ab.x;
+            }
+        }
+    }
+    s.passed[threadIdx.x] = make_float4(pm[0], pm[1], pb[0], pb[1]);
+    __syncthreads();
+    h[0] = s.state[l].x;
+    h[1] = s.state[l].y;
+    for (int u = min(kWaves, d) - 1; u >= 0; --u) {
+        const float4 v = s.passed[u * GS_WAVE + l];
+        h[0] = fmaf(v.x, h[0], v.z);
+        h[1] = fmaf(v.y, h[1], v.w);
+    }
+}
+
+// One wave's part: the state behind the chunk, from the one in front.
+__device__ __forceinline__ void publish_state(const Recur& r, int chunk, int block, const float4* own, const uint32_t* anew,
+                                              const float* h) {
+    const int l = lane_id();
+    const int64_t at = (int64_t)block * r.chunks + chunk;
+    float m[2], b[2];
     whole_map(own, anew, l, m, b);
-    put(states + (int64_t)chunk * GS_WAVE + l, pair(fmaf(m[0], h[0], b[0]), fmaf(m[1], h[1], b[1])));
-    announce(flags + chunk, kState);
+    put(r.states + at * GS_WAVE + l, pair(fmaf(m[0], h[0], b[0]), fmaf(m[1], h[1], b[1])));
+    announce(r.flags + at, kState);
 }
 
 // The next chunk (in the order of the recurrence) and its block of channels; false: none is left.
@@ -361,20 +411,28 @@ __device__ __forceinline__ bool take_chunk(const Recur& r, uint32_t* shared, int
     return t < (uint32_t)all;
 }
 
-// ALONE: the list is one chunk, which looks nowhere and has no map of places.
-// Two workgroups a compute unit (4 waves a SIMD) where the registers allow it.
-template <typename T, bool ONE, bool ALONE>
-__global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur(Recur r, RecurOut o) {
-    __shared__ float4 maps[kWaves * GS_WAVE];
-    __shared__ float2 front[GS_WAVE];
-    __shared__ uint32_t anew[kWaves], ticket;
+// ALONE: the list is one chunk, which looks nowhere; workgroups behind those of
+// the channels see to empty segments.  SHORT: the first states of all segments
+// are loaded at once (steps of served sequences start one at every token);
+// otherwise where they are used, and 16-bit tokens leave room for three
+// workgroups a unit instead of two.
+template <typename T, bool ONE, bool ALONE, bool SHORT>
+__global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHORT ? (ALONE || sizeof(T) == 2 ? 4 : 2) : sizeof(T) == 4 ? 4 : 6) k_recur(Recur r, RecurOut o) {
+    constexpr int WAVES = ALONE ? kAloneWaves : kWaves;
+    __shared__ float4 maps[WAVES * GS_WAVE];
+    __shared__ Lookers look;
+    __shared__ uint32_t anew[WAVES], ticket;
     const gs_recur& a = r.a;
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
     int chunk = 0, block = blockIdx.x;
+    if (ALONE && block >= r.blocks) {
+        pass_empty(a, a.initial, o.final, (block - r.blocks) * WAVES + w, (gridDim.x - r.blocks) * WAVES);
+        return;
+    }
     if (!ALONE && !take_chunk(r, &ticket, chunk, block)) return;
     const uint32_t col = column(a, block, r.width);
     Tokens tk;
-    tk.find<!ALONE>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
+    tk.p0 = __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps);
     Two<T, ONE> gs[kSteps], xs[kSteps];
     // behind the last place the last one's row, whose values are not used
     const int32_t first = min(tk.p0, a.n - 1);
@@ -386,38 +444,57 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur(Recur r, RecurOut
         gate.next(tk.p0 + i + 1 < a.n);
         x.next(tk.p0 + i + 1 < a.n);
     }
-    float A[kSteps][2], B[kSteps][2], m[2] = {1.0f, 1.0f}, h[2] = {0.0f, 0.0f};
-    const uint32_t firsts = a.initial ? tk.starts & tk.inside : 0u;
+    tk.find(a, tk.p0);                         // while the tokens are on their way
+    // tokens outside every segment: a gate that holds, and zeros
+    if (tk.inside != kAllSteps) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {         // the initial states, all on their way at once
-        B[i][0] = B[i][1] = 0.0f;
+        for (int i = 0; i < kSteps; ++i)
+            if (!bit(tk.inside, i)) {
+                rare();
+                gs[i].fill(INFINITY);
+                xs[i].fill(0.0f);
+            }
+    }
+    const uint32_t firsts = a.initial ? tk.starts & tk.inside : 0u;
+    // a segment's first state
+    auto first_of = [&](int i, float* h) {
+        h[0] = h[1] = 0.0f;
         if (bit(firsts, i)) {
             Two<float, ONE> v;
             v.load(a.initial, tk.segment(i), a.cols, col);
-            B[i][0] = v[0];
-            B[i][1] = v[1];
+            h[0] = v[0];
+            h[1] = v[1];
         }
-    }
+    };
+    float h0[SHORT ? kSteps : 1][2];
+    if (SHORT)
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) first_of(i, h0[SHORT ? i : 0]);
+    auto start = [&](int i, float* h) {
+        rare();
+        if (SHORT) {
+            h[0] = h0[SHORT ? i : 0][0];
+            h[1] = h0[SHORT ? i : 0][1];
+        } else {
+            first_of(i, h);
+        }
+    };
+    // The wave's map.  A gate is kept in one register and x as it was loaded, so
+    // that three workgroups fit a unit.
+    float S[kSteps][2], m[2] = {1.0f, 1.0f}, h[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         if (bit(tk.starts, i)) {
-            rare();
-            m[0] = m[1] = h[0] = h[1] = 0.0f;
+            m[0] = m[1] = 0.0f;
+            start(i, h);
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            float z;
-            open(gate_of(gs[i][c]), A[i][c], z);
-            B[i][c] = fmaf(A[i][c], B[i][c], z * xs[i][c]);
-        }
-        if (!bit(tk.inside, i)) {
-            rare();
-            B[i][0] = B[i][1] = A[i][0] = A[i][1] = 0.0f;
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            m[c] *= A[i][c];
-            h[c] = fmaf(A[i][c], h[c], B[i][c]);
+            float A, z;
+            S[i][c] = gate_of(gs[i][c]);
+            open(S[i][c], A, z);
+            m[c] *= A;
+            h[c] = fmaf(A, h[c], z * xs[i][c]);
         }
     }
     maps[w * GS_WAVE + l] = make_float4(m[0], m[1], h[0], h[1]);
@@ -425,14 +502,15 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur(Recur r, RecurOut
     __syncthreads();
     h[0] = h[1] = 0.0f;
     if (!ALONE) {
+        bool any = false;
         if (w == 0) {
-            float f[2];
-            look_back<4>(r, chunk, block, maps, anew, !bit(tk.starts, 0), f);
-            front[l] = make_float2(f[0], f[1]);
+            any = publish(r, chunk, block, maps, anew);
+            const int d = bit(tk.starts, 0) ? kNotNeeded : wait_for_state(r, chunk, block);
+            if (l == 0) look.distance = d;
         }
         __syncthreads();
-        h[0] = front[l].x;
-        h[1] = front[l].y;
+        front_state<2>(r, chunk, block, look, h);
+        if (w == 0 && !any) publish_state(r, chunk, block, maps, anew, h);
     }
     through(maps, anew, 0, w, l, h);
     if (o.kept && tk.p0 % GS_RECUR_KEEP == 0 && tk.p0 < a.n)
@@ -442,12 +520,15 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur(Recur r, RecurOut
     Rows y = Rows::of<T>(a, tk, o.y, o.ld_y, first, false);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        if (bit(tk.starts, i)) {
-            rare();
-            h[0] = h[1] = 0.0f;
-        }
+        if (bit(tk.starts, i)) start(i, h);
+        xs[i].again();
 #pragma unroll
-        for (int c = 0; c < 2; ++c) h[c] = fmaf(A[i][c], h[c], B[i][c]);
+        for (int c = 0; c < 2; ++c) {
+            float A, z;
+            loaded(S[i][c]);
+            open(S[i][c], A, z);
+            h[c] = fmaf(A, h[c], z * xs[i][c]);
+        }
         if (bit(written, i)) Two<T, ONE>::store(y.p, col, h[0], h[1]);
         y.next();
         if (bit(lasts, i)) Two<float, ONE>::store(o.final, tk.segment(i), a.cols, col, h[0], h[1]);
@@ -460,42 +541,38 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur(Recur r, RecurOut
 // h is formed again from the states that the forward kept every GS_RECUR_KEEP
 // tokens, in fp32, not read in the tokens' type.
 template <typename T, bool ONE, bool ALONE>
-__global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur_bwd(Recur r, gs_recur_grads o) {
-    __shared__ float4 maps[kWaves * GS_WAVE], back[kWaves * GS_WAVE];
-    __shared__ float2 front[GS_WAVE];
-    __shared__ uint32_t anew[kWaves], ended[kWaves], ticket;
+__global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k_recur_bwd(Recur r, gs_recur_grads o) {
+    constexpr int WAVES = ALONE ? kAloneWaves : kWaves;
+    __shared__ float4 maps[WAVES * GS_WAVE], back[WAVES * GS_WAVE];
+    __shared__ Lookers look;
+    __shared__ uint32_t anew[WAVES], ended[WAVES], ticket;
     const gs_recur& a = r.a;
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
     int turn = 0, block = blockIdx.x;          // chunks are taken from the last one on
+    if (ALONE && block >= r.blocks) {
+        pass_empty(a, o.dfinal, o.dinitial, (block - r.blocks) * WAVES + w, (gridDim.x - r.blocks) * WAVES);
+        return;
+    }
     if (!ALONE && !take_chunk(r, &ticket, turn, block)) return;
     const int chunk = r.chunks - 1 - turn;
     const uint32_t col = column(a, block, r.width);
     Tokens tk;
-    tk.find<!ALONE>(r, __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps));
+    tk.p0 = __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps);
     Two<T, ONE> gs[kSteps], xs[kSteps], ds[kSteps];
     // behind the last place the last one's row, whose values are not used
     const int32_t first = min(tk.p0, a.n - 1), end = min(tk.p0 + kSteps, a.n) - 1;
     Rows gate = Rows::of<T>(a, tk, a.gate, a.ld_gate, first, false), x = Rows::of<T>(a, tk, a.x, a.ld_x, first, false);
+    Rows dy = Rows::of<T>(a, tk, o.dy, o.ld_dy, first, false);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         gs[i].load(gate.p, col);
         xs[i].load(x.p, col);
+        ds[i].load(dy.p, col);
         gate.next(tk.p0 + i + 1 < a.n);
         x.next(tk.p0 + i + 1 < a.n);
+        dy.next(tk.p0 + i + 1 < a.n);
     }
-    auto load_dy = [&]() {
-        Rows dy = Rows::of<T>(a, tk, o.dy, o.ld_dy, first, false);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            ds[i].load(dy.p, col);
-            dy.next(tk.p0 + i + 1 < a.n);
-            if (!bit(tk.inside, i)) {
-                rare();
-                ds[i].fill(0.0f);
-            }
-        }
-    };
-    load_dy();
+    tk.find(a, tk.p0);                         // while the tokens are on their way
     // tokens outside every segment: a gate that holds, and zeros
     if (tk.inside != kAllSteps) {
 #pragma unroll
@@ -504,6 +581,7 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur_bwd(Recur r, gs_r
                 rare();
                 gs[i].fill(INFINITY);
                 xs[i].fill(0.0f);
+                ds[i].fill(0.0f);
             }
     }
     const uint32_t firsts = a.initial ? tk.starts & tk.inside : 0u, lasts = o.dfinal ? tk.ends & tk.inside : 0u;
@@ -551,18 +629,18 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur_bwd(Recur r, gs_r
         }
     }
     if (tk.ends) bm[0] = bm[1] = 0.0f;
-    back[(kWaves - 1 - w) * GS_WAVE + l] = make_float4(bm[0], bm[1], b[0], b[1]);
+    back[(WAVES - 1 - w) * GS_WAVE + l] = make_float4(bm[0], bm[1], b[0], b[1]);
     maps[w * GS_WAVE + l] = make_float4(m[0], m[1], h[0], h[1]);
     if (l == 0) {
-        ended[kWaves - 1 - w] = tk.ends != 0;
+        ended[WAVES - 1 - w] = tk.ends != 0;
         anew[w] = tk.starts != 0;
     }
     __syncthreads();
+    bool any = false;
     if (!ALONE && w == kWaves - 1) {
-        float f[2];
-        look_back<sizeof(T) == 4 ? 1 : 4>(r, turn, block, back, ended, !bit(tk.ends, kSteps - 1), f);
-        front[l] = make_float2(f[0], f[1]);
-        if (sizeof(T) == 4) load_dy();         // there are no registers to hold it meanwhile
+        any = publish(r, turn, block, back, ended);
+        const int d = bit(tk.ends, kSteps - 1) ? kNotNeeded : wait_for_state(r, turn, block);
+        if (l == 0) look.distance = d;
     }
     // the states again, from the kept one in front
     h[0] = h[1] = 0.0f;
@@ -596,10 +674,22 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur_bwd(Recur r, gs_r
     float g[2] = {0.0f, 0.0f};
     if (!ALONE) {
         __syncthreads();
-        g[0] = front[l].x;
-        g[1] = front[l].y;
+        front_state<sizeof(T) == 4 ? 1 : 4>(r, turn, block, look, g);
+        if (w == kWaves - 1 && !any) publish_state(r, turn, block, back, ended, g);
     }
-    through(back, ended, 0, kWaves - 1 - w, l, g);
+    through(back, ended, 0, WAVES - 1 - w, l, g);
+    if (sizeof(T) == 4) {                      // dy once more: there are no registers to hold it meanwhile
+        Rows again = Rows::of<T>(a, tk, o.dy, o.ld_dy, first, false);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            ds[i].load(again.p, col);
+            again.next(tk.p0 + i + 1 < a.n);
+            if (!bit(tk.inside, i)) {
+                rare();
+                ds[i].fill(0.0f);
+            }
+        }
+    }
     const uint32_t written = a.fill ? tk.there(a) : tk.inside, starts = o.dinitial ? tk.starts & tk.inside : 0u;
     Rows dxs = Rows::of<T>(a, tk, o.dx, o.ld_dx, end, true), dgs = Rows::of<T>(a, tk, o.dgate, o.ld_dgate, end, true);
 #pragma unroll
@@ -633,12 +723,12 @@ __global__ void __launch_bounds__(kWaves * GS_WAVE, 4) k_recur_bwd(Recur r, gs_r
 
 struct RecurPlan {
     int32_t chunks, blocks, width;
-    size_t map, maps, states, flags, bytes;
+    size_t maps, states, flags, bytes;
 };
 
 RecurPlan recur_plan(int32_t n, int32_t cols) {
     RecurPlan p;
-    p.chunks = (int32_t)div_up(n, kChunk);
+    p.chunks = n <= kAloneChunk ? 1 : (int32_t)div_up(n, kChunk);
     p.width = kCols;                           // so that no block has a single channel
     while (cols > 1 && cols % p.width == 1) p.width -= 2;
     p.blocks = (int32_t)div_up(cols, p.width);
@@ -649,7 +739,6 @@ RecurPlan recur_plan(int32_t n, int32_t cols) {
         return here;
     };
     const size_t all = p.chunks <= 1 ? 0 : (size_t)p.chunks * p.blocks;
-    p.map = take(all ? (size_t)n * 4 : 0);
     p.maps = take(all * GS_WAVE * 16);
     p.states = take(all * GS_WAVE * 8);
     p.flags = take(all ? (all + 1) * 4 : 0);
@@ -665,45 +754,51 @@ Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
     r.blocks = p.blocks;
     r.width = p.width;
     const bool alone = p.chunks <= 1;
-    r.map = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.map);
     r.maps = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.maps);
     r.states = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.states);
     r.flags = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.flags);
     return r;
 }
 
-// The map of the places and cleared flags.
-void recur_map(const Recur& r, hipStream_t st) {
+// Flags cleared for the chunks' workgroups; their number for the only ones'.
+void clear_flags(const Recur& r, const float* from, float* to, hipStream_t st) {
     const int32_t flags = r.chunks * r.blocks + 1;
-    k_recur_map<<<div_up(std::max(r.a.n, flags), GS_BLOCK), GS_BLOCK, 0, st>>>(r.a, const_cast<uint32_t*>(r.map), r.flags, flags);
+    const uint32_t most = std::max(div_up(flags, GS_BLOCK), to && r.a.cu ? div_up(r.a.n_seg, GS_BLOCK) : 1u);
+    k_recur_clear<<<std::min(most, 1024u), GS_BLOCK, 0, st>>>(r.a, from, to, r.flags, flags);
 }
 
-void empty_segments(const gs_recur& a, const float* from, float* to, hipStream_t st) {
-    if (to && (a.n == 0 || a.cu))
-        k_recur_empty<<<std::min(a.n_seg, 4096), GS_BLOCK, 0, st>>>(a, from, to);
+uint32_t alone_grid(const Recur& r, const float* to) {
+    return r.blocks + (to && r.a.cu ? std::min(div_up(r.a.n_seg, kAloneWaves * GS_WAVE), 256u) : 0u);
 }
 
 template <typename T, bool ONE>
 hipError_t recur_go(const Recur& r, const RecurOut& o, hipStream_t st) {
-    const uint32_t grid = (uint32_t)r.chunks * r.blocks;
     if (r.chunks == 1) {
-        k_recur<T, ONE, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        k_recur<T, ONE, true, true><<<alone_grid(r, o.final), kAloneWaves * GS_WAVE, 0, st>>>(r, o);
     } else {
-        recur_map(r, st);
-        k_recur<T, ONE, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        clear_flags(r, r.a.initial, o.final, st);
+        const uint32_t grid = (uint32_t)r.chunks * r.blocks;
+        // a segment in every four tokens: waiting for one state after the other would take longer than all else
+        if (r.a.initial && r.a.n_seg >= r.a.n / 4) k_recur<T, ONE, false, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        else k_recur<T, ONE, false, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
     }
     return hipGetLastError();
 }
 
 template <typename T, bool ONE>
 hipError_t recur_bwd_go(const Recur& r, const gs_recur_grads& g, hipStream_t st) {
-    const uint32_t grid = (uint32_t)r.chunks * r.blocks;
     if (r.chunks == 1) {
-        k_recur_bwd<T, ONE, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
+        k_recur_bwd<T, ONE, true><<<alone_grid(r, g.dinitial), kAloneWaves * GS_WAVE, 0, st>>>(r, g);
     } else {
-        recur_map(r, st);
-        k_recur_bwd<T, ONE, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, g);
+        clear_flags(r, g.dfinal, g.dinitial, st);
+        k_recur_bwd<T, ONE, false><<<(uint32_t)r.chunks * r.blocks, kWaves * GS_WAVE, 0, st>>>(r, g);
     }
+    return hipGetLastError();
+}
+
+// No tokens at all: the segments' states alone.
+hipError_t no_tokens(const gs_recur& a, const float* from, float* to, hipStream_t st) {
+    if (to) k_recur_clear<<<std::min(div_up(a.n_seg, GS_BLOCK), 1024u), GS_BLOCK, 0, st>>>(a, from, to, nullptr, 0);
     return hipGetLastError();
 }
 
@@ -723,8 +818,7 @@ size_t recurrence_ws_bytes(const gs_recur& a) { return recur_plan(a.n, a.cols).b
 
 hipError_t launch_recurrence(const gs_recur& a, void* y, int64_t ld_y, float* final, float* kept, void* ws,
                              hipStream_t st) {
-    empty_segments(a, a.initial, final, st);
-    if (a.n == 0) return hipGetLastError();
+    if (a.n == 0) return no_tokens(a, a.initial, final, st);
     const RecurPlan p = recur_plan(a.n, a.cols);
     const Recur r = recur_of(a, p, ws);
     const RecurOut o = {y, final, kept, ld_y};
@@ -733,8 +827,7 @@ hipError_t launch_recurrence(const gs_recur& a, void* y, int64_t ld_y, float* fi
 }
 
 hipError_t launch_recurrence_bwd(const gs_recur& a, const gs_recur_grads& g, void* ws, hipStream_t st) {
-    empty_segments(a, g.dfinal, g.dinitial, st);
-    if (a.n == 0) return hipGetLastError();
+    if (a.n == 0) return no_tokens(a, g.dfinal, g.dinitial, st);
     const RecurPlan p = recur_plan(a.n, a.cols);
     const Recur r = recur_of(a, p, ws);
     if (a.dtype == GS_F32) return recur_bwd_type<float>(r, g, st);

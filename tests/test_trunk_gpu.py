@@ -261,7 +261,9 @@ RUNS = {  # lengths, channels
     "one token": ([1], 1), "one token, many channels": ([1], 300), "steps": ([1] * 40, 130), "steps past a chunk": ([1] * 300, 66),
     "a chunk": ([128], 64), "less": ([127], 128), "more": ([129], 129), "odd": ([77], 33), "kept edges": ([63, 1, 64, 65, 128, 129], 20),
     "long": ([3000], 40), "ragged": ([5, 0, 700, 3, 1, 0, 0, 257, 16, 15, 17], 70), "empty": ([0, 0, 0], 10),
-    "empty ends": ([0, 50, 0], 257), "many": ([(i * 7) % 23 for i in range(150)], 18), "wave edges": ([16, 15, 1, 17, 31, 32, 33], 131),
+    "empty ends": ([0, 50, 0], 257), "many": ([(i * 7) % 23 for i in range(150)], 18),
+    "empties": ([3] + [0] * 200 + [5] + [0] * 70 + [1, 1, 2] + [0] * 130 + [400, 0, 1], 12), "alone": ([100, 0, 156], 66),
+    "past alone": ([257], 66), "very many": ([i % 2 for i in range(5000)], 4), "wave edges": ([16, 15, 1, 17, 31, 32, 33], 131),
 }
 
 
