@@ -266,8 +266,10 @@ __device__ __forceinline__ void through(const float4* maps, const uint32_t* anew
 // every chunk that one waits for belongs to a workgroup that is already running
 // and publishes its map before it waits itself: every wait ends.  (Calls that
 // run at the same time on one workspace would clear each other's flags; a wait
-// gives up after kPolls then, with NaN.)  What is published moves past the
-// caches of the units (agent scope); a flag follows the values it announces.
+// gives up after kPolls then, with NaN.)  What is published is written past the
+// caches (agent scope), and a flag follows the values it announces.  The values
+// are read through the caches: their lines hold nothing else and nobody reads
+// them before their flag, so no cache can have held them earlier in the kernel.
 // ---------------------------------------------------------------------------
 
 constexpr uint32_t kMap = 1, kState = 2;
@@ -278,9 +280,6 @@ __device__ __forceinline__ float2 unpair(uint64_t v) {
     return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 __device__ __forceinline__ void put(uint64_t* p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ uint64_t get(const uint64_t* p) {
-    return __hip_atomic_load(const_cast<uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 // by the wave that wrote what the flag announces
 __device__ __forceinline__ void announce(uint32_t* flag, uint32_t what) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -342,7 +341,7 @@ __device__ __forceinline__ int wait_for_state(const Recur& r, int chunk, int blo
         const uint32_t f = c >= 0 ? __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
         const uint64_t known = __ballot(f == kState), there = __ballot(f != 0u);
         if (known && (~there & ((known & -known) - 1)) == 0) return __ffsll((unsigned long long)known) - 1;
-        __builtin_amdgcn_s_sleep(1);
+        __builtin_amdgcn_s_sleep(32);          // 1: 219 us for the 131,072 tokens that take 212 with 24 to 64
     }
     return kGaveUp;
 }
@@ -356,7 +355,7 @@ __device__ __forceinline__ void front_state(const Recur& r, int chunk, int block
     if (d < 0) return;
     const int64_t nearest = (int64_t)block * r.chunks + chunk - 1;
     asm volatile("" ::: "memory");             // read behind the flags
-    if (w == kWaves - 1) s.state[l] = unpair(get(r.states + (nearest - d) * GS_WAVE + l));
+    if (w == kWaves - 1) s.state[l] = unpair(r.states[(nearest - d) * GS_WAVE + l]);
     const int per = (d + kWaves - 1) / kWaves, end = min((w + 1) * per, d);
     float pm[2] = {1.0f, 1.0f}, pb[2] = {0.0f, 0.0f};
     for (int k = w * per; k < end; k += kAhead) {
@@ -364,8 +363,8 @@ __device__ __forceinline__ void front_state(const Recur& r, int chunk, int block
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const uint64_t* p = r.maps + (nearest - min(k + i, end - 1)) * (2 * GS_WAVE) + l;
-            v[i][0] = get(p);
-            v[i][1] = get(p + GS_WAVE);
+            v[i][0] = p[0];
+            v[i][1] = p[GS_WAVE];
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
