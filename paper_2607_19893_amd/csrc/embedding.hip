@@ -75,15 +75,16 @@ __global__ void __launch_bounds__(GS_BLOCK) k_embedding(gs_embed_args a, int tok
 // share go to partial rows, which k_embed_join adds in ascending order.  Nothing
 // is summed by atomics: the same call gives the same bits.
 //
-// The sort: passes of `bits` <= 10 bits, lowest first, each a count of digits by
-// block, a scan of the counts, and a scatter whose ranks come from the lanes
-// that hold the same digit.  Ids outside the table become `rows`, the last key.
+// The sort: passes of at most kMostBits bits, lowest first, each a count of
+// digits by block, a scan of the counts, and a scatter whose ranks come from the
+// lanes that hold the same digit; a list of one block needs the scatter alone.
+// Ids outside the table become `rows`, the last key.
 // ---------------------------------------------------------------------------
 
-constexpr int kSortItems = 16;                 // of a thread
-constexpr int kSortBlock = GS_BLOCK * kSortItems;
-constexpr int kMostBits = 10;
+constexpr int kMostBits = 11;
 constexpr int kMostBins = 1 << kMostBits;
+constexpr int kFew = 4, kMany = 16;            // sorted items of a thread
+constexpr int32_t kManyFrom = 1 << 20;         // tokens from which a thread takes many: fewer blocks to scan
 
 struct SortPass {
     const int32_t* ids;                        // the first pass reads these,
@@ -91,7 +92,7 @@ struct SortPass {
     uint2* to;
     uint32_t* counts;                          // [bins][blocks]
     uint32_t* totals;                          // [bins]
-    uint8_t* marks;                            // first pass: rows that have tokens (NULL: not wanted)
+    uint32_t* marks;                           // first pass: words to clear (NULL: none)
     int32_t n, rows, shift, bits, blocks;
 };
 
@@ -101,21 +102,28 @@ __device__ __forceinline__ uint2 sort_item(const SortPass& s, int64_t i) {
     return make_uint2((uint32_t)id < (uint32_t)s.rows ? (uint32_t)id : (uint32_t)s.rows, (uint32_t)i);
 }
 
+// The marks of the rows that have tokens, cleared on the way (k_embed_sum sets them).
+__device__ __forceinline__ void clear_marks(const SortPass& s) {
+    if (s.marks == nullptr) return;
+    const int64_t words = ((int64_t)s.rows + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x; i < words; i += (int64_t)gridDim.x * GS_BLOCK) s.marks[i] = 0;
+}
+
+template <int ITEMS>
 __global__ void __launch_bounds__(GS_BLOCK) k_sort_count(SortPass s) {
     __shared__ uint32_t count[kMostBins];
     const int bins = 1 << s.bits;
+    const int64_t first = (int64_t)blockIdx.x * (GS_BLOCK * ITEMS) + threadIdx.x;
+    uint32_t key[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+        if (first + k * GS_BLOCK < s.n) key[k] = sort_item(s, first + k * GS_BLOCK).x;
     for (int b = threadIdx.x; b < bins; b += GS_BLOCK) count[b] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kSortBlock;
-#pragma unroll 4
-    for (int k = 0; k < kSortItems; ++k) {
-        const int64_t i = first + k * GS_BLOCK + threadIdx.x;
-        if (i < s.n) {
-            const uint2 v = sort_item(s, i);
-            atomicAdd(&count[(v.x >> s.shift) & (bins - 1)], 1u);
-            if (s.marks && v.x < (uint32_t)s.rows) s.marks[v.x] = 1;
-        }
-    }
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+        if (first + k * GS_BLOCK < s.n) atomicAdd(&count[(key[k] >> s.shift) & (bins - 1)], 1u);
+    clear_marks(s);
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += GS_BLOCK) s.counts[(int64_t)b * s.blocks + blockIdx.x] = count[b];
 }
@@ -126,35 +134,52 @@ __global__ void __launch_bounds__(GS_BLOCK) k_sort_scan(SortPass s) {
     if (b >= 1 << s.bits) return;
     uint32_t* c = s.counts + (int64_t)b * s.blocks;
     uint32_t before = 0;
-    for (int i = 0; i < s.blocks; i += GS_WAVE) {
-        const uint32_t v = i + lane_id() < s.blocks ? c[i + lane_id()] : 0;
-        const uint32_t inc = wave_incl_scan(v);
-        if (i + lane_id() < s.blocks) c[i + lane_id()] = before + inc - v;
-        before += __shfl(inc, GS_WAVE - 1, GS_WAVE);
+    for (int i0 = 0; i0 < s.blocks; i0 += 4 * GS_WAVE) {
+        uint32_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + j * GS_WAVE + lane_id();
+            v[j] = i < s.blocks ? c[i] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + j * GS_WAVE + lane_id();
+            const uint32_t inc = wave_incl_scan(v[j]);
+            if (i < s.blocks) c[i] = before + inc - v[j];
+            before += __shfl(inc, GS_WAVE - 1, GS_WAVE);
+        }
     }
     if (lane_id() == 0) s.totals[b] = before;
 }
 
 // ALONE: the only block, which needs no counts of others.
-template <bool ALONE>
+template <int ITEMS, bool ALONE>
 __global__ void __launch_bounds__(GS_BLOCK) k_sort_scatter(SortPass s) {
-    constexpr int W = GS_BLOCK / GS_WAVE;
+    constexpr int W = GS_BLOCK / GS_WAVE, MOST = kMostBins / GS_BLOCK;
     __shared__ uint32_t count[W][kMostBins];
     __shared__ uint32_t scratch[W];
     const int bins = 1 << s.bits, w = threadIdx.x / GS_WAVE;
-    for (int b = threadIdx.x; b < W * kMostBins; b += GS_BLOCK) (&count[0][0])[b] = 0;
-    __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kSortBlock + w * (GS_WAVE * kSortItems) + lane_id();
-    uint2 item[kSortItems];
-    uint32_t rank[kSortItems];
+    const int per = max(1, bins / GS_BLOCK);   // bins of a thread
+    const int64_t first = (int64_t)blockIdx.x * (GS_BLOCK * ITEMS) + w * (GS_WAVE * ITEMS) + lane_id();
+    uint2 item[ITEMS];
+    uint32_t rank[ITEMS], tot[MOST], own[MOST];
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k)
+    for (int k = 0; k < ITEMS; ++k)
         item[k] = first + k * GS_WAVE < s.n ? sort_item(s, first + k * GS_WAVE) : make_uint2(0u, 0u);
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k) {
+    for (int j = 0; j < MOST; ++j) {           // where a bin starts, and this block's share of it
+        const int b = threadIdx.x * per + j;
+        const bool there = !ALONE && j < per && b < bins;
+        tot[j] = there ? s.totals[b] : 0u;
+        own[j] = there ? s.counts[(int64_t)b * s.blocks + blockIdx.x] : 0u;
+    }
+    for (int b = threadIdx.x; b < W * bins; b += GS_BLOCK) count[b >> s.bits][b & (bins - 1)] = 0;
+    if (ALONE) clear_marks(s);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
         const bool in = first + k * GS_WAVE < s.n;
         const uint32_t d = (item[k].x >> s.shift) & (bins - 1);
-        if (s.marks && ALONE && in && item[k].x < (uint32_t)s.rows) s.marks[item[k].x] = 1;
         uint64_t same = __ballot(in);
         for (int i = 0; i < s.bits; ++i) {
             const uint64_t m = __ballot((d >> i) & 1);
@@ -168,81 +193,85 @@ __global__ void __launch_bounds__(GS_BLOCK) k_sort_scatter(SortPass s) {
         rank[k] = old + popc64(same & lanemask_lt());
     }
     __syncthreads();
-    // a thread's four bins: where the bin starts, where this block's share of it does, then wave by wave
-    uint32_t tot[kMostBins / GS_BLOCK], sum = 0;
+    uint32_t sum = 0;
 #pragma unroll
-    for (int j = 0; j < kMostBins / GS_BLOCK; ++j) {
-        const int b = threadIdx.x * (kMostBins / GS_BLOCK) + j;
-        tot[j] = 0;
-        if (b < bins) {
-            if (ALONE) {
+    for (int j = 0; j < MOST; ++j) {
+        const int b = threadIdx.x * per + j;
+        if (j < per && b < bins) {
+            if (ALONE)
 #pragma unroll
                 for (int u = 0; u < W; ++u) tot[j] += count[u][b];
-            } else {
-                tot[j] = s.totals[b];
-            }
+            sum += tot[j];
         }
-        sum += tot[j];
     }
     uint32_t all, before = block_excl_scan(sum, scratch, &all);
 #pragma unroll
-    for (int j = 0; j < kMostBins / GS_BLOCK; ++j) {
-        const int b = threadIdx.x * (kMostBins / GS_BLOCK) + j;
-        if (b < bins) {
-            uint32_t at = before + (ALONE ? 0u : s.counts[(int64_t)b * s.blocks + blockIdx.x]);
+    for (int j = 0; j < MOST; ++j) {
+        const int b = threadIdx.x * per + j;
+        if (j < per && b < bins) {
+            uint32_t at = before + own[j];
 #pragma unroll
-            for (int u = 0; u < W; ++u) {
+            for (int u = 0; u < W; ++u) {      // wave by wave
                 const uint32_t c = count[u][b];
                 count[u][b] = at;
                 at += c;
             }
+            before += tot[j];
         }
-        before += tot[j];
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortItems; ++k)
+    for (int k = 0; k < ITEMS; ++k)
         if (first + k * GS_WAVE < s.n) s.to[count[w][(item[k].x >> s.shift) & (bins - 1)] + rank[k]] = item[k];
 }
 
 // -- the touched rows alone: the sorted keys become places among the unique ids ---
 
-__device__ __forceinline__ bool run_starts(const uint2* pairs, int64_t i, uint32_t rows) {
-    return pairs[i].x < rows && (i == 0 || pairs[i - 1].x != pairs[i].x);
+constexpr int kRunItems = 4;                   // of a thread
+
+__device__ __forceinline__ bool run_starts(const uint2* pairs, int64_t i, int32_t n, uint32_t rows) {
+    return i < n && pairs[i].x < rows && (i == 0 || pairs[i - 1].x != pairs[i].x);
 }
 
 __global__ void __launch_bounds__(GS_BLOCK) k_run_count(const uint2* __restrict__ pairs, int32_t n, uint32_t rows,
                                                         uint32_t* __restrict__ counts) {
-    __shared__ uint32_t scratch[GS_BLOCK / GS_WAVE];
-    const int64_t first = (int64_t)blockIdx.x * GS_TILE_ITEMS;
+    __shared__ uint32_t part[GS_BLOCK / GS_WAVE];
+    const int64_t first = (int64_t)blockIdx.x * (GS_BLOCK * kRunItems) + threadIdx.x;
     uint32_t c = 0;
-    for (int k = 0; k < GS_ITEMS; ++k) {
-        const int64_t i = first + k * GS_BLOCK + threadIdx.x;
-        if (i < n) c += run_starts(pairs, i, rows);
-    }
-    c = block_sum_u32(c, scratch);
-    if (threadIdx.x == 0) counts[blockIdx.x] = c;
+#pragma unroll
+    for (int k = 0; k < kRunItems; ++k) c += popc64(__ballot(run_starts(pairs, first + k * GS_BLOCK, n, rows)));
+    if (lane_id() == 0) part[threadIdx.x / GS_WAVE] = c;
+    __syncthreads();
+    if (threadIdx.x == 0) counts[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
 __global__ void __launch_bounds__(GS_BLOCK) k_run_place(const uint2* __restrict__ pairs, int32_t n, uint32_t rows,
                                                         const uint32_t* __restrict__ counts, uint2* __restrict__ to,
                                                         int32_t* __restrict__ unique, int32_t* __restrict__ total) {
-    __shared__ uint32_t scratch[GS_BLOCK / GS_WAVE];
-    uint32_t before = block_sum_prefix(counts, blockIdx.x, scratch);
-    const int64_t first = (int64_t)blockIdx.x * GS_TILE_ITEMS;
-    for (int k = 0; k < GS_ITEMS; ++k) {
-        const int64_t i = first + k * GS_BLOCK + threadIdx.x;
-        const bool starts = i < n && run_starts(pairs, i, rows);
-        uint32_t all;
-        const uint32_t mine = before + block_excl_scan(starts, scratch, &all) + starts;    // runs up to here
+    constexpr int W = GS_BLOCK / GS_WAVE;
+    __shared__ uint32_t scratch[W], part[kRunItems * W];
+    const int64_t first = (int64_t)blockIdx.x * (GS_BLOCK * kRunItems) + threadIdx.x;
+    uint64_t starts[kRunItems];
+#pragma unroll
+    for (int k = 0; k < kRunItems; ++k) {
+        starts[k] = __ballot(run_starts(pairs, first + k * GS_BLOCK, n, rows));
+        if (lane_id() == 0) part[k * W + threadIdx.x / GS_WAVE] = popc64(starts[k]);
+    }
+    uint32_t before = block_sum_prefix(counts, blockIdx.x, scratch);       // synchronizes
+    for (int i = 0; i < (int)threadIdx.x / GS_WAVE; ++i) before += part[i];
+#pragma unroll
+    for (int k = 0; k < kRunItems; ++k) {
+        const int64_t i = first + k * GS_BLOCK;
+        const bool mine = (starts[k] >> lane_id()) & 1;
+        const uint32_t place = before + popc64(starts[k] & lanemask_lt()) + mine;          // runs up to here
         if (i < n) {
             const uint2 v = pairs[i];
-            to[i] = make_uint2(v.x < rows ? mine - 1 : rows, v.y);
-            if (starts) unique[mine - 1] = (int32_t)v.x;
+            to[i] = make_uint2(v.x < rows ? place - 1 : rows, v.y);
+            if (mine) unique[place - 1] = (int32_t)v.x;
         }
-        before += all;
+        if (i == n - 1) *total = (int32_t)place;
+        for (int j = 0; j < W && k + 1 < kRunItems; ++j) before += part[k * W + threadIdx.x / GS_WAVE + j];
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *total = (int32_t)before;
 }
 
 // -- the sums --------------------------------------------------------------------
@@ -253,14 +282,14 @@ struct EmbedSum {
     int64_t ld_dout, ld_grad;
     float* grad;
     float* parts;                              // [2 * chunks][dim]: a chunk's first and last row
-    const uint8_t* marks;                      // rows that are not marked get zeros (NULL: none)
+    uint8_t* marks;                            // rows that have a token (NULL: not wanted)
     int64_t rows;
-    int32_t n, dim, chunks;
+    int32_t n, dim, per, chunks;               // per: sorted tokens of a chunk
     uint32_t limit;                            // rows from here on are no one's
     float scale;
 };
 
-constexpr int kChunk = 32;                     // sorted tokens of a chunk
+constexpr int kMostChunk = 64;
 
 template <typename T, bool TAIL>
 __device__ __forceinline__ void put_row(float* p, int there, const float* f) {
@@ -269,45 +298,56 @@ __device__ __forceinline__ void put_row(float* p, int there, const float* f) {
     for (int i = 0; i < N; i += 4) Span<float, TAIL>::store(p + i, there - i, f + i);
 }
 
-// G lanes a chunk, blockIdx.y: slabs of G * N columns.
+// G lanes a chunk, blockIdx.y: slabs of G * N columns.  The workgroup's pairs go
+// to LDS first, then AHEAD rows are on their way while AHEAD are added.
 template <typename T, bool TAIL, int G>
 __global__ void __launch_bounds__(GS_BLOCK) k_embed_sum(EmbedSum a) {
-    constexpr int N = Piece<T>::N, AHEAD = 8;
+    constexpr int N = Piece<T>::N, AHEAD = 8, GROUPS = GS_BLOCK / G;
+    __shared__ uint2 list[GROUPS * kMostChunk + 2];        // from the position in front of the workgroup's first
+    const int64_t base = (int64_t)blockIdx.x * GROUPS * a.per;
+    const int count = (int)min((int64_t)GROUPS * a.per, (int64_t)a.n - base);
+    for (int i = threadIdx.x; i < count + 2; i += GS_BLOCK) {
+        const int64_t p = base + i - 1;
+        list[i] = p >= 0 && p < a.n ? a.pairs[p] : make_uint2(a.limit, 0u);
+    }
+    __syncthreads();
     const int col = blockIdx.y * (G * N) + (threadIdx.x % G) * N, there = a.dim - col;
-    const int64_t g = (int64_t)blockIdx.x * (GS_BLOCK / G) + threadIdx.x / G;
-    if (g >= a.chunks) return;
-    const int64_t p0 = g * kChunk, p1 = min(p0 + kChunk, (int64_t)a.n);
-    const uint32_t before = p0 > 0 ? a.pairs[p0 - 1].x : a.limit, after = p1 < a.n ? a.pairs[p1].x : a.limit;
+    const int64_t g = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
+    const int p0 = 1 + threadIdx.x / G * a.per, p1 = min(p0 + a.per, count + 1);
+    if (p0 >= p1) return;
+    const uint32_t before = list[p0 - 1].x, after = list[p1].x;
+    uint32_t row = list[p0].x;
+    bool shared = row == before;               // with the chunk in front
     float acc[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.0f;
-    uint32_t row = a.pairs[p0].x;
-    bool shared = row == before;               // with the chunk in front
     auto flush = [&](bool last) {
         if (row >= a.limit) return;
-        float v[N];
+        const bool goes_on = last && row == after, whole = !shared && !goes_on;
         float* to = a.grad + (int64_t)row * a.ld_grad + col;
-        if (shared) to = a.parts + (2 * g) * a.dim + col;
-        else if (last && row == after) to = a.parts + (2 * g + 1) * a.dim + col;
-        const bool whole = !shared && !(last && row == after);
+        if (!whole) to = a.parts + (2 * g + (shared ? 0 : 1)) * a.dim + col;
+        if (a.marks && !shared && threadIdx.x % G == 0) a.marks[row] = 1;
+        float v[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = whole ? acc[i] * a.scale : acc[i];
         put_row<T, TAIL>(to, there, v);
     };
-    for (int64_t p = p0; p < p1; p += AHEAD) {
-        uint2 v[AHEAD];
-        Span<T, TAIL> s[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) v[k] = p + k < p1 ? a.pairs[p + k] : make_uint2(a.limit, 0u);
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            s[k].load(static_cast<const T*>(a.dout) + (int64_t)v[k].y * a.ld_dout + col, v[k].x < a.limit ? there : 0);
+    Span<T, TAIL> now[AHEAD], next[AHEAD];
+    auto load = [&](Span<T, TAIL>* s, int p) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            if (p + k >= p1) break;
-            if (v[k].x != row) {
+            const uint2 v = list[min(p + k, p1 - 1)];
+            s[k].load(static_cast<const T*>(a.dout) + (int64_t)v.y * a.ld_dout + col,
+                      p + k < p1 && v.x < a.limit ? there : 0);
+        }
+    };
+    auto add = [&](const Span<T, TAIL>* s, int p) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const uint32_t mine = list[min(p + k, p1 - 1)].x;          // past the end: the last row, nothing to add
+            if (mine != row) {
                 flush(false);
-                row = v[k].x;
+                row = mine;
                 shared = false;
 #pragma unroll
                 for (int i = 0; i < N; ++i) acc[i] = 0.0f;
@@ -317,65 +357,109 @@ __global__ void __launch_bounds__(GS_BLOCK) k_embed_sum(EmbedSum a) {
 #pragma unroll
             for (int i = 0; i < N; ++i) acc[i] += f[i];
         }
+    };
+    load(now, p0);
+    for (int p = p0; p < p1; p += 2 * AHEAD) {
+        load(next, p + AHEAD);
+        add(now, p);
+        if (p + AHEAD >= p1) break;
+        load(now, p + 2 * AHEAD);
+        add(next, p + AHEAD);
     }
     flush(true);
 }
 
-// Sum of the partial rows of one run, from the chunk that holds its start: the
-// last row of that chunk, then the first rows of those behind it.  The groups of
-// the workgroup take equal slices of them, added in ascending order.
+// Sums of the partial rows of a run, from the chunk that holds its start: the
+// last row of that chunk, then the first rows of those behind it.  A group of
+// lanes takes a run of few chunks; the workgroup together one of many, in equal
+// slices that are added in ascending order.  Workgroups behind these write zeros
+// to the rows that have no token.
+constexpr int kJoin = 512;
+
 template <typename T, bool TAIL, int G>
-__global__ void __launch_bounds__(GS_BLOCK) k_embed_join(EmbedSum a) {
-    constexpr int N = Piece<T>::N, GROUPS = GS_BLOCK / G;
+__global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_blocks, int rows_a_block) {
+    constexpr int N = Piece<T>::N, GROUPS = kJoin / G;
     __shared__ float sums[GROUPS][G * N];
-    const int64_t g = blockIdx.x, p0 = g * kChunk, p1 = p0 + kChunk;
-    if (p1 >= a.n) return;
-    const uint32_t row = a.pairs[p1 - 1].x;
-    if (row >= a.limit || a.pairs[p1].x != row) return;
-    if (p0 > 0 && a.pairs[p0].x == row && a.pairs[p0 - 1].x == row) return;    // it started before
-    // the end of the run: the first position behind p1 with another row
-    int64_t lo = p1, hi = a.n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (a.pairs[mid].x == row) lo = mid + 1;
-        else hi = mid;
+    __shared__ int many[GROUPS], n_many, ends;
+    if ((int)blockIdx.x >= join_blocks) {
+        if (blockIdx.y > 0) return;
+        const int64_t r0 = (int64_t)(blockIdx.x - join_blocks) * rows_a_block, r1 = min(r0 + rows_a_block, a.rows);
+        for (int64_t r = r0 + threadIdx.x / GS_WAVE; r < r1; r += kJoin / GS_WAVE) {
+            if (a.marks && a.marks[r]) continue;
+            for (int c = lane_id(); c < a.dim; c += GS_WAVE) a.grad[r * a.ld_grad + c] = 0.0f;
+        }
+        return;
     }
-    const int64_t last = (lo - 1) / kChunk, m = last - g;      // chunks g + 1 .. last
     const int group = threadIdx.x / G, lane = threadIdx.x % G;
     const int col = blockIdx.y * (G * N) + lane * N, there = a.dim - col;
-    const int64_t per = (m + GROUPS - 1) / GROUPS;
-    float acc[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.0f;
-    auto add = [&](const float* p) {
+    if (threadIdx.x == 0) n_many = 0;
+    __syncthreads();
+    const int64_t g = (int64_t)blockIdx.x * GROUPS + group, p0 = g * a.per, p1 = p0 + a.per;
+    // whether a run starts here and goes on, and how many chunks behind this one it reaches
+    uint32_t row = a.limit;
+    bool mine = p1 < a.n;
+    if (mine) {
+        const uint32_t last = a.pairs[p1 - 1].x, next = a.pairs[p1].x, first = a.pairs[p0].x;
+        const uint32_t front = p0 > 0 ? a.pairs[p0 - 1].x : a.limit;
+        row = last;
+        mine = last < a.limit && next == last && !(first == last && front == last);
+    }
+    // a run ends in chunk c if the position behind c is another row's
+    auto ends_in = [&](int64_t c, uint32_t row) { return (c + 1) * a.per >= a.n || a.pairs[(c + 1) * a.per].x != row; };
+    const uint64_t lanes = G == GS_WAVE ? ~0ull : ((1ull << G) - 1) << (lane_id() / G * G);
+    const uint64_t ending = __ballot(mine && ends_in(g + 1 + lane, row)) & lanes;
+    const int m = ending ? __ffsll((unsigned long long)ending) - 1 - lane_id() / G * G + 1 : 0;
+    auto add = [&](float* acc, const float* p) {
         float f[N];
         load_floats<N, TAIL>(p + col, 0, there, f);
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] += f[i];
     };
-    if (group == 0) add(a.parts + (2 * g + 1) * a.dim);
-#pragma unroll 4
-    for (int64_t j = group * per; j < min((group + 1) * per, m); ++j) add(a.parts + 2 * (g + 1 + j) * a.dim);
+    float acc[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) sums[group][lane * N + i] = acc[i];
-    __syncthreads();
-    if (group == 0) {
-#pragma unroll
-        for (int u = 1; u < GROUPS; ++u)
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] += sums[u][lane * N + i];
+    for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+    if (mine && m > 0) {
+        add(acc, a.parts + (2 * g + 1) * a.dim);
+#pragma unroll 8
+        for (int j = 1; j <= m; ++j) add(acc, a.parts + 2 * (g + j) * a.dim);
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] *= a.scale;
         put_row<T, TAIL>(a.grad + (int64_t)row * a.ld_grad + col, there, acc);
     }
-}
-
-// Zeros for the rows that no token marked.
-__global__ void __launch_bounds__(GS_BLOCK) k_embed_zeros(EmbedSum a, int rows_a_block) {
-    const int64_t r0 = (int64_t)blockIdx.x * rows_a_block, r1 = min(r0 + rows_a_block, a.rows);
-    for (int64_t r = r0 + threadIdx.x / GS_WAVE; r < r1; r += GS_BLOCK / GS_WAVE) {
-        if (a.marks && a.marks[r]) continue;
-        for (int c = lane_id(); c < a.dim; c += GS_WAVE) a.grad[r * a.ld_grad + c] = 0.0f;
+    if (mine && m == 0 && lane == 0) many[atomicAdd(&n_many, 1)] = group;
+    __syncthreads();
+    const int runs = n_many;
+    for (int k = 0; k < runs; ++k) {
+        const int64_t c0 = (int64_t)blockIdx.x * GROUPS + many[k];
+        const uint32_t run = a.pairs[(c0 + 1) * a.per - 1].x;
+        int64_t chunks = 0;                    // behind c0
+        for (int64_t c = c0 + 1; chunks == 0; c += kJoin) {
+            if (threadIdx.x == 0) ends = kJoin;
+            __syncthreads();
+            if (ends_in(c + threadIdx.x, run)) atomicMin(&ends, (int)threadIdx.x);
+            __syncthreads();
+            if (ends < kJoin) chunks = c + ends - c0;
+            __syncthreads();
+        }
+        const int64_t per = (chunks + GROUPS - 1) / GROUPS;
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+        if (group == 0) add(acc, a.parts + (2 * c0 + 1) * a.dim);
+#pragma unroll 8
+        for (int64_t j = group * per; j < min((group + 1) * per, chunks); ++j) add(acc, a.parts + 2 * (c0 + 1 + j) * a.dim);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sums[group][lane * N + i] = acc[i];
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll 4
+            for (int u = 1; u < GROUPS; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[i] += sums[u][lane * N + i];
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i] *= a.scale;
+            put_row<T, TAIL>(a.grad + (int64_t)run * a.ld_grad + col, there, acc);
+        }
+        __syncthreads();
     }
 }
 
@@ -384,18 +468,33 @@ __global__ void k_zero_words(uint32_t* p, int64_t n) {
 }
 
 struct EmbedPlan {
-    int32_t bits, passes, digit, blocks, chunks;
+    int32_t bits, passes, digit, blocks, per, chunks;
+    bool many;
     size_t pairs[2], counts, totals, marks, parts, bytes;
 };
 
-EmbedPlan embed_plan(int32_t n, int32_t rows, int32_t dim, bool touched) {
+// Lanes that walk a chunk together: a power of two that holds the row's 16-byte pieces.
+inline int chunk_lanes(int32_t dim, int n) {
+    int g = 4;
+    while (g < GS_WAVE && g * n < dim) g *= 2;
+    return g;
+}
+
+EmbedPlan embed_plan(int32_t n, int32_t rows, int32_t dim, int32_t size, bool touched) {
     EmbedPlan p;
     p.bits = 1;
     while (p.bits < 31 && (uint32_t)rows >> p.bits) ++p.bits;              // of the key `rows`
     p.passes = (p.bits + kMostBits - 1) / kMostBits;
     p.digit = (p.bits + p.passes - 1) / p.passes;
-    p.blocks = (int32_t)div_up(n, kSortBlock);
-    p.chunks = (int32_t)div_up(n, kChunk);
+    // one block takes up to kMany items a thread; more blocks of few do better
+    p.many = n <= GS_BLOCK * kMany || n >= kManyFrom;
+    p.blocks = (int32_t)div_up(n, GS_BLOCK * (p.many ? kMany : kFew));
+    // chunks as long as leaves 1024 waves: longer ones have fewer ends that others share
+    const int elements = 16 / size, lanes = chunk_lanes(dim, elements);
+    const int64_t waves = (int64_t)n * lanes / GS_WAVE * div_up(dim, lanes * elements);
+    p.per = kMostChunk;
+    while (p.per > 8 && waves / p.per < 1024) p.per /= 2;
+    p.chunks = (int32_t)div_up(n, p.per);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -405,35 +504,51 @@ EmbedPlan embed_plan(int32_t n, int32_t rows, int32_t dim, bool touched) {
     p.pairs[0] = take((size_t)n * 8);
     p.pairs[1] = take((size_t)n * 8);
     // counts of the sort, then of the runs
-    p.counts = take(std::max(((size_t)p.blocks << p.digit) * 4, (size_t)div_up(n, GS_TILE_ITEMS) * 4 + 16));
+    p.counts = take(std::max(((size_t)p.blocks << p.digit) * 4, (size_t)div_up(n, GS_BLOCK * kRunItems) * 4 + 16));
     p.totals = take((size_t)kMostBins * 4);
-    p.marks = take(touched ? 0 : (size_t)rows);
+    p.marks = take(touched ? 0 : (size_t)rows + 4);
     p.parts = take((size_t)p.chunks * 2 * dim * 4);
     p.bytes = at;
     return p;
 }
 
 template <typename T, bool TAIL, int G>
-hipError_t sum_go(const EmbedSum& a, hipStream_t st) {
+hipError_t sum_go(const EmbedSum& a, int zero_blocks, int rows_a_block, hipStream_t st) {
     const uint32_t slabs = div_up(a.dim, G * Piece<T>::N);
     k_embed_sum<T, TAIL, G><<<dim3(div_up(a.chunks, GS_BLOCK / G), slabs), GS_BLOCK, 0, st>>>(a);
-    if (a.chunks > 1) k_embed_join<T, TAIL, G><<<dim3(a.chunks, slabs), GS_BLOCK, 0, st>>>(a);
+    const int join = a.chunks > 1 ? (int)div_up(a.chunks, kJoin / G) : 0;
+    if (join + zero_blocks > 0)
+        k_embed_join<T, TAIL, G><<<dim3(join + zero_blocks, slabs), kJoin, 0, st>>>(a, join, rows_a_block);
     return hipGetLastError();
 }
 
 template <typename T, bool TAIL>
-hipError_t sum_lanes(const EmbedSum& a, hipStream_t st) {
-    const int pieces = (int)div_up(a.dim, Piece<T>::N);
-    if (pieces <= 4) return sum_go<T, TAIL, 4>(a, st);
-    if (pieces <= 8) return sum_go<T, TAIL, 8>(a, st);
-    if (pieces <= 16) return sum_go<T, TAIL, 16>(a, st);
-    if (pieces <= 32) return sum_go<T, TAIL, 32>(a, st);
-    return sum_go<T, TAIL, 64>(a, st);
+hipError_t sum_lanes(const EmbedSum& a, int zero_blocks, int rows_a_block, hipStream_t st) {
+    switch (chunk_lanes(a.dim, Piece<T>::N)) {
+        case 4: return sum_go<T, TAIL, 4>(a, zero_blocks, rows_a_block, st);
+        case 8: return sum_go<T, TAIL, 8>(a, zero_blocks, rows_a_block, st);
+        case 16: return sum_go<T, TAIL, 16>(a, zero_blocks, rows_a_block, st);
+        case 32: return sum_go<T, TAIL, 32>(a, zero_blocks, rows_a_block, st);
+        default: return sum_go<T, TAIL, 64>(a, zero_blocks, rows_a_block, st);
+    }
 }
 
 template <typename T>
-hipError_t sum_type(const EmbedSum& a, hipStream_t st) {
-    return a.dim % Piece<T>::N ? sum_lanes<T, true>(a, st) : sum_lanes<T, false>(a, st);
+hipError_t sum_type(const EmbedSum& a, int zero_blocks, int rows_a_block, hipStream_t st) {
+    return a.dim % Piece<T>::N ? sum_lanes<T, true>(a, zero_blocks, rows_a_block, st)
+                               : sum_lanes<T, false>(a, zero_blocks, rows_a_block, st);
+}
+
+void sort_pass(const SortPass& q, bool many, hipStream_t st) {
+    if (q.blocks == 1) {
+        k_sort_scatter<kMany, true><<<1, GS_BLOCK, 0, st>>>(q);
+        return;
+    }
+    if (many) k_sort_count<kMany><<<q.blocks, GS_BLOCK, 0, st>>>(q);
+    else k_sort_count<kFew><<<q.blocks, GS_BLOCK, 0, st>>>(q);
+    k_sort_scan<<<div_up(1u << q.bits, GS_BLOCK / GS_WAVE), GS_BLOCK, 0, st>>>(q);
+    if (many) k_sort_scatter<kMany, false><<<q.blocks, GS_BLOCK, 0, st>>>(q);
+    else k_sort_scatter<kFew, false><<<q.blocks, GS_BLOCK, 0, st>>>(q);
 }
 
 template <typename TT, typename T>
@@ -466,80 +581,66 @@ hipError_t launch_embedding(const gs_embed_args& a, hipStream_t st) {
     return a.dtype == GS_BF16 ? embed_go<bf16_t, bf16_t>(a, st) : embed_go<f16_t, f16_t>(a, st);
 }
 
+// For the most that any type's kernels take.
 size_t embedding_bwd_ws_bytes(int32_t tokens, int32_t rows, int32_t dim, bool touched) {
-    return embed_plan(tokens, rows, dim, touched).bytes;
+    return std::max(embed_plan(tokens, rows, dim, 2, touched).bytes, embed_plan(tokens, rows, dim, 4, touched).bytes);
 }
 
 hipError_t launch_embedding_bwd(const gs_embed_bwd_args& g, void* ws, hipStream_t st) {
     const bool touched = g.unique != nullptr;
-    const EmbedPlan p = embed_plan(g.tokens, g.rows, g.dim, touched);
+    const EmbedPlan p = embed_plan(g.tokens, g.rows, g.dim, g.dtype == GS_F32 ? 4 : 2, touched);
     char* base = static_cast<char*>(ws);
     EmbedSum s;
+    s.pairs = nullptr;
     s.dout = g.dout;
     s.ld_dout = g.ld_dout;
     s.ld_grad = g.ld_grad;
     s.grad = g.grad;
     s.parts = reinterpret_cast<float*>(base + p.parts);
-    s.marks = nullptr;
+    s.marks = touched || g.tokens == 0 ? nullptr : reinterpret_cast<uint8_t*>(base + p.marks);
     s.rows = g.rows;
     s.n = g.tokens;
     s.dim = g.dim;
+    s.per = p.per;
     s.chunks = p.chunks;
     s.limit = (uint32_t)g.rows;
     s.scale = g.scale;
-    uint8_t* marks = touched || g.tokens == 0 ? nullptr : reinterpret_cast<uint8_t*>(base + p.marks);
-    if (marks) {
-        const int64_t words = ((int64_t)g.rows + 3) / 4;
-        k_zero_words<<<(uint32_t)std::min<int64_t>(1024, div_up(words, GS_BLOCK)), GS_BLOCK, 0, st>>>(
-            reinterpret_cast<uint32_t*>(marks), words);
+    // rows without a token: about 4096 elements a workgroup, at most 2^22 workgroups
+    const int64_t rows_a_block = std::max<int64_t>(std::max<int64_t>(8, 4096 / g.dim), ((int64_t)g.rows >> 22) + 1);
+    const int zero_blocks = touched ? 0 : (int)div_up(g.rows, rows_a_block);
+    if (g.tokens == 0) {
+        if (touched) k_zero_words<<<1, 1, 0, st>>>(reinterpret_cast<uint32_t*>(g.count), 1);
+        else k_embed_join<float, true, 64><<<zero_blocks, kJoin, 0, st>>>(s, 0, (int)rows_a_block);
+        return hipGetLastError();
     }
-    if (g.tokens > 0) {
-        uint2* buf[2] = {reinterpret_cast<uint2*>(base + p.pairs[0]), reinterpret_cast<uint2*>(base + p.pairs[1])};
-        uint32_t* counts = reinterpret_cast<uint32_t*>(base + p.counts);
-        int at = 0;
-        for (int i = 0; i < p.passes; ++i, at ^= 1) {
-            SortPass q;
-            q.ids = g.ids;
-            q.from = i ? buf[at ^ 1] : nullptr;
-            q.to = buf[at];
-            q.counts = counts;
-            q.totals = reinterpret_cast<uint32_t*>(base + p.totals);
-            q.marks = i ? nullptr : marks;
-            q.n = g.tokens;
-            q.rows = g.rows;
-            q.shift = i * p.digit;
-            q.bits = std::min(p.digit, p.bits - i * p.digit);
-            q.blocks = p.blocks;
-            if (p.blocks == 1) {
-                k_sort_scatter<true><<<1, GS_BLOCK, 0, st>>>(q);
-                continue;
-            }
-            k_sort_count<<<p.blocks, GS_BLOCK, 0, st>>>(q);
-            k_sort_scan<<<div_up(1u << q.bits, GS_BLOCK / GS_WAVE), GS_BLOCK, 0, st>>>(q);
-            k_sort_scatter<false><<<p.blocks, GS_BLOCK, 0, st>>>(q);
-        }
-        s.pairs = buf[at ^ 1];
-        if (touched) {
-            const uint32_t blocks = div_up(g.tokens, GS_TILE_ITEMS);
-            k_run_count<<<blocks, GS_BLOCK, 0, st>>>(s.pairs, g.tokens, (uint32_t)g.rows, counts);
-            k_run_place<<<blocks, GS_BLOCK, 0, st>>>(s.pairs, g.tokens, (uint32_t)g.rows, counts, buf[at], g.unique,
-                                                     g.count);
-            s.pairs = buf[at];
-        }
-        hipError_t e = g.dtype == GS_F32    ? sum_type<float>(s, st)
-                       : g.dtype == GS_BF16 ? sum_type<bf16_t>(s, st)
-                                            : sum_type<f16_t>(s, st);
-        if (e != hipSuccess) return e;
-    } else if (touched) {
-        k_zero_words<<<1, 1, 0, st>>>(reinterpret_cast<uint32_t*>(g.count), 1);
+    uint2* buf[2] = {reinterpret_cast<uint2*>(base + p.pairs[0]), reinterpret_cast<uint2*>(base + p.pairs[1])};
+    uint32_t* counts = reinterpret_cast<uint32_t*>(base + p.counts);
+    int at = 0;
+    for (int i = 0; i < p.passes; ++i, at ^= 1) {
+        SortPass q;
+        q.ids = g.ids;
+        q.from = i ? buf[at ^ 1] : nullptr;
+        q.to = buf[at];
+        q.counts = counts;
+        q.totals = reinterpret_cast<uint32_t*>(base + p.totals);
+        q.marks = i ? nullptr : reinterpret_cast<uint32_t*>(s.marks);
+        q.n = g.tokens;
+        q.rows = g.rows;
+        q.shift = i * p.digit;
+        q.bits = std::min(p.digit, p.bits - i * p.digit);
+        q.blocks = p.blocks;
+        sort_pass(q, p.many, st);
     }
-    if (!touched) {
-        s.marks = marks;
-        // about 4096 elements a block, at most 2^23 blocks
-        const int64_t per = std::max<int64_t>(std::max<int64_t>(4, 4096 / std::max(1, g.dim)), ((int64_t)g.rows >> 23) + 1);
-        k_embed_zeros<<<div_up(g.rows, per), GS_BLOCK, 0, st>>>(s, (int)per);
+    s.pairs = buf[at ^ 1];
+    if (touched) {
+        const uint32_t blocks = div_up(g.tokens, GS_BLOCK * kRunItems);
+        k_run_count<<<blocks, GS_BLOCK, 0, st>>>(s.pairs, g.tokens, (uint32_t)g.rows, counts);
+        k_run_place<<<blocks, GS_BLOCK, 0, st>>>(s.pairs, g.tokens, (uint32_t)g.rows, counts, buf[at], g.unique, g.count);
+        s.pairs = buf[at];
     }
-    return hipGetLastError();
+    if (g.dtype == GS_F32) return sum_type<float>(s, zero_blocks, (int)rows_a_block, st);
+    return g.dtype == GS_BF16 ? sum_type<bf16_t>(s, zero_blocks, (int)rows_a_block, st)
+                              : sum_type<f16_t>(s, zero_blocks, (int)rows_a_block, st);
 }
 
 }  // namespace gsmi
