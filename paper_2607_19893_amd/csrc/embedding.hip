@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(GS_BLOCK) k_embedding(gs_embed_args a, int tok
                 f[k][i] = (uint32_t)id[k] < (uint32_t)a.rows ? f[k][i] * a.scale : 0.0f;
                 loaded(f[k][i]);               // an fp32 product for every type: fp16's could be fused with its rounding
             }
-            Span<T, TAIL>::store(static_cast<T*>(a.out) + (t0 + tok[k]) * a.ld_out + col[k], a.dim - col[k], f[k]);
+            Span<T, TAIL>::template store<true>(static_cast<T*>(a.out) + (t0 + tok[k]) * a.ld_out + col[k], a.dim - col[k], f[k]);
         }
     }
 }
@@ -290,6 +290,7 @@ struct EmbedSum {
 };
 
 constexpr int kMostChunk = 64;
+constexpr int kSum = 64;                       // threads of a workgroup: few, so that the units share the chunks evenly
 
 template <typename T, bool TAIL>
 __device__ __forceinline__ void put_row(float* p, int there, const float* f) {
@@ -301,12 +302,12 @@ __device__ __forceinline__ void put_row(float* p, int there, const float* f) {
 // G lanes a chunk, blockIdx.y: slabs of G * N columns.  The workgroup's pairs go
 // to LDS first, then AHEAD rows are on their way while AHEAD are added.
 template <typename T, bool TAIL, int G>
-__global__ void __launch_bounds__(GS_BLOCK) k_embed_sum(EmbedSum a) {
-    constexpr int N = Piece<T>::N, AHEAD = 8, GROUPS = GS_BLOCK / G;
+__global__ void __launch_bounds__(kSum) k_embed_sum(EmbedSum a) {
+    constexpr int N = Piece<T>::N, AHEAD = 8, GROUPS = kSum / G;
     __shared__ uint2 list[GROUPS * kMostChunk + 2];        // from the position in front of the workgroup's first
     const int64_t base = (int64_t)blockIdx.x * GROUPS * a.per;
     const int count = (int)min((int64_t)GROUPS * a.per, (int64_t)a.n - base);
-    for (int i = threadIdx.x; i < count + 2; i += GS_BLOCK) {
+    for (int i = threadIdx.x; i < count + 2; i += kSum) {
         const int64_t p = base + i - 1;
         list[i] = p >= 0 && p < a.n ? a.pairs[p] : make_uint2(a.limit, 0u);
     }
@@ -515,7 +516,7 @@ EmbedPlan embed_plan(int32_t n, int32_t rows, int32_t dim, int32_t size, bool to
 template <typename T, bool TAIL, int G>
 hipError_t sum_go(const EmbedSum& a, int zero_blocks, int rows_a_block, hipStream_t st) {
     const uint32_t slabs = div_up(a.dim, G * Piece<T>::N);
-    k_embed_sum<T, TAIL, G><<<dim3(div_up(a.chunks, GS_BLOCK / G), slabs), GS_BLOCK, 0, st>>>(a);
+    k_embed_sum<T, TAIL, G><<<dim3(div_up(a.chunks, kSum / G), slabs), kSum, 0, st>>>(a);
     const int join = a.chunks > 1 ? (int)div_up(a.chunks, kJoin / G) : 0;
     if (join + zero_blocks > 0)
         k_embed_join<T, TAIL, G><<<dim3(join + zero_blocks, slabs), kJoin, 0, st>>>(a, join, rows_a_block);

@@ -75,13 +75,15 @@ struct Span {
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = (float)v[i];
     }
-    // rounded to nearest even
+    // rounded to nearest even; STREAM: past the caches, for what nobody reads soon
+    template <bool STREAM = false>
     static __device__ __forceinline__ void store(T* p, int there, const float* f) {
         vec v;
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = (T)f[i];
         if (there >= N) {
-            *reinterpret_cast<loose*>(p) = v;
+            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<loose*>(p));
+            else *reinterpret_cast<loose*>(p) = v;
         } else if (TAIL) {
 #pragma unroll
             for (int i = 0; i < N - 1; ++i)
