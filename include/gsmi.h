@@ -942,7 +942,8 @@ gs_status gs_embedding(const gs_embed_args* args, void* stream);
  *     without a token are 0); count is not used.
  *   unique [min(tokens, rows)] int32: the ids that have a token, ascending;
  *     count [1] how many; grad [min(tokens, rows), ld_grad] fp32 their rows, in
- *     that order.  What gs_sparse_adam takes as its idx, count and grad_rows.
+ *     that order.  What gs_sparse_adam takes as its idx, count and grad_rows (rows
+ *     of up to 64 columns).
  *     Behind the first *count, unique and grad are left as they were.
  *   ws: gs_embedding_bwd_ws_bytes(tokens, rows, dim, unique != NULL) bytes,
  *     16-byte aligned
@@ -980,14 +981,16 @@ gs_status gs_embedding_bwd(const gs_embed_bwd_args* args, void* ws, size_t ws_by
  *     outside [0, n] are taken as the nearest in it.  Tokens outside every
  *     segment reach nothing, and their y is left as it was (fill != 0: 0).
  *   initial, final [n_seg, cols] fp32, dense, or NULL (final: not written).  An
- *     empty segment's final is its initial.
+ *     empty segment's final is its initial.  final may be initial itself: a
+ *     served sequence's states in place.
  *   kept NULL, or [ceil(n / GS_RECUR_KEEP), cols] fp32, dense: for the gradient,
  *     row j is the state in front of place j * GS_RECUR_KEEP (places are counted
  *     in the direction of the recurrence), 0 where that is a segment's first or
  *     no segment's.
  *   ws: gs_recurrence_ws_bytes(a) bytes (can be 0: ws may be NULL), 16-byte
  *     aligned, for gs_recurrence and its gradient alike.  The size follows from
- *     the sizes in `a`, not from cu's values.
+ *     the sizes in `a`, not from cu's values.  Calls that may run at the same
+ *     time (on two streams) need a workspace each.
  * A segment of one token is a step of a served sequence.  The tokens are taken in
  * an order that the sizes alone fix: the same call gives the same bits.  A NaN
  * or infinity stays in its channel and segment, from its token on.

@@ -3,17 +3,23 @@
 One token per visible primitive.  The pool's ids are cut into regions of
 `region` consecutive primitives (a spatially ordered pool makes them compact);
 a token attends to the tokens of its own region, turned by its primitive's
-place in space.  The network writes a correction of every visible row; the view
+place in space.  With trunk="recurrence" the cost is linear in the tokens, and
+regions may be as long as the pool: a token adds the vector of its cell in
+space, two gated recurrences run along its region and against it, and the
+activations are kept in 8 bits for the gradient.
+The network writes a correction of every visible row; the view
 is rendered with the corrected rows, and the gradient rows of its backward go
 back through the network.  The tokens' last norm in 8 bits can be published to
 a replica as any other rows are.
 
-The norms, rotations and attention are the package's token operators; the plain
-matrix products and the weights' Adam are torch's.
+The lookups, norms, rotations, attention, recurrences and gates are the package's
+token operators; the plain matrix products and the weights' Adam are torch's.
 
-    python -m paper_2607_19893_amd.refiner
+    python -m paper_2607_19893_amd.refiner [attention | recurrence]
 """
 from __future__ import annotations
+
+import sys
 
 import torch
 
@@ -26,12 +32,15 @@ AXES = 3
 class RegionRefiner:
     """Corrections for the rows of `trainer`'s pool, which itself stays as it is between steps."""
 
-    def __init__(self, trainer: ViewTrainer, region=1024, width=128, heads=4, kv_heads=2, gain=1.0, lr=1e-3, seed=0):
+    def __init__(self, trainer: ViewTrainer, region=1024, width=128, heads=4, kv_heads=2, gain=1.0, lr=1e-3, seed=0,
+                 trunk="attention", cells=16):
+        if trunk not in ("attention", "recurrence"):
+            raise ValueError("trunk is attention or recurrence, not %r" % (trunk,))
         if width % heads or width % 4 or heads % kv_heads or (width // heads) % 8:
             raise ValueError("width %d does not fit %d heads over %d" % (width, heads, kv_heads))
         self.tr, self.region, self.width, self.heads, self.kv_heads = trainer, int(region), width, heads, kv_heads
         self.dim = width // heads
-        self.gain, self.eps = gain, 1e-6
+        self.gain, self.eps, self.trunk, self.cells = gain, 1e-6, trunk, int(cells)
         dev = trainer.dev
         n = trainer.n
         base = self.base
@@ -45,6 +54,7 @@ class RegionRefiner:
         self.axis_pairs = (per,) * AXES
         extent = float((base[:, :3].amax(0) - base[:, :3].amin(0)).amax())
         self.place = 100.0 / max(extent, 1e-6)
+        self.corner, self.cell = base[:, :3].amin(0), max(extent, 1e-6) / self.cells
         g = torch.Generator(device=dev)
         g.manual_seed(seed)
 
@@ -52,12 +62,23 @@ class RegionRefiner:
             return (torch.randn(rows, cols, generator=g, device=dev) * (scale * rows ** -0.5)).requires_grad_()
 
         row = trainer.row_len
-        self.w = dict(inp=matrix(row, width), qkv=matrix(width, (heads + 2 * kv_heads) * self.dim),
-                      out=matrix(width, width), up=matrix(width, 4 * width), down=matrix(4 * width, width),
-                      head=matrix(width, row, 0.1))
+        if trunk == "attention":
+            self.w = dict(inp=matrix(row, width), qkv=matrix(width, (heads + 2 * kv_heads) * self.dim),
+                          out=matrix(width, width), up=matrix(width, 4 * width), down=matrix(4 * width, width),
+                          head=matrix(width, row, 0.1))
+        else:
+            # mix: a gate and a token for each of the two directions; up: the two sides of the gated activation
+            self.w = dict(inp=matrix(row, width), mix=matrix(width, 4 * width), out=matrix(2 * width, width),
+                          up=matrix(width, 8 * width), down=matrix(4 * width, width), head=matrix(width, row, 0.1))
+            for k in ("bias1", "bias2"):
+                self.w[k] = torch.zeros(width, device=dev, requires_grad=True)
+            # `table` is looked up by row, no matrix product's operand
+            self.table = (0.1 * torch.randn(self.cells ** 3, width, generator=g, device=dev)).requires_grad_()
+            # gates that hold a state for some tokens at the start
+            self.hold = 1.5
         for k in ("norm1", "norm2", "norm3"):
             self.w[k] = torch.ones(width, device=dev, requires_grad=True)
-        self.opt = torch.optim.Adam(list(self.w.values()), lr=lr)
+        self.opt = torch.optim.Adam(list(self.w.values()) + ([self.table] if trunk == "recurrence" else []), lr=lr)
         self.last = self.last_norm = None     # (ids, total) of the last forward and its last norm's weight, for publish()
 
     def rows(self, ids):
@@ -84,6 +105,9 @@ class RegionRefiner:
         cu = torch.searchsorted(ids, self.starts).int()
         pos = (rows[:, :AXES] * self.place).contiguous()
         x = ((rows - self.shift) / self.spread).to(bf) @ w["inp"]
+        if self.trunk == "recurrence":
+            h, total = self._recurrence(x, rows, w, cu)
+            return self._head(h, total, ids, w)
         y, total = tokens.RmsNorm.apply(x, None, w["norm1"], self.eps)
         qkv = (y @ w["qkv"]).view(-1, self.heads + 2 * self.kv_heads, self.dim)
         q, k = tokens.Rotary.apply(qkv[:, :self.heads], qkv[:, self.heads:self.heads + self.kv_heads], pos, self.freq,
@@ -91,9 +115,27 @@ class RegionRefiner:
         o, _ = tokens.Attention.apply(q, k, qkv[:, self.heads + self.kv_heads:], dict(cu_q=cu, cu_k=cu))
         y, total = tokens.RmsNorm.apply(o.reshape(-1, self.width) @ w["out"], total, w["norm2"], self.eps)
         h = torch.nn.functional.silu(y @ w["up"]) @ w["down"]
+        return self._head(h, total, ids, w)
+
+    def _head(self, h, total, ids, w):
         y, last = tokens.RmsNorm.apply(h, total, w["norm3"], self.eps)
         self.last, self.last_norm = (ids, last.detach()), w["norm3"].detach().clone()
         return (y @ w["head"]).float() * (self.gain * self.spread)
+
+    def cell_ids(self, rows):
+        """The rows' cells in space, int32."""
+        at = ((rows[:, :AXES] - self.corner) / self.cell).long().clamp(0, self.cells - 1)
+        return ((at[:, 0] * self.cells + at[:, 1]) * self.cells + at[:, 2]).int()
+
+    def _recurrence(self, x, rows, w, cu):
+        """(the last block's output, the sum in front of it)."""
+        where = tokens.Embedding.apply(self.table, self.cell_ids(rows), 1.0, x.dtype)
+        y, total = tokens.LayerNorm.apply(x, where, w["norm1"], w["bias1"], self.eps)
+        mix = (y @ w["mix"]).view(-1, 4, self.width)
+        along, _ = tokens.Recurrence.apply(mix[:, 0], mix[:, 1] + self.hold, None, dict(cu=cu))
+        against, _ = tokens.Recurrence.apply(mix[:, 2], mix[:, 3] + self.hold, None, dict(cu=cu, reverse=True))
+        y, total = tokens.LayerNorm.apply(torch.cat((along, against), 1) @ w["out"], total, w["norm2"], w["bias2"], self.eps)
+        return tokens.GatedProjection.apply(y @ w["up"], w["down"]), total
 
     def write_rows(self, ids, rows):
         """Rows of the pool's groups."""
@@ -163,7 +205,7 @@ class RegionRefiner:
         return q * rows[:, a:a + b].repeat_interleave(gsmi.GS_NORM_BLOCK, 1)[:, :self.width]
 
 
-def main(steps=60, n=10_000, seed=0):
+def main(steps=60, n=10_000, seed=0, trunk="attention"):
     from . import scenes
 
     w = scenes.spatially_ordered(scenes.tiny(seed=seed, n=n))
@@ -171,7 +213,7 @@ def main(steps=60, n=10_000, seed=0):
     tr = ViewTrainer(w.scene, capacity=1 << 18, max_width=cam.width, max_height=cam.height)
     tr.ensure_capacity([cam], margin=4.0)
     tr.set_target(w.target(0))
-    net = RegionRefiner(tr, seed=seed)
+    net = RegionRefiner(tr, seed=seed, trunk=trunk, region=1024 if trunk == "attention" else n)
     losses = [net.step(cam) for _ in range(steps)]
     status, versions = torch.zeros(4, dtype=torch.int32, device=tr.dev), torch.zeros(n, dtype=torch.int32, device=tr.dev)
     table, replica, msg = net.replica_table(), net.replica_table(), net.message()
@@ -184,4 +226,4 @@ def main(steps=60, n=10_000, seed=0):
 
 
 if __name__ == "__main__":
-    main()
+    main(trunk=(sys.argv[1:] or ["attention"])[0])

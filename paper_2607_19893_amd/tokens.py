@@ -5,8 +5,8 @@ inputs are kept in 8 bits, each with its gradient.
 
 The functions allocate their outputs and workspaces with torch on the current
 stream of their tensors' GPU and call the gs_* entry points there; every step
-runs in libgsmi's kernels.  `RmsNorm`, `LayerNorm`, `Embedding`, `Rotary`, `Attention`, `Recurrence` and `GatedSilu`
-put them under torch's autograd; their gradients have none of their own, a second derivative raises.
+runs in libgsmi's kernels.  `RmsNorm`, `LayerNorm`, `Embedding`, `Rotary`, `Attention`, `Recurrence`, `GatedSilu` and
+`GatedProjection` put them under torch's autograd; their gradients have none of their own, a second derivative raises.
 """
 from __future__ import annotations
 
@@ -417,3 +417,32 @@ class GatedSilu(torch.autograd.Function):
     def backward(ctx, dh):
         du, dv, _ = gated_silu_backward(dh.contiguous(), *ctx.saved_tensors, again=False)
         return du, dv
+
+
+class GatedProjection(torch.autograd.Function):
+    """GatedProjection.apply(both, down) -> silu(u) * v @ down, for both [rows, 2 * hidden] = (u, v) as one projection
+    gives them and down [hidden, cols].
+
+    Saved for the gradient are u and v in 8 bits and `down`; the product's operand is formed again from them, so that
+    none of the three [rows, hidden] matrices is held in the tokens' type.  The gradients are those at the kept values."""
+
+    @staticmethod
+    def forward(ctx, both, down):
+        hidden = both.shape[1] // 2
+        if both.shape[1] != 2 * hidden or down.shape[0] != hidden:
+            raise ValueError("both %s is not twice as wide as down %s is high" % (tuple(both.shape), tuple(down.shape)))
+        r = gated_silu(both[:, :hidden], both[:, hidden:])
+        ctx.save_for_backward(r.u8, r.u_scale, r.v8, r.v_scale, down)
+        return r.h @ down
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        u8, u_scale, v8, v_scale, down = ctx.saved_tensors
+        rows, hidden = u8.shape
+        dh = dout @ down.T
+        with _device_of(dh, u8):
+            dboth = torch.empty(rows, 2 * hidden, dtype=dh.dtype, device=dh.device)
+            h = torch.empty_like(dh, memory_format=_DENSE)
+            gsmi.gs_gated_silu_bwd(dh, u8, u_scale, dboth[:, :hidden], v8, v_scale, dboth[:, hidden:], h)
+        return dboth, h.T @ dout

@@ -1,0 +1,196 @@
+"""How the trunk's operators sit in torch: second derivatives, devices, tensors that change between the passes.  The
+library's calls are replaced, so all of it runs without a GPU."""
+import pytest
+import torch
+
+from test_tokens_torch import Elsewhere, rand
+
+
+@pytest.fixture
+def tk(monkeypatch):
+    from paper_2607_19893_amd import tokens
+
+    def layer_norm(x, weight, bias=None, eps=1e-5, residual=None):
+        s = x if residual is None else x + residual
+        y = torch.nn.functional.layer_norm(s, s.shape[1:], weight, bias, eps)
+        return tokens.LayerNormed(y, s)
+
+    def layer_norm_backward(dy, total, weight, eps=1e-5, dtotal=None):
+        with torch.enable_grad():
+            t, w, b = total.detach().requires_grad_(), weight.detach().requires_grad_(), torch.zeros_like(weight).requires_grad_()
+            y = torch.nn.functional.layer_norm(t, t.shape[1:], w, b, eps)
+            dx, dw, db = torch.autograd.grad(y, (t, w, b), dy)
+        return dx if dtotal is None else dx + dtotal, dw, db
+
+    def embedding(table, ids, scale=1.0, dtype=None):
+        return scale * table[ids.long()]
+
+    def embedding_backward(dout, ids, rows, scale=1.0):
+        return torch.zeros(rows, dout.shape[1], dtype=dout.dtype).index_add_(0, ids.long(), dout) * scale
+
+    def scan(x, gate, initial):
+        a, h, out = torch.sigmoid(gate), initial[0], []
+        for t in range(x.shape[0]):
+            h = a[t] * h + (1 - a[t]) * x[t]
+            out.append(h)
+        return torch.stack(out)
+
+    def recurrence(x, gate, cu=None, n_seg=1, initial=None, reverse=False, keep=False):
+        y = scan(x, gate, initial)
+        return tokens.Scanned(y, y[-1:].clone(), y[:1].clone() if keep else None)
+
+    def recurrence_backward(dy, x, gate, kept, cu=None, n_seg=1, initial=None, dfinal=None, reverse=False):
+        with torch.enable_grad():
+            t = [v.detach().requires_grad_() for v in (x, gate, initial)]
+            y = scan(*t)
+            d = dy.clone()
+            if dfinal is not None:
+                d[-1] += dfinal[0]
+            return torch.autograd.grad(y, t, d)
+
+    def gated_silu(u, v=None, keep=True):
+        h = torch.nn.functional.silu(u) * (1 if v is None else v)
+        return tokens.Gated(h, u.clone(), u.clone(), None if v is None else v.clone(), None if v is None else v.clone())
+
+    def gated_silu_backward(dh, u8, u_scale, v8=None, v_scale=None, again=True):
+        with torch.enable_grad():
+            t = [v.detach().requires_grad_() for v in (u8, v8) if v is not None]
+            h = torch.nn.functional.silu(t[0]) * (t[1] if len(t) > 1 else 1)
+            d = torch.autograd.grad(h, t, dh)
+        return d[0], d[1] if len(t) > 1 else None, h.detach() if again else None
+
+    for f in (layer_norm, layer_norm_backward, embedding, embedding_backward, recurrence, recurrence_backward, gated_silu,
+              gated_silu_backward):
+        monkeypatch.setattr(tokens, f.__name__, f)
+    return tokens
+
+
+def layer_call(tk, move=0.0):
+    w = (1 + rand(16) + move).requires_grad_()
+    y, _ = tk.LayerNorm.apply(rand(5, 16).requires_grad_(), None, w, None, 1e-5)
+    return y, w
+
+
+def embedding_call(tk, move=0.0):
+    t = (rand(4, 8) + move).requires_grad_()
+    return tk.Embedding.apply(t, torch.tensor([0, 3, 3], dtype=torch.int32), 2.0, None), t
+
+
+def recurrence_call(tk, move=0.0):
+    x = (rand(6, 4) + move).requires_grad_()
+    y, _ = tk.Recurrence.apply(x, rand(6, 4, seed=1), rand(1, 4), dict(n_seg=1))
+    return y, x
+
+
+def silu_call(tk, move=0.0):
+    u = (rand(3, 8) + move).requires_grad_()
+    return tk.GatedSilu.apply(u, rand(3, 8, seed=1)), u
+
+
+CALLS = [layer_call, embedding_call, recurrence_call, silu_call]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_a_second_derivative_is_refused(tk, call):
+    y, x = call(tk)
+    (g,) = torch.autograd.grad(y.pow(2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (g.pow(2).sum() + x.sum()).backward()
+    y, x = call(tk)
+    y.pow(2).sum().backward()
+    assert x.grad is not None and bool(torch.isfinite(x.grad).all())
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_gradients_are_the_formulas(tk, call):
+    """What the autograd forms pass on is what the functions give, in the inputs' order (against differences)."""
+    y, x = call(tk)
+    d = rand(*y.shape, seed=9)
+    (g,) = torch.autograd.grad(y, x, d)
+    v, h = rand(*x.shape, seed=10), 1e-6
+    up, down = (float((call(tk, m * v)[0].detach() * d).sum()) for m in (h, -h))
+    # the differences' own error (third derivative, h^2, and 2^-53 / h of the sums)
+    assert abs((up - down) / (2 * h) - float((g * v).sum())) <= 1e-6 * (1 + float((g * v).abs().sum()))
+
+
+def test_outputs_that_nobody_uses(tk):
+    """A gradient through one of two outputs, through the sum alone, and through the last states alone."""
+    w = (1 + rand(16)).requires_grad_()
+    x, r = rand(5, 16).requires_grad_(), rand(5, 16, seed=1).requires_grad_()
+    y, total = tk.LayerNorm.apply(x, r, w, None, 1e-5)
+    gx, gr = torch.autograd.grad(total.sum(), (x, r))
+    assert torch.equal(gx, torch.ones_like(x)) and torch.equal(gr, torch.ones_like(r))
+    a = rand(6, 4).requires_grad_()
+    _, final = tk.Recurrence.apply(a, rand(6, 4, seed=1), rand(1, 4), dict(n_seg=1))
+    (g,) = torch.autograd.grad(final.sum(), a)
+    assert bool((g > 0).all())
+
+
+def test_starts_that_change_before_the_backward_are_noticed(tk):
+    cu = torch.tensor([0, 6], dtype=torch.int32)
+    a = rand(6, 4).requires_grad_()
+    y, _ = tk.Recurrence.apply(a, rand(6, 4, seed=1), rand(1, 4), dict(cu=cu))
+    cu.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+def test_projection_shapes_are_checked(tk):
+    with pytest.raises(ValueError, match="twice"):
+        tk.GatedProjection.apply(rand(3, 9), rand(4, 5))
+    with pytest.raises(ValueError, match="twice"):
+        tk.GatedProjection.apply(rand(3, 8), rand(5, 5))
+
+
+def test_a_call_runs_on_its_tensors_device(monkeypatch):
+    """Tensors of GPU 1 while GPU 0 is current: the library's call is made with GPU 1 current, and GPU 0 is so again."""
+    import contextlib
+
+    from paper_2607_19893_amd import gsmi, tokens
+    now, seen = [0], []
+
+    @contextlib.contextmanager
+    def device(d):
+        before, now[0] = now[0], d
+        yield
+        now[0] = before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    names = ("gs_layer_norm", "gs_layer_norm_bwd", "gs_embedding", "gs_embedding_bwd", "gs_recurrence", "gs_recurrence_bwd",
+             "gs_gated_silu", "gs_gated_silu_bwd")
+    for name in names:
+        monkeypatch.setattr(gsmi, name, lambda *a, name=name, **k: seen.append((name, now[0])))
+
+    def there(*shape, dtype=torch.float32):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(Elsewhere)
+
+    x, w, ids = there(4, 64), there(64), there(4, dtype=torch.int32)
+    tokens.layer_norm(x, w, w, residual=x)
+    tokens.layer_norm_backward(x, x, w)
+    tokens.embedding(x, ids)
+    tokens.embedding_backward(x, ids, 9)
+    tokens.recurrence(x, x)
+    tokens.recurrence_backward(x, x, x, there(1, 64))
+    r = tokens.gated_silu(x, x)
+    tokens.gated_silu_backward(x, *(t.as_subclass(Elsewhere) for t in r[1:]))
+    assert seen == [(n, 1) for n in names] and now == [0]
+    with pytest.raises(ValueError, match="tensors on"):
+        tokens.layer_norm(x, torch.zeros(64))
+
+
+@pytest.mark.parametrize("what", ["ids", "cu", "initial", "kept", "types", "u8"])
+def test_tensors_that_do_not_fit_are_refused(monkeypatch, what):
+    """By the binding, before the library is called."""
+    from paper_2607_19893_amd import gsmi
+    x = torch.zeros(70, 8)
+    bad = {
+        "ids": lambda: gsmi.gs_embedding(x, torch.zeros(70, dtype=torch.int64), 1.0, x),
+        "cu": lambda: gsmi.make_recur(x, x, torch.zeros(3, dtype=torch.int64)),
+        "initial": lambda: gsmi.make_recur(x, x, None, 2, torch.zeros(1, 8)),
+        "kept": lambda: gsmi.gs_recurrence(gsmi.make_recur(x, x), x, None, torch.zeros(1, 8)),
+        "types": lambda: gsmi.make_recur(x, x.half()),
+        "u8": lambda: gsmi.gs_gated_silu(x, None, x, torch.zeros(70, 8), torch.zeros(70, 1)),
+    }
+    with pytest.raises(ValueError):
+        bad[what]()
