@@ -385,9 +385,14 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_block
     if ((int)blockIdx.x >= join_blocks) {
         if (blockIdx.y > 0) return;
         const int64_t r0 = (int64_t)(blockIdx.x - join_blocks) * rows_a_block, r1 = min(r0 + rows_a_block, a.rows);
-        for (int64_t r = r0 + threadIdx.x / GS_WAVE; r < r1; r += kJoin / GS_WAVE) {
-            if (a.marks && a.marks[r]) continue;
-            for (int c = lane_id(); c < a.dim; c += GS_WAVE) a.grad[r * a.ld_grad + c] = 0.0f;
+        // pieces of four floats, each thread its own row's mark
+        const int pieces = (a.dim + 3) / 4, items = (int)(r1 - r0) * pieces;
+        const float inv = 1.0f / (float)pieces, none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int i = threadIdx.x; i < items; i += kJoin) {
+            const int r = (int)(((float)i + 0.5f) * inv), c = (i - r * pieces) * 4;   // fewer than 2^18 items
+            if (a.marks && a.marks[r0 + r]) continue;
+            Span<float, TAIL>::store(a.grad + (r0 + r) * a.ld_grad + c, a.dim - c, none);
         }
         return;
     }
@@ -606,8 +611,8 @@ hipError_t launch_embedding_bwd(const gs_embed_bwd_args& g, void* ws, hipStream_
     s.chunks = p.chunks;
     s.limit = (uint32_t)g.rows;
     s.scale = g.scale;
-    // rows without a token: about 4096 elements a workgroup, at most 2^22 workgroups
-    const int64_t rows_a_block = std::max<int64_t>(std::max<int64_t>(8, 4096 / g.dim), ((int64_t)g.rows >> 22) + 1);
+    // rows without a token: 2^14 elements a workgroup (a row at least; 2^22 workgroups at most)
+    const int64_t rows_a_block = std::max<int64_t>(std::max<int64_t>(1, 16384 / g.dim), ((int64_t)g.rows >> 22) + 1);
     const int zero_blocks = touched ? 0 : (int)div_up(g.rows, rows_a_block);
     if (g.tokens == 0) {
         if (touched) k_zero_words<<<1, 1, 0, st>>>(reinterpret_cast<uint32_t*>(g.count), 1);

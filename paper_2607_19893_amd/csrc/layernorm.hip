@@ -248,7 +248,9 @@ hipError_t layer_go(const gs_layer_args& a, hipStream_t st) {
     const uint32_t by4 = div_up(a.rows, 4), narrow = div_up(a.rows, GS_BLOCK / NARROW);
     if (a.cols <= 128) k_layer_norm<T, TAIL, NARROW, N><<<narrow, GS_BLOCK, 0, st>>>(a);
     else if (a.cols <= 256) k_layer_norm<T, TAIL, NARROW, 2 * N><<<narrow, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 512) k_layer_norm<T, TAIL, 32, 16><<<div_up(a.rows, 8), GS_BLOCK, 0, st>>>(a);
     else if (a.cols <= 1024) k_layer_norm<T, TAIL, 64, 16><<<by4, GS_BLOCK, 0, st>>>(a);
+    else if (a.cols <= 1536) k_layer_norm<T, TAIL, 64, 24><<<by4, GS_BLOCK, 0, st>>>(a);
     else if (a.cols <= 2048) k_layer_norm<T, TAIL, 64, 32><<<by4, GS_BLOCK, 0, st>>>(a);
     else if (a.cols <= 8192) k_layer_norm<T, TAIL, 256, 32><<<a.rows, GS_BLOCK, 0, st>>>(a);
     else k_layer_norm<T, TAIL, 256, 64><<<a.rows, GS_BLOCK, 0, st>>>(a);
@@ -263,10 +265,12 @@ hipError_t layer_type(const gs_layer_args& a, hipStream_t st) {
 template <typename T, bool TAIL>
 hipError_t layer_bwd_go(const gs_layer_bwd_args& a, float* parts, hipStream_t st) {
     constexpr int N = Piece<T>::N, NARROW = 128 / N;
-    const int n = layer_parts(a.rows, a.cols <= 256 ? GS_BLOCK / NARROW : (a.cols <= 2048 ? 4 : 1));
+    const int n = layer_parts(a.rows, a.cols <= 256 ? GS_BLOCK / NARROW : a.cols <= 512 ? 8 : a.cols <= 2048 ? 4 : 1);
     if (a.cols <= 128) k_layer_norm_bwd<T, TAIL, NARROW, N><<<n, GS_BLOCK, 0, st>>>(a, parts);
     else if (a.cols <= 256) k_layer_norm_bwd<T, TAIL, NARROW, 2 * N><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 512) k_layer_norm_bwd<T, TAIL, 32, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
     else if (a.cols <= 1024) k_layer_norm_bwd<T, TAIL, 64, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
+    else if (a.cols <= 1536) k_layer_norm_bwd<T, TAIL, 64, 24><<<n, GS_BLOCK, 0, st>>>(a, parts);
     else if (a.cols <= 2048) k_layer_norm_bwd<T, TAIL, 64, 32><<<n, GS_BLOCK, 0, st>>>(a, parts);
     else if (a.cols <= 4096) k_layer_norm_bwd<T, TAIL, 256, 16><<<n, GS_BLOCK, 0, st>>>(a, parts);
     else k_layer_norm_bwd<T, TAIL, 512, 32><<<n, 512, 0, st>>>(a, parts);

@@ -38,7 +38,7 @@ struct Recur {
     gs_recur a;
     uint64_t* maps;                            // [blocks][chunks][2 * 64]: (A, B) of a lane's two channels
     uint64_t* states;                          // [blocks][chunks][64]: a lane's two states behind the chunk
-    uint32_t* flags;                           // [blocks][chunks]: kMap, then kState; behind them the ticket
+    uint32_t* flags;                           // [blocks][chunks]: kMap, then kState; behind them the counters
     int32_t chunks, blocks, width;             // width: channels of a block
 };
 
@@ -75,7 +75,7 @@ __device__ __forceinline__ void pass_empty(const gs_recur& a, const float* from,
     }
 }
 
-// The flags and the ticket cleared, the empty segments' states.
+// The flags and the counters cleared, the empty segments' states.
 __global__ void __launch_bounds__(GS_BLOCK) k_recur_clear(gs_recur a, const float* from, float* to, uint32_t* flags,
                                                           int32_t n_flags) {
     for (int64_t i = (int64_t)blockIdx.x * GS_BLOCK + threadIdx.x; i < n_flags; i += (int64_t)gridDim.x * GS_BLOCK) flags[i] = 0;
@@ -262,7 +262,7 @@ __device__ __forceinline__ void through(const float4* maps, const uint32_t* anew
 }
 
 // ---------------------------------------------------------------------------
-// Looking back.  The workgroups take chunks by a ticket, chunk after chunk, so
+// Looking back.  The workgroups take chunks from a counter, one after the other, so
 // every chunk that one waits for belongs to a workgroup that is already running
 // and publishes its map before it waits itself: every wait ends.  (Calls that
 // run at the same time on one workspace would clear each other's flags; a wait
@@ -307,8 +307,9 @@ __device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* an
     return any;
 }
 
+constexpr int kFold = 16;                      // maps that are fetched together
 struct Lookers {                               // in LDS
-    float4 passed[kWaves * GS_WAVE];           // a wave's maps of the chunks in front, as one
+    float4 passed[kFold * GS_WAVE];            // maps of chunks in front
     float2 state[GS_WAVE];                     // behind the chunk that the nearest known state is of
     int32_t distance;                          // chunks from the nearest to that one
 };
@@ -346,9 +347,11 @@ __device__ __forceinline__ int wait_for_state(const Recur& r, int chunk, int blo
     return kGaveUp;
 }
 
-// Every wave's part, `distance` the same for all: the maps between are cut into
-// slices, one a wave, all on their way at once; h: the state in front of the chunk.
-template <int kAhead>                          // maps on their way at once
+// Every wave's part, `distance` the same for all: the maps between are fetched
+// kFold at a time by the waves together, and every wave passes the state through
+// them, one after the other from the farthest on.  That is what the chunks
+// themselves do with their states, so the same bits come out whichever chunk's
+// state was known first.  h: the state in front of the chunk.
 __device__ __forceinline__ void front_state(const Recur& r, int chunk, int block, Lookers& s, float* h) {
     const int l = lane_id(), w = threadIdx.x / GS_WAVE, d = s.distance;
     h[0] = h[1] = d == kGaveUp ? NAN : 0.0f;
@@ -356,36 +359,39 @@ __device__ __forceinline__ void front_state(const Recur& r, int chunk, int block
     const int64_t nearest = (int64_t)block * r.chunks + chunk - 1;
     asm volatile("" ::: "memory");             // read behind the flags
     if (w == kWaves - 1) s.state[l] = unpair(r.states[(nearest - d) * GS_WAVE + l]);
-    const int per = (d + kWaves - 1) / kWaves, end = min((w + 1) * per, d);
-    float pm[2] = {1.0f, 1.0f}, pb[2] = {0.0f, 0.0f};
-    for (int k = w * per; k < end; k += kAhead) {
-        uint64_t v[kAhead][2];
+    int far = d;
+    do {
+        constexpr int EACH = kFold / kWaves;
+        const int near = max(far - kFold, 0);
+        uint64_t v[EACH][2];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const uint64_t* p = r.maps + (nearest - min(k + i, end - 1)) * (2 * GS_WAVE) + l;
-            v[i][0] = p[0];
-            v[i][1] = p[GS_WAVE];
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (k + i >= end) break;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const float2 ab = unpair(v[i][c]);
-                pb[c] = fmaf(pm[c], ab.y, pb[c]);
-                pm[c] *= ab.x;
+        for (int i = 0; i < EACH; ++i) {
+            const uint64_t* p = r.maps + (nearest - min(near + w + i * kWaves, max(far - 1, 0))) * (2 * GS_WAVE) + l;
+            if (near + w + i * kWaves < far) {
+                v[i][0] = p[0];
+                v[i][1] = p[GS_WAVE];
             }
         }
-    }
-    s.passed[threadIdx.x] = make_float4(pm[0], pm[1], pb[0], pb[1]);
-    __syncthreads();
-    h[0] = s.state[l].x;
-    h[1] = s.state[l].y;
-    for (int u = min(kWaves, d) - 1; u >= 0; --u) {
-        const float4 v = s.passed[u * GS_WAVE + l];
-        h[0] = fmaf(v.x, h[0], v.z);
-        h[1] = fmaf(v.y, h[1], v.w);
-    }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (near + w + i * kWaves < far) {
+                const float2 a = unpair(v[i][0]), b = unpair(v[i][1]);
+                s.passed[(w + i * kWaves) * GS_WAVE + l] = make_float4(a.x, b.x, a.y, b.y);
+            }
+        __syncthreads();
+        if (far == d) {
+            h[0] = s.state[l].x;
+            h[1] = s.state[l].y;
+        }
+#pragma unroll 2
+        for (int k = far - near - 1; k >= 0; --k) {
+            const float4 m = s.passed[k * GS_WAVE + l];
+            h[0] = fmaf(m.x, h[0], m.z);
+            h[1] = fmaf(m.y, h[1], m.w);
+        }
+        far = near;
+        if (far > 0) __syncthreads();
+    } while (far > 0);
 }
 
 // One wave's part: the state behind the chunk, from the one in front.
@@ -399,15 +405,20 @@ __device__ __forceinline__ void publish_state(const Recur& r, int chunk, int blo
     announce(r.flags + at, kState);
 }
 
-// The next chunk (in the order of the recurrence) and its block of channels; false: none is left.
-__device__ __forceinline__ bool take_chunk(const Recur& r, uint32_t* shared, int& chunk, int& block) {
-    const int32_t all = r.chunks * r.blocks;
-    if (threadIdx.x == 0) *shared = atomicAdd(r.flags + all, 1u);
+// The next chunk of the workgroup's block of channels, in the order of the
+// recurrence.  A counter a block, each on a line of its own: 768 workgroups that
+// start together wait 5 us for one counter.
+constexpr int kCounter = 32;                   // words between the counters
+
+// A workgroup's block of channels: each has as many workgroups as chunks, and they
+// are spread over the XCDs (workgroups go round those in turn; a block on one of
+// them alone took 290 us for the 131,072 tokens that take 212).
+__device__ __forceinline__ int block_of(const Recur& r) { return (int)((blockIdx.x + blockIdx.x / r.blocks) % r.blocks); }
+
+__device__ __forceinline__ int take_chunk(const Recur& r, uint32_t* shared, int block) {
+    if (threadIdx.x == 0) *shared = atomicAdd(r.flags + r.chunks * r.blocks + block * kCounter, 1u);
     __syncthreads();
-    const uint32_t t = __builtin_amdgcn_readfirstlane(*shared);
-    chunk = (int)(t / (uint32_t)r.blocks);
-    block = (int)(t % (uint32_t)r.blocks);
-    return t < (uint32_t)all;
+    return (int)__builtin_amdgcn_readfirstlane(*shared);
 }
 
 // ALONE: the list is one chunk, which looks nowhere; workgroups behind those of
@@ -416,19 +427,22 @@ __device__ __forceinline__ bool take_chunk(const Recur& r, uint32_t* shared, int
 // otherwise where they are used, and 16-bit tokens leave room for three
 // workgroups a unit instead of two.
 template <typename T, bool ONE, bool ALONE, bool SHORT>
-__global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHORT ? (ALONE || sizeof(T) == 2 ? 4 : 2) : sizeof(T) == 4 ? 4 : 6) k_recur(Recur r, RecurOut o) {
+__global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHORT && !ALONE && sizeof(T) == 4 ? 2 : SHORT || sizeof(T) == 4 ? 4 : 6) k_recur(Recur r, RecurOut o) {
     constexpr int WAVES = ALONE ? kAloneWaves : kWaves;
     __shared__ float4 maps[WAVES * GS_WAVE];
     __shared__ Lookers look;
     __shared__ uint32_t anew[WAVES], ticket;
     const gs_recur& a = r.a;
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
-    int chunk = 0, block = blockIdx.x;
+    int chunk = 0, block = ALONE ? blockIdx.x : block_of(r);
     if (ALONE && block >= r.blocks) {
         pass_empty(a, a.initial, o.final, (block - r.blocks) * WAVES + w, (gridDim.x - r.blocks) * WAVES);
         return;
     }
-    if (!ALONE && !take_chunk(r, &ticket, chunk, block)) return;
+    if (!ALONE) {
+        chunk = take_chunk(r, &ticket, block);
+        if (chunk >= r.chunks) return;
+    }
     const uint32_t col = column(a, block, r.width);
     Tokens tk;
     tk.p0 = __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps);
@@ -478,9 +492,9 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
             first_of(i, h);
         }
     };
-    // The wave's map.  A gate is kept in one register and x as it was loaded, so
-    // that three workgroups fit a unit.
-    float S[kSteps][2], m[2] = {1.0f, 1.0f}, h[2] = {0.0f, 0.0f};
+    // The wave's map.  Gates and x stay as they were loaded, so that three
+    // workgroups of 16-bit tokens fit a unit (opened gates: two, 236 us for 214).
+    float m[2] = {1.0f, 1.0f}, h[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         if (bit(tk.starts, i)) {
@@ -490,8 +504,7 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float A, z;
-            S[i][c] = gate_of(gs[i][c]);
-            open(S[i][c], A, z);
+            open(gate_of(gs[i][c]), A, z);
             m[c] *= A;
             h[c] = fmaf(A, h[c], z * xs[i][c]);
         }
@@ -508,7 +521,7 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
             if (l == 0) look.distance = d;
         }
         __syncthreads();
-        front_state<2>(r, chunk, block, look, h);
+        front_state(r, chunk, block, look, h);
         if (w == 0 && !any) publish_state(r, chunk, block, maps, anew, h);
     }
     through(maps, anew, 0, w, l, h);
@@ -521,11 +534,11 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
     for (int i = 0; i < kSteps; ++i) {
         if (bit(tk.starts, i)) start(i, h);
         xs[i].again();
+        gs[i].again();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float A, z;
-            loaded(S[i][c]);
-            open(S[i][c], A, z);
+            open(gate_of(gs[i][c]), A, z);
             h[c] = fmaf(A, h[c], z * xs[i][c]);
         }
         if (bit(written, i)) Two<T, ONE>::store(y.p, col, h[0], h[1]);
@@ -547,12 +560,15 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
     __shared__ uint32_t anew[WAVES], ended[WAVES], ticket;
     const gs_recur& a = r.a;
     const int w = threadIdx.x / GS_WAVE, l = lane_id();
-    int turn = 0, block = blockIdx.x;          // chunks are taken from the last one on
+    int turn = 0, block = ALONE ? blockIdx.x : block_of(r);    // chunks are taken from the last one on
     if (ALONE && block >= r.blocks) {
         pass_empty(a, o.dfinal, o.dinitial, (block - r.blocks) * WAVES + w, (gridDim.x - r.blocks) * WAVES);
         return;
     }
-    if (!ALONE && !take_chunk(r, &ticket, turn, block)) return;
+    if (!ALONE) {
+        turn = take_chunk(r, &ticket, block);
+        if (turn >= r.chunks) return;
+    }
     const int chunk = r.chunks - 1 - turn;
     const uint32_t col = column(a, block, r.width);
     Tokens tk;
@@ -673,7 +689,7 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
     float g[2] = {0.0f, 0.0f};
     if (!ALONE) {
         __syncthreads();
-        front_state<sizeof(T) == 4 ? 1 : 4>(r, turn, block, look, g);
+        front_state(r, turn, block, look, g);
         if (w == kWaves - 1 && !any) publish_state(r, turn, block, back, ended, g);
     }
     through(back, ended, 0, WAVES - 1 - w, l, g);
@@ -740,7 +756,7 @@ RecurPlan recur_plan(int32_t n, int32_t cols) {
     const size_t all = p.chunks <= 1 ? 0 : (size_t)p.chunks * p.blocks;
     p.maps = take(all * GS_WAVE * 16);
     p.states = take(all * GS_WAVE * 8);
-    p.flags = take(all ? (all + 1) * 4 : 0);
+    p.flags = take((all + (all ? (size_t)p.blocks * kCounter : 0)) * 4);
     p.bytes = at;
     return p;
 }
@@ -761,7 +777,7 @@ Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
 
 // Flags cleared for the chunks' workgroups; their number for the only ones'.
 void clear_flags(const Recur& r, const float* from, float* to, hipStream_t st) {
-    const int32_t flags = r.chunks * r.blocks + 1;
+    const int32_t flags = r.chunks * r.blocks + r.blocks * kCounter;
     const uint32_t most = std::max(div_up(flags, GS_BLOCK), to && r.a.cu ? div_up(r.a.n_seg, GS_BLOCK) : 1u);
     k_recur_clear<<<std::min(most, 1024u), GS_BLOCK, 0, st>>>(r.a, from, to, r.flags, flags);
 }
@@ -777,8 +793,10 @@ hipError_t recur_go(const Recur& r, const RecurOut& o, hipStream_t st) {
     } else {
         clear_flags(r, r.a.initial, o.final, st);
         const uint32_t grid = (uint32_t)r.chunks * r.blocks;
-        // a segment in every four tokens: waiting for one state after the other would take longer than all else
-        if (r.a.initial && r.a.n_seg >= r.a.n / 4) k_recur<T, ONE, false, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
+        // A segment in every four tokens: waiting for one state after the other would
+        // take longer than all else.  And states in place are read once, before
+        // anyone can know the segment's last one.
+        if (r.a.initial && (r.a.n_seg >= r.a.n / 4 || r.a.initial == o.final)) k_recur<T, ONE, false, true><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
         else k_recur<T, ONE, false, false><<<grid, kWaves * GS_WAVE, 0, st>>>(r, o);
     }
     return hipGetLastError();

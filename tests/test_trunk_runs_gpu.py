@@ -199,6 +199,29 @@ def test_served_states_in_place(tk, gs):
                 assert torch.equal(y, want.y) and torch.equal(state, want.final), (lengths[:3], turn, reverse)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_recurrence_gives_the_same_bits(tk, dtype):
+    """Whichever chunk's state is known first when another looks back: fp32 states and gradients, call after call, also
+    beside work on another stream that delays some of the workgroups."""
+    g = gen(16)
+    n, cols = 40_000, 300
+    x, gate, dy = (randn(g, n, cols, dtype=dtype) for _ in range(3))
+    gate = (gate.float() + 3).to(dtype)                # states that reach over chunks
+    first = randn(g, 2, cols)
+    cu = starts([0, 7, n])
+    want = tk.recurrence(x, gate, cu=cu, initial=first, keep=True)
+    grads = tk.recurrence_backward(dy, x, gate, want.kept, cu=cu, initial=first, dfinal=first)
+    other, big = torch.cuda.Stream(), randn(g, 4096, 4096)
+    for turn in range(30):
+        if turn % 3:
+            with torch.cuda.stream(other):
+                big.mul_(1.0)
+        got = tk.recurrence(x, gate, cu=cu, initial=first, keep=True)
+        assert same(got, want), turn
+        assert same(tk.recurrence_backward(dy, x, gate, want.kept, cu=cu, initial=first, dfinal=first), grads), turn
+    torch.cuda.synchronize()
+
+
 def test_recurrence_past_two_to_the_31_elements(tk):
     """2,100,000 tokens of 1040 channels: the ends of the list are what they are alone."""
     n, cols, part = 2_100_000, 1040, 4096
