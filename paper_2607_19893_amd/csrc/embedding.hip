@@ -376,6 +376,7 @@ __global__ void __launch_bounds__(kSum) k_embed_sum(EmbedSum a) {
 // slices that are added in ascending order.  Workgroups behind these write zeros
 // to the rows that have no token.
 constexpr int kJoin = 512;
+constexpr int kShort = 64;                     // chunks of a run that a group joins alone
 
 template <typename T, bool TAIL, int G>
 __global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_blocks, int rows_a_block) {
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_block
         for (int i = threadIdx.x; i < items; i += kJoin) {
             const int r = (int)(((float)i + 0.5f) * inv), c = (i - r * pieces) * 4;   // fewer than 2^18 items
             if (a.marks && a.marks[r0 + r]) continue;
-            Span<float, TAIL>::store(a.grad + (r0 + r) * a.ld_grad + c, a.dim - c, none);
+            Span<float, TAIL>::template store<true>(a.grad + (r0 + r) * a.ld_grad + c, a.dim - c, none);
         }
         return;
     }
@@ -412,9 +413,15 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_block
     }
     // a run ends in chunk c if the position behind c is another row's
     auto ends_in = [&](int64_t c, uint32_t row) { return (c + 1) * a.per >= a.n || a.pairs[(c + 1) * a.per].x != row; };
-    const uint64_t lanes = G == GS_WAVE ? ~0ull : ((1ull << G) - 1) << (lane_id() / G * G);
-    const uint64_t ending = __ballot(mine && ends_in(g + 1 + lane, row)) & lanes;
-    const int m = ending ? __ffsll((unsigned long long)ending) - 1 - lane_id() / G * G + 1 : 0;
+    const int lane0 = lane_id() / G * G;
+    const uint64_t lanes = G == GS_WAVE ? ~0ull : ((1ull << G) - 1) << lane0;
+    int m = 0;
+    for (int c = 0; c < kShort; c += G) {
+        const bool looks = mine && m == 0;
+        if (!__any(looks)) break;
+        const uint64_t ending = __ballot(looks && ends_in(g + 1 + c + lane, row)) & lanes;
+        if (looks && ending) m = c + __ffsll((unsigned long long)ending) - lane0;
+    }
     auto add = [&](float* acc, const float* p) {
         float f[N];
         load_floats<N, TAIL>(p + col, 0, there, f);
