@@ -17,9 +17,8 @@ namespace {
 // of up to 128 channels, two a lane, and finds its own map with every gate and token
 // in registers; the maps of a chunk's waves meet in LDS, those of the chunks in
 // global memory.  `reverse` turns the list around (place p is token n - 1 - p).
-// One pass: a chunk publishes its map, looks back over the chunks in front of it
-// to the nearest whose last state is known, publishes its own last state, and
-// goes through its tokens.  Bound by HBM bytes.
+// One pass: a chunk publishes its map, looks back over those in front of it for
+// the state that it starts from, and goes through its tokens.  Bound by HBM bytes.
 // ---------------------------------------------------------------------------
 
 constexpr int kSteps = 16;                     // tokens of a wave
@@ -37,9 +36,11 @@ constexpr uint32_t kStart = 1, kEnd = 2, kOutside = 0xFFFFFFFFu;
 struct Recur {
     gs_recur a;
     uint64_t* maps;                            // [blocks][chunks][2 * 64]: (A, B) of a lane's two channels
-    uint64_t* states;                          // [blocks][chunks][64]: a lane's two states behind the chunk
-    uint32_t* flags;                           // [blocks][chunks]: kMap, then kState; behind them the counters
-    int32_t chunks, blocks, width;             // width: channels of a block
+    uint64_t* group_maps;                      // [blocks][groups][2 * 64]: the same of kGroup chunks
+    uint64_t* states;                          // [blocks][groups][64]: a lane's two states behind the group
+    uint32_t* flags;                           // [blocks][chunks]: kMap or kAnew; [blocks][groups]: kMap, then kState;
+                                               // a counter a block
+    int32_t chunks, groups, blocks, width;     // width: channels of a block
 };
 
 struct RecurOut {
@@ -262,18 +263,27 @@ __device__ __forceinline__ void through(const float4* maps, const uint32_t* anew
 }
 
 // ---------------------------------------------------------------------------
-// Looking back.  The workgroups take chunks from a counter, one after the other, so
-// every chunk that one waits for belongs to a workgroup that is already running
-// and publishes its map before it waits itself: every wait ends.  (Calls that
-// run at the same time on one workspace would clear each other's flags; a wait
-// gives up after kPolls then, with NaN.)  What is published is written past the
-// caches (agent scope), and a flag follows the values it announces.  The values
-// are read through the caches: their lines hold nothing else and nobody reads
-// them before their flag, so no cache can have held them earlier in the kernel.
+// Looking back.  kGroup chunks are a group.  A chunk joins the maps of those in
+// front of it in its group; the last of a group publishes the group's map, and
+// when it knows the state that the group starts from, the state behind it.  The
+// others look for that state over up to 64 groups.  (Chunk by chunk, 64 chunks a
+// look, 400,000 tokens of 128 channels took 324 us: one look after the other.)
+// Maps are joined and states passed on in one order, from the front, so the same
+// bits come out whichever group's state was known first.
+//   The workgroups take chunks from a counter, one after the other, so every chunk
+// that one waits for belongs to a workgroup that is already running, and the
+// first that is not done waits for nobody: every wait ends.  (Calls that run at
+// the same time on one workspace would clear each other's flags; a wait gives up
+// after kPolls then, with NaN.)  What is published is written past the caches
+// (agent scope), and a flag follows the values it announces.  The values are
+// read through the caches: their lines hold nothing else and nobody reads them
+// before their flag, so no cache can have held them earlier in the kernel.
 // ---------------------------------------------------------------------------
 
-constexpr uint32_t kMap = 1, kState = 2;
+constexpr uint32_t kMap = 1, kAnew = 2, kState = 2;
 constexpr int kPolls = 1 << 22;
+constexpr int kPause = 32;                     // between looks (s_sleep): with 1, 3% slower
+constexpr int kGroup = 16;                     // chunks
 
 __device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
 __device__ __forceinline__ float2 unpair(uint64_t v) {
@@ -307,102 +317,176 @@ __device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* an
     return any;
 }
 
-constexpr int kFold = 16;                      // maps that are fetched together
-struct Lookers {                               // in LDS
-    float4 passed[kFold * GS_WAVE];            // maps of chunks in front
-    float2 state[GS_WAVE];                     // behind the chunk that the nearest known state is of
-    int32_t distance;                          // chunks from the nearest to that one
-};
 constexpr int kNotNeeded = -1, kGaveUp = -2;
 
-// One wave's part: publishes the chunk's map, or where a segment starts in the
-// chunk its last state; true then.
-__device__ __forceinline__ bool publish(const Recur& r, int chunk, int block, const float4* own, const uint32_t* anew) {
-    const int l = lane_id();
-    const int64_t at = (int64_t)block * r.chunks + chunk;
+struct Lookers {                               // in LDS
+    float4 fetched[kGroup * GS_WAVE];          // maps: of chunks in the group, then of groups
+    float4 own[GS_WAVE];                       // the chunk's map
+    float4 front[GS_WAVE];                     // the map through the group's chunks in front
+    float2 state[GS_WAVE];                     // behind the group that the nearest known state is of
+    int32_t anew, distance, speaks;            // speaks: the group's map and state are the chunk's to say
+};
+
+__device__ __forceinline__ void put_map(uint64_t* p, const float* m, const float* b) {
+    put(p + lane_id(), pair(m[0], b[0]));
+    put(p + GS_WAVE + lane_id(), pair(m[1], b[1]));
+}
+
+// `count` maps from p on, into LDS by all waves together.
+__device__ __forceinline__ void fetch(const uint64_t* p, int count, float4* to) {
+    constexpr int EACH = kGroup / kWaves;
+    const int l = lane_id(), w = threadIdx.x / GS_WAVE;
+    uint64_t v[EACH][2];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (w + i * kWaves < count) {
+            const uint64_t* q = p + (int64_t)(w + i * kWaves) * (2 * GS_WAVE) + l;
+            v[i][0] = q[0];
+            v[i][1] = q[GS_WAVE];
+        }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (w + i * kWaves < count) {
+            const float2 a = unpair(v[i][0]), b = unpair(v[i][1]);
+            to[(w + i * kWaves) * GS_WAVE + l] = make_float4(a.x, b.x, a.y, b.y);
+        }
+}
+
+// One wave's part: publishes the chunk's map and waits for those in front of it
+// in its group.  In s.anew: the last of them in which a segment starts, -1: none.
+// `needed`: someone reads the state in front of the chunk.
+__device__ __forceinline__ void publish(const Recur& r, int chunk, int block, const float4* own, const uint32_t* starts,
+                                        bool needed, Lookers& s) {
+    const int o = chunk % kGroup, l = lane_id();
+    const int64_t first = (int64_t)block * r.chunks + chunk - o;
     float m[2], b[2];
-    const bool any = whole_map(own, anew, l, m, b);
-    if (any) {
-        put(r.states + at * GS_WAVE + l, pair(b[0], b[1]));
-        announce(r.flags + at, kState);
-    } else {
-        put(r.maps + at * (2 * GS_WAVE) + l, pair(m[0], b[0]));
-        put(r.maps + at * (2 * GS_WAVE) + GS_WAVE + l, pair(m[1], b[1]));
-        announce(r.flags + at, kMap);
+    const bool any = whole_map(own, starts, l, m, b);
+    put_map(r.maps + (first + o) * (2 * GS_WAVE), m, b);
+    announce(r.flags + first + o, any ? kAnew : kMap);
+    if (any && o == kGroup - 1) {
+        const int64_t g = (int64_t)block * r.groups + chunk / kGroup;
+        put(r.states + g * GS_WAVE + l, pair(b[0], b[1]));
+        announce(r.flags + (int64_t)r.chunks * r.blocks + g, kState);
     }
-    return any;
+    s.own[l] = make_float4(m[0], m[1], b[0], b[1]);
+    int from = kNotNeeded - 1;
+    if (needed) {
+        from = kGaveUp - 1;
+        for (int polls = 0; polls < kPolls; ++polls) {
+            const uint32_t f = l < o ? __hip_atomic_load(r.flags + first + l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+            const uint32_t there = (uint32_t)__ballot(f != 0u), anew = (uint32_t)__ballot(f == kAnew);
+            const int p = anew ? 31 - __clz(anew) : -1;
+            const uint32_t front = (1u << o) - 1, known = p < 0 ? 0u : (2u << p) - 1;
+            if ((front & ~known & ~there) == 0) {
+                from = p;
+                break;
+            }
+            __builtin_amdgcn_s_sleep(kPause);
+        }
+    }
+    if (l == 0) {
+        s.anew = from;
+        s.speaks = o == kGroup - 1 && !any;
+    }
 }
 
-// One wave's part: waits until a state is known within the 64 chunks in front and
-// the maps of those between are there; its distance.
-__device__ __forceinline__ int wait_for_state(const Recur& r, int chunk, int block) {
-    const int c = chunk - 1 - lane_id();
-    const uint32_t* flag = r.flags + (int64_t)block * r.chunks + c;
-    for (int polls = 0; polls < kPolls; ++polls) {
-        const uint32_t f = c >= 0 ? __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
-        const uint64_t known = __ballot(f == kState), there = __ballot(f != 0u);
-        if (known && (~there & ((known & -known) - 1)) == 0) return __ffsll((unsigned long long)known) - 1;
-        __builtin_amdgcn_s_sleep(32);          // 1: 219 us for the 131,072 tokens that take 212 with 24 to 64
-    }
-    return kGaveUp;
+// Every wave's part, behind a barrier: the maps of the group's chunks in front,
+// back to the last in which a segment starts.
+__device__ __forceinline__ void fetch_group(const Recur& r, int chunk, int block, Lookers& s) {
+    const int o = chunk % kGroup, from = max(s.anew, 0);
+    asm volatile("" ::: "memory");             // read behind the flags
+    if (s.anew >= -1) fetch(r.maps + ((int64_t)block * r.chunks + chunk - o + from) * (2 * GS_WAVE), o - from, s.fetched);
 }
 
-// Every wave's part, `distance` the same for all: the maps between are fetched
-// kFold at a time by the waves together, and every wave passes the state through
-// them, one after the other from the farthest on.  That is what the chunks
-// themselves do with their states, so the same bits come out whichever chunk's
-// state was known first.  h: the state in front of the chunk.
+// One wave's part, behind another: joins them, says the group's map if the chunk
+// is its last, and waits until a state is known within the 64 groups in front and
+// the maps of those between are there; in s.distance how many those are.
+__device__ __forceinline__ void join_and_wait(const Recur& r, int chunk, int block, Lookers& s) {
+    const int o = chunk % kGroup, l = lane_id(), p = s.anew, from = max(p, 0);
+    float fm[2] = {1.0f, 1.0f}, fb[2] = {0.0f, 0.0f};
+    if (p >= -1) {
+#pragma unroll 2
+        for (int k = 0; k < o - from; ++k) {
+            const float4 v = s.fetched[k * GS_WAVE + l];
+            const bool whole = k == 0 && p >= 0;           // a segment starts in it: its map is the constant b
+            fb[0] = whole ? v.z : fmaf(v.x, fb[0], v.z);
+            fb[1] = whole ? v.w : fmaf(v.y, fb[1], v.w);
+            fm[0] *= v.x;
+            fm[1] *= v.y;
+        }
+        if (s.speaks) {
+            const int64_t g = (int64_t)block * r.groups + chunk / kGroup;
+            uint32_t* flag = r.flags + (int64_t)r.chunks * r.blocks + g;
+            const float4 own = s.own[l];
+            const float gb[2] = {fmaf(own.x, fb[0], own.z), fmaf(own.y, fb[1], own.w)};
+            if (p >= 0) {
+                put(r.states + g * GS_WAVE + l, pair(gb[0], gb[1]));
+                announce(flag, kState);
+            } else {
+                const float gm[2] = {own.x * fm[0], own.y * fm[1]};
+                put_map(r.group_maps + g * (2 * GS_WAVE), gm, gb);
+                announce(flag, kMap);
+            }
+        }
+    }
+    s.front[l] = make_float4(fm[0], fm[1], fb[0], fb[1]);
+    int d = p == kGaveUp - 1 ? kGaveUp : kNotNeeded;
+    if (p == -1) {
+        const int c = chunk / kGroup - 1 - l;
+        const uint32_t* flag = r.flags + (int64_t)r.chunks * r.blocks + (int64_t)block * r.groups + c;
+        d = kGaveUp;
+        for (int polls = 0; polls < kPolls; ++polls) {
+            const uint32_t v = c >= 0 ? __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+            const uint64_t known = __ballot(v == kState), there = __ballot(v != 0u);
+            if (known && (~there & ((known & -known) - 1)) == 0) {
+                d = __ffsll((unsigned long long)known) - 1;
+                break;
+            }
+            __builtin_amdgcn_s_sleep(kPause);
+        }
+    }
+    if (l == 0) s.distance = d;
+}
+
+// Every wave's part, behind a barrier: h, the state in front of the chunk; from
+// the group's last chunk the state behind the group.
 __device__ __forceinline__ void front_state(const Recur& r, int chunk, int block, Lookers& s, float* h) {
     const int l = lane_id(), w = threadIdx.x / GS_WAVE, d = s.distance;
-    h[0] = h[1] = d == kGaveUp ? NAN : 0.0f;
-    if (d < 0) return;
-    const int64_t nearest = (int64_t)block * r.chunks + chunk - 1;
+    if (d < 0) {
+        h[0] = d == kGaveUp ? NAN : s.front[l].z;
+        h[1] = d == kGaveUp ? NAN : s.front[l].w;
+        return;
+    }
+    const int64_t g = (int64_t)block * r.groups + chunk / kGroup;
     asm volatile("" ::: "memory");             // read behind the flags
-    if (w == kWaves - 1) s.state[l] = unpair(r.states[(nearest - d) * GS_WAVE + l]);
+    if (w == kWaves - 1) s.state[l] = unpair(r.states[(g - 1 - d) * GS_WAVE + l]);
+    float q[2] = {0.0f, 0.0f};
     int far = d;
     do {
-        constexpr int EACH = kFold / kWaves;
-        const int near = max(far - kFold, 0);
-        uint64_t v[EACH][2];
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const uint64_t* p = r.maps + (nearest - min(near + w + i * kWaves, max(far - 1, 0))) * (2 * GS_WAVE) + l;
-            if (near + w + i * kWaves < far) {
-                v[i][0] = p[0];
-                v[i][1] = p[GS_WAVE];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (near + w + i * kWaves < far) {
-                const float2 a = unpair(v[i][0]), b = unpair(v[i][1]);
-                s.passed[(w + i * kWaves) * GS_WAVE + l] = make_float4(a.x, b.x, a.y, b.y);
-            }
+        const int count = min(far, kGroup);    // groups g - far .. g - far + count - 1
+        fetch(r.group_maps + (g - far) * (2 * GS_WAVE), count, s.fetched);
         __syncthreads();
         if (far == d) {
-            h[0] = s.state[l].x;
-            h[1] = s.state[l].y;
+            q[0] = s.state[l].x;
+            q[1] = s.state[l].y;
         }
 #pragma unroll 2
-        for (int k = far - near - 1; k >= 0; --k) {
-            const float4 m = s.passed[k * GS_WAVE + l];
-            h[0] = fmaf(m.x, h[0], m.z);
-            h[1] = fmaf(m.y, h[1], m.w);
+        for (int k = 0; k < count; ++k) {
+            const float4 v = s.fetched[k * GS_WAVE + l];
+            q[0] = fmaf(v.x, q[0], v.z);
+            q[1] = fmaf(v.y, q[1], v.w);
         }
-        far = near;
+        far -= count;
         if (far > 0) __syncthreads();
     } while (far > 0);
-}
-
-// One wave's part: the state behind the chunk, from the one in front.
-__device__ __forceinline__ void publish_state(const Recur& r, int chunk, int block, const float4* own, const uint32_t* anew,
-                                              const float* h) {
-    const int l = lane_id();
-    const int64_t at = (int64_t)block * r.chunks + chunk;
-    float m[2], b[2];
-    whole_map(own, anew, l, m, b);
-    put(r.states + at * GS_WAVE + l, pair(fmaf(m[0], h[0], b[0]), fmaf(m[1], h[1], b[1])));
-    announce(r.flags + at, kState);
+    const float4 f = s.front[l];
+    h[0] = fmaf(f.x, q[0], f.z);
+    h[1] = fmaf(f.y, q[1], f.w);
+    if (w != 0 || !s.speaks) return;
+    const float4 own = s.own[l];               // by the group's map, as the groups behind join it
+    put(r.states + g * GS_WAVE + l, pair(fmaf(own.x * f.x, q[0], fmaf(own.x, f.z, own.z)),
+                                         fmaf(own.y * f.y, q[1], fmaf(own.y, f.w, own.w))));
+    announce(r.flags + (int64_t)r.chunks * r.blocks + g, kState);
 }
 
 // The next chunk of the workgroup's block of channels, in the order of the
@@ -416,7 +500,7 @@ constexpr int kCounter = 32;                   // words between the counters
 __device__ __forceinline__ int block_of(const Recur& r) { return (int)((blockIdx.x + blockIdx.x / r.blocks) % r.blocks); }
 
 __device__ __forceinline__ int take_chunk(const Recur& r, uint32_t* shared, int block) {
-    if (threadIdx.x == 0) *shared = atomicAdd(r.flags + r.chunks * r.blocks + block * kCounter, 1u);
+    if (threadIdx.x == 0) *shared = atomicAdd(r.flags + (r.chunks + r.groups) * r.blocks + block * kCounter, 1u);
     __syncthreads();
     return (int)__builtin_amdgcn_readfirstlane(*shared);
 }
@@ -514,15 +598,13 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
     __syncthreads();
     h[0] = h[1] = 0.0f;
     if (!ALONE) {
-        bool any = false;
-        if (w == 0) {
-            any = publish(r, chunk, block, maps, anew);
-            const int d = bit(tk.starts, 0) ? kNotNeeded : wait_for_state(r, chunk, block);
-            if (l == 0) look.distance = d;
-        }
+        if (w == 0) publish(r, chunk, block, maps, anew, !bit(tk.starts, 0), look);
+        __syncthreads();
+        fetch_group(r, chunk, block, look);
+        __syncthreads();
+        if (w == 0) join_and_wait(r, chunk, block, look);
         __syncthreads();
         front_state(r, chunk, block, look, h);
-        if (w == 0 && !any) publish_state(r, chunk, block, maps, anew, h);
     }
     through(maps, anew, 0, w, l, h);
     if (o.kept && tk.p0 % GS_RECUR_KEEP == 0 && tk.p0 < a.n)
@@ -651,11 +733,12 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
         anew[w] = tk.starts != 0;
     }
     __syncthreads();
-    bool any = false;
-    if (!ALONE && w == kWaves - 1) {
-        any = publish(r, turn, block, back, ended);
-        const int d = bit(tk.ends, kSteps - 1) ? kNotNeeded : wait_for_state(r, turn, block);
-        if (l == 0) look.distance = d;
+    if (!ALONE) {
+        if (w == kWaves - 1) publish(r, turn, block, back, ended, !bit(tk.ends, kSteps - 1), look);
+        __syncthreads();
+        fetch_group(r, turn, block, look);
+        __syncthreads();
+        if (w == kWaves - 1) join_and_wait(r, turn, block, look);
     }
     // the states again, from the kept one in front
     h[0] = h[1] = 0.0f;
@@ -690,7 +773,6 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
     if (!ALONE) {
         __syncthreads();
         front_state(r, turn, block, look, g);
-        if (w == kWaves - 1 && !any) publish_state(r, turn, block, back, ended, g);
     }
     through(back, ended, 0, WAVES - 1 - w, l, g);
     if (sizeof(T) == 4) {                      // dy once more: there are no registers to hold it meanwhile
@@ -737,8 +819,8 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
 }
 
 struct RecurPlan {
-    int32_t chunks, blocks, width;
-    size_t maps, states, flags, bytes;
+    int32_t chunks, groups, blocks, width;
+    size_t maps, group_maps, states, flags, bytes;
 };
 
 RecurPlan recur_plan(int32_t n, int32_t cols) {
@@ -753,10 +835,12 @@ RecurPlan recur_plan(int32_t n, int32_t cols) {
         at += align256(bytes);
         return here;
     };
-    const size_t all = p.chunks <= 1 ? 0 : (size_t)p.chunks * p.blocks;
+    p.groups = (int32_t)div_up(p.chunks, kGroup);
+    const size_t many = p.chunks > 1 ? p.blocks : 0, all = many * p.chunks, groups = many * p.groups;
     p.maps = take(all * GS_WAVE * 16);
-    p.states = take(all * GS_WAVE * 8);
-    p.flags = take((all + (all ? (size_t)p.blocks * kCounter : 0)) * 4);
+    p.group_maps = take(groups * GS_WAVE * 16);
+    p.states = take(groups * GS_WAVE * 8);
+    p.flags = take((all + groups + many * kCounter) * 4);
     p.bytes = at;
     return p;
 }
@@ -766,10 +850,12 @@ Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
     Recur r;
     r.a = a;
     r.chunks = p.chunks;
+    r.groups = p.groups;
     r.blocks = p.blocks;
     r.width = p.width;
     const bool alone = p.chunks <= 1;
     r.maps = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.maps);
+    r.group_maps = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.group_maps);
     r.states = alone ? nullptr : reinterpret_cast<uint64_t*>(base + p.states);
     r.flags = alone ? nullptr : reinterpret_cast<uint32_t*>(base + p.flags);
     return r;
@@ -777,7 +863,7 @@ Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
 
 // Flags cleared for the chunks' workgroups; their number for the only ones'.
 void clear_flags(const Recur& r, const float* from, float* to, hipStream_t st) {
-    const int32_t flags = r.chunks * r.blocks + r.blocks * kCounter;
+    const int32_t flags = (r.chunks + r.groups + kCounter) * r.blocks;
     const uint32_t most = std::max(div_up(flags, GS_BLOCK), to && r.a.cu ? div_up(r.a.n_seg, GS_BLOCK) : 1u);
     k_recur_clear<<<std::min(most, 1024u), GS_BLOCK, 0, st>>>(r.a, from, to, r.flags, flags);
 }

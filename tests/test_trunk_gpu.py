@@ -314,6 +314,42 @@ def test_recurrence_backward(tk, name, reverse, dtype):
         assert all(a is None or torch.equal(a, b) for a, b in zip(got, again))
 
 
+# Lists of many chunks: states that reach over all of them, past 64 looks ahead, segments that start at a chunk's or at
+# many chunks' end, next to it and inside.
+LONG = {"one": (9_000, [0]), "few": (9_000, [0, 2047, 2048, 4095, 4097, 6144, 8191]), "a place": (2049, [0, 2048]),
+        "far": (280_000, [0]), "far, few": (280_000, [0, 130, 2048 * 3 - 1, 2048 * 70, 2048 * 70 + 1, 2048 * 136 + 129])}
+
+
+def test_the_long_reference_is_the_short_one():
+    g = torch.Generator().manual_seed(3)
+    x, gate, dy = (torch.randn(60, 3, generator=g) for _ in range(3))
+    for reverse in (False, True):
+        cu = [0, 7, 8, 30, 60]
+        f, (b, e) = ref.recurrence(x, gate, cu, None, reverse), ref.recurrence_bwd(dy, x, gate, cu, None, None, reverse)
+        values, bounds = ref.long_recurrence(x, gate, cu, dy, reverse)
+        for s, t in zip(values + bounds, (f["y"], b[0], b[1], f["By"], e[0], e[1])):
+            assert torch.allclose(s, t, rtol=1e-11, atol=1e-13)
+
+
+@pytest.mark.parametrize("name", list(LONG))
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_recurrence(tk, name, reverse, dtype):
+    n, cu = LONG[name]
+    cu = cu + [n]
+    cols = 3 if n > 10_000 else 130
+    g = gen(17)
+    say(name, reverse, dtype)
+    x, dy = randn(g, n, cols, dtype=dtype), randn(g, n, cols, dtype=dtype)
+    gate = (randn(g, n, cols) + 3 * torch.arange(1, cols + 1, device="cuda").clamp(max=4)).to(dtype)
+    (y, dx, dg), (By, Bx, Bg) = ref.long_recurrence(x, gate, cu, dy, reverse)
+    got = tk.recurrence(x, gate, cu=starts(cu), reverse=reverse, keep=True)
+    within(got.y.cpu(), y, By, "y")
+    a, b, _ = tk.recurrence_backward(dy, x, gate, got.kept, cu=starts(cu), reverse=reverse)
+    within(a.cpu(), dx, Bx, "dx")
+    within(b.cpu(), dg, Bg, "dgate")
+
+
 def test_recurrence_of_equal_segments(tk):
     g = gen(8)
     x, gate = randn(g, 6 * 45, 24), randn(g, 6 * 45, 24)

@@ -148,6 +148,45 @@ def recurrence_bwd(dy, x, gate, cu, initial=None, dfinal=None, reverse=False):
     return (dx, dg, di), (bx + u * dx.abs() + tiny, bg + u * dg.abs() + tiny, bi + 1e-38)
 
 
+def _scan(a, b):
+    """h_t = a_t h_{t-1} + b_t along the first axis in double, by doubling."""
+    a, b = a.clone(), b.clone()
+    d = 1
+    while d < len(a):
+        b[d:] = b[d:] + a[d:] * b[:-d]
+        a[d:] = a[d:] * a[:-d]
+        d *= 2
+    return b
+
+
+def long_recurrence(x, gate, cu, dy, reverse=False):
+    """((y, dx, dgate), bounds) as the two above give them, for lists of which cu's segments hold every token."""
+    a, z, c = _gates(gate)
+    xd, dyd = x.double().cpu(), dy.double().cpu()
+    if reverse:
+        n = len(xd)
+        (y, dx, dg), b = long_recurrence(x.flip(0), gate.flip(0), [n - v for v in cu][::-1], dy.flip(0))
+        return tuple(t.flip(0) for t in (y, dx, dg)), tuple(t.flip(0) for t in b)
+    first = torch.zeros(len(xd), 1, dtype=torch.float64)
+    first[torch.tensor([v for v in cu if v < len(xd)])] = 1
+    last = first.roll(-1, 0)
+    behind = lambda t: t.roll(1, 0) * (1 - first)          # of the token in front
+    ahead = lambda t: t.roll(-1, 0) * (1 - last)
+    A = a * (1 - first)
+    h, size = _scan(A, z * xd), _scan(A, z * xd.abs())
+    far = _scan(A, A * behind(size))
+    back = lambda p, q: _scan(p.flip(0), q.flip(0)).flip(0)
+    P = ahead(a)
+    D, sD = back(P, dyd), back(P, dyd.abs())
+    eD = c * (sD + back(P, P * ahead(sD)))
+    e = behind(h) - xd
+    dx, dg = z * D, a * z * e * D
+    bx = z * (eD + c * D.abs())
+    bg = a * z * (behind(c * (size + far)) * (D.abs() + eD) + e.abs() * eD + c * (behind(h).abs() + xd.abs()) * D.abs())
+    u, tiny = UNIT[x.dtype], TINY[x.dtype]
+    return (h, dx, dg), (c * (size + far) + u * h.abs() + tiny, bx + u * dx.abs() + tiny, bg + u * dg.abs() + tiny)
+
+
 def eight(u):
     """(rows in e4m3, scale bytes) on u's device: exact quotients by the least power of two, one rounding."""
     rows, cols = u.shape
