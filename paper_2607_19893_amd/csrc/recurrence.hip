@@ -629,6 +629,59 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
     }
 }
 
+// Steps of served sequences: a wave walks one segment alone, four tokens' loads on
+// the way at a time; the wave behind the last segment's fills the tokens that are
+// in none.  Bound by the latency of three loads, one after the other (160 steps
+// of 2048 channels in a graph 3.0 us; a chunk, whose waves look for their
+// segments and meet, 11.6).
+template <typename T, bool ONE>
+__global__ void __launch_bounds__(GS_BLOCK) k_recur_step(Recur r, RecurOut o) {
+    constexpr int AHEAD = 4;
+    const gs_recur& a = r.a;
+    const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE);
+    const int s = item / r.blocks, block = item % r.blocks;
+    if (s > a.n_seg) return;
+    const uint32_t col = column(a, block, r.width);
+    Two<float, ONE> first;
+    first.fill(0.0f);
+    const bool outside = s == a.n_seg;
+    if (!outside && a.initial) first.load(a.initial, s, a.cols, col);
+    if (outside) {
+        auto zeros = [&](int32_t t, int32_t end) {
+            for (; t < end; ++t) Two<T, ONE>::store(o.y, t, o.ld_y, col, 0.0f, 0.0f);
+        };
+        if (a.fill && a.cu) {
+            zeros(0, start_of(a, 0));
+            zeros(start_of(a, a.n_seg), a.n);
+        }
+        return;
+    }
+    const int32_t t0 = start_of(a, s), t1 = start_of(a, s + 1);
+    float h[2] = {first[0], first[1]};
+    for (int32_t t = t0; t < t1; t += AHEAD) {
+        Two<T, ONE> gs[AHEAD], xs[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int32_t at = min(t + i, t1 - 1), row = a.reverse ? t0 + t1 - 1 - at : at;
+            gs[i].load(a.gate, row, a.ld_gate, col);
+            xs[i].load(a.x, row, a.ld_x, col);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (t + i >= t1) break;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float A, z;
+                open(gate_of(gs[i][c]), A, z);
+                h[c] = fmaf(A, h[c], z * xs[i][c]);
+                loaded(h[c]);                  // fused with the rounding to fp16, it gives other last bits
+            }
+            Two<T, ONE>::store(o.y, a.reverse ? t0 + t1 - 1 - t - i : t + i, o.ld_y, col, h[0], h[1]);
+        }
+    }
+    if (o.final) Two<float, ONE>::store(o.final, s, a.cols, col, h[0], h[1]);
+}
+
 // Gradient: D_t = dy_t + a_{t+1} D_{t+1} from the last token to the first (dfinal
 // comes in at a segment's last one), c_t = a_t D_t passes on;
 //   dx_t = (1 - a_t) D_t;  dgate_t = a_t (1 - a_t) (h_{t-1} - x_t) D_t;  dinitial = c of the first token.
@@ -872,9 +925,21 @@ uint32_t alone_grid(const Recur& r, const float* to) {
     return r.blocks + (to && r.a.cu ? std::min(div_up(r.a.n_seg, kAloneWaves * GS_WAVE), 256u) : 0u);
 }
 
+// Whether a wave takes a segment: a token each, as far as the sizes tell (a list
+// of more tokens may be one that is being read in beside others' steps, and one
+// wave would walk it), or equal segments of a few.
+bool steps(const Recur& r, const RecurOut& o) {
+    constexpr int32_t kTokens = 1024, kEach = 4;
+    const gs_recur& a = r.a;
+    if (o.kept || (int64_t)(a.n_seg + 1) * r.blocks >= 1 << 24) return false;
+    return a.cu ? a.n <= a.n_seg && a.n <= kTokens : a.n <= (int64_t)a.n_seg * kEach;
+}
+
 template <typename T, bool ONE>
 hipError_t recur_go(const Recur& r, const RecurOut& o, hipStream_t st) {
-    if (r.chunks == 1) {
+    if (steps(r, o)) {
+        k_recur_step<T, ONE><<<div_up((r.a.n_seg + 1) * r.blocks, GS_BLOCK / GS_WAVE), GS_BLOCK, 0, st>>>(r, o);
+    } else if (r.chunks == 1) {
         k_recur<T, ONE, true, true><<<alone_grid(r, o.final), kAloneWaves * GS_WAVE, 0, st>>>(r, o);
     } else {
         clear_flags(r, r.a.initial, o.final, st);

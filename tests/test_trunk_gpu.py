@@ -350,6 +350,44 @@ def test_long_recurrence(tk, name, reverse, dtype):
     within(b.cpu(), dg, Bg, "dgate")
 
 
+STEPS = {  # tokens, segments' starts (a number: that many equal segments)
+    "one": (1, 1), "each one": (300, 300), "each four": (300, 75), "each five": (300, 60), "many": (5000, 5000),
+    "skewed": (251, [0] * 201 + [200] + list(range(201, 252))), "past the ends": (40, [-3] + list(range(0, 37)) + [90] * 5),
+    "outside": (50, [7] * 30 + list(range(8, 30)) + [31]), "none": (20, [20] * 41), "in front": (20, [0] * 41),
+}
+
+
+@pytest.mark.parametrize("name", list(STEPS))
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("cols", [1, 2, 131, 600])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_steps(tk, gs, name, reverse, cols, dtype):
+    """Many segments of few tokens: from strided tokens, states in place, tokens outside left alone or zeros."""
+    n, cu = STEPS[name]
+    segments = cu if isinstance(cu, int) else len(cu) - 1
+    g = gen(19)
+    say(name, reverse, cols, dtype)
+    x, gate = randn(g, n, cols + 3, dtype=dtype)[:, 1:cols + 1], randn(g, n, 2 * cols, dtype=dtype)[:, cols:]
+    initial = randn(g, segments, cols)
+    at = list(range(0, n + 1, n // segments)) if isinstance(cu, int) else cu
+    kw = dict(n_seg=cu) if isinstance(cu, int) else dict(cu=starts(cu))
+    want = ref.recurrence(x, gate, at, initial, reverse)
+    got = tk.recurrence(x, gate, initial=initial, reverse=reverse, **kw)
+    within(got.y.cpu(), want["y"], want["By"], "y")
+    within(got.final.cpu(), want["final"], want["Bfinal"], "final")
+    state, y = initial.clone(), torch.full((n, cols), 7.0, dtype=dtype, device="cuda")
+    r = gs.make_recur(x, gate, None if isinstance(cu, int) else starts(cu), n_seg=segments, initial=state, reverse=reverse)
+    ws = torch.empty(max(1, gs.gs_recurrence_ws_bytes(r)), dtype=torch.uint8, device="cuda")
+    gs.gs_recurrence(r, y, state, ws=ws)
+    inside = torch.zeros(n, dtype=torch.bool, device="cuda")
+    inside[min(max(at[0], 0), n):min(max(at[-1], 0), n)] = True
+    assert torch.equal(state, got.final) and torch.equal(y[inside], got.y[inside])
+    assert bool((y[~inside] == 7.0).all()) and bool((got.y[~inside] == 0).all())
+    if name != "skewed":                                   # a segment longer than a wave's tokens is joined from maps
+        assert torch.equal(tk.recurrence(x, gate, reverse=reverse, **kw).y,
+                           tk.recurrence(x, gate, reverse=reverse, keep=True, **kw).y)
+
+
 def test_recurrence_of_equal_segments(tk):
     g = gen(8)
     x, gate = randn(g, 6 * 45, 24), randn(g, 6 * 45, 24)
