@@ -771,6 +771,8 @@ def gs_recurrence_ws_bytes(recur: gs_recur) -> int:
 
 def gs_recurrence(recur: gs_recur, y, final=None, kept=None, ws=None, stream=None):
     n, cols = y.shape
+    if token_dtype(y) != recur.dtype:
+        raise ValueError("y has x's type")
     _states(final, (recur.n_seg, cols), "final")
     _states(kept, (-(-n // GS_RECUR_KEEP), cols), "kept")
     p, nb = _ws(ws)

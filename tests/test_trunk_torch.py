@@ -179,7 +179,7 @@ def test_a_call_runs_on_its_tensors_device(monkeypatch):
         tokens.layer_norm(x, torch.zeros(64))
 
 
-@pytest.mark.parametrize("what", ["ids", "cu", "initial", "kept", "types", "u8"])
+@pytest.mark.parametrize("what", ["ids", "cu", "initial", "kept", "types", "y", "u8"])
 def test_tensors_that_do_not_fit_are_refused(monkeypatch, what):
     """By the binding, before the library is called."""
     from paper_2607_19893_amd import gsmi
@@ -190,6 +190,7 @@ def test_tensors_that_do_not_fit_are_refused(monkeypatch, what):
         "initial": lambda: gsmi.make_recur(x, x, None, 2, torch.zeros(1, 8)),
         "kept": lambda: gsmi.gs_recurrence(gsmi.make_recur(x, x), x, None, torch.zeros(1, 8)),
         "types": lambda: gsmi.make_recur(x, x.half()),
+        "y": lambda: gsmi.gs_recurrence(gsmi.make_recur(x, x), x.half()),
         "u8": lambda: gsmi.gs_gated_silu(x, None, x, torch.zeros(70, 8), torch.zeros(70, 1)),
     }
     with pytest.raises(ValueError):
