@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(TPR > GS_BLOCK ? TPR : GS_BLOCK) k_layer_norm_
         }
         ss = row_sum<TPR>(ss, part);
         gs = row_sum<TPR>(gs, part);
-        const float r = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+        // a row past the end adds 0, with eps 0 too
+        const float r = cols ? 1.0f / sqrtf(ss / (float)a.cols + a.eps) : 0.0f;
         const float gn = gs * r * inv;                     // mean of g n
         T* dx = static_cast<T*>(a.dx) + row * a.ld_dx;
 #pragma unroll

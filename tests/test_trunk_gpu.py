@@ -100,6 +100,19 @@ def test_layer_norm_backward(tk, rows, cols, dtype):
         assert all(torch.equal(a, b) for a, b in zip(again, got))
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 24), (5, 128), (3, 250), (7, 500), (5, 700), (2, 1400), (3, 2000), (2, 3000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer_norm_without_epsilon(tk, rows, cols, dtype):
+    """The rows that share a wave with the last ones, or lie behind them, add nothing to the weights' gradients."""
+    g = gen(23)
+    x, dy, w, b = randn(g, rows, cols, dtype=dtype), randn(g, rows, cols, dtype=dtype), randn(g, cols), randn(g, cols)
+    want, _, bound = ref.layer(x, w, b, 0.0)
+    within(tk.layer_norm(x, w, b, 0.0).y, want, bound, "y")
+    grads, bounds = ref.layer_bwd(dy, x, w, 0.0)
+    for got, v, e, what in zip(tk.layer_norm_backward(dy, x, w, 0.0), grads, bounds, ("dx", "dweight", "dbias")):
+        within(got, v, e, what)
+
+
 def test_layer_norm_backward_of_no_rows(tk):
     z = torch.zeros(0, 96, device="cuda")
     dx, dw, db = tk.layer_norm_backward(z, z, torch.ones(96, device="cuda"))
