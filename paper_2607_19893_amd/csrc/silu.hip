@@ -13,7 +13,9 @@ namespace {
 // quad one block of GS_KEEP_BLOCK columns: its scale is the power of two 2^k,
 // k the least with max|u| <= 448 2^k, so u / 2^k is exact in fp32 and the one
 // rounding is that to e4m3.  Bound by HBM bytes: 8 and 1/16 an element of two
-// 16-bit inputs, forward and (with h again) 10 and 1/16 on the way back.
+// 16-bit inputs, forward and (with h again) 10 and 1/16 on the way back.  40,000
+// rows of 2048 bf16 columns: 118 us and 142, 5.6 and 5.8 TB/s (some of it stays in
+// the last-level cache).
 // ---------------------------------------------------------------------------
 
 constexpr int kCols = 8;                       // of a thread
