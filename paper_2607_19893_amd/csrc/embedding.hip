@@ -89,8 +89,11 @@ __global__ void __launch_bounds__(GS_BLOCK) k_embedding(gs_embed_args a, int tok
 
 constexpr int kMostBits = 11;
 constexpr int kMostBins = 1 << kMostBits;
-constexpr int kFew = 4, kMany = 16;            // sorted items of a thread
-constexpr int32_t kManyFrom = 1 << 20;         // tokens from which a thread takes many: fewer blocks to scan
+// Sorted items of a thread.  Few fill the units sooner, many leave fewer blocks to
+// scan: 300,000 tokens of 8 take 49 us with 4 and 61 with 16, 2^20 the same, four
+// million 252 and 197.
+constexpr int kFew = 4, kMany = 16;
+constexpr int32_t kManyFrom = 1 << 20;
 
 struct SortPass {
     const int32_t* ids;                        // the first pass reads these,

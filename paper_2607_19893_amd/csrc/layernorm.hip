@@ -246,6 +246,8 @@ __global__ void __launch_bounds__(1024) k_layer_join(const float* __restrict__ p
     }
 }
 
+// Lanes of a row and their registers by the width: as few as hold it.  46,332 fp16
+// rows of 390 columns take 25 us with 32 lanes of 16, 40 with 64 of 16.
 template <typename T, bool TAIL>
 hipError_t layer_go(const gs_layer_args& a, hipStream_t st) {
     constexpr int N = Piece<T>::N, NARROW = 128 / N;       // lanes that hold 128 columns
