@@ -170,7 +170,7 @@ using global = __attribute__((address_space(1))) P;
 
 // A lane's two channels of a row, at any alignment of an element, as floats.
 // The row is the same for the wave: an address is a scalar and the lane's
-// column.  ONE: there is one channel in all.
+// column.  ONE: a lane has one channel.
 template <typename T, bool ONE>
 struct Two {
     typedef T vec __attribute__((ext_vector_type(2)));
@@ -231,9 +231,12 @@ struct Rows {
 };
 
 // A lane's first channel.  Lanes past the block's or the row's end take its last
-// two once more, and write the same values there: no lane is ever left out.
+// two (ONE: its last) once more, and write the same values there: no lane is
+// ever left out.
+template <bool ONE>
 __device__ __forceinline__ uint32_t column(const gs_recur& a, int block, int width) {
-    return (uint32_t)max(0, min(block * width + min(2 * lane_id(), width - 2), a.cols - 2));
+    if (ONE) return (uint32_t)min(lane_id(), a.cols - 1);
+    return (uint32_t)min(block * width + min(2 * lane_id(), width - 2), a.cols - 2);
 }
 
 // A gate in one register: the smaller of a and 1 - a, t / (1 + t) with t =
@@ -531,7 +534,7 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
         chunk = take_chunk(r, &ticket, block);
         if (chunk >= r.chunks) return;
     }
-    const uint32_t col = column(a, block, r.width);
+    const uint32_t col = column<ONE>(a, block, r.width);
     Tokens tk;
     tk.p0 = __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps);
     Two<T, ONE> gs[kSteps], xs[kSteps];
@@ -645,7 +648,7 @@ __global__ void __launch_bounds__(GS_BLOCK) k_recur_step(Recur r, RecurOut o) {
     const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * (GS_BLOCK / GS_WAVE) + threadIdx.x / GS_WAVE);
     const int s = item / r.blocks, block = item % r.blocks;
     if (s > a.n_seg) return;
-    const uint32_t col = column(a, block, r.width);
+    const uint32_t col = column<ONE>(a, block, r.width);
     Two<float, ONE> first;
     first.fill(0.0f);
     const bool outside = s == a.n_seg;
@@ -710,7 +713,7 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
         if (turn >= r.chunks) return;
     }
     const int chunk = r.chunks - 1 - turn;
-    const uint32_t col = column(a, block, r.width);
+    const uint32_t col = column<ONE>(a, block, r.width);
     Tokens tk;
     tk.p0 = __builtin_amdgcn_readfirstlane(chunk * kChunk + w * kSteps);
     Two<T, ONE> gs[kSteps], xs[kSteps], ds[kSteps];
@@ -978,12 +981,12 @@ hipError_t no_tokens(const gs_recur& a, const float* from, float* to, hipStream_
 
 template <typename T>
 hipError_t recur_type(const Recur& r, const RecurOut& o, hipStream_t st) {
-    return r.a.cols == 1 ? recur_go<T, true>(r, o, st) : recur_go<T, false>(r, o, st);
+    return r.a.cols <= GS_WAVE ? recur_go<T, true>(r, o, st) : recur_go<T, false>(r, o, st);
 }
 
 template <typename T>
 hipError_t recur_bwd_type(const Recur& r, const gs_recur_grads& g, hipStream_t st) {
-    return r.a.cols == 1 ? recur_bwd_go<T, true>(r, g, st) : recur_bwd_go<T, false>(r, g, st);
+    return r.a.cols <= GS_WAVE ? recur_bwd_go<T, true>(r, g, st) : recur_bwd_go<T, false>(r, g, st);
 }
 
 }  // namespace
