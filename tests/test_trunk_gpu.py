@@ -488,6 +488,39 @@ def test_nan_stays_in_its_channel_and_segment(tk, reverse):
     assert torch.equal(dx[:, keep], grads[0][:, keep]) and torch.equal(dg[:, keep], grads[1][:, keep])
 
 
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", [F32, HF])
+def test_nan_stays_in_its_channel_and_segment_of_long_lists(tk, reverse, dtype):
+    """Segments of many chunks that start inside one, at its end and at that of many."""
+    g = gen(29)
+    n, cols = 40_000, 70
+    cu = [0, 2048 * 3, 2048 * 7 + 128, 2048 * 9 - 5, n]
+    x, gate, dy = (randn(g, n, cols, dtype=dtype) for _ in range(3))
+    gate = gate + 8
+    clean = tk.recurrence(x, gate, cu=starts(cu), reverse=reverse, keep=True)
+    grads = tk.recurrence_backward(dy, x, gate, clean.kept, cu=starts(cu), reverse=reverse)
+    bad = torch.zeros(n, cols, dtype=torch.bool, device="cuda")
+    x2, gate2, dy2 = x.clone(), gate.clone(), dy.clone()
+    for s, (t, c) in enumerate([(5000, 3), (2048 * 4 + 1, 64), (2048 * 8, 3), (20_000, 69)]):
+        (x2 if s % 2 else gate2)[t, c] = math.nan
+        dy2[t, c + 1 - 2 * (c == 69)] = math.nan
+        if reverse:
+            bad[cu[s]:t + 1, c] = True
+        else:
+            bad[t:cu[s + 1], c] = True
+    got = tk.recurrence(x2, gate2, cu=starts(cu), reverse=reverse, keep=True)
+    assert torch.equal(got.y.isnan(), bad) and torch.equal(got.y[~bad], clean.y[~bad])
+    dx, dg, _ = tk.recurrence_backward(dy2, x, gate, clean.kept, cu=starts(cu), reverse=reverse)
+    bad[:] = False
+    for s, (t, c) in enumerate([(5000, 4), (2048 * 4 + 1, 65), (2048 * 8, 4), (20_000, 68)]):
+        if reverse:
+            bad[t:cu[s + 1], c] = True
+        else:
+            bad[cu[s]:t + 1, c] = True
+    assert torch.equal(dx.isnan(), bad) and torch.equal(dg.isnan(), bad)
+    assert torch.equal(dx[~bad], grads[0][~bad]) and torch.equal(dg[~bad], grads[1][~bad])
+
+
 def test_gates_at_the_ends(tk):
     """Gates that hold or drop the state entirely, and very large ones."""
     x = torch.arange(1, 301, device="cuda", dtype=F32)[:, None].repeat(1, 6).contiguous()

@@ -267,6 +267,24 @@ def test_lookup_and_gate_past_two_to_the_31_elements(tk):
     assert bool((grad[[0, 1, 2, 4]] == 0).all())
 
 
+def test_layer_norm_gradient_past_two_to_the_31_elements(tk):
+    g = gen(10)
+    rows, cols = 2_200_000, 1000
+    x = torch.empty(rows, cols, dtype=BF, device="cuda").normal_(generator=g)
+    dy = torch.empty(rows, cols, dtype=BF, device="cuda").normal_(generator=g)
+    w = randn(g, cols)
+    dx, dw, db = tk.layer_norm_backward(dy, x, w, dtotal=x)
+    assert torch.equal(dx[-300:], tk.layer_norm_backward(dy[-300:], x[-300:], w, dtotal=x[-300:])[0])
+    want, size, wb, sb = (torch.zeros(cols, dtype=torch.float64, device="cuda") for _ in range(4))
+    for a, b in zip(x.split(100_000), dy.split(100_000)):
+        s, d = a.double(), b.double()
+        n = (s - s.mean(1, keepdim=True)) / torch.sqrt(s.var(1, unbiased=False, keepdim=True) + 1e-5)
+        want, size, wb, sb = want + (d * n).sum(0), size + (d * n).abs().sum(0), wb + d.sum(0), sb + d.abs().sum(0)
+    # a workgroup's rows one after the other, then the partial rows; n's own roundings
+    walk = (rows / 512 + 200) * ref.F
+    assert bool(((dw.double() - want).abs() <= walk * size).all()) and bool(((db.double() - wb).abs() <= walk * sb).all())
+
+
 def test_a_wait_that_nobody_ends_is_not_reached(tk):
     """Lists whose chunks outnumber what the card holds at once: every chunk finds its state."""
     g = gen(9)
