@@ -94,6 +94,9 @@ constexpr int kMostBins = 1 << kMostBits;
 // million 252 and 197.
 constexpr int kFew = 4, kMany = 16;
 constexpr int32_t kManyFrom = 1 << 20;
+// At most, of the only block's threads, which needs one launch a pass: 2000 tokens
+// take 22 us with 8 and 28 in blocks of 4, 4000 30 with 16 and 28.
+constexpr int kAlone = 8;
 
 struct SortPass {
     const int32_t* ids;                        // the first pass reads these,
@@ -508,9 +511,8 @@ EmbedPlan embed_plan(int32_t n, int32_t rows, int32_t dim, int32_t size, bool to
     while (p.bits < 31 && (uint32_t)rows >> p.bits) ++p.bits;              // of the key `rows`
     p.passes = (p.bits + kMostBits - 1) / kMostBits;
     p.digit = (p.bits + p.passes - 1) / p.passes;
-    // one block takes up to kMany items a thread; more blocks of few do better
-    p.many = n <= GS_BLOCK * kMany || n >= kManyFrom;
-    p.blocks = (int32_t)div_up(n, GS_BLOCK * (p.many ? kMany : kFew));
+    p.many = n >= kManyFrom;
+    p.blocks = n <= GS_BLOCK * kAlone ? 1 : (int32_t)div_up(n, GS_BLOCK * (p.many ? kMany : kFew));
     // chunks as long as leaves 1024 waves: longer ones have fewer ends that others share
     const int elements = 16 / size, lanes = chunk_lanes(dim, elements);
     const int64_t waves = (int64_t)n * lanes / GS_WAVE * div_up(dim, lanes * elements);
@@ -563,7 +565,8 @@ hipError_t sum_type(const EmbedSum& a, int zero_blocks, int rows_a_block, hipStr
 
 void sort_pass(const SortPass& q, bool many, hipStream_t st) {
     if (q.blocks == 1) {
-        k_sort_scatter<kMany, true><<<1, GS_BLOCK, 0, st>>>(q);
+        if (q.n <= GS_BLOCK * kFew) k_sort_scatter<kFew, true><<<1, GS_BLOCK, 0, st>>>(q);
+        else k_sort_scatter<kAlone, true><<<1, GS_BLOCK, 0, st>>>(q);
         return;
     }
     if (many) k_sort_count<kMany><<<q.blocks, GS_BLOCK, 0, st>>>(q);

@@ -191,7 +191,8 @@ GRADS = [  # tokens, rows, dim, ids
     (1, 1, 1, "any"), (1, 100, 8, "any"), (33, 5, 16, "any"), (31, 5, 12, "one"), (100, 1000, 7, "any"),
     (4096, 300, 40, "any"), (4097, 300, 24, "any"), (5000, 1, 64, "any"), (20000, 50, 33, "few"), (9000, 9000, 8, "each"),
     (30000, 2000, 128, "few"), (3000, 1 << 20, 8, "any"), (8000, 1500000, 4, "any"), (700, 40, 1000, "any"),
-    (300, 9, 4104, "any"), (64, 1023, 256, "any"), (64, 1024, 256, "any"), (6000, 1025, 20, "runs"), (2000, 64, 96, "none")]
+    (300, 9, 4104, "any"), (64, 1023, 256, "any"), (64, 1024, 256, "any"), (6000, 1025, 20, "runs"), (2000, 64, 96, "none"),
+    (1024, 5000, 8, "any"), (1025, 5000, 8, "any"), (2048, 70_000, 8, "runs"), (2049, 5000, 12, "any"), ((1 << 20) + 3, 3000, 8, "few")]
 
 
 @pytest.mark.parametrize("tokens,rows,dim,how", GRADS)
