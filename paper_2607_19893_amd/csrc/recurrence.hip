@@ -283,7 +283,8 @@ __device__ __forceinline__ void through(const float4* maps, const uint32_t* anew
 // the same time on one workspace would clear each other's flags; a wait gives up
 // after kPolls then, with NaN.)  What is published is written past the caches
 // (agent scope), and a flag follows the values it announces.  The values are
-// read through the caches: their lines hold nothing else and nobody reads them
+// read through the caches: their lines hold nothing else (maps and states start
+// at multiples of kLine, wherever the workspace does) and nobody reads them
 // before their flag, so no cache can have held them earlier in the kernel.
 // ---------------------------------------------------------------------------
 
@@ -291,6 +292,8 @@ constexpr uint32_t kMap = 1, kAnew = 2, kState = 2;
 constexpr int kPolls = 1 << 22;
 constexpr int kPause = 32;                     // between looks (s_sleep): with 1, 3% slower
 constexpr int kGroup = 16;                     // chunks
+constexpr size_t kLine = 256;                  // bytes; a cache line is 128
+static_assert(GS_WAVE * sizeof(uint64_t) % 128 == 0, "no two chunks' maps or groups' states share a line");
 
 __device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
 __device__ __forceinline__ float2 unpair(uint64_t v) {
@@ -902,12 +905,12 @@ RecurPlan recur_plan(int32_t n, int32_t cols) {
     p.group_maps = take(groups * GS_WAVE * 16);
     p.states = take(groups * GS_WAVE * 8);
     p.flags = take((all + groups + many * kCounter) * 4);
-    p.bytes = at;
+    p.bytes = at > 0 ? at + kLine - 16 : 0;    // from the first multiple of kLine in a 16-byte aligned workspace
     return p;
 }
 
 Recur recur_of(const gs_recur& a, const RecurPlan& p, void* ws) {
-    char* base = static_cast<char*>(ws);
+    char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ws) + kLine - 1) & ~(uintptr_t)(kLine - 1));
     Recur r;
     r.a = a;
     r.chunks = p.chunks;
