@@ -857,7 +857,9 @@ gs_status gs_attention_bwd(const gs_attn* a, const gs_attn_grads* g, void* ws, s
  *     NULL: s = x; total or y NULL: not written.  total may be x or residual
  *     itself, y may be x (the same rows, not shifted ones).
  *   weight [cols] fp32; bias [cols] fp32 or NULL (0)
- * A NaN or infinity in x or residual makes its row's y NaN.
+ * A NaN or infinity in x or residual makes its row's y NaN, and so does a row
+ * whose sum, or a difference from whose mean, is past fp32's range.  The
+ * differences themselves may be anything: their squares need not fit.
  * Errors: GS_ERR_INVALID_ARG (null pointers, sizes below 0, a row stride below
  * cols, pointers that are not a multiple of the element size, eps negative or
  * not finite, nothing to write); GS_ERR_UNSUPPORTED for cols above

@@ -18,6 +18,21 @@ namespace {
 // alignment of an element, so an odd width costs nothing; a copy runs at 4.8).
 // ---------------------------------------------------------------------------
 
+// Rows whose squares leave fp32's range (differences of 2^57 and more; or, with
+// next to no eps, of 2^-40 and less): their sums are taken over the differences
+// times a power of two, and 1/sqrt(mean + eps) is that power times the root of
+// what they sum to.  1 for any other row; fp16 reaches neither end.
+template <typename T>
+__device__ __forceinline__ float fitting(float ss, float eps) {
+    if (sizeof(T) == 2 && !__is_same(T, bf16_t)) return 1.0f;
+    return ss == INFINITY ? 0x1p-72f : ss < 0x1p-80f && eps < 0x1p-100f ? 0x1p100f : 1.0f;
+}
+
+// NaN where even the differences are infinite.
+__device__ __forceinline__ float root(float ss, int cols, float eps, float k) {
+    return ss == INFINITY ? NAN : 1.0f / sqrtf(ss / (float)cols + eps * k * k);
+}
+
 template <typename T, bool TAIL, int TPR, int E>
 __global__ void __launch_bounds__(GS_BLOCK) k_layer_norm(gs_layer_args a) {
     constexpr int N = Piece<T>::N, CH = E / N, RPB = GS_BLOCK / TPR;
@@ -83,7 +98,16 @@ __global__ void __launch_bounds__(GS_BLOCK) k_layer_norm(gs_layer_args a) {
         }
     }
     ss = row_sum<TPR>(ss, part);
-    const float rho = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
+    const float k = fitting<T>(ss, a.eps);
+    if (__any(k != 1.0f)) {                    // the same for all waves of a row
+        ss = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < N; ++i) ss = fmaf(s[c][i] * k, s[c][i] * k, ss);
+        ss = row_sum<TPR>(ss, part);
+    }
+    const float rho = k * root(ss, a.cols, a.eps, k);
     T* __restrict__ o = static_cast<T*>(a.y) + row * a.ld_y;
     if (a.y)
 #pragma unroll
@@ -191,9 +215,23 @@ __global__ void __launch_bounds__(TPR > GS_BLOCK ? TPR : GS_BLOCK) k_layer_norm_
         }
         ss = row_sum<TPR>(ss, part);
         gs = row_sum<TPR>(gs, part);
+        const float k = fitting<T>(ss, a.eps);
+        if (__any(k != 1.0f)) {
+            ss = gs = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    ss = fmaf(s[c][i] * k, s[c][i] * k, ss);
+                    gs = fmaf(s[c][i] * k * g[c][i], w[c][i], gs);         // g w of above would be held until here
+                }
+            ss = row_sum<TPR>(ss, part);
+            gs = row_sum<TPR>(gs, part);
+        }
         // a row past the end adds 0, with eps 0 too
-        const float r = cols ? 1.0f / sqrtf(ss / (float)a.cols + a.eps) : 0.0f;
+        float r = cols ? root(ss, a.cols, a.eps, k) : 0.0f;
         const float gn = gs * r * inv;                     // mean of g n
+        r *= k;
         T* dx = static_cast<T*>(a.dx) + row * a.ld_dx;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
