@@ -995,7 +995,9 @@ gs_status gs_embedding_bwd(const gs_embed_bwd_args* args, void* ws, size_t ws_by
  *     time (on two streams) need a workspace each.
  * A segment of one token is a step of a served sequence.  The tokens are taken in
  * an order that the sizes alone fix: the same call gives the same bits.  A NaN
- * or infinity stays in its channel and segment, from its token on.
+ * or infinity stays in its channel and segment, from its token on; an infinite
+ * state stays infinite while the gates are above -80, and so does an infinite
+ * gradient on its way back.
  * Errors: GS_ERR_INVALID_ARG (null pointers, sizes, strides, alignment, dtype,
  * n_seg that does not divide n without cu); GS_ERR_UNSUPPORTED (n above 2^30,
  * n_seg above 2^28, or n / 128 * cols / 128 near 2^22 and above);

@@ -253,6 +253,14 @@ __device__ __forceinline__ void open(float gate, float& a, float& z) {
     z = low ? big : small;
 }
 
+// A product of gates of which `least` is the smallest.  It may have run to 0 though
+// no gate is 0: then it is the least number, so that an infinite state stays
+// infinite (0 * inf is NaN), as it does token by token.  What a finite state
+// leaves behind so, 2^-149 of it, is at the end of fp32's range as well.
+__device__ __forceinline__ float product(float m, float least) { return fmaxf(m, fminf(least, 1.40129846e-45f)); }
+// of two runs' products
+__device__ __forceinline__ float behind(float m, float a) { return product(m * a, fminf(m, a)); }
+
 __device__ __forceinline__ bool bit(uint32_t mask, int i) { return (mask >> i & 1u) != 0; }
 
 // The state that a chunk's earlier waves leave, from the one in front of wave `from`.
@@ -308,6 +316,7 @@ __device__ __forceinline__ void announce(uint32_t* flag, uint32_t what) {
 
 // The chunk's own map, from those of its waves; true: a segment starts (ends) in it.
 __device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* anew, int lane, float* m, float* b) {
+    float least[2] = {1.0f, 1.0f};
     m[0] = m[1] = 1.0f;
     b[0] = b[1] = 0.0f;
     bool any = false;
@@ -323,7 +332,11 @@ __device__ __forceinline__ bool whole_map(const float4* maps, const uint32_t* an
         }
         m[0] *= v.x;
         m[1] *= v.y;
+        least[0] = fminf(least[0], v.x);
+        least[1] = fminf(least[1], v.y);
     }
+    m[0] = product(m[0], least[0]);
+    m[1] = product(m[1], least[1]);
     return any;
 }
 
@@ -413,7 +426,7 @@ __device__ __forceinline__ void fetch_group(const Recur& r, int chunk, int block
 // the maps of those between are there; in s.distance how many those are.
 __device__ __forceinline__ void join_and_wait(const Recur& r, int chunk, int block, Lookers& s) {
     const int o = chunk % kGroup, l = lane_id(), p = s.anew, from = max(p, 0);
-    float fm[2] = {1.0f, 1.0f}, fb[2] = {0.0f, 0.0f};
+    float fm[2] = {1.0f, 1.0f}, fb[2] = {0.0f, 0.0f}, least[2] = {1.0f, 1.0f};
     if (p >= -1) {
 #pragma unroll 2
         for (int k = 0; k < o - from; ++k) {
@@ -423,7 +436,11 @@ __device__ __forceinline__ void join_and_wait(const Recur& r, int chunk, int blo
             fb[1] = whole ? v.w : fmaf(v.y, fb[1], v.w);
             fm[0] *= v.x;
             fm[1] *= v.y;
+            least[0] = fminf(least[0], v.x);
+            least[1] = fminf(least[1], v.y);
         }
+        fm[0] = product(fm[0], least[0]);
+        fm[1] = product(fm[1], least[1]);
         if (s.speaks) {
             const int64_t g = (int64_t)block * r.groups + chunk / kGroup;
             uint32_t* flag = r.flags + (int64_t)r.chunks * r.blocks + g;
@@ -433,7 +450,7 @@ __device__ __forceinline__ void join_and_wait(const Recur& r, int chunk, int blo
                 put(r.states + g * GS_WAVE + l, pair(gb[0], gb[1]));
                 announce(flag, kState);
             } else {
-                const float gm[2] = {own.x * fm[0], own.y * fm[1]};
+                const float gm[2] = {behind(fm[0], own.x), behind(fm[1], own.y)};
                 put_map(r.group_maps + g * (2 * GS_WAVE), gm, gb);
                 announce(flag, kMap);
             }
@@ -494,8 +511,8 @@ __device__ __forceinline__ void front_state(const Recur& r, int chunk, int block
     h[1] = fmaf(f.y, q[1], f.w);
     if (w != 0 || !s.speaks) return;
     const float4 own = s.own[l];               // by the group's map, as the groups behind join it
-    put(r.states + g * GS_WAVE + l, pair(fmaf(own.x * f.x, q[0], fmaf(own.x, f.z, own.z)),
-                                         fmaf(own.y * f.y, q[1], fmaf(own.y, f.w, own.w))));
+    put(r.states + g * GS_WAVE + l, pair(fmaf(behind(f.x, own.x), q[0], fmaf(own.x, f.z, own.z)),
+                                         fmaf(behind(f.y, own.y), q[1], fmaf(own.y, f.w, own.w))));
     announce(r.flags + (int64_t)r.chunks * r.blocks + g, kState);
 }
 
@@ -602,6 +619,18 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, SHOR
             m[c] *= A;
             h[c] = fmaf(A, h[c], z * xs[i][c]);
         }
+    }
+    if (!tk.starts && __any(m[0] == 0.0f || m[1] == 0.0f)) {   // which gates it ran through
+        m[0] = m[1] = 1.0f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                gs[i].again();
+                float A, z;
+                open(gate_of(gs[i][c]), A, z);
+                m[c] = behind(m[c], A);
+            }
     }
     maps[w * GS_WAVE + l] = make_float4(m[0], m[1], h[0], h[1]);
     if (l == 0) anew[w] = tk.starts != 0;
@@ -787,6 +816,31 @@ __global__ void __launch_bounds__((ALONE ? kAloneWaves : kWaves) * GS_WAVE, 4) k
                 b[0] = fmaf(bm[0], d[0], b[0]);
                 b[1] = fmaf(bm[1], d[1], b[1]);
             }
+        }
+    }
+    // A product of the gates has run to 0, and may have met an infinite dy: token by
+    // token, where it has.
+    const bool gone = bm[0] == 0.0f || bm[1] == 0.0f || (!tk.starts && (m[0] == 0.0f || m[1] == 0.0f));
+    if (__any(gone)) {
+        float c[2] = {0.0f, 0.0f}, p[2] = {1.0f, 1.0f};
+#pragma unroll
+        for (int i = kSteps - 1; i >= 0; --i)
+            if (i <= first_end) {
+                if (bit(lasts, i)) state_of(o.dfinal, i, c);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float gate = S[i][k], A, z;
+                    loaded(gate);              // opened again: held open since the walk above, it would take registers
+                    open(gate, A, z);
+                    c[k] = A * (ds[i][k] + c[k]);
+                    p[k] = behind(p[k], A);
+                }
+            }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            b[k] = b[k] != b[k] ? c[k] : b[k];
+            bm[k] = bm[k] == 0.0f ? p[k] : bm[k];
+            m[k] = !tk.starts && m[k] == 0.0f ? p[k] : m[k];           // no start among them: p is of all
         }
     }
     if (tk.ends) bm[0] = bm[1] = 0.0f;

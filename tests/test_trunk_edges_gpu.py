@@ -78,3 +78,83 @@ def test_layer_norm_at_the_end_of_the_range(tk):
     assert bool(y[1].isnan().all()) and bool(y[2].isnan().all())
     want, _, bound = ref.layer(x[3:], w, b, 1e-5)
     within(y[3:], want, bound, "an ordinary row")
+
+
+# -- infinite states --------------------------------------------------------------------
+
+
+def walked(x, gate, dy, cu, initial, dfinal, reverse):
+    """y, final, dx, dgate and dinitial token by token in double, on the CPU."""
+    x, gate, dy, initial, dfinal = (t.double().cpu() for t in (x, gate, dy, initial, dfinal))
+    a, z = torch.sigmoid(gate), torch.sigmoid(-gate)
+    y, before, final, dx, dg, di = (torch.zeros_like(t) for t in (x, x, initial, x, x, initial))
+    for s, (lo, hi) in enumerate(zip(cu, cu[1:])):
+        order = range(hi - 1, lo - 1, -1) if reverse else range(lo, hi)
+        h = initial[s]
+        for t in order:
+            before[t], h = h, a[t] * h + z[t] * x[t]
+            y[t] = h
+        final[s], D = h, dfinal[s]
+        for t in reversed(order):
+            D = D + dy[t]
+            dx[t], dg[t], D = z[t] * D, a[t] * z[t] * (before[t] - x[t]) * D, a[t] * D
+        di[s] = D
+    return y, final, dx, dg, di
+
+
+def alike(got, want, what):
+    """Infinite with the same sign, NaN and finite at the same places."""
+    got = got.double().cpu()
+    for sort in (torch.isposinf, torch.isneginf, torch.isnan):
+        assert torch.equal(sort(got), sort(want)), (what, sort.__name__, int((sort(got) != sort(want)).sum()))
+
+
+@pytest.mark.parametrize("n,cu", [(40, [0]), (250, [0, 90]), (300, [0, 100]), (9000, [0, 130, 2600, 4096])])
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_infinite_states_stay_infinite(tk, n, cu, reverse, dtype):
+    """Through runs of gates whose product is 0 in fp32: what they are token by token, and the other channels' bits as they
+    are without them."""
+    cu = cu + [n]
+    g = gen(31 + n)
+    x, dy = randn(g, n, 7, dtype=dtype), randn(g, n, 7, dtype=dtype)
+    gate = (-8 + 4 * torch.rand(n, 7, generator=g, device="cuda")).to(dtype)
+    first, last = randn(g, len(cu) - 1, 7), randn(g, len(cu) - 1, 7)
+    clean = tk.recurrence(x, gate, cu=starts(cu), initial=first, reverse=reverse, keep=True)
+    grads = tk.recurrence_backward(dy, x, gate, clean.kept, cu=starts(cu), initial=first, dfinal=last, reverse=reverse)
+    for lo, hi in zip(cu, cu[1:]):
+        near, mid, far = lo + 3, (lo + hi) // 2, hi - 4
+        x[far if reverse else near, 1] = dy[near if reverse else far, 1] = math.inf
+        x[far if reverse else near, 2] = dy[near if reverse else far, 2] = -math.inf
+        x[mid, 2] = dy[mid, 2] = math.inf              # with the infinity of the other sign: NaN from here on
+        x[mid, 3] = -math.inf
+        dy[mid, 4] = -math.inf
+    first[:, 5] = math.inf
+    last[:, 6] = -math.inf
+    got = tk.recurrence(x, gate, cu=starts(cu), initial=first, reverse=reverse, keep=True)
+    back = tk.recurrence_backward(dy, x, gate, got.kept, cu=starts(cu), initial=first, dfinal=last, reverse=reverse)
+    want = walked(x, gate, dy, cu, first, last, reverse)
+    for a, b, what in zip((got.y, got.final, *back), want, ("y", "final", "dx", "dgate", "dinitial")):
+        alike(a, b, what)
+    for c in (0, 4, 6):
+        assert torch.equal(got.y[:, c], clean.y[:, c]) and torch.equal(got.final[:, c], clean.final[:, c])
+    for c in (0, 3, 5):
+        assert torch.equal(back[0][:, c], grads[0][:, c]) and torch.equal(back[2][:, c], grads[2][:, c])
+    assert torch.equal(back[1][:, 0], grads[1][:, 0])
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("n", [40, 250, 9000])
+def test_a_gate_of_zero_leaves_nothing_of_the_state(tk, n, reverse):
+    """Of a finite state, whatever the gates around it: exactly 0 where the tokens are; nor of a gradient."""
+    g = gen(n)
+    gate = -12 * torch.rand(n, 6, generator=g, device="cuda")
+    at = n // 3
+    gate[at, :3] = -math.inf
+    zero, first = torch.zeros(n, 6, device="cuda"), torch.full((1, 6), 1e30, device="cuda")
+    r = tk.recurrence(zero, gate, initial=first, reverse=reverse, keep=True)
+    behind = slice(0, at + 1) if reverse else slice(at, n)
+    assert bool((r.y[behind, :3] == 0).all()) and bool((r.final[0, :3] == 0).all())
+    dx, _, di = tk.recurrence_backward(zero, zero, gate, r.kept, initial=first, dfinal=first, reverse=reverse)
+    front = slice(at + 1, n) if reverse else slice(0, at)
+    assert bool((dx[front, :3] == 0).all()) and bool((di[0, :3] == 0).all())
