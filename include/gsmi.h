@@ -937,8 +937,10 @@ gs_status gs_embedding(const gs_embed_args* args, void* stream);
 
 /*
  * Its gradient: row j is scale * the sum of dout[t] over the tokens with
- * ids[t] = j, in fp32 and in an order that ids alone fix: the same call gives the
- * same bits.  Ids outside [0, rows) add to nothing.
+ * ids[t] = j, in an order that ids alone fix: the same call gives the same bits.
+ * Up to 64 tokens are added in fp32, and up to 65 of their sums; a row of more
+ * adds those sums in 64 bits, so its error does not grow with its tokens.  Ids
+ * outside [0, rows) add to nothing.
  *   dout [tokens, dim] of `dtype`, rows ld_dout elements apart
  *   unique NULL: grad [rows, ld_grad] fp32 is the table's whole gradient (rows
  *     without a token are 0); count is not used.

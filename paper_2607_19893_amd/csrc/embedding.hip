@@ -385,15 +385,17 @@ __global__ void __launch_bounds__(kSum) k_embed_sum(EmbedSum a) {
 // Sums of the partial rows of a run, from the chunk that holds its start: the
 // last row of that chunk, then the first rows of those behind it.  A group of
 // lanes takes a run of few chunks; the workgroup together one of many, in equal
-// slices that are added in ascending order.  Workgroups behind these write zeros
-// to the rows that have no token.
+// slices that are added in ascending order.  A slice's sum moves to 64 bits every
+// kShort chunks: in 32 throughout, a row's sum loses a bit with every doubling of
+// its tokens (400,000 equal numbers came out 8e-6 off, 2^28 would by 0.4%).
+// Workgroups behind these write zeros to the rows that have no token.
 constexpr int kJoin = 512;
 constexpr int kShort = 64;                     // chunks of a run that a group joins alone
 
 template <typename T, bool TAIL, int G>
 __global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_blocks, int rows_a_block) {
     constexpr int N = Piece<T>::N, GROUPS = kJoin / G;
-    __shared__ float sums[GROUPS][G * N];
+    __shared__ double sums[GROUPS][N][G];
     __shared__ int many[GROUPS], n_many, ends;
     if ((int)blockIdx.x >= join_blocks) {
         if (blockIdx.y > 0) return;
@@ -466,23 +468,31 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(EmbedSum a, int join_block
             if (ends < kJoin) chunks = c + ends - c0;
             __syncthreads();
         }
-        const int64_t per = (chunks + GROUPS - 1) / GROUPS;
+        const int64_t per = (chunks + GROUPS - 1) / GROUPS, last = min((group + 1) * per, chunks);
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < N; ++i) {
+            acc[i] = 0.0f;
+            sums[group][i][lane] = 0.0;
+        }
         if (group == 0) add(acc, a.parts + (2 * c0 + 1) * a.dim);
+        for (int64_t j0 = group * per; j0 < last; j0 += kShort) {
+            const int n = (int)min((int64_t)kShort, last - j0);
+            const float* p = a.parts + 2 * (c0 + 1 + j0) * a.dim;
 #pragma unroll 8
-        for (int64_t j = group * per; j < min((group + 1) * per, chunks); ++j) add(acc, a.parts + 2 * (c0 + 1 + j) * a.dim);
+            for (int j = 0; j < n; ++j, p += 2 * a.dim) add(acc, p);
 #pragma unroll
-        for (int i = 0; i < N; ++i) sums[group][lane * N + i] = acc[i];
+            for (int i = 0; i < N; ++i) {
+                sums[group][i][lane] += acc[i];
+                acc[i] = 0.0f;
+            }
+        }
         __syncthreads();
-        if (group == 0) {
-#pragma unroll 4
-            for (int u = 1; u < GROUPS; ++u)
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc[i] += sums[u][lane * N + i];
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] *= a.scale;
-            put_row<T, TAIL>(a.grad + (int64_t)run * a.ld_grad + col, there, acc);
+        if (threadIdx.x < G * N) {             // a column each
+            double sum = 0.0;
+#pragma unroll 8
+            for (int u = 0; u < GROUPS; ++u) sum += sums[u][threadIdx.x % N][threadIdx.x / N];
+            const int to = blockIdx.y * (G * N) + threadIdx.x;
+            if (to < a.dim) a.grad[(int64_t)run * a.ld_grad + to] = (float)sum * a.scale;
         }
         __syncthreads();
     }

@@ -158,3 +158,22 @@ def test_a_gate_of_zero_leaves_nothing_of_the_state(tk, n, reverse):
     dx, _, di = tk.recurrence_backward(zero, zero, gate, r.kept, initial=first, dfinal=first, reverse=reverse)
     front = slice(at + 1, n) if reverse else slice(0, at)
     assert bool((dx[front, :3] == 0).all()) and bool((di[0, :3] == 0).all())
+
+
+# -- long sums ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("tokens,rows,dim", [(400_000, 1, 512), (400_001, 3, 200), (16_000_000, 1, 64), (30_000_000, 2, 5)])
+@pytest.mark.parametrize("value", [0.1, 0.7])
+def test_embedding_gradient_of_very_many_tokens_a_row(tk, tokens, rows, dim, value):
+    """Equal numbers, whose roundings do not cancel: as near as the sums of a few tokens."""
+    dout = torch.full((tokens, dim), value, device="cuda")
+    ids = (torch.arange(tokens, device="cuda") * rows // tokens).int()
+    count = torch.bincount(ids.long(), minlength=rows)[:, None]
+    want = (count.double() * float(dout[0, 0]) * 1.5).expand(rows, dim)
+    # 64 tokens in fp32, 64 and one of their sums in fp32, those in 64 bits, rounded once, the product with the scale
+    bound = (64 + 65 + 2) * ref.F * want
+    got = tk.embedding_backward(dout, ids, rows, 1.5)
+    within(got, want, bound, "grad")
+    unique, n, touched = tk.embedding_rows(dout, ids, rows, 1.5)
+    assert int(n) == rows and torch.equal(touched, got)
