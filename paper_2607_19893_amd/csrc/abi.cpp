@@ -840,7 +840,7 @@ static gs_status check_recur(const gs_recur* a, const char* what) {
     // places run up to a chunk past the end, and a launch holds fewer than 2^32 threads
     if (a->n > 1 << 30) return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^30 tokens", what);
     if (a->n_seg > 1 << 28) return fail(GS_ERR_UNSUPPORTED, "%s: more than 2^28 segments", what);
-    if (((int64_t)a->n / 128 + 1) * ((int64_t)a->cols / 128 + 1) >= 1 << 22)
+    if (((int64_t)a->n / 128 + 1) * ((int64_t)a->cols / 128 + 1) >= 1 << 22 || !gsmi::recurrence_fits(*a))
         return fail(GS_ERR_UNSUPPORTED, "%s: %d tokens of %d channels are more than 2^22 workgroups", what, a->n, a->cols);
     const size_t es = type_size(a->dtype);
     gs_status s;

@@ -137,6 +137,7 @@ size_t embedding_bwd_ws_bytes(int32_t tokens, int32_t rows, int32_t dim, bool to
 hipError_t launch_embedding_bwd(const gs_embed_bwd_args& a, void* ws, hipStream_t st);
 
 // recurrence.hip
+bool recurrence_fits(const gs_recur& a);      // its launches hold fewer than 2^32 threads
 size_t recurrence_ws_bytes(const gs_recur& a);
 hipError_t launch_recurrence(const gs_recur& a, void* y, int64_t ld_y, float* final, float* kept, void* ws,
                              hipStream_t st);

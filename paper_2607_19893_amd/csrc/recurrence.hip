@@ -986,8 +986,10 @@ void clear_flags(const Recur& r, const float* from, float* to, hipStream_t st) {
     k_recur_clear<<<std::min(most, 1024u), GS_BLOCK, 0, st>>>(r.a, from, to, r.flags, flags);
 }
 
+constexpr uint32_t kEmptyBlocks = 256;         // that see to empty segments, at most
+
 uint32_t alone_grid(const Recur& r, const float* to) {
-    return r.blocks + (to && r.a.cu ? std::min(div_up(r.a.n_seg, kAloneWaves * GS_WAVE), 256u) : 0u);
+    return r.blocks + (to && r.a.cu ? std::min(div_up(r.a.n_seg, kAloneWaves * GS_WAVE), kEmptyBlocks) : 0u);
 }
 
 // Whether a wave takes a segment: a token each, as far as the sizes tell (a list
@@ -1051,6 +1053,13 @@ hipError_t recur_bwd_type(const Recur& r, const gs_recur_grads& g, hipStream_t s
 }
 
 }  // namespace
+
+bool recurrence_fits(const gs_recur& a) {
+    const RecurPlan p = recur_plan(a.n, a.cols);
+    const uint64_t threads = p.chunks == 1 ? ((uint64_t)p.blocks + kEmptyBlocks) * kAloneWaves * GS_WAVE
+                                           : (uint64_t)p.chunks * p.blocks * kWaves * GS_WAVE;
+    return threads < 1ull << 32;
+}
 
 size_t recurrence_ws_bytes(const gs_recur& a) { return recur_plan(a.n, a.cols).bytes; }
 

@@ -20,3 +20,18 @@ def test_recurrence_workspace_holds_lines_of_its_own(gs, n, cols):
 
 def test_recurrence_of_one_chunk_needs_no_workspace(gs):
     assert gs.gs_recurrence_ws_bytes(recur(gs, n=256, n_seg=1)) == 0
+
+
+@pytest.mark.parametrize("n,cols", [(1, 2 ** 29 - 129), (127, (2 ** 22 * 126 - 25_000) // 128 * 128 + 1)])
+def test_recurrence_of_more_threads_than_a_launch_holds(gs, n, cols):
+    """The only chunk's workgroups have 1024 threads, blocks of channels can be narrower than 128, and workgroups that see to
+    empty segments come on top."""
+    import ctypes
+
+    L = gs.raw()
+    a = recur(gs, n=n, cols=cols, ld_x=cols, ld_gate=cols, n_seg=1, cu=256)
+    blocks = -(-cols // (126 if cols % 128 == 1 else 128))
+    assert (n // 128 + 1) * (cols // 128 + 1) < 1 << 22 and (blocks + 256) * 1024 >= 1 << 32
+    refused(gs, L.gs_recurrence(ctypes.byref(a), 256, cols, 256, 256, None, 0, None), "2^22", gs.GS_ERR_UNSUPPORTED)
+    g = gs.gs_recur_grads(256, 256, 256, 256, 256, 256, cols, cols, cols)
+    refused(gs, L.gs_recurrence_bwd(ctypes.byref(a), ctypes.byref(g), None, 0, None), "2^22", gs.GS_ERR_UNSUPPORTED)
