@@ -797,13 +797,19 @@ def gs_recurrence_bwd(recur: gs_recur, dy, kept, dx, dgate, dfinal=None, dinitia
                                                               stream if stream is not None else current_stream()))
 
 
+def _eight(t, kind):
+    """Bytes, or torch's type of what they stand for: another type of 8 bits would be read as other numbers."""
+    import torch
+    return t.element_size() == 1 and (not t.is_floating_point() or t.dtype == getattr(torch, kind, None))
+
+
 def _kept8(q, scale, shape, name):
     """(addresses and strides) of rows in 8 bits and their scale bytes."""
     if q is None:
         return None, None, 0, 0
     blocks = (shape[0], -(-shape[1] // GS_KEEP_BLOCK))
-    if q.element_size() != 1 or scale is None or scale.element_size() != 1:
-        raise ValueError("%s and its scales are bytes" % name)
+    if scale is None or not (_eight(q, "float8_e4m3fn") and _eight(scale, "float8_e8m0fnu")):
+        raise ValueError("%s is float8_e4m3fn or its bytes, its scales are bytes" % name)
     return q.data_ptr(), scale.data_ptr(), _ld(q, shape, name), _ld(scale, blocks, name + "'s scale")
 
 

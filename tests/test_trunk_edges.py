@@ -35,3 +35,30 @@ def test_recurrence_of_more_threads_than_a_launch_holds(gs, n, cols):
     refused(gs, L.gs_recurrence(ctypes.byref(a), 256, cols, 256, 256, None, 0, None), "2^22", gs.GS_ERR_UNSUPPORTED)
     g = gs.gs_recur_grads(256, 256, 256, 256, 256, 256, cols, cols, cols)
     refused(gs, L.gs_recurrence_bwd(ctypes.byref(a), ctypes.byref(g), None, 0, None), "2^22", gs.GS_ERR_UNSUPPORTED)
+
+
+@pytest.mark.parametrize("q,scale", [("float8_e5m2", "uint8"), ("float8_e4m3fnuz", "uint8"), ("float8_e4m3fn", "float8_e4m3fn"),
+                                     ("float16", "uint8"), ("float8_e4m3fn", None)])
+def test_other_numbers_of_eight_bits_are_refused(q, scale):
+    """By the binding, before the library reads them as e4m3 and powers of two."""
+    from paper_2607_19893_amd import gsmi
+
+    made = lambda name, *shape: None if name is None else torch.zeros(*shape).to(getattr(torch, name))
+    x, q, s = torch.zeros(5, 64), made(q, 5, 64), made(scale, 5, 2)
+    with pytest.raises(ValueError, match="e4m3"):
+        gsmi.gs_gated_silu(x, None, x, q, s)
+    with pytest.raises(ValueError, match="e4m3"):
+        gsmi.gs_gated_silu_bwd(x, q, s, x)
+
+
+def test_bytes_and_their_types_are_taken(monkeypatch):
+    from paper_2607_19893_amd import gsmi
+
+    seen = []
+    monkeypatch.setattr(gsmi, "current_stream", lambda: None)
+    monkeypatch.setattr(gsmi._lib, "gs_gated_silu_bwd", lambda a, s: seen.append(1) or 0, raising=False)
+    x = torch.zeros(5, 64)
+    for q in (torch.uint8, torch.int8, torch.float8_e4m3fn):
+        for s in (torch.uint8, torch.float8_e8m0fnu):
+            gsmi.gs_gated_silu_bwd(x, torch.zeros(5, 64, dtype=torch.uint8).view(q), torch.zeros(5, 2, dtype=torch.uint8).view(s), x)
+    assert len(seen) == 6
