@@ -1054,8 +1054,9 @@ gs_status gs_recurrence_bwd(const gs_recur* a, const gs_recur_grads* g, void* ws
  *     u and v in e4m3 (4 exponent bits, 3 mantissa bits, largest 448), in blocks
  *     of GS_KEEP_BLOCK columns of a row (the last may be shorter), with a scale
  *     byte a block: u ~ 2^(u_scale - 127) * u8, ties to even.  The power is the
- *     least with max|u| <= 448 * it (and 2^-127 at least).  A NaN or infinity
- *     becomes a NaN of u8 and does not touch the scale.
+ *     least with max|u| <= 448 * it (and 2^-127 at least).  A value is off by at
+ *     most a 16th of itself or 2^-10 of the power, whichever is more.  A NaN or
+ *     infinity becomes a NaN of u8 and does not touch the scale.
  *   u_scale, v_scale [rows, ld_*_scale] uint8 (with u8, v8)
  * Errors: GS_ERR_INVALID_ARG (null pointers, sizes, strides, alignment, dtype,
  * nothing to write, u8 and v8 not together); GS_ERR_UNSUPPORTED for cols above

@@ -177,3 +177,29 @@ def test_embedding_gradient_of_very_many_tokens_a_row(tk, tokens, rows, dim, val
     within(got, want, bound, "grad")
     unique, n, touched = tk.embedding_rows(dout, ids, rows, 1.5)
     assert int(n) == rows and torch.equal(touched, got)
+
+
+# -- kept values beside a block's largest -----------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_kept_values_beside_large_ones(tk, dtype):
+    """As far off as the documentation says: a 16th, or 2^-10 of the block's power of two; not always a 16th."""
+    g = gen(41)
+    u = (randn(g, 300, 64) * torch.exp(-14 * torch.rand(300, 64, generator=g, device="cuda"))).to(dtype)
+    u[:, 7], u[:, 40] = 448.0 * 2.0 ** -3, -300.0
+    r = tk.gated_silu(u, u)
+    power = torch.exp2(r.u_scale.double() - 127).repeat_interleave(32, 1)
+    top = u.double().abs().view(300, 2, 32).amax(2).repeat_interleave(32, 1)
+    assert bool((power <= top / 224).all())
+    x, back = u.double().abs(), ref.wide(r.u8, r.u_scale)
+    off = (back - u.double()).abs()
+    assert bool((off <= torch.maximum(x / 16, power * 2.0 ** -10)).all())
+    assert bool((off <= x / 16)[x >= top / 14336].all()) and bool((off > x / 16).any())
+    assert bool((back != 0)[x > top / 229376].all()) and bool((back == 0)[x > 0].any())
+    # the gradient is that at the kept values
+    dh = randn(g, 300, 64, dtype=dtype)
+    du, dv, _ = tk.gated_silu_backward(dh, r.u8, r.u_scale, r.v8, r.v_scale)
+    want, bounds = ref.silu_bwd(dh, back, back)
+    within(du, want[0], bounds[0], "du")
+    within(dv, want[1], bounds[1], "dv")
