@@ -572,9 +572,17 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+def _count(n, what):
+    """A size that the library takes in 32 bits (ctypes would cut a larger one down to its low bits)."""
+    if not 0 <= n <= 0x7FFFFFFF:
+        raise ValueError("%s: %d is not between 0 and 2^31 - 1" % (what, n))
+    return n
+
+
 def make_rows(t) -> gs_rows:
     """A [rows, heads, dim] tensor whose heads' elements are contiguous."""
     st = t.stride()
+    _count(t.shape[0], "rows")
     if len(st) != 3 or (st[2] != 1 and t.shape[2] > 1):
         raise ValueError("a token matrix is [rows, heads, dim] with contiguous elements, not %s with strides %s"
                          % (tuple(t.shape), st))
@@ -590,6 +598,8 @@ def _ld(t, shape, what, dtype=None):
         raise ValueError("%s is %s with contiguous rows, not %s with strides %s" % (what, list(shape), list(t.shape), st))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s is %s, not %s" % (what, dtype, t.dtype))
+    if (shape[0] | shape[1]) >> 31:
+        raise ValueError("%s: %s is past 2^31 - 1" % (what, list(shape)))
     return st[0] if shape[0] > 1 else max(shape[1], st[0])
 
 
@@ -664,6 +674,7 @@ def make_attn(q, k, v, scale, n_seg=1, cu_q=None, cu_k=None, key_on=None, left=-
         if cu_k is None or cu_k.numel() != n_seg + 1 or cu_q.element_size() != 4 or cu_q.is_floating_point() \
                 or cu_k.dtype != cu_q.dtype or not cu_q.is_contiguous() or not cu_k.is_contiguous():
             raise ValueError("cu_q and cu_k are contiguous int32 of the same length")
+    _count(n_seg, "n_seg")
     if key_on is not None and (key_on.numel() != ks[0] or key_on.element_size() != 1 or not key_on.is_contiguous()):
         raise ValueError("key_on is one contiguous byte per key")
     return gs_attn(token_dtype(q) | (GS_ATTN_FILL if fill else 0), qs[0], ks[0], n_seg, qs[1], ks[1], qs[2], left, right, scale, _at(cu_q), _at(cu_k),
@@ -732,7 +743,7 @@ def gs_embedding_bwd(dout, ids, rows, scale, grad, ws, unique=None, count=None, 
     import torch
     tokens, dim = dout.shape
     _int32(ids, tokens, "ids")
-    most = rows
+    most = _count(rows, "rows")
     if unique is not None:
         most = min(tokens, rows)
         _int32(unique, most, "unique")
@@ -760,6 +771,7 @@ def make_recur(x, gate, cu=None, n_seg=1, initial=None, reverse=False, fill=Fals
     if cu is not None:
         n_seg = cu.numel() - 1
         _int32(cu, n_seg + 1, "cu")
+    _count(n_seg, "n_seg")
     _states(initial, (n_seg, shape[1]), "initial")
     return gs_recur(token_dtype(x), shape[0], shape[1], n_seg, reverse, fill, _at(cu), x.data_ptr(), gate.data_ptr(),
                     _at(initial), _ld(x, shape, "x"), _ld(gate, shape, "gate", x.dtype))

@@ -62,3 +62,33 @@ def test_bytes_and_their_types_are_taken(monkeypatch):
         for s in (torch.uint8, torch.float8_e8m0fnu):
             gsmi.gs_gated_silu_bwd(x, torch.zeros(5, 64, dtype=torch.uint8).view(q), torch.zeros(5, 2, dtype=torch.uint8).view(s), x)
     assert len(seen) == 6
+
+
+PAST = 2 ** 32 + 5                                     # 5 in its low 32 bits
+
+
+@pytest.mark.parametrize("what", ["rms norm", "rotary", "layer", "layer gradient", "lookup", "lookup's table", "touched rows",
+                                  "table's gradient", "recurrence", "segments", "silu", "silu gradient"])
+def test_sizes_past_32_bits_are_refused(what):
+    """By the binding: the library would see their low bits and leave the other rows as they were."""
+    from paper_2607_19893_amd import gsmi
+
+    far = torch.empty(PAST, 1, device="meta", dtype=torch.bfloat16)
+    one, x, w = torch.zeros(1, 1, dtype=torch.bfloat16), torch.zeros(5, 1, dtype=torch.bfloat16), torch.zeros(1)
+    ids, q, s = torch.zeros(5, dtype=torch.int32), far.to(torch.uint8), far.to(torch.uint8)
+    calls = {
+        "rms norm": lambda: gsmi.gs_rms_norm(far, w, 1e-5, y=far),
+        "rotary": lambda: gsmi.make_rows(far.unsqueeze(1)),
+        "layer": lambda: gsmi.gs_layer_norm(far, w, None, 1e-5, y=far),
+        "layer gradient": lambda: gsmi.gs_layer_norm_bwd(far, far, w, 1e-5, far, w, w, None),
+        "lookup": lambda: gsmi.gs_embedding(one, torch.empty(PAST, dtype=torch.int32, device="meta"), 1.0, far),
+        "lookup's table": lambda: gsmi.gs_embedding(far, ids, 1.0, x),
+        "touched rows": lambda: gsmi.gs_embedding_bwd(x, ids, PAST, 1.0, x.float(), None, ids, ids[:1]),
+        "table's gradient": lambda: gsmi.gs_embedding_bwd(x, ids, PAST, 1.0, far.float(), None),
+        "recurrence": lambda: gsmi.make_recur(far, far),
+        "segments": lambda: gsmi.make_recur(x, x, n_seg=PAST),
+        "silu": lambda: gsmi.gs_gated_silu(far, None, far),
+        "silu gradient": lambda: gsmi.gs_gated_silu_bwd(far, q, s, far),
+    }
+    with pytest.raises(ValueError, match="2.31 - 1"):
+        calls[what]()
