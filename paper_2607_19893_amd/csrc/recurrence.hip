@@ -298,8 +298,11 @@ __device__ __forceinline__ void through(const float4* maps, const uint32_t* anew
 
 constexpr uint32_t kMap = 1, kAnew = 2, kState = 2;
 constexpr int kPolls = 1 << 22;
-constexpr int kPause = 32;                     // between looks (s_sleep): with 1, 3% slower
-constexpr int kGroup = 16;                     // chunks
+constexpr int kPause = 32;                     // between looks (s_sleep): 1 is 3% slower, 64 is 2%, 4 and 16 are the same
+// Chunks of a group.  400,000 tokens of 128 channels take 122 us (gradient 170); with
+// 8 of them 129 (178), with 32 130 (197, registers spilled).  131,072 tokens of 1024
+// channels 222, 217 with 8, 243 with 32.
+constexpr int kGroup = 16;
 constexpr size_t kLine = 256;                  // bytes; a cache line is 128
 static_assert(GS_WAVE * sizeof(uint64_t) % 128 == 0, "no two chunks' maps or groups' states share a line");
 
