@@ -203,3 +203,23 @@ def test_kept_values_beside_large_ones(tk, dtype):
     want, bounds = ref.silu_bwd(dh, back, back)
     within(du, want[0], bounds[0], "du")
     within(dv, want[1], bounds[1], "dv")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_gated_silu_gradient_far_out(tk, dtype):
+    """Against the formula at the kept values, a value a block: on the negative side down to the least numbers, on the
+    positive side the factor alone."""
+    u = torch.tensor([-1e30, -1e4, -200.0, -120.0, -100.0, -90.0, -75.0, -60.0, 60.0, 75.0, 90.0, 120.0, 1e4, 1e30])
+    x, f, d = torch.zeros(14, 32, device="cuda", dtype=dtype), torch.zeros(14, 32, device="cuda", dtype=dtype), torch.ones(14, 32)
+    x[:, 0], f[:, 0] = u.to(dtype).cuda(), -3e4
+    d = (d * 1.5).to(dtype).cuda()
+    r = tk.gated_silu(x, f)
+    got = tk.gated_silu_backward(d, r.u8, r.u_scale, r.v8, r.v_scale)
+    U, V = ref.wide(r.u8, r.u_scale)[:, 0], ref.wide(r.v8, r.v_scale)[:, 0]
+    s, rest = torch.sigmoid(U), torch.sigmoid(-U)
+    want = (1.5 * V * (s + U * s * rest), 1.5 * U * s, U * s * V)
+    # exp's rounded argument counts where it is not lost beside 1: up to |u| = 104, behind which fp32 holds nothing
+    c = torch.where(U < 0, 14 + 2 * U.abs().clamp(max=110), 14.0) * ref.F + ref.UNIT[dtype]
+    for t, w, what in zip(got, want, ("du", "dv", "h")):
+        within(t[:, 0], w, c * w.abs() + 2.0 ** -147 * 1e5, what)
+        assert bool((t[:, 1:] == 0).all()), what
